@@ -38,7 +38,7 @@ def listed():
         # the router's gradient in training
         {"name": "route_grad", "op": "route_grad", "tokens": 16384, "experts": 128, "topk": 8, "score": "softmax", "dtype": "f32"},
         # the tokens of a prefill batch to their experts: plan and MX rows
-        {"name": "dispatch", "op": "dispatch", "tokens": 8192, "dim": 4096, "experts": 64, "topk": 8, "align": 32},
+        {"name": "dispatch", "op": "dispatch", "tokens": 8192, "dim": 4096, "experts": 64, "topk": 8, "align": 64},
         # the experts' outputs back to the tokens, in training: gradients of outputs and routing weights
         {"name": "combine_grad", "op": "combine_grad", "tokens": 8192, "dim": 4096, "experts": 64, "topk": 4, "align": 128, "dtype": "bf16"},
         # one decoding step: a few rows for each of many experts, FP4 weights: bound by reading the weights
@@ -85,7 +85,7 @@ def draw(rng):
     if op in ("dispatch", "combine", "combine_grad"):
         experts = rng.choice([8, 16, 32, 64, 128, 256])
         c = {"op": op, "tokens": _log(rng, 8, 8192), "dim": _log(rng, 512, 8192, rng.choice([32, 128])), "experts": experts,
-             "topk": rng.choice([1, 2, 4, 6, 8]), "align": rng.choice([32, 128])}
+             "topk": rng.choice([1, 2, 4, 6, 8]), "align": rng.choice([64, 128])}
         if op != "dispatch":
             c["dtype"] = dtype
         return c
@@ -228,7 +228,7 @@ def prepare(case, seed):
         return s
     E = case["experts"]
     counts = _split(g, case["rows"], E, case["active"])
-    align = 32 if op == "experts" else 128
+    align = 64 if op == "experts" else 128
     offsets = _offsets(counts, align)
     # rows that a program allocates before it knows how the groups fall
     R = _rows_bound(case["rows"], 1, E, align)
