@@ -9,6 +9,10 @@
  *   mx_gemm        Section 4.1 ("Compute Flow"): dot products of two MX operands,
  *                  scalar-float (FP32) output
  *
+ * and what a mixture-of-experts transformer layer needs between its products: the RMS norm that
+ * ends in an MX tensor, routing, moving MX rows to their experts and back, and products over ragged
+ * groups of rows -- each with the gradient that training needs.
+ *
  * An MX block is k = 32 elements P_i that share one E8M0 scale X = 2^(byte-127)
  * (Section 2, Table 1).  Element formats: FP8 E4M3 / E5M2, FP6 E3M2 / E2M3,
  * FP4 E2M1 and INT8 (Table 1).
@@ -397,6 +401,176 @@ int mx_im2col(const void* elems_in, const uint8_t* scales_in, void* elems_out, u
 int mx_conv2d(const void* x_elems, const uint8_t* x_scales, const void* w_elems, const uint8_t* w_scales,
               void* y, mx_dtype_t y_dtype, const mx_conv_t* conv, int64_t Cout, mx_fmt_t fmt_x,
               mx_fmt_t fmt_w, const mx_opts_t* opts);
+
+/* ------------------------------------------------------------------------- */
+/* RMS norm with the residual's addition and MX output                       */
+/* ------------------------------------------------------------------------- */
+/*
+ * What stands in front of a dot-product operation of a transformer layer: the residual addition,
+ * the root-mean-square norm and the conversion of its result to MX (Section 4.1 quantizes every
+ * operand right before the product), in one pass over the data.
+ *   h[r,:] = x[r,:] + residual[r,:]                      (h = x without a residual)
+ *   y[r,:] = h[r,:] * rsqrt(mean(h[r,:]^2) + eps) * weight[:]
+ *   (elems, scales) = mx_quantize(y, shape {rows, dim}, axis 1, fmt, rounding)
+ * All arithmetic is in FP32 and y is not rounded on its way to Algorithm 1; h_out and y_out are
+ * rounded once, when they are stored, and y is the norm of the unrounded sum.
+ *   x, residual  contiguous [rows x dim] of opts->dtype; residual may be NULL
+ *   weight       [dim], FP32 or BF16 (weight_dtype)
+ *   h_out        NULL, or [rows x dim] of opts->dtype: the new residual stream (may be x or residual)
+ *   y_out        NULL, or [rows x dim] of opts->dtype: y itself (training quantizes it along the
+ *                tokens as well)
+ *   elems_out, scales_out  what mx_quantize writes for y, every byte of both
+ * Any rows >= 0 and dim >= 1; every tensor 16-byte aligned.  Errors: MX_ERR_NULL, MX_ERR_SHAPE (a
+ * negative extent, dim 0, eps negative or not finite), MX_ERR_FMT, MX_ERR_ALIGN,
+ * MX_ERR_UNSUPPORTED (pad_k128, an extent of 2^31 or more), MX_ERR_CUDA.  A row of zeros gives y = 0 * rsqrt(eps): zeros for
+ * eps > 0, NaN for eps = 0; Inf or NaN in a row reach every block of that row as the norm carries
+ * them (Inf / Inf is NaN).
+ */
+int mx_rmsnorm_quantize(const void* x, const void* residual, const void* weight, mx_dtype_t weight_dtype,
+                        float eps, int64_t rows, int64_t dim, void* h_out, void* y_out, void* elems_out,
+                        uint8_t* scales_out, mx_fmt_t fmt, mx_round_t rounding, const mx_opts_t* opts);
+
+/*
+ * Gradient of y = h * rsqrt(mean(h^2) + eps) * weight.  With s = rsqrt(mean(h^2) + eps),
+ * n = h s and g = dy weight:
+ *   dh[r,:]   = s (g - n mean(g n)) + dres[r,:]      the gradient of x and of the residual alike
+ *   dweight[:] = sum over rows of dy n
+ *   dy, h, dres, dh  [rows x dim] of opts->dtype; dres (the gradient that arrives along the residual
+ *                    stream) may be NULL; dh may be dy or dres
+ *   dweight          FP32 [dim], overwritten; always summed in the same order (no atomics)
+ *   workspace        at least mx_rmsnorm_backward_workspace_bytes(rows, dim) bytes, 256-byte aligned
+ * Errors as mx_rmsnorm_quantize, and MX_ERR_WORKSPACE.  rows == 0 writes a zero dweight.
+ */
+size_t mx_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t dim);
+int mx_rmsnorm_backward(const void* dy, const void* h, const void* weight, mx_dtype_t weight_dtype, float eps,
+                        const void* dres, int64_t rows, int64_t dim, void* dh, float* dweight,
+                        const mx_opts_t* opts, void* workspace, size_t workspace_bytes);
+
+/* ------------------------------------------------------------------------- */
+/* Mixture of experts: routing, moving rows, the experts' products           */
+/* ------------------------------------------------------------------------- */
+typedef enum { MX_SCORE_SOFTMAX = 0, MX_SCORE_SIGMOID = 1 } mx_score_t;
+typedef enum { MX_GROUP_MAX = 0, MX_GROUP_TOP2 = 1 } mx_group_score_t;
+
+typedef struct {
+  int32_t topk;         /* experts per token, 1 .. 32                                     */
+  int32_t score;        /* mx_score_t: s = softmax over the experts, or 1 / (1 + e^-x)    */
+  int32_t groups;       /* experts in groups of E / groups consecutive ones (1: no groups) */
+  int32_t topk_groups;  /* groups a token may choose from                                 */
+  int32_t group_score;  /* mx_group_score_t: a group's best c, or the sum of its best two */
+  int32_t renormalize;  /* nonzero: weights divided by their sum                          */
+  float scale;          /* weights multiplied by this                                     */
+} mx_route_t;
+
+/*
+ * mx_route -- which experts each token goes to, and with what weight.
+ *   logits   [tokens x experts] of opts->dtype
+ *   bias     NULL, or FP32 [experts]: added to the scores for the choice only (load balance)
+ *   s = softmax(logits) or sigmoid(logits), FP32;   c = s + bias   (softmax without a bias: the
+ *       choice compares the logits, whose order is that of s)
+ *   the topk_groups groups with the largest group score are kept, and of their experts the topk
+ *   with the largest c are chosen, in descending order.  Equal values go to the lower index; NaN
+ *   ranks above everything (and shows in the weights).
+ *   ids_out      int32 [tokens x topk]
+ *   weights_out  FP32 [tokens x topk]: s of the chosen experts (without the bias), divided by their
+ *                sum with renormalize (0 where that sum is 0), times scale.  In a row of softmax logits that
+ *                are all -Inf every score is 0.
+ * experts <= 1024, groups <= 32, experts % groups == 0, topk <= topk_groups * (experts / groups).
+ * Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN (logits 16 bytes, the others 4),
+ * MX_ERR_UNSUPPORTED (more than 1024 experts or 32 groups, topk > 32, 2^31 or more tokens), MX_ERR_CUDA.
+ */
+int mx_route(const void* logits, const float* bias, int64_t tokens, int64_t experts, const mx_route_t* route,
+             int32_t* ids_out, float* weights_out, const mx_opts_t* opts);
+
+/*
+ * Gradient of the weights with respect to the logits, the choice held fixed (the bias and the
+ * groups have no gradient).  dweights FP32 [tokens x topk], ids as mx_route wrote them (an id outside
+ * [0, experts) contributes nothing), dlogits [tokens x experts] of opts->dtype, overwritten.
+ * Of `route` topk, score, renormalize and scale are used.  Errors as mx_route.
+ */
+int mx_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t tokens,
+                      int64_t experts, const mx_route_t* route, void* dlogits, const mx_opts_t* opts);
+
+/*
+ * mx_moe_plan -- where the rows go.  The tokens x topk choices are sorted by expert, choices of
+ * one expert in token order; the group of expert e is rows offsets[e] .. offsets[e+1], its size
+ * rounded up to a multiple of `align`.
+ *   ids      int32 [tokens x topk]; an id outside [0, experts) is a choice that is dropped
+ *   offsets  int32 [experts + 1]
+ *   counts   int32 [experts]: rows of each group that hold a choice (the rest is padding)
+ *   row_of   int32 [tokens x topk]: the row of a choice, -1 for a dropped one
+ *   workspace  mx_moe_plan_workspace_bytes(tokens, topk, experts) bytes, 16-byte aligned
+ * mx_moe_rows(tokens, topk, experts, align) is the largest offsets[experts] can become: the rows
+ * to allocate without asking the device (0 on bad arguments).  experts <= 1024, 1 <= align <= 1024,
+ * fewer than 2^31 - 2^21 choices.  Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_ALIGN, MX_ERR_UNSUPPORTED
+ * (more than 1024 experts), MX_ERR_WORKSPACE, MX_ERR_CUDA.
+ */
+int64_t mx_moe_rows(int64_t tokens, int64_t topk, int64_t experts, int64_t align);
+size_t mx_moe_plan_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts);
+int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t experts, int64_t align,
+                int32_t* offsets, int32_t* counts, int32_t* row_of, const mx_opts_t* opts,
+                void* workspace, size_t workspace_bytes);
+
+/*
+ * mx_moe_gather -- the MX rows of the tokens in the order of a plan: output row row_of[t,j] is row t
+ * of the MX tensor [tokens x dim] (codes and scale bytes moved, nothing requantized).  Rows
+ * 0 .. rows-1 that no choice maps to are zero blocks (codes 0, scale byte 0), so that products with
+ * them are zero.  scales_in and scales_out in opts->scale_layout; every byte of both outputs is
+ * written.  dim % 32 == 0; tensors 16-byte aligned; rows as allocated for the plan (a row_of outside
+ * [0, rows) is skipped).  Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN,
+ * MX_ERR_UNSUPPORTED (pad_k128, more than 1024 experts), MX_ERR_CUDA.
+ */
+int mx_moe_gather(const void* elems_in, const uint8_t* scales_in, int64_t tokens, int64_t topk, int64_t dim,
+                  mx_fmt_t fmt, const int32_t* offsets, const int32_t* counts, const int32_t* row_of,
+                  int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts);
+
+/*
+ * mx_moe_combine -- out[t,:] = sum over j (ascending) of weights[t,j] * y[row_of[t,j],:], FP32,
+ * rounded once.  y [rows x dim], out [tokens x dim] of opts->dtype; weights FP32 [tokens x topk] or
+ * NULL (all 1: the backward pass of a gather).  A row_of outside [0, rows) adds nothing.
+ *
+ * mx_moe_combine_backward -- dy[row_of[t,j],:] = weights[t,j] * dout[t,:], rows that no choice maps
+ * to zero (offsets and counts of the plan say which); dweights[t,j] = <dout[t,:], y[row_of[t,j],:]>,
+ * FP32, 0 for a dropped choice.  y and dweights may both be NULL; with weights NULL as well it
+ * is the gather of a float tensor's rows.
+ * Any dim >= 1, topk >= 1; float tensors 16-byte aligned.  Errors: MX_ERR_NULL, MX_ERR_SHAPE,
+ * MX_ERR_FMT, MX_ERR_ALIGN, MX_ERR_UNSUPPORTED, MX_ERR_CUDA.
+ */
+int mx_moe_combine(const void* y, const float* weights, const int32_t* row_of, int64_t tokens, int64_t topk,
+                   int64_t dim, int64_t rows, void* out, const mx_opts_t* opts);
+int mx_moe_combine_backward(const void* dout, const void* y, const float* weights, const int32_t* offsets,
+                            const int32_t* counts, const int32_t* row_of, int64_t tokens, int64_t topk,
+                            int64_t dim, int64_t experts, int64_t rows, void* dy, float* dweights,
+                            const mx_opts_t* opts);
+
+/*
+ * mx_gemm_grouped -- the experts' products: every row of A meets the weights of its group.
+ *   C[r,:] = A[r,:] . B[g]^T   for offsets[g] <= r < offsets[g+1]
+ * A  packed [rows x K] codes, sA its SWIZZLED scales; B  the stack [groups x N x K] (what mx_quantize
+ * writes for that 3-D tensor along its last axis), sB its scales; C [rows x N], FP32 or BF16, each dot
+ * product accumulated in FP32 as in mx_gemm.  offsets: int32 [groups + 1] in DEVICE memory (of
+ * mx_moe_plan, or any ascending row numbers that are multiples of 64; the last may also be `rows`).
+ * Rows of C before offsets[0] or from offsets[groups] on are not written.  An offset that breaks
+ * the rule is clamped to [0, rows] and rounded down to a multiple of 64, a descending pair is an
+ * empty group: nothing outside C is ever touched.
+ * The gradient of A is the same call on dC quantized along N and B quantized along N ([groups x K x N]).
+ * N % 128 == 0; K as mx_gemm (a multiple of 32, of 128 with 6- or 4-bit codes); groups <= 1024.
+ * A, B 32-byte, sA, sB, C 16-byte aligned, offsets 4-byte.
+ *
+ * mx_gemm_grouped_k -- the experts' weight gradients: the groups cut the reduction axis.
+ *   C[g] = A[:, offsets[g] .. offsets[g+1]] . B[:, offsets[g] .. offsets[g+1]]^T
+ * A packed [M x rows], B packed [N x rows] (K-major: mx_quantize of dC and of A's float rows along
+ * axis 0), SWIZZLED scales; C [groups x M x N], FP32 or BF16, all of it written: zero for an
+ * empty group.  offsets multiples of 128 (clamped and rounded down as above); the padding rows of a group
+ * have to be zero blocks.  rows % 32 == 0 (% 128 with 6- or 4-bit codes); N a multiple of 8.
+ * Errors of both: as mx_gemm; MX_ERR_UNSUPPORTED for more than 1024 groups or pad_k128.
+ */
+int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                    void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
+                    mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts);
+int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                      void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
+                      mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts);
 
 /* ------------------------------------------------------------------------- */
 /* Host-buffer variants                                                      */

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -24,6 +24,9 @@ FORMATS = {"e4m3": MX_E4M3, "e5m2": MX_E5M2, "e3m2": MX_E3M2, "e2m3": MX_E2M3,
 MX_RNE, MX_RHAZ = 0, 1
 MX_F32, MX_BF16 = 0, 1
 MX_SCALES_LINEAR, MX_SCALES_SWIZZLED = 0, 1
+MX_SCORE_SOFTMAX, MX_SCORE_SIGMOID = 0, 1
+SCORES = {"softmax": MX_SCORE_SOFTMAX, "sigmoid": MX_SCORE_SIGMOID}
+MX_GROUP_MAX, MX_GROUP_TOP2 = 0, 1
 MX_OK = 0
 MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN = -1, -2, -3, -4
 MX_ERR_UNSUPPORTED, MX_ERR_CUDA, MX_ERR_TIMEOUT, MX_ERR_WORKSPACE = -5, -6, -7, -8
@@ -37,6 +40,9 @@ EXPORTS = [
     "mx_quantize_host_workspace_bytes", "mx_quantize_host", "mx_quantize_host_static",
     "mx_dequantize_host_workspace_bytes", "mx_dequantize_host",
     "mx_gemm_host_workspace_bytes", "mx_gemm_host",
+    "mx_rmsnorm_quantize", "mx_rmsnorm_backward_workspace_bytes", "mx_rmsnorm_backward", "mx_route",
+    "mx_route_backward", "mx_moe_rows", "mx_moe_plan_workspace_bytes", "mx_moe_plan", "mx_moe_gather",
+    "mx_moe_combine", "mx_moe_combine_backward", "mx_gemm_grouped", "mx_gemm_grouped_k",
 ]
 
 
@@ -58,6 +64,12 @@ class mx_conv_t(ctypes.Structure):
                 ("stride_h", ctypes.c_int32), ("stride_w", ctypes.c_int32),
                 ("pad_h", ctypes.c_int32), ("pad_w", ctypes.c_int32),
                 ("dil_h", ctypes.c_int32), ("dil_w", ctypes.c_int32)]
+
+
+class mx_route_t(ctypes.Structure):
+    _fields_ = [("topk", ctypes.c_int32), ("score", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("topk_groups", ctypes.c_int32), ("group_score", ctypes.c_int32),
+                ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class MxError(RuntimeError):
@@ -119,6 +131,23 @@ def _load() -> ctypes.CDLL:
     lib.mx_gemm_host_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
     lib.mx_gemm_host_workspace_bytes.restype = sz
     lib.mx_gemm_host.argtypes = [vp, u8p, vp, u8p, vp, i64, i64, i64, ci, ci, op, vp, sz]
+    cf, rp = ctypes.c_float, ctypes.POINTER(mx_route_t)
+    lib.mx_rmsnorm_quantize.argtypes = [vp, vp, vp, ci, cf, i64, i64, vp, vp, vp, u8p, ci, ci, op]
+    lib.mx_rmsnorm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.mx_rmsnorm_backward_workspace_bytes.restype = sz
+    lib.mx_rmsnorm_backward.argtypes = [vp, vp, vp, ci, cf, vp, i64, i64, vp, vp, op, vp, sz]
+    lib.mx_route.argtypes = [vp, vp, i64, i64, rp, vp, vp, op]
+    lib.mx_route_backward.argtypes = [vp, vp, vp, i64, i64, rp, vp, op]
+    lib.mx_moe_rows.argtypes = [i64, i64, i64, i64]
+    lib.mx_moe_rows.restype = i64
+    lib.mx_moe_plan_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mx_moe_plan_workspace_bytes.restype = sz
+    lib.mx_moe_plan.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, op, vp, sz]
+    lib.mx_moe_gather.argtypes = [vp, u8p, i64, i64, i64, ci, vp, vp, vp, i64, i64, vp, u8p, op]
+    lib.mx_moe_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, op]
+    lib.mx_moe_combine_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, op]
+    lib.mx_gemm_grouped.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
+    lib.mx_gemm_grouped_k.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
     return lib
 
 
@@ -376,6 +405,283 @@ def mx_conv2d(x_elems: torch.Tensor, x_scales: torch.Tensor, w_elems: torch.Tens
     _check(_lib.mx_conv2d(x_elems.data_ptr(), x_scales.data_ptr(), w_elems.data_ptr(), w_scales.data_ptr(),
                           out.data_ptr(), _dtype_code(out.dtype), ctypes.byref(conv), Cout, fmt_x, fmt_w,
                           ctypes.byref(o)), "mx_conv2d")
+    return out
+
+
+# ---- RMS norm, routing, moving rows, the experts' products ----------------------------
+
+def _on_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
+    """Every given tensor is contiguous and on ``device``, which is the current CUDA device (the
+    library launches there)."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors have to be on the current CUDA device, not on {device}")
+    for name, t in tensors.items():
+        if t is not None and (t.device != device or not t.is_contiguous()):
+            raise ValueError(f"{name} has to be a contiguous tensor on {device}")
+
+
+def _typed(dtype: torch.dtype, shape: Sequence[int], **tensors: Optional[torch.Tensor]) -> None:
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{name} has to be {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _holds(nbytes: int, **tensors: torch.Tensor) -> None:
+    for name, t in tensors.items():
+        if t.numel() * t.element_size() < nbytes:
+            raise ValueError(f"{name} holds {t.numel() * t.element_size()} bytes, {nbytes} are needed")
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int, eps: float = 1e-6,
+                        residual: Optional[torch.Tensor] = None, rounding: int = MX_RNE,
+                        layout: int = MX_SCALES_SWIZZLED, y_out: Optional[torch.Tensor] = None,
+                        h_out: Optional[torch.Tensor] = None,
+                        out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
+                        ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """RMS norm of ``x + residual`` [rows, dim] as an MX tensor along the rows: (elems, scales, h).
+
+    ``h`` is the new residual stream (None without a residual, unless ``h_out`` is given; ``h_out`` may
+    be ``x`` or ``residual``).  ``y_out`` also receives the norm itself."""
+    if x.dim() != 2:
+        raise ValueError("x has to be [rows, dim]")
+    rows, dim = x.shape
+    _on_device(x.device, x=x, weight=weight, residual=residual, y_out=y_out, h_out=h_out)
+    _typed(x.dtype, x.shape, residual=residual, y_out=y_out, h_out=h_out)
+    _typed(weight.dtype, (dim,), weight=weight)
+    if residual is not None and h_out is None:
+        h_out = torch.empty_like(x)
+    ne, ns = mx_elems_bytes((rows, dim), 1, fmt), mx_scales_bytes((rows, dim), 1, layout)
+    if out is None:
+        elems = torch.empty(ne, dtype=torch.uint8, device=x.device)
+        scales = torch.empty(ns, dtype=torch.uint8, device=x.device)
+    else:
+        elems, scales = out
+        _on_device(x.device, elems=elems, scales=scales)
+        _holds(ne, elems=elems)
+        _holds(ns, scales=scales)
+    o = _opts(_dtype_code(x.dtype), layout)
+    _check(_lib.mx_rmsnorm_quantize(x.data_ptr(), _ptr(residual), weight.data_ptr(), _dtype_code(weight.dtype), eps,
+                                    rows, dim, _ptr(h_out), _ptr(y_out), elems.data_ptr(), scales.data_ptr(), fmt,
+                                    rounding, ctypes.byref(o)), "mx_rmsnorm_quantize")
+    return elems, scales, h_out
+
+
+def mx_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
+                        dres: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Gradients of the norm: (dh [rows, dim], dweight FP32 [dim]).  ``dres`` is added to dh; ``out``
+    receives dh and may be ``dy`` or ``dres``."""
+    if h.dim() != 2:
+        raise ValueError("h has to be [rows, dim]")
+    rows, dim = h.shape
+    _on_device(h.device, dy=dy, h=h, weight=weight, dres=dres, out=out, workspace=workspace)
+    _typed(h.dtype, h.shape, dy=dy, dres=dres, out=out)
+    _typed(weight.dtype, (dim,), weight=weight)
+    need = int(_lib.mx_rmsnorm_backward_workspace_bytes(rows, dim))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=h.device)
+    dh = torch.empty_like(h) if out is None else out
+    dweight = torch.empty(dim, dtype=torch.float32, device=h.device)
+    o = _opts(_dtype_code(h.dtype), MX_SCALES_SWIZZLED)
+    _check(_lib.mx_rmsnorm_backward(dy.data_ptr(), h.data_ptr(), weight.data_ptr(), _dtype_code(weight.dtype), eps,
+                                    _ptr(dres), rows, dim, dh.data_ptr(), dweight.data_ptr(), ctypes.byref(o),
+                                    workspace.data_ptr(), workspace.numel() * workspace.element_size()),
+           "mx_rmsnorm_backward")
+    return dh, dweight
+
+
+def mx_route(logits: torch.Tensor, topk: int, score: int = MX_SCORE_SOFTMAX, bias: Optional[torch.Tensor] = None,
+             groups: int = 1, topk_groups: int = 1, group_score: int = MX_GROUP_MAX, renormalize: bool = True,
+             scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Experts of every token of ``logits`` [tokens, experts] and their weights: (ids int32, weights
+    FP32), both [tokens, topk], the best first."""
+    if logits.dim() != 2:
+        raise ValueError("logits has to be [tokens, experts]")
+    tokens, experts = logits.shape
+    _on_device(logits.device, logits=logits, bias=bias)
+    _typed(torch.float32, (experts,), bias=bias)
+    ids = torch.empty((tokens, topk), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((tokens, topk), dtype=torch.float32, device=logits.device)
+    r = mx_route_t(topk, score, groups, topk_groups, group_score, 1 if renormalize else 0, scale)
+    o = _opts(_dtype_code(logits.dtype), MX_SCALES_SWIZZLED)
+    _check(_lib.mx_route(logits.data_ptr(), _ptr(bias), tokens, experts, ctypes.byref(r), ids.data_ptr(),
+                         weights.data_ptr(), ctypes.byref(o)), "mx_route")
+    return ids, weights
+
+
+def mx_route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor,
+                      score: int = MX_SCORE_SOFTMAX, renormalize: bool = True, scale: float = 1.0) -> torch.Tensor:
+    """Gradient of mx_route's weights with respect to the logits (the choice ``ids`` held fixed)."""
+    if logits.dim() != 2 or ids.dim() != 2:
+        raise ValueError("logits has to be [tokens, experts], ids [tokens, topk]")
+    tokens, experts = logits.shape
+    _on_device(logits.device, dweights=dweights, logits=logits, ids=ids)
+    _typed(torch.int32, (tokens, ids.shape[1]), ids=ids)
+    _typed(torch.float32, ids.shape, dweights=dweights)
+    dlogits = torch.empty_like(logits)
+    r = mx_route_t(ids.shape[1], score, 1, 1, MX_GROUP_MAX, 1 if renormalize else 0, scale)
+    o = _opts(_dtype_code(logits.dtype), MX_SCALES_SWIZZLED)
+    _check(_lib.mx_route_backward(dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), tokens, experts,
+                                  ctypes.byref(r), dlogits.data_ptr(), ctypes.byref(o)), "mx_route_backward")
+    return dlogits
+
+
+class MoePlan(NamedTuple):
+    """Where the rows of a batch go: group e holds rows offsets[e] .. offsets[e + 1], the first counts[e]
+    of them choices; row_of [tokens, topk] is the row of a choice (-1: dropped); ``rows`` bounds
+    offsets[-1] and is what row tensors are allocated with."""
+    offsets: torch.Tensor
+    counts: torch.Tensor
+    row_of: torch.Tensor
+    rows: int
+
+
+def mx_moe_rows(tokens: int, topk: int, experts: int, align: int = 64) -> int:
+    return int(_lib.mx_moe_rows(tokens, topk, experts, align))
+
+
+def mx_moe_plan(ids: torch.Tensor, experts: int, align: int = 64,
+                workspace: Optional[torch.Tensor] = None) -> MoePlan:
+    """Sort the choices ``ids`` [tokens, topk] by expert, groups padded to ``align`` rows: a multiple of
+    64 for mx_gemm_grouped, of 128 for mx_gemm_grouped_k."""
+    if ids.dim() != 2:
+        raise ValueError("ids has to be [tokens, topk]")
+    tokens, topk = ids.shape
+    _on_device(ids.device, ids=ids, workspace=workspace)
+    _typed(torch.int32, ids.shape, ids=ids)
+    need = int(_lib.mx_moe_plan_workspace_bytes(tokens, topk, experts))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=ids.device)
+    i32 = dict(dtype=torch.int32, device=ids.device)
+    plan = MoePlan(torch.empty(max(experts, 0) + 1, **i32), torch.empty(max(experts, 0), **i32), torch.empty_like(ids),
+                   mx_moe_rows(tokens, topk, experts, align))
+    o = _opts(MX_F32, MX_SCALES_SWIZZLED)
+    _check(_lib.mx_moe_plan(ids.data_ptr(), tokens, topk, experts, align, plan.offsets.data_ptr(),
+                            plan.counts.data_ptr(), plan.row_of.data_ptr(), ctypes.byref(o), workspace.data_ptr(),
+                            workspace.numel() * workspace.element_size()), "mx_moe_plan")
+    return plan
+
+
+def _check_plan(device: torch.device, plan: MoePlan) -> Tuple[int, int, int]:
+    _on_device(device, offsets=plan.offsets, counts=plan.counts, row_of=plan.row_of)
+    tokens, topk = plan.row_of.shape
+    experts = plan.counts.numel()
+    _typed(torch.int32, (experts + 1,), offsets=plan.offsets)
+    _typed(torch.int32, (experts,), counts=plan.counts)
+    _typed(torch.int32, (tokens, topk), row_of=plan.row_of)
+    return tokens, topk, experts
+
+
+def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int, plan: MoePlan,
+                  layout: int = MX_SCALES_SWIZZLED,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The rows of an MX tensor [tokens, dim] in the order of ``plan``: (elems, scales) of an MX tensor
+    [plan.rows, dim], rows without a choice zero."""
+    tokens, topk, experts = _check_plan(elems.device, plan)
+    _on_device(elems.device, elems=elems, scales=scales)
+    _holds(mx_elems_bytes((tokens, dim), 1, fmt), elems=elems)
+    _holds(mx_scales_bytes((tokens, dim), 1, layout), scales=scales)
+    ne, ns = mx_elems_bytes((plan.rows, dim), 1, fmt), mx_scales_bytes((plan.rows, dim), 1, layout)
+    if out is None:
+        out = (torch.empty(ne, dtype=torch.uint8, device=elems.device),
+               torch.empty(ns, dtype=torch.uint8, device=elems.device))
+    else:
+        _on_device(elems.device, out_elems=out[0], out_scales=out[1])
+        _holds(ne, out_elems=out[0])
+        _holds(ns, out_scales=out[1])
+    o = _opts(MX_F32, layout)
+    _check(_lib.mx_moe_gather(elems.data_ptr(), scales.data_ptr(), tokens, topk, dim, fmt, plan.offsets.data_ptr(),
+                              plan.counts.data_ptr(), plan.row_of.data_ptr(), experts, plan.rows,
+                              out[0].data_ptr(), out[1].data_ptr(), ctypes.byref(o)), "mx_moe_gather")
+    return out
+
+
+def mx_moe_combine(y: torch.Tensor, weights: Optional[torch.Tensor], plan: MoePlan,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[t] = sum over j of weights[t, j] * y[row_of[t, j]] (``weights`` None: all 1); y [plan.rows, dim]."""
+    tokens, topk, _ = _check_plan(y.device, plan)
+    if y.dim() != 2 or y.shape[0] != plan.rows:
+        raise ValueError(f"y has to be [{plan.rows}, dim]")
+    _on_device(y.device, y=y, weights=weights, out=out)
+    _typed(torch.float32, (tokens, topk), weights=weights)
+    _typed(y.dtype, (tokens, y.shape[1]), out=out)
+    if out is None:
+        out = torch.empty((tokens, y.shape[1]), dtype=y.dtype, device=y.device)
+    o = _opts(_dtype_code(y.dtype), MX_SCALES_SWIZZLED)
+    _check(_lib.mx_moe_combine(y.data_ptr(), _ptr(weights), plan.row_of.data_ptr(), tokens, topk, y.shape[1],
+                               plan.rows, out.data_ptr(), ctypes.byref(o)), "mx_moe_combine")
+    return out
+
+
+def mx_moe_combine_backward(dout: torch.Tensor, y: Optional[torch.Tensor], weights: Optional[torch.Tensor],
+                            plan: MoePlan) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Gradients of mx_moe_combine: (dy [plan.rows, dim], dweights FP32 [tokens, topk]).  Without ``y``
+    only dy; without ``weights`` as well it is the gather of the rows of a float tensor."""
+    tokens, topk, experts = _check_plan(dout.device, plan)
+    if dout.dim() != 2 or dout.shape[0] != tokens:
+        raise ValueError(f"dout has to be [{tokens}, dim]")
+    dim = dout.shape[1]
+    _on_device(dout.device, dout=dout, y=y, weights=weights)
+    _typed(dout.dtype, (plan.rows, dim), y=y)
+    _typed(torch.float32, (tokens, topk), weights=weights)
+    dy = torch.empty((plan.rows, dim), dtype=dout.dtype, device=dout.device)
+    dw = None if y is None else torch.empty((tokens, topk), dtype=torch.float32, device=dout.device)
+    o = _opts(_dtype_code(dout.dtype), MX_SCALES_SWIZZLED)
+    _check(_lib.mx_moe_combine_backward(dout.data_ptr(), _ptr(y), _ptr(weights), plan.offsets.data_ptr(),
+                                        plan.counts.data_ptr(), plan.row_of.data_ptr(), tokens, topk, dim, experts,
+                                        plan.rows, dy.data_ptr(), _ptr(dw), ctypes.byref(o)),
+           "mx_moe_combine_backward")
+    return dy, dw
+
+
+def _check_operand(elems: torch.Tensor, scales: torch.Tensor, rows: int, K: int, fmt: int, name: str) -> None:
+    _on_device(elems.device, **{name: elems, "s" + name: scales})
+    _holds(mx_elems_bytes((rows, K), 1, fmt), **{name: elems})
+    _holds(mx_scales_bytes((rows, K), 1), **{"s" + name: scales})
+
+
+def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
+                    rows: int, N: int, K: int, fmtA: int, fmtB: int, out: Optional[torch.Tensor] = None,
+                    out_dtype: torch.dtype = torch.float32, check_status: bool = False) -> torch.Tensor:
+    """C[r] = A[r] . B[g]^T for the rows r of group g, offsets[g] .. offsets[g + 1] (int32, on the device,
+    multiples of 64): A is the MX tensor [rows, K], B that of [groups, N, K]; rows in no group are not
+    written."""
+    groups = offsets.numel() - 1
+    _on_device(A.device, offsets=offsets, out=out)
+    _typed(torch.int32, (groups + 1,), offsets=offsets)
+    _check_operand(A, sA, rows, K, fmtA, "A")
+    _check_operand(B, sB, groups * N, K, fmtB, "B")
+    if out is None:
+        out = torch.empty((rows, N), dtype=out_dtype, device=A.device)
+    _typed(out.dtype, (rows, N), out=out)
+    o = _opts(MX_F32, MX_SCALES_SWIZZLED, check=check_status)
+    _check(_lib.mx_gemm_grouped(A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), offsets.data_ptr(),
+                                out.data_ptr(), _dtype_code(out.dtype), groups, rows, N, K, fmtA, fmtB,
+                                ctypes.byref(o)), "mx_gemm_grouped")
+    return out
+
+
+def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
+                      M: int, N: int, rows: int, fmtA: int, fmtB: int, out: Optional[torch.Tensor] = None,
+                      out_dtype: torch.dtype = torch.float32, check_status: bool = False) -> torch.Tensor:
+    """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128): A is the
+    MX tensor [M, rows], B [N, rows], both quantized along the rows; C [groups, M, N]."""
+    groups = offsets.numel() - 1
+    _on_device(A.device, offsets=offsets, out=out)
+    _typed(torch.int32, (groups + 1,), offsets=offsets)
+    _check_operand(A, sA, M, rows, fmtA, "A")
+    _check_operand(B, sB, N, rows, fmtB, "B")
+    if out is None:
+        out = torch.empty((groups, M, N), dtype=out_dtype, device=A.device)
+    _typed(out.dtype, (groups, M, N), out=out)
+    o = _opts(MX_F32, MX_SCALES_SWIZZLED, check=check_status)
+    _check(_lib.mx_gemm_grouped_k(A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), offsets.data_ptr(),
+                                  out.data_ptr(), _dtype_code(out.dtype), groups, M, N, rows, fmtA, fmtB,
+                                  ctypes.byref(o)), "mx_gemm_grouped_k")
     return out
 
 

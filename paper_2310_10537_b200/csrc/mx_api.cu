@@ -868,6 +868,311 @@ int mx_conv2d(const void* x_elems, const uint8_t* x_scales, const void* w_elems,
   return MX_OK;
 }
 
+// ---------------------------------------------------------------------------
+// RMS norm, routing, moving rows, the experts' products
+// ---------------------------------------------------------------------------
+
+static bool misaligned16(const void* p) { return (uintptr_t)p % 16 != 0; }
+static bool big(int64_t v) { return v >= (int64_t)1 << 31; }
+
+int mx_rmsnorm_quantize(const void* x, const void* residual, const void* weight, mx_dtype_t weight_dtype,
+                        float eps, int64_t rows, int64_t dim, void* h_out, void* y_out, void* elems_out,
+                        uint8_t* scales_out, mx_fmt_t fmt, mx_round_t rounding, const mx_opts_t* opts) {
+  Opts o;
+  View v;
+  if (!fmt_ok((int)fmt) || (rounding != MX_RNE && rounding != MX_RHAZ) || !read_opts(opts, &o) ||
+      ((int)weight_dtype != MX_F32 && (int)weight_dtype != MX_BF16))
+    return MX_ERR_FMT;
+  if (o.pad128) return MX_ERR_UNSUPPORTED;
+  const int64_t shape[2] = {rows, dim};
+  if (dim < 1 || !(eps >= 0.0f) || eps > 3.4e38f || !make_view(shape, 2, 1, &v)) return MX_ERR_SHAPE;
+  if (big(rows) || big(dim)) return MX_ERR_UNSUPPORTED;
+  if (rows == 0) return MX_OK;
+  if (!x || !weight || !elems_out || !scales_out) return MX_ERR_NULL;
+  if (misaligned16(x) || misaligned16(residual) || misaligned16(weight) || misaligned16(h_out) || misaligned16(y_out) ||
+      misaligned16(elems_out) || misaligned16(scales_out))
+    return MX_ERR_ALIGN;
+  cudaError_t e;
+  mx::RmsnormArgs a;
+  a.x = x; a.residual = residual; a.weight = weight; a.h_out = h_out; a.y_out = y_out;
+  a.elems = (uint8_t*)elems_out; a.scales = scales_out; a.rows = rows; a.dim = dim; a.eps = eps;
+  a.w_bf16 = (int)weight_dtype == MX_BF16; a.fmt = (int)fmt; a.rounding = (int)rounding; a.dtype = o.dtype;
+  a.layout = o.layout; a.stream = o.stream;
+  a.sm_count = sm_count(&e);
+  if (e != cudaSuccess) return fail_cuda(e);
+  e = mx::launch_rmsnorm_quantize(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+size_t mx_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t dim) {
+  if (rows < 0 || dim < 1 || big(rows) || big(dim)) return 0;
+  return align_up((size_t)mx::kNormPartials * (size_t)dim * 4, 256) + align_up((size_t)rows * 8, 256);
+}
+
+int mx_rmsnorm_backward(const void* dy, const void* h, const void* weight, mx_dtype_t weight_dtype, float eps,
+                        const void* dres, int64_t rows, int64_t dim, void* dh, float* dweight,
+                        const mx_opts_t* opts, void* workspace, size_t workspace_bytes) {
+  Opts o;
+  View v;
+  if (!read_opts(opts, &o) || ((int)weight_dtype != MX_F32 && (int)weight_dtype != MX_BF16)) return MX_ERR_FMT;
+  if (o.pad128) return MX_ERR_UNSUPPORTED;
+  const int64_t shape[2] = {rows, dim};
+  if (dim < 1 || !(eps >= 0.0f) || eps > 3.4e38f || !make_view(shape, 2, 1, &v)) return MX_ERR_SHAPE;
+  if (big(rows) || big(dim)) return MX_ERR_UNSUPPORTED;
+  if (!weight || !dweight || !workspace || (rows > 0 && (!dy || !h || !dh))) return MX_ERR_NULL;
+  if (misaligned16(dy) || misaligned16(h) || misaligned16(weight) || misaligned16(dres) || misaligned16(dh) ||
+      misaligned16(dweight) || (uintptr_t)workspace % 256)
+    return MX_ERR_ALIGN;
+  if (workspace_bytes < mx_rmsnorm_backward_workspace_bytes(rows, dim)) return MX_ERR_WORKSPACE;
+  cudaError_t e;
+  if (rows == 0) {
+    e = cudaMemsetAsync(dweight, 0, (size_t)dim * 4, o.stream);
+    return e == cudaSuccess ? MX_OK : fail_cuda(e);
+  }
+  mx::RmsnormBackwardArgs a;
+  a.dy = dy; a.h = h; a.weight = weight; a.dres = dres; a.dh = dh; a.dweight = dweight;
+  a.partial = (float*)workspace;
+  a.stats = (float2*)((char*)workspace + align_up((size_t)mx::kNormPartials * (size_t)dim * 4, 256));
+  a.rows = rows; a.dim = dim; a.eps = eps; a.w_bf16 = (int)weight_dtype == MX_BF16; a.dtype = o.dtype;
+  a.stream = o.stream;
+  a.sm_count = sm_count(&e);
+  if (e != cudaSuccess) return fail_cuda(e);
+  e = mx::launch_rmsnorm_backward(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+// What mx_route and mx_route_backward ask of their arguments alike; `choice`: the groups count too.
+static int route_validate(int64_t tokens, int64_t experts, const mx_route_t* r, const Opts& o, bool choice) {
+  if (r->score != MX_SCORE_SOFTMAX && r->score != MX_SCORE_SIGMOID) return MX_ERR_FMT;
+  if (choice && r->group_score != MX_GROUP_MAX && r->group_score != MX_GROUP_TOP2) return MX_ERR_FMT;
+  if (o.pad128) return MX_ERR_UNSUPPORTED;
+  if (tokens < 0 || experts < 1 || r->topk < 1 || r->topk > experts) return MX_ERR_SHAPE;
+  if (choice && (r->groups < 1 || experts % r->groups || r->topk_groups < 1 || r->topk_groups > r->groups ||
+                 r->topk > r->topk_groups * (experts / r->groups)))
+    return MX_ERR_SHAPE;
+  if (experts > 1024 || r->topk > 32 || (choice && r->groups > 32) || big(tokens)) return MX_ERR_UNSUPPORTED;
+  return MX_OK;
+}
+
+int mx_route(const void* logits, const float* bias, int64_t tokens, int64_t experts, const mx_route_t* route,
+             int32_t* ids_out, float* weights_out, const mx_opts_t* opts) {
+  Opts o;
+  if (!route) return MX_ERR_NULL;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = route_validate(tokens, experts, route, o, true);
+  if (rc != MX_OK) return rc;
+  if (tokens == 0) return MX_OK;
+  if (!logits || !ids_out || !weights_out) return MX_ERR_NULL;
+  if (misaligned16(logits) || (uintptr_t)bias % 4 || (uintptr_t)ids_out % 4 || (uintptr_t)weights_out % 4)
+    return MX_ERR_ALIGN;
+  mx::RouteArgs a = {};
+  a.logits = logits; a.bias = bias; a.ids = ids_out; a.weights = weights_out; a.tokens = tokens; a.experts = experts;
+  a.route = *route; a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_route(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+int mx_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t tokens,
+                      int64_t experts, const mx_route_t* route, void* dlogits, const mx_opts_t* opts) {
+  Opts o;
+  if (!route) return MX_ERR_NULL;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = route_validate(tokens, experts, route, o, false);
+  if (rc != MX_OK) return rc;
+  if (tokens == 0) return MX_OK;
+  if (!dweights || !logits || !ids || !dlogits) return MX_ERR_NULL;
+  if (misaligned16(logits) || misaligned16(dlogits) || (uintptr_t)dweights % 4 || (uintptr_t)ids % 4) return MX_ERR_ALIGN;
+  mx::RouteArgs a = {};
+  a.logits = logits; a.dweights = dweights; a.ids = const_cast<int32_t*>(ids); a.dlogits = dlogits;
+  a.tokens = tokens; a.experts = experts; a.route = *route; a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_route_backward(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+// The choices of a plan, and that row numbers stay below 2^31 with every group padded.
+static bool plan_ok(int64_t tokens, int64_t topk, int64_t experts, int64_t align) {
+  int64_t n;
+  return tokens >= 0 && topk >= 1 && experts >= 1 && align >= 1 && align <= 1024 &&
+         !__builtin_mul_overflow(tokens, topk, &n) && n < ((int64_t)1 << 31) - ((int64_t)1 << 21);
+}
+
+int64_t mx_moe_rows(int64_t tokens, int64_t topk, int64_t experts, int64_t align) {
+  if (!plan_ok(tokens, topk, experts, align)) return 0;
+  const int64_t n = tokens * topk, used = n < experts ? n : experts;
+  return (n + used * (align - 1)) / align * align;
+}
+
+size_t mx_moe_plan_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts) {
+  if (!plan_ok(tokens, topk, experts, 1) || experts > 1024) return 0;
+  const int64_t chunks = (tokens * topk + mx::kPlanChunk - 1) / mx::kPlanChunk;
+  return align_up((size_t)(chunks < 1 ? 1 : chunks) * (size_t)experts * 4, 256);
+}
+
+int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t experts, int64_t align,
+                int32_t* offsets, int32_t* counts, int32_t* row_of, const mx_opts_t* opts,
+                void* workspace, size_t workspace_bytes) {
+  Opts o;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  if (!plan_ok(tokens, topk, experts, align)) return MX_ERR_SHAPE;
+  if (experts > 1024 || o.pad128) return MX_ERR_UNSUPPORTED;
+  const int64_t n = tokens * topk;
+  if (!offsets || !counts || !workspace || (n > 0 && (!ids || !row_of))) return MX_ERR_NULL;
+  if ((uintptr_t)ids % 4 || (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4 ||
+      misaligned16(workspace))
+    return MX_ERR_ALIGN;
+  if (workspace_bytes < mx_moe_plan_workspace_bytes(tokens, topk, experts)) return MX_ERR_WORKSPACE;
+  mx::MoePlanArgs a;
+  a.ids = ids; a.offsets = offsets; a.counts = counts; a.row_of = row_of; a.hist = (int32_t*)workspace;
+  a.n = n; a.experts = experts; a.align = align; a.sm_count = 0; a.stream = o.stream;
+  const cudaError_t e = mx::launch_moe_plan(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+// Extents that the row-moving calls share.  Row and choice numbers are 32-bit in the kernels.
+static int move_validate(int64_t tokens, int64_t topk, int64_t dim, int64_t rows, const Opts& o) {
+  int64_t n;
+  if (tokens < 0 || topk < 1 || dim < 1 || rows < 0) return MX_ERR_SHAPE;
+  if (__builtin_mul_overflow(tokens, topk, &n)) return MX_ERR_SHAPE;
+  if (o.pad128 || big(n) || big(rows + 128) || big(dim) || dim > kMaxElements / (rows + 128)) return MX_ERR_UNSUPPORTED;
+  return MX_OK;
+}
+
+int mx_moe_gather(const void* elems_in, const uint8_t* scales_in, int64_t tokens, int64_t topk, int64_t dim,
+                  mx_fmt_t fmt, const int32_t* offsets, const int32_t* counts, const int32_t* row_of,
+                  int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts) {
+  Opts o;
+  if (!fmt_ok((int)fmt) || !read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = move_validate(tokens, topk, dim, rows, o);
+  if (rc != MX_OK) return rc;
+  if (dim % 32 || experts < 1) return MX_ERR_SHAPE;
+  if (experts > 1024) return MX_ERR_UNSUPPORTED;
+  if (rows == 0) return MX_OK;
+  if (!offsets || !counts || !elems_out || !scales_out || (tokens > 0 && (!elems_in || !scales_in || !row_of)))
+    return MX_ERR_NULL;
+  if (misaligned16(elems_in) || misaligned16(scales_in) || misaligned16(elems_out) || misaligned16(scales_out) ||
+      (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4)
+    return MX_ERR_ALIGN;
+  mx::MoeMoveArgs a = {};
+  a.src = elems_in; a.scales_in = scales_in; a.offsets = offsets; a.counts = counts; a.row_of = row_of;
+  a.dst = elems_out; a.scales_out = scales_out; a.tokens = tokens; a.topk = topk; a.dim = dim; a.experts = experts;
+  a.rows = rows; a.bits = fmt_bits((int)fmt); a.layout = o.layout; a.stream = o.stream;
+  const cudaError_t e = mx::launch_moe_gather(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+int mx_moe_combine(const void* y, const float* weights, const int32_t* row_of, int64_t tokens, int64_t topk,
+                   int64_t dim, int64_t rows, void* out, const mx_opts_t* opts) {
+  Opts o;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = move_validate(tokens, topk, dim, rows, o);
+  if (rc != MX_OK) return rc;
+  if (tokens == 0) return MX_OK;
+  if ((rows > 0 && !y) || !row_of || !out) return MX_ERR_NULL;
+  if (misaligned16(y) || misaligned16(out) || (uintptr_t)weights % 4 || (uintptr_t)row_of % 4) return MX_ERR_ALIGN;
+  mx::MoeMoveArgs a = {};
+  a.y = y; a.weights = weights; a.row_of = row_of; a.dst = out; a.tokens = tokens; a.topk = topk; a.dim = dim;
+  a.rows = rows; a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_moe_combine(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+int mx_moe_combine_backward(const void* dout, const void* y, const float* weights, const int32_t* offsets,
+                            const int32_t* counts, const int32_t* row_of, int64_t tokens, int64_t topk,
+                            int64_t dim, int64_t experts, int64_t rows, void* dy, float* dweights,
+                            const mx_opts_t* opts) {
+  Opts o;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = move_validate(tokens, topk, dim, rows, o);
+  if (rc != MX_OK) return rc;
+  if (experts < 1) return MX_ERR_SHAPE;
+  if (experts > 1024) return MX_ERR_UNSUPPORTED;
+  if (tokens == 0 && rows == 0) return MX_OK;
+  if (!offsets || !counts || (rows > 0 && !dy) || (tokens > 0 && (!dout || !row_of))) return MX_ERR_NULL;
+  if (rows > 0 && (y == nullptr) != (dweights == nullptr)) return MX_ERR_NULL;
+  if (misaligned16(dout) || misaligned16(y) || misaligned16(dy) || (uintptr_t)weights % 4 || (uintptr_t)dweights % 4 ||
+      (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4)
+    return MX_ERR_ALIGN;
+  mx::MoeMoveArgs a = {};
+  a.src = dout; a.y = y; a.weights = weights; a.offsets = offsets; a.counts = counts; a.row_of = row_of; a.dst = dy;
+  a.dweights = dweights; a.tokens = tokens; a.topk = topk; a.dim = dim; a.experts = experts; a.rows = rows;
+  a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_moe_combine_backward(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+static int grouped_run(const mx::GroupedArgs& args, const Opts& o) {
+  mx::GroupedArgs a = args;
+  cudaError_t e;
+  a.stream = o.stream;
+  a.sm_count = sm_count(&e);
+  if (e != cudaSuccess) return fail_cuda(e);
+  int rc = mx::launch_gemm_grouped(a, &e);
+  if (rc != MX_OK) return rc == MX_ERR_CUDA ? fail_cuda(e) : rc;
+  if (o.check) {
+    unsigned int st = 0;
+    rc = mx::gemm_grouped_status(o.stream, &st, &e);
+    if (rc != MX_OK) return fail_cuda(e);
+    if (st != 0) {
+      std::snprintf(g_cuda_error, sizeof(g_cuda_error), "device-side wait %u of a grouped product gave up (1 producer/"
+                    "stage empty, 2 MMA/stage full, 3 MMA/accumulator free, 4 epilogue/accumulator full)", st);
+      return MX_ERR_TIMEOUT;
+    }
+  }
+  return MX_OK;
+}
+
+int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                    void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
+                    mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+  Opts o;
+  if (!fmt_ok((int)fmtA) || !fmt_ok((int)fmtB) || !read_opts(opts, &o) ||
+      ((int)c_dtype != MX_F32 && (int)c_dtype != MX_BF16))
+    return MX_ERR_FMT;
+  if (fmtA == MX_INT8 || fmtB == MX_INT8 || o.pad128 || o.layout != MX_SCALES_SWIZZLED) return MX_ERR_UNSUPPORTED;
+  if (groups < 0 || rows < 0 || N < 0 || N % 128 || K < 32 || K % 32) return MX_ERR_SHAPE;
+  if ((fmt_bits((int)fmtA) < 8 || fmt_bits((int)fmtB) < 8) && K % 128) return MX_ERR_SHAPE;
+  if (big(rows + 1024) || big(N) || big(K)) return MX_ERR_SHAPE;
+  if (groups > 1024) return MX_ERR_UNSUPPORTED;
+  if (big(groups * N) || big((N / 128 + 1) * (groups + rows / 64))) return MX_ERR_SHAPE;  // rows of B, work items
+  if (groups == 0 || rows == 0 || N == 0) return MX_OK;
+  if (!A || !sA || !B || !sB || !offsets || !C) return MX_ERR_NULL;
+  if ((uintptr_t)A % 32 || (uintptr_t)B % 32 || misaligned16(sA) || misaligned16(sB) || misaligned16(C) ||
+      (uintptr_t)offsets % 4)
+    return MX_ERR_ALIGN;
+  mx::GroupedArgs a = {};
+  a.W = B; a.sW = sB; a.X = A; a.sX = sA; a.offsets = offsets; a.C = C; a.c_bf16 = (int)c_dtype == MX_BF16;
+  a.k_groups = 0; a.groups = groups; a.w_rows = N; a.x_rows = rows; a.K = K; a.fmtW = (int)fmtB; a.fmtX = (int)fmtA;
+  return grouped_run(a, o);
+}
+
+int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                      void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
+                      mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+  Opts o;
+  if (!fmt_ok((int)fmtA) || !fmt_ok((int)fmtB) || !read_opts(opts, &o) ||
+      ((int)c_dtype != MX_F32 && (int)c_dtype != MX_BF16))
+    return MX_ERR_FMT;
+  if (fmtA == MX_INT8 || fmtB == MX_INT8 || o.pad128 || o.layout != MX_SCALES_SWIZZLED) return MX_ERR_UNSUPPORTED;
+  if (groups < 0 || M < 0 || N < 0 || rows < 0 || N % 8 || rows % 32) return MX_ERR_SHAPE;
+  if ((fmt_bits((int)fmtA) < 8 || fmt_bits((int)fmtB) < 8) && rows % 128) return MX_ERR_SHAPE;
+  if (big(M + 1024) || big(N) || big(rows)) return MX_ERR_SHAPE;
+  if (groups > 1024) return MX_ERR_UNSUPPORTED;
+  if (big(groups * (N / 256 + 1) * (M / 64 + 1)) || groups * M > kMaxElements / (N + 1)) return MX_ERR_SHAPE;
+  if (groups == 0 || M == 0 || N == 0) return MX_OK;
+  if (!C || !offsets) return MX_ERR_NULL;
+  if (misaligned16(C) || (uintptr_t)offsets % 4) return MX_ERR_ALIGN;
+  if (rows == 0) {  // every group is empty
+    const cudaError_t e = cudaMemsetAsync(C, 0, (size_t)(groups * M * N) * ((int)c_dtype == MX_BF16 ? 2 : 4), o.stream);
+    return e == cudaSuccess ? MX_OK : fail_cuda(e);
+  }
+  if (!A || !sA || !B || !sB) return MX_ERR_NULL;
+  if ((uintptr_t)A % 32 || (uintptr_t)B % 32 || misaligned16(sA) || misaligned16(sB)) return MX_ERR_ALIGN;
+  mx::GroupedArgs a = {};
+  a.W = B; a.sW = sB; a.X = A; a.sX = sA; a.offsets = offsets; a.C = C; a.c_bf16 = (int)c_dtype == MX_BF16;
+  a.k_groups = 1; a.groups = groups; a.w_rows = N; a.x_rows = M; a.K = rows; a.fmtW = (int)fmtB; a.fmtX = (int)fmtA;
+  return grouped_run(a, o);
+}
+
 size_t mx_gemm_host_workspace_bytes(int64_t M, int64_t N, int64_t K, mx_fmt_t fmtA, mx_fmt_t fmtB) {
   if (!fmt_ok((int)fmtA) || !fmt_ok((int)fmtB) || M < 0 || N < 0 || K < 0 || K % 32) return 0;
   return align_up((size_t)(M * K / 8 * fmt_bits((int)fmtA)), 256) +

@@ -1,0 +1,448 @@
+// The experts' products of a mixture-of-experts layer on MX operands, tcgen05 block-scaled MMA.
+//
+//   row groups   C[r, n]    = sum_k X[r, k] W[g(r), n, k]          X: the tokens' rows, sorted by group
+//   K groups     C[g, m, n] = sum_{k in group g} X[m, k] W[n, k]   (weight gradients)
+//
+// The group sizes are known on the device only, and they are ragged.  Therefore the regular operand W
+// takes the M side of the MMA -- a CTA pair multiplies 256 of its rows -- and the ragged operand X its
+// N side, whose extent is a run-time field of the instruction: a tile has as many columns as the
+// group has rows left (a multiple of 32, at most max_n), and no MMA work is spent on rows that are not
+// there.  With X on the M side a group of 300 rows would cost 512.  The accumulator holds C transposed
+// (lane = column of C, TMEM column = row of C); a warp stores 32 consecutive columns of one row at a time.
+//
+// One pair of CTAs per two SMs, persistent over the items (group, W tile, X tile) in that order, which
+// every role of the kernel walks by itself from a table of the groups' first items that each CTA
+// makes in shared memory.  Per CTA:
+//   warp 0     copies: 128 rows of W, its half of the X rows, the stage's scale chunks -> one
+//              barrier per stage (the leader's)
+//   warp 1     (leader) scale chunks shared -> tensor memory, then four MMAs, from the same thread:
+//              copies and MMAs of one thread execute in order, so no hand-over lies between them
+//   warps 2-9  epilogue; two accumulators, so that it runs under the next item's MMAs
+// Every wait is bounded (see mbar_wait); on expiry a status word is set and all roles fall through to
+// the common exit.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "mx.h"
+#include "mx_device.cuh"
+#include "mx_launch.h"
+#include "mx_tcgen05.cuh"
+#include "mx_tmap.h"
+
+namespace mx {
+namespace {
+
+constexpr int kBK = 128;               // K elements per stage: 4 MX blocks, 4 MMAs
+constexpr uint32_t kThreads = 320;     // 10 warps
+constexpr uint32_t kTmemCols = 512;
+constexpr long long kSpinLimit = 2000000000LL;  // budget of a wait in cycles (~1 s)
+constexpr uint32_t kMaxStages = 10;
+constexpr uint32_t kWBytes = 128 * kBK;         // one byte per element in shared memory
+constexpr uint32_t kXBoxRows = 16;              // rows of X per copy (half a 32-row step per CTA)
+
+enum : unsigned int {
+  ST_PRODUCER_WAIT = 1,   // a stage never became empty
+  ST_MMA_WAIT_FULL = 2,   // a stage never became full
+  ST_MMA_WAIT_ACC = 3,    // an accumulator was never drained
+  ST_EPILOGUE_WAIT = 4,   // an accumulator never became full
+};
+__device__ unsigned int g_grouped_status;
+
+struct GroupedParams {
+  const int32_t* offsets;
+  void* C;
+  uint32_t c_bf16, groups, w_rows, x_rows, k_chunks;  // k_chunks: of the whole K axis
+  uint32_t max_n, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
+  long long spin_limit;
+};
+
+// One tile of C for a pair: W rows w0 .. w0 + 255, X rows x0 .. x0 + n - 1 (n a multiple of 32, those
+// from x_end on are not stored), K chunks k0 .. k0 + nk - 1.
+struct Item {
+  uint32_t group, w0, x0, n, x_end, k0, nk;
+};
+
+// Tables in shared memory: groups' offsets (rows, or K chunks) and first items.
+struct Tables {
+  const uint32_t* offset;
+  const uint32_t* first;
+};
+
+// X rows of a group in tiles of at most max_n, as even as whole steps of 32 allow, starting at
+// multiples of 64 (where the scale bytes of a tile's first row may lie in their TMEM columns).
+__device__ __forceinline__ uint32_t x_tiles(uint32_t rows, uint32_t max_n) { return (rows + max_n - 1) / max_n; }
+__device__ __forceinline__ uint32_t x_step(uint32_t rows, uint32_t tiles) { return ((rows + tiles - 1) / tiles + 63u) & ~63u; }
+
+template <bool KG>
+__device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& tb, uint32_t t, uint32_t& g, Item& it) {
+  while (g < p.groups && t >= tb.first[g + 1]) ++g;
+  if (g >= p.groups) return false;
+  const uint32_t o = tb.offset[g], len = tb.offset[g + 1] > o ? tb.offset[g + 1] - o : 0u;
+  const uint32_t rows = KG ? p.x_rows : len;
+  const uint32_t tiles = x_tiles(rows, p.max_n), step = x_step(rows, tiles);
+  const uint32_t j = t - tb.first[g], wt = j / tiles, xt = j - wt * tiles;
+  it.group = g;
+  it.w0 = wt * 256;
+  it.x0 = xt * step;
+  const uint32_t left = it.x0 < rows ? rows - it.x0 : 0u;  // (rounding the step up can leave a last tile without rows)
+  it.n = min(step, (left + 31u) & ~31u);
+  it.x_end = min(rows, it.x0 + it.n);
+  if (KG) {
+    it.k0 = o;
+    it.nk = len;
+  } else {
+    it.x0 += o;
+    it.x_end += o;
+    it.k0 = 0;
+    it.nk = p.k_chunks;
+  }
+  return true;
+}
+
+// Offsets as the kernel may use them: clamped to the tensor, on the grid, in units of rows (KG: of K chunks).
+template <bool KG>
+__device__ __forceinline__ uint32_t sane_offset(const GroupedParams& p, int32_t raw) {
+  const uint32_t v = raw > 0 ? (uint32_t)raw : 0u;
+  if (KG) return min(v / (uint32_t)kBK, p.k_chunks);
+  return v >= p.x_rows ? p.x_rows : (v & ~63u);
+}
+
+__device__ __forceinline__ void raise_abort(volatile uint32_t* abort_flag, unsigned int code) {
+  atomicCAS(&g_grouped_status, 0u, code);
+  *abort_flag = 1u;
+}
+
+template <bool KG>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
+                       const __grid_constant__ CUtensorMap tmap_sw, const __grid_constant__ CUtensorMap tmap_sx,
+                       const GroupedParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t stage_bytes = kWBytes + p.x_stage_bytes;   // operands; a multiple of 1024
+  const uint32_t sf_bytes = 512u * p.sf_per_stage;
+  const uint32_t off_sf = p.stages * stage_bytes, off_bar = off_sf + p.stages * sf_bytes;
+  constexpr uint32_t kBars = 2 * kMaxStages + 4;
+  const uint32_t bar0 = smem_base + off_bar;
+  auto full_bar = [&](uint32_t s) { return bar0 + 8 * s; };
+  auto empty_bar = [&](uint32_t s) { return bar0 + 8 * (kMaxStages + s); };
+  auto acc_full_bar = [&](uint32_t a) { return bar0 + 8 * (2 * kMaxStages + a); };
+  auto acc_empty_bar = [&](uint32_t a) { return bar0 + 8 * (2 * kMaxStages + 2 + a); };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + off_bar + kBars * 8);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* offset = reinterpret_cast<uint32_t*>(smem_gen + off_bar + kBars * 8 + 16);
+  uint32_t* first = offset + p.groups + 1;
+
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const uint32_t bar0_leader = map_to_cta(bar0, 0);
+  auto leader_bar = [&](uint32_t local_bar) { return bar0_leader + (local_bar - bar0); };
+
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < p.stages; ++s) {
+      mbar_init(full_bar(s), 1);   // used in the leader: its producer's arrive + the bytes of both CTAs
+      mbar_init(empty_bar(s), 1);  // a tcgen05.commit, delivered to both
+    }
+    for (uint32_t a = 0; a < 2; ++a) {
+      mbar_init(acc_full_bar(a), 1);
+      mbar_init(acc_empty_bar(a), 16);  // used in the leader: eight epilogue warps in each CTA
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_w)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_x)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_sw)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmap_sx)) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  // Programmatic stream serialization: all above overlapped the kernel before; from here on its
+  // results are read (the offsets first).
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (uint32_t g = threadIdx.x; g <= p.groups; g += kThreads) offset[g] = sane_offset<KG>(p, __ldg(p.offsets + g));
+  __syncthreads();
+  if (warp == 0) {  // first item of every group: a running sum, 32 groups at a time
+    const uint32_t w_tiles = (p.w_rows + 255) / 256;
+    uint32_t run = 0;
+    for (uint32_t g0 = 0; g0 <= p.groups; g0 += 32) {
+      const uint32_t g = g0 + lane;
+      uint32_t items = 0;
+      if (g < p.groups) {
+        const uint32_t len = offset[g + 1] > offset[g] ? offset[g + 1] - offset[g] : 0u;
+        items = w_tiles * x_tiles(KG ? p.x_rows : len, p.max_n);
+      }
+      uint32_t scan = items;
+#pragma unroll
+      for (uint32_t o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += v;
+      }
+      if (g <= p.groups) first[g] = run + scan - items;
+      run += __shfl_sync(0xffffffffu, scan, 31);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // the peer's barriers exist before anything is signalled remotely
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const Tables tb = {offset, first};
+  const uint32_t sf_col0 = 2 * p.max_n;
+
+  if (warp == 0) {
+    // ------------------------------ copies (both CTAs) ------------------------------
+    uint32_t stage = 0, phase = 0, g = 0;
+    bool ok = true;
+    Item it;
+    for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
+      const uint32_t wrow = (KG ? 0u : it.group * p.w_rows) + it.w0 + rank * 128u;
+      const uint32_t half = it.n >> 1, xrow = it.x0 + rank * half, boxes = half / kXBoxRows;
+      const uint32_t sx0 = it.x0 >> 7, sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
+      const uint32_t tx = 2u * (p.w_box_bytes + boxes * p.x_box_bytes + 512u * (1u + sx_n));
+      for (uint32_t kc = 0; kc < it.nk; ++kc) {
+        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit));
+        if (!ok) {
+          raise_abort(abort_flag, ST_PRODUCER_WAIT);
+          break;
+        }
+        if (elect_one()) {
+          const uint32_t fb = leader_bar(full_bar(stage));
+          if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), tx);
+          const int kx = (int)((it.k0 + kc) * kBK), kz = (int)(it.k0 + kc);
+          const uint32_t dw = smem_base + stage * stage_bytes, dx = dw + kWBytes;
+          tma_load_3d_pair(dw, &tmap_w, kx, (int)wrow, 0, fb);
+          for (uint32_t b = 0; b < boxes; ++b)
+            tma_load_3d_pair(dx + b * (kXBoxRows * 128u), &tmap_x, kx, (int)(xrow + b * kXBoxRows), 0, fb);
+          const uint32_t ds = smem_base + off_sf + stage * sf_bytes;
+          tma_load_3d_pair(ds, &tmap_sw, 0, kz, (int)(wrow >> 7), fb);
+          for (uint32_t c = 0; c < sx_n; ++c) tma_load_3d_pair(ds + 512u * (1u + c), &tmap_sx, 0, kz, (int)(sx0 + c), fb);
+        }
+        __syncwarp();
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok) {  // let copies that are still in flight land before the CTA goes away
+      const long long t0 = clock64();
+      while (clock64() - t0 < 2000000LL) {}
+    }
+  } else if (warp == 1) {
+    // ------------------------------ MMA issuer (leader) ------------------------------
+    if (rank == 0) {
+      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, g = 0;
+      bool ok = true;
+      Item it;
+      for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_empty_bar(acc), acc_phase ^ 1u, abort_flag, 4 * p.spin_limit))) {
+          raise_abort(abort_flag, ST_MMA_WAIT_ACC);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + acc * p.max_n;
+        const uint32_t sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
+        const uint32_t sx_col = 4 + ((it.x0 & 127u) >> 5);  // a tile starts on row 0 or 64 of a scale chunk
+        const uint32_t idesc0 = p.idesc | ((it.n >> 3) << 17);
+        for (uint32_t kc = 0; kc < it.nk; ++kc) {
+          ok = __all_sync(0xffffffffu, mbar_wait(full_bar(stage), phase, abort_flag, p.spin_limit));
+          if (!ok) {
+            raise_abort(abort_flag, ST_MMA_WAIT_FULL);
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sf_smem = smem_base + off_sf + stage * sf_bytes;
+          const uint32_t sf_tmem = tmem_base + sf_col0 + stage * (4u * p.sf_per_stage);
+          const uint64_t wdesc = operand_desc(smem_base + stage * stage_bytes);
+          const uint64_t xdesc = operand_desc(smem_base + stage * stage_bytes + kWBytes);
+          if (elect_one()) {
+            for (uint32_t c = 0; c <= sx_n; ++c) tc_cp_scales_pair(sf_tmem + 4 * c, scale_desc(sf_smem + 512 * c));
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)  // byte k of each scale column belongs to MX block k of the stage
+              tc_mma_pair(d_tmem, wdesc + 2 * k, xdesc + 2 * k, idesc0 | (k << 4) | (k << 29), sf_tmem, sf_tmem + sx_col,
+                          (kc | k) != 0 ? 1u : 0u);
+            tc_commit_pair(empty_bar(stage));
+          }
+          __syncwarp();
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok && elect_one()) tc_commit_pair(acc_full_bar(acc));
+        __syncwarp();
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------ epilogue (both CTAs) ------------------------------
+    // Warps q and q + 4 share the TMEM lanes 32 q .. 32 q + 31 and take alternate steps of 32 X rows.
+    const uint32_t quarter = warp & 3u, odd = (warp - 2u) >> 2;
+    uint32_t acc = 0, acc_phase = 0, g = 0;
+    Item it;
+    for (uint32_t t = pair; next_item<KG>(p, tb, t, g, it); t += num_pairs) {
+      if (!mbar_wait(acc_full_bar(acc), acc_phase, abort_flag, 4 * p.spin_limit)) {
+        if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t n = it.w0 + rank * 128u + quarter * 32u + lane;  // this thread's column of C
+      const size_t row_base = KG ? (size_t)it.group * p.x_rows : 0;
+      const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + acc * p.max_n;
+      for (uint32_t c = 32 * odd; c < it.n; c += 64) {
+        uint32_t r[32];
+        if (it.nk != 0) {
+          tc_ld32(taddr + c, r);
+          tc_wait_ld();
+        } else {  // an empty K group: no MMA has written the accumulator
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = 0u;
+        }
+        if (n < p.w_rows) {
+          const uint32_t r0 = it.x0 + c, live = it.x_end > r0 ? it.x_end - r0 : 0u;
+          const size_t at = (row_base + r0) * p.w_rows + n;
+          if (p.c_bf16) {
+            uint16_t* dst = reinterpret_cast<uint16_t*>(p.C) + at;
+#pragma unroll
+            for (uint32_t j = 0; j < 32; ++j) {
+              uint16_t h;
+              asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(__uint_as_float(r[j])));
+              if (j < live) dst[(size_t)j * p.w_rows] = h;
+            }
+          } else {
+            float* dst = reinterpret_cast<float*>(p.C) + at;
+#pragma unroll
+            for (uint32_t j = 0; j < 32; ++j)
+              if (j < live) dst[(size_t)j * p.w_rows] = __uint_as_float(r[j]);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(leader_bar(acc_empty_bar(acc)));
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  // common exit: both CTAs leave together, then the pair's tensor memory is freed
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+  }
+}
+
+// ---- host side ---------------------------------------------------------------
+
+int fmt_bits(int f) { return f == MX_E2M1 ? 4 : ((f == MX_E3M2 || f == MX_E2M3) ? 6 : 8); }
+
+uint32_t mma_fmt_code(int f) {  // format field of the instruction descriptor
+  switch (f) {
+    case MX_E4M3: return 0;
+    case MX_E5M2: return 1;
+    case MX_E2M3: return 3;
+    case MX_E3M2: return 4;
+    default: return 5;  // MX_E2M1
+  }
+}
+
+bool encode(EncodeTiledFn fn, CUtensorMap* map, CUtensorMapDataType dt, const void* ptr, const cuuint64_t (&dims)[3],
+            const cuuint64_t (&strides)[2], const cuuint32_t (&box)[3], CUtensorMapSwizzle swz) {
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, dt, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Packed K-major operand [rows x K], box 128 elements x box_rows, 128-byte swizzle; 6- and 4-bit codes
+// are expanded to a byte each on the way in.
+bool operand_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, int fmt, uint64_t rows, uint64_t K, uint32_t box_rows) {
+  const int bits = fmt_bits(fmt);
+  const CUtensorMapDataType dt = bits == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                 : bits == 6 ? CU_TENSOR_MAP_DATA_TYPE_16U6_ALIGN16B
+                                             : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B;
+  const cuuint64_t pitch = K * (uint64_t)bits / 8;
+  return encode(fn, map, dt, ptr, {K, rows, 1}, {pitch, pitch * rows}, {(cuuint32_t)kBK, box_rows, 1},
+                CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+// Swizzled scale tensor as [groups of 128 rows][K chunks][128 words], a box per 512-byte chunk.
+bool scale_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K) {
+  const uint64_t k_chunks = (K + kBK - 1) / kBK;
+  return encode(fn, map, CU_TENSOR_MAP_DATA_TYPE_UINT32, ptr, {128, k_chunks, (rows + 127) / 128},
+                {512, 512 * k_chunks}, {128, 1, 1}, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+template <bool KG>
+cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
+  CUtensorMap mw, mx_, msw, msx;
+  const uint64_t w_all = (uint64_t)a.w_rows * (KG ? 1u : (uint64_t)a.groups);
+  if (!operand_map(fn, &mw, a.W, a.fmtW, w_all, (uint64_t)a.K, 128) ||
+      !operand_map(fn, &mx_, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, kXBoxRows) ||
+      !scale_map(fn, &msw, a.sW, w_all, (uint64_t)a.K) || !scale_map(fn, &msx, a.sX, (uint64_t)a.x_rows, (uint64_t)a.K))
+    return cudaErrorInvalidValue;
+  GroupedParams p;
+  p.offsets = a.offsets; p.C = a.C; p.c_bf16 = (uint32_t)a.c_bf16; p.groups = (uint32_t)a.groups;
+  p.w_rows = (uint32_t)a.w_rows; p.x_rows = (uint32_t)a.x_rows; p.k_chunks = (uint32_t)((a.K + kBK - 1) / kBK);
+  // The widest tile: 192 columns, twice (two accumulators), leave 128 TMEM columns for the scales of
+  // seven stages.  Groups that hold 64 rows on average take tiles of 64: a stage is then smaller and
+  // more stages of W are in flight, which is what bounds a product with few rows.
+  const int64_t avg = KG ? a.x_rows : a.x_rows / (a.groups ? a.groups : 1);
+  p.max_n = avg <= 64 ? 64 : avg <= 128 ? 128 : 192;
+  // scale chunks per stage: one of W, and X rows 64 .. 64 + max_n - 1 of a chunk grid of 128
+  p.sf_per_stage = 1 + (p.max_n == 64 ? 1 : 2);
+  p.x_stage_bytes = p.max_n / 2 * 128;
+  const uint32_t fixed = 1024 + (2 * kMaxStages + 4) * 8 + 16 + 2 * (p.groups + 1) * 4;
+  const uint32_t per_stage = kWBytes + p.x_stage_bytes + 512 * p.sf_per_stage;
+  p.stages = (232448u - fixed) / per_stage;
+  const uint32_t tmem_stages = (kTmemCols - 2 * p.max_n) / (4 * p.sf_per_stage);
+  if (p.stages > tmem_stages) p.stages = tmem_stages;
+  if (p.stages > kMaxStages) p.stages = kMaxStages;
+  const uint32_t smem = fixed + p.stages * per_stage;
+  // a_format [7,10), b_format [10,13), scale format E8M0 (bit 23), M = 256; N is set per item
+  p.idesc = (mma_fmt_code(a.fmtW) << 7) | (mma_fmt_code(a.fmtX) << 10) | (1u << 23) | ((uint32_t)(256 >> 4) << 24);
+  // bytes a copy reports: packed source bytes, rows past the end included
+  p.w_box_bytes = (uint32_t)(128 * kBK * fmt_bits(a.fmtW) / 8);
+  p.x_box_bytes = (uint32_t)(kXBoxRows * kBK * fmt_bits(a.fmtX) / 8);
+  p.spin_limit = kSpinLimit;
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(mx_gemm_grouped_kernel<KG>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  // no more pairs than items there can be: every group at most one tile more than its share of rows
+  const int64_t w_tiles = (a.w_rows + 255) / 256;
+  const int64_t most = KG ? a.groups * w_tiles * ((a.x_rows + p.max_n - 1) / p.max_n)
+                          : w_tiles * (a.groups + a.x_rows / p.max_n);
+  const uint32_t pairs = most < a.sm_count / 2 ? (uint32_t)most : (uint32_t)(a.sm_count / 2);
+  return launch_pdl(mx_gemm_grouped_kernel<KG>, dim3(2 * pairs), dim3(kThreads), smem, a.stream, mw, mx_, msw, msx, p);
+}
+
+}  // namespace
+
+int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err) {
+  *cuda_err = cudaSuccess;
+  EncodeTiledFn fn = encode_fn(cuda_err);
+  if (!fn) return MX_ERR_CUDA;
+  *cuda_err = a.k_groups ? launch_kernel<true>(a, fn) : launch_kernel<false>(a, fn);
+  return *cuda_err == cudaSuccess ? MX_OK : MX_ERR_CUDA;
+}
+
+// Reads and clears the device status word (synchronises the stream first).
+int gemm_grouped_status(cudaStream_t stream, unsigned int* out, cudaError_t* cuda_err) {
+  *cuda_err = cudaStreamSynchronize(stream);
+  if (*cuda_err == cudaSuccess) *cuda_err = cudaMemcpyFromSymbol(out, g_grouped_status, sizeof(unsigned int));
+  if (*cuda_err == cudaSuccess && *out != 0) {
+    const unsigned int zero = 0;
+    *cuda_err = cudaMemcpyToSymbol(g_grouped_status, &zero, sizeof(unsigned int));
+  }
+  return *cuda_err == cudaSuccess ? MX_OK : MX_ERR_CUDA;
+}
+
+}  // namespace mx

@@ -116,4 +116,92 @@ int launch_gemm(const GemmArgs& a, cudaError_t* cuda_err);
 // bounded device-side wait sets when it gives up (0 = every wait completed).
 int gemm_status(cudaStream_t stream, unsigned int* status, cudaError_t* cuda_err);
 
+struct RmsnormArgs {
+  const void *x, *residual, *weight;
+  void *h_out, *y_out;
+  uint8_t *elems, *scales;
+  int64_t rows, dim;
+  float eps;
+  int w_bf16, fmt, rounding, dtype, layout;
+  int sm_count;
+  cudaStream_t stream;
+};
+cudaError_t launch_rmsnorm_quantize(const RmsnormArgs& a);
+
+// Partial sums of the weight gradient (rows of `partial`) that the backward pass writes at most.
+constexpr int kNormPartials = 296;
+struct RmsnormBackwardArgs {
+  const void *dy, *h, *weight, *dres;
+  void* dh;
+  float* dweight;
+  float* partial;   // [kNormPartials x dim]
+  float2* stats;    // [rows]
+  int64_t rows, dim;
+  float eps;
+  int w_bf16, dtype;
+  int sm_count;
+  cudaStream_t stream;
+};
+cudaError_t launch_rmsnorm_backward(const RmsnormBackwardArgs& a);
+
+struct RouteArgs {
+  const void* logits;
+  const float* bias;
+  const float* dweights;  // backward only
+  int32_t* ids;           // written forward, read backward
+  float* weights;
+  void* dlogits;
+  int64_t tokens, experts;
+  mx_route_t route;
+  int dtype;
+  int sm_count;
+  cudaStream_t stream;
+};
+cudaError_t launch_route(const RouteArgs& a);
+cudaError_t launch_route_backward(const RouteArgs& a);
+
+constexpr int kPlanChunk = 2048;  // choices that one CTA of the plan sorts
+struct MoePlanArgs {
+  const int32_t* ids;
+  int32_t *offsets, *counts, *row_of, *hist;  // hist: [chunks x experts]
+  int64_t n, experts, align;
+  int sm_count;
+  cudaStream_t stream;
+};
+cudaError_t launch_moe_plan(const MoePlanArgs& a);
+
+struct MoeMoveArgs {
+  const void *src, *y;       // rows of the tokens (MX codes or floats); combine: src unused
+  const uint8_t* scales_in;
+  const float* weights;
+  const int32_t *offsets, *counts, *row_of;
+  void* dst;
+  uint8_t* scales_out;
+  float* dweights;
+  int64_t tokens, topk, dim, experts, rows;
+  int bits, dtype, layout;
+  int sm_count;
+  cudaStream_t stream;
+};
+cudaError_t launch_moe_gather(const MoeMoveArgs& a);
+cudaError_t launch_moe_combine(const MoeMoveArgs& a);
+cudaError_t launch_moe_combine_backward(const MoeMoveArgs& a);
+
+// The experts' products (see mx_gemm_grouped() and mx_gemm_grouped_k()).  W is the operand on the
+// M side of the MMA, X the ragged one on its N side; C is [.. x X rows x W rows].
+struct GroupedArgs {
+  const void *W, *X;
+  const uint8_t *sW, *sX;
+  const int32_t* offsets;
+  void* C;
+  int c_bf16;
+  int k_groups;  // 0: groups of X rows, each with w_rows rows of W; 1: groups along K
+  int64_t groups, w_rows, x_rows, K;
+  int fmtW, fmtX;
+  int sm_count;
+  cudaStream_t stream;
+};
+int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err);
+int gemm_grouped_status(cudaStream_t stream, unsigned int* status, cudaError_t* cuda_err);
+
 }  // namespace mx

@@ -1,0 +1,440 @@
+// Rows of tokens to their experts and back: the plan (a stable counting sort of the choices by expert),
+// the gather of MX rows into expert order, the weighted sum back to the tokens and its backward pass.
+// Everything here is bound by the rows it moves: each is read once and written once.
+#include <cuda_runtime.h>
+
+#include "mx.h"
+#include "mx_device.cuh"
+#include "mx_launch.h"
+#include "mx_rows.cuh"
+
+namespace mx {
+namespace {
+
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr uint32_t kPlanThreads = 1024, kPlanWarps = 32, kPlanPerWarp = kPlanChunk / kPlanWarps;
+
+// ---- plan ------------------------------------------------------------------------------------------
+// A CTA sorts a chunk of kPlanChunk choices.  Ranks are exact and independent of timing: a warp takes
+// 64 consecutive choices, lanes with the same expert find each other with match_any, and the warps'
+// counts are added up in warp order.  With more than one chunk the chunks' histograms come first, in
+// a launch of their own, and every CTA adds up those before its own.
+
+struct PlanParams {
+  const int32_t* ids;
+  int32_t *offsets, *counts, *row_of, *hist;
+  uint32_t n, experts, align, chunks;
+};
+
+__global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const PlanParams p) {
+  extern __shared__ uint32_t count[];
+  pdl_prologue();
+  for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads) count[e] = 0;
+  __syncthreads();
+  const uint32_t c0 = blockIdx.x * kPlanChunk;
+  for (uint32_t i = c0 + threadIdx.x; i < min(p.n, c0 + kPlanChunk); i += kPlanThreads) {
+    const uint32_t e = (uint32_t)__ldg(p.ids + i);
+    if (e < p.experts) atomicAdd(&count[e], 1u);
+  }
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < p.experts; e += kPlanThreads)
+    p.hist[(size_t)blockIdx.x * p.experts + e] = (int32_t)count[e];
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanParams p) {
+  extern __shared__ uint32_t smem[];
+  uint32_t* first = smem;                                           // [experts] row of the chunk's first choice
+  uint16_t* count = reinterpret_cast<uint16_t*>(smem + p.experts);  // [warps][experts]
+  __shared__ uint32_t warp_total[32];
+  pdl_prologue();
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = p.experts;
+  for (uint32_t i = threadIdx.x; i < kPlanWarps * E; i += kPlanThreads) count[i] = 0;
+  __syncthreads();
+  uint32_t expert[kPlanPerWarp / 32], rank[kPlanPerWarp / 32];
+  uint16_t* mine = count + warp * E;
+  const uint32_t i0 = blockIdx.x * kPlanChunk + warp * kPlanPerWarp + lane;
+#pragma unroll
+  for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
+    const uint32_t i = i0 + 32 * k;
+    const uint32_t e = i < p.n ? (uint32_t)__ldg(p.ids + i) : 0xffffffffu;
+    const bool live = e < E;
+    const uint32_t peers = __match_any_sync(kFull, live ? e : 0xffffffffu);
+    const uint32_t before = live ? mine[e] : 0u;
+    __syncwarp();
+    if (live && (peers & ((1u << lane) - 1u)) == 0) mine[e] = (uint16_t)(before + __popc(peers));
+    __syncwarp();
+    expert[k] = live ? e : 0xffffffffu;
+    rank[k] = before + __popc(peers & ((1u << lane) - 1u));
+  }
+  __syncthreads();
+  // thread e: the warps' counts become ranks, the chunks' counts the chunk's start and the group's size
+  const uint32_t e = threadIdx.x;
+  uint32_t total = 0, base = 0;
+  if (e < E) {
+    for (uint32_t w = 0; w < kPlanWarps; ++w) {
+      const uint32_t c = count[w * E + e];
+      count[w * E + e] = (uint16_t)total;
+      total += c;
+    }
+    if (p.chunks > 1) {
+      total = 0;
+#pragma unroll 8
+      for (uint32_t c = 0; c < p.chunks; ++c) {
+        const uint32_t h = (uint32_t)p.hist[(size_t)c * E + e];
+        if (c < blockIdx.x) base += h;
+        total += h;
+      }
+    }
+  }
+  const uint32_t padded = (total + p.align - 1) / p.align * p.align;
+  uint32_t scan = padded;  // inclusive, over the experts
+#pragma unroll
+  for (uint32_t o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(kFull, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_total[warp] = scan;
+  __syncthreads();
+  uint32_t w = lane < warp ? warp_total[lane] : 0u;
+#pragma unroll
+  for (uint32_t o = 16; o; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
+  scan += w;
+  if (e < E) {
+    first[e] = scan - padded + base;
+    if (blockIdx.x == 0) {
+      p.counts[e] = (int32_t)total;
+      p.offsets[e] = (int32_t)(scan - padded);
+      if (e == E - 1) p.offsets[E] = (int32_t)scan;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
+    const uint32_t i = i0 + 32 * k;
+    if (i < p.n)
+      p.row_of[i] = expert[k] < E ? (int32_t)(first[expert[k]] + mine[expert[k]] + rank[k]) : -1;
+  }
+}
+
+// ---- rows that no choice maps to ---------------------------------------------------------------------
+// The blocks behind the tokens' blocks of a launch write them as zeros: `split` blocks per expert for
+// the rows that pad its group, then kTailBlocks blocks for the rows behind the last group.
+constexpr uint32_t kTailBlocks = 64;
+
+struct ZeroRows {
+  const int32_t *offsets, *counts;
+  uint32_t experts, rows, split;
+};
+inline uint32_t zero_split(int64_t experts) { return experts >= 256 ? 1u : (uint32_t)(256 / experts); }
+inline uint32_t zero_blocks(int64_t experts) { return (uint32_t)experts * zero_split(experts) + kTailBlocks; }
+
+// Calls f(row) for the rows that block `z` of the zero blocks owns.
+template <typename F>
+__device__ __forceinline__ void for_zero_rows(const ZeroRows& q, uint32_t z, F f) {
+  int64_t r0, r1;
+  uint32_t step, at;
+  if (z < q.experts * q.split) {
+    const uint32_t e = z / q.split;
+    r0 = (int64_t)__ldg(q.offsets + e) + __ldg(q.counts + e);
+    r1 = __ldg(q.offsets + e + 1);
+    step = q.split;
+    at = z - e * q.split;
+  } else {
+    r0 = __ldg(q.offsets + q.experts);
+    r1 = q.rows;
+    step = kTailBlocks;
+    at = z - q.experts * q.split;
+  }
+  if (r0 < 0) r0 = 0;
+  if (r1 > (int64_t)q.rows) r1 = q.rows;
+  for (int64_t r = r0 + at; r < r1; r += step) f((uint32_t)r);
+}
+
+// ---- gather ------------------------------------------------------------------------------------------
+
+struct GatherParams {
+  const uint8_t *elems_in, *scales_in;
+  const int32_t* row_of;
+  uint8_t *elems_out, *scales_out;
+  uint32_t tokens, topk, kblocks, row_bytes, layout, token_blocks;
+  ZeroRows zero;
+};
+
+constexpr uint32_t kMoveWarps = 8;
+
+// A warp per token: the row's codes pass through registers once and go to every row it is chosen for.
+template <typename Vec>
+__global__ void __launch_bounds__(32 * kMoveWarps) gather_kernel(const GatherParams p) {
+  constexpr uint32_t U = 8;  // vectors in flight per lane
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t vecs = p.row_bytes / sizeof(Vec), kchunks = (p.kblocks + 3) >> 2;
+  const bool swizzled = p.layout == MX_SCALES_SWIZZLED;
+  if (blockIdx.x < p.token_blocks) {
+    const uint32_t t = blockIdx.x * kMoveWarps + warp;
+    if (t >= p.tokens) return;
+    const int32_t* rows = p.row_of + (size_t)t * p.topk;
+    const Vec* src = reinterpret_cast<const Vec*>(p.elems_in + (size_t)t * p.row_bytes);
+    for (uint32_t v0 = lane; v0 < vecs; v0 += 32 * U) {
+      Vec v[U];
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u)
+        if (v0 + 32 * u < vecs) v[u] = __ldg(src + v0 + 32 * u);
+      for (uint32_t j = 0; j < p.topk; ++j) {
+        const uint32_t r = (uint32_t)__ldg(rows + j);
+        if (r >= p.zero.rows) continue;
+        Vec* dst = reinterpret_cast<Vec*>(p.elems_out + (size_t)r * p.row_bytes);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u)
+          if (v0 + 32 * u < vecs) dst[v0 + 32 * u] = v[u];
+      }
+    }
+    if (swizzled) {
+      for (uint32_t c = lane; c < kchunks; c += 32) {
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(
+            p.scales_in + scale_offset<MX_SCALES_SWIZZLED>(t, 4 * c, p.kblocks)));
+        for (uint32_t j = 0; j < p.topk; ++j) {
+          const uint32_t r = (uint32_t)__ldg(rows + j);
+          if (r < p.zero.rows)
+            *reinterpret_cast<uint32_t*>(p.scales_out + scale_offset<MX_SCALES_SWIZZLED>(r, 4 * c, p.kblocks)) = w;
+        }
+      }
+    } else {
+      for (uint32_t k = lane; k < p.kblocks; k += 32) {
+        const uint8_t b = __ldg(p.scales_in + (size_t)t * p.kblocks + k);
+        for (uint32_t j = 0; j < p.topk; ++j) {
+          const uint32_t r = (uint32_t)__ldg(rows + j);
+          if (r < p.zero.rows) p.scales_out[(size_t)r * p.kblocks + k] = b;
+        }
+      }
+    }
+    return;
+  }
+  const uint32_t z = blockIdx.x - p.token_blocks;
+  auto zero_scales = [&](uint32_t r) {
+    if (swizzled) {
+      for (uint32_t c = threadIdx.x; c < kchunks; c += blockDim.x)
+        *reinterpret_cast<uint32_t*>(p.scales_out + scale_offset<MX_SCALES_SWIZZLED>(r, 4 * c, p.kblocks)) = 0u;
+    } else {
+      for (uint32_t k = threadIdx.x; k < p.kblocks; k += blockDim.x) p.scales_out[(size_t)r * p.kblocks + k] = 0;
+    }
+  };
+  for_zero_rows(p.zero, z, [&](uint32_t r) {
+    Vec* dst = reinterpret_cast<Vec*>(p.elems_out + (size_t)r * p.row_bytes);
+    for (uint32_t v = threadIdx.x; v < vecs; v += blockDim.x) dst[v] = Vec{};
+    zero_scales(r);
+  });
+  if (swizzled && z >= p.zero.experts * p.zero.split) {  // scale rows that pad the tensor to 128
+    const uint32_t at = z - p.zero.experts * p.zero.split;
+    for (uint32_t r = p.zero.rows + at; r < ((p.zero.rows + 127u) & ~127u); r += kTailBlocks) zero_scales(r);
+  }
+}
+
+// ---- combine -----------------------------------------------------------------------------------------
+
+struct CombineParams {
+  const void *y, *dout;
+  const float* weights;
+  const int32_t* row_of;
+  void *out, *dy;
+  float* dweights;
+  uint32_t tokens, topk, dim, rows, token_blocks;
+  ZeroRows zero;
+};
+
+// A CTA per token.  VEC: 8 elements at a time (dim % 8 == 0), else one.
+template <int DTYPE, bool VEC>
+__global__ void __launch_bounds__(128) combine_kernel(const CombineParams p) {
+  pdl_prologue();
+  const uint32_t t = blockIdx.x;
+  const int32_t* rows = p.row_of + (size_t)t * p.topk;
+  const float* wt = p.weights ? p.weights + (size_t)t * p.topk : nullptr;
+  if constexpr (VEC) {
+    for (uint32_t g = threadIdx.x; g < p.dim / 8; g += blockDim.x) {
+      float acc[8] = {};
+#pragma unroll 4
+      for (uint32_t j = 0; j < p.topk; ++j) {
+        const uint32_t r = (uint32_t)__ldg(rows + j);
+        if (r >= p.rows) continue;
+        const float w = wt ? __ldg(wt + j) : 1.0f;
+        float f[8];
+        widen<DTYPE>(load_raw8<DTYPE>(p.y, (size_t)r * p.dim + 8 * (size_t)g), f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, f[e], acc[e]);
+      }
+      store8<DTYPE>(p.out, (size_t)t * p.dim + 8 * (size_t)g, acc);
+    }
+  } else {
+    for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {
+      float acc = 0.0f;
+      for (uint32_t j = 0; j < p.topk; ++j) {
+        const uint32_t r = (uint32_t)__ldg(rows + j);
+        if (r < p.rows) acc = fmaf(wt ? __ldg(wt + j) : 1.0f, load1<DTYPE>(p.y, (size_t)r * p.dim + c), acc);
+      }
+      store1<DTYPE>(p.out, (size_t)t * p.dim + c, acc);
+    }
+  }
+}
+
+// A CTA per token, kJ of its choices at a time: every choice's row of dy is written while its dot
+// product with dout is formed; the warps' partial products meet in shared memory in warp order.
+constexpr uint32_t kJ = 8, kBackWarps = 8;
+
+template <int DTYPE, bool VEC>
+__global__ void __launch_bounds__(32 * kBackWarps) combine_backward_kernel(const CombineParams p) {
+  pdl_prologue();
+  constexpr uint32_t G = VEC ? 8 : 1;
+  const uint32_t units = p.dim / G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x >= p.token_blocks) {
+    for_zero_rows(p.zero, blockIdx.x - p.token_blocks, [&](uint32_t r) {
+      for (uint32_t g = threadIdx.x; g < units; g += blockDim.x) {
+        if constexpr (VEC) {
+          const float zero[8] = {};
+          store8<DTYPE>(p.dy, (size_t)r * p.dim + 8 * (size_t)g, zero);
+        } else {
+          store1<DTYPE>(p.dy, (size_t)r * p.dim + g, 0.0f);
+        }
+      }
+    });
+    return;
+  }
+  __shared__ float dots[kBackWarps][kJ];
+  const uint32_t t = blockIdx.x;
+  for (uint32_t j0 = 0; j0 < p.topk; j0 += kJ) {
+    const uint32_t nj = min(kJ, p.topk - j0);
+    uint32_t row[kJ];
+    float w[kJ], dot[kJ];
+#pragma unroll
+    for (uint32_t j = 0; j < kJ; ++j) {
+      row[j] = j < nj ? (uint32_t)__ldg(p.row_of + (size_t)t * p.topk + j0 + j) : 0xffffffffu;
+      w[j] = j < nj && p.weights ? __ldg(p.weights + (size_t)t * p.topk + j0 + j) : 1.0f;
+      dot[j] = 0.0f;
+    }
+    for (uint32_t g = threadIdx.x; g < units; g += blockDim.x) {
+      if constexpr (VEC) {
+        float d[8];
+        widen<DTYPE>(load_raw8<DTYPE>(p.dout, (size_t)t * p.dim + 8 * (size_t)g), d);
+        Raw8<DTYPE> raw[kJ];
+        if (p.y) {
+#pragma unroll
+          for (uint32_t j = 0; j < kJ; ++j)
+            if (row[j] < p.rows) raw[j] = load_raw8<DTYPE>(p.y, (size_t)row[j] * p.dim + 8 * (size_t)g);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kJ; ++j) {
+          if (row[j] >= p.rows) continue;
+          float o[8];
+          if (p.y) {
+            widen<DTYPE>(raw[j], o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot[j] = fmaf(d[e], o[e], dot[j]);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = w[j] * d[e];
+          store8<DTYPE>(p.dy, (size_t)row[j] * p.dim + 8 * (size_t)g, o);
+        }
+      } else {
+        const float d = load1<DTYPE>(p.dout, (size_t)t * p.dim + g);
+#pragma unroll
+        for (uint32_t j = 0; j < kJ; ++j) {
+          if (row[j] >= p.rows) continue;
+          if (p.y) dot[j] = fmaf(d, load1<DTYPE>(p.y, (size_t)row[j] * p.dim + g), dot[j]);
+          store1<DTYPE>(p.dy, (size_t)row[j] * p.dim + g, w[j] * d);
+        }
+      }
+    }
+    if (!p.dweights) continue;
+#pragma unroll
+    for (uint32_t j = 0; j < kJ; ++j) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) dot[j] += __shfl_xor_sync(kFull, dot[j], o);
+      if (lane == 0) dots[warp][j] = dot[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < nj) {
+      float s = 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < kBackWarps; ++i) s += dots[i][threadIdx.x];
+      p.dweights[(size_t)t * p.topk + j0 + threadIdx.x] = s;
+    }
+    __syncthreads();
+  }
+}
+
+ZeroRows zero_rows(const MoeMoveArgs& a) {
+  ZeroRows z;
+  z.offsets = a.offsets; z.counts = a.counts; z.experts = (uint32_t)a.experts; z.rows = (uint32_t)a.rows;
+  z.split = zero_split(a.experts);
+  return z;
+}
+
+}  // namespace
+
+cudaError_t launch_moe_plan(const MoePlanArgs& a) {
+  PlanParams p;
+  p.ids = a.ids; p.offsets = a.offsets; p.counts = a.counts; p.row_of = a.row_of; p.hist = a.hist;
+  p.n = (uint32_t)a.n; p.experts = (uint32_t)a.experts; p.align = (uint32_t)a.align;
+  p.chunks = (uint32_t)((a.n + kPlanChunk - 1) / kPlanChunk);
+  const size_t smem = (size_t)a.experts * (sizeof(uint32_t) + kPlanWarps * sizeof(uint16_t));
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             1024 * (int)(sizeof(uint32_t) + kPlanWarps * sizeof(uint16_t)));
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  if (p.chunks > 1) {
+    e = launch_pdl(plan_count_kernel, dim3(p.chunks), dim3(kPlanThreads), sizeof(uint32_t) * a.experts, a.stream, p);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(plan_place_kernel, dim3(p.chunks ? p.chunks : 1), dim3(kPlanThreads), smem, a.stream, p);
+}
+
+cudaError_t launch_moe_gather(const MoeMoveArgs& a) {
+  GatherParams p;
+  p.elems_in = (const uint8_t*)a.src; p.scales_in = a.scales_in; p.row_of = a.row_of;
+  p.elems_out = (uint8_t*)a.dst; p.scales_out = a.scales_out;
+  p.tokens = (uint32_t)a.tokens; p.topk = (uint32_t)a.topk; p.kblocks = (uint32_t)(a.dim / 32);
+  p.row_bytes = (uint32_t)(a.dim * a.bits / 8); p.layout = (uint32_t)a.layout;
+  p.token_blocks = (p.tokens + kMoveWarps - 1) / kMoveWarps;
+  p.zero = zero_rows(a);
+  const dim3 grid(p.token_blocks + zero_blocks(a.experts)), block(32 * kMoveWarps);
+  // rows of 6-bit codes are multiples of 24 bytes: 8-byte vectors unless dim is a multiple of 64
+  return p.row_bytes % 16 == 0 ? launch_pdl(gather_kernel<uint4>, grid, block, 0, a.stream, p)
+                               : launch_pdl(gather_kernel<uint2>, grid, block, 0, a.stream, p);
+}
+
+static CombineParams combine_params(const MoeMoveArgs& a) {
+  CombineParams p;
+  p.y = a.y; p.dout = a.src; p.weights = a.weights; p.row_of = a.row_of; p.out = a.dst; p.dy = a.dst;
+  p.dweights = a.dweights; p.tokens = (uint32_t)a.tokens; p.topk = (uint32_t)a.topk; p.dim = (uint32_t)a.dim;
+  p.rows = (uint32_t)a.rows; p.token_blocks = p.tokens;
+  p.zero = {};
+  return p;
+}
+
+cudaError_t launch_moe_combine(const MoeMoveArgs& a) {
+  const CombineParams p = combine_params(a);
+  const dim3 grid(p.tokens), block(128);
+  if (a.dtype == MX_BF16)
+    return a.dim % 8 == 0 ? launch_pdl(combine_kernel<MX_BF16, true>, grid, block, 0, a.stream, p)
+                          : launch_pdl(combine_kernel<MX_BF16, false>, grid, block, 0, a.stream, p);
+  return a.dim % 8 == 0 ? launch_pdl(combine_kernel<MX_F32, true>, grid, block, 0, a.stream, p)
+                        : launch_pdl(combine_kernel<MX_F32, false>, grid, block, 0, a.stream, p);
+}
+
+cudaError_t launch_moe_combine_backward(const MoeMoveArgs& a) {
+  CombineParams p = combine_params(a);
+  p.zero = zero_rows(a);
+  const dim3 grid(p.token_blocks + zero_blocks(a.experts)), block(32 * kBackWarps);
+  if (a.dtype == MX_BF16)
+    return a.dim % 8 == 0 ? launch_pdl(combine_backward_kernel<MX_BF16, true>, grid, block, 0, a.stream, p)
+                          : launch_pdl(combine_backward_kernel<MX_BF16, false>, grid, block, 0, a.stream, p);
+  return a.dim % 8 == 0 ? launch_pdl(combine_backward_kernel<MX_F32, true>, grid, block, 0, a.stream, p)
+                        : launch_pdl(combine_backward_kernel<MX_F32, false>, grid, block, 0, a.stream, p);
+}
+
+}  // namespace mx

@@ -1,0 +1,487 @@
+// RMS norm with the residual's addition and MX output, and its backward pass.
+//
+//   h = x + residual;  s = rsqrt(mean(h^2) + eps);  y = h s w;  (P, X) = Algorithm 1 (y)
+//
+// Forward: one CTA per row.  The row is read once and stays in registers (FP32) while its sum of
+// squares is formed, so that the traffic is x, residual in and h, codes, scales out; a thread holds
+// groups of 8 consecutive elements, four neighbouring lanes an MX block, whose maximum takes two
+// shuffles.  y is never rounded before Algorithm 1.
+#include <cuda_runtime.h>
+
+#include "mx.h"
+#include "mx_device.cuh"
+#include "mx_launch.h"
+#include "mx_rows.cuh"
+
+namespace mx {
+namespace {
+
+struct NormParams {
+  const void *x, *residual, *weight;
+  void *h_out, *y_out;
+  uint8_t *elems, *scales;
+  uint32_t rows, dim, kblocks;
+  float eps, inv_dim;
+  uint32_t w_bf16, sticky, layout;
+};
+
+// 8 weights; the weights are shared by all rows and stay in the L1
+__device__ __forceinline__ void load_weight8(const void* w, uint32_t w_bf16, uint32_t elem, float (&f)[8]) {
+  if (w_bf16) {
+    widen4(__ldg(reinterpret_cast<const uint4*>((const char*)w + (size_t)elem * 2)), f);
+  } else {
+    const float4 a = __ldg(reinterpret_cast<const float4*>((const char*)w + (size_t)elem * 4));
+    const float4 b = __ldg(reinterpret_cast<const float4*>((const char*)w + (size_t)elem * 4) + 1);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+}
+__device__ __forceinline__ float weight1(const void* w, uint32_t w_bf16, uint32_t c) {
+  return w_bf16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)w + c) << 16) : __ldg((const float*)w + c);
+}
+
+// Sum over the CTA; every thread gets it.  `red` holds a float per warp and is not read again by
+// the caller before its next barrier.
+__device__ __forceinline__ float cta_sum(float v, float* red) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const uint32_t warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  float t = lane < warps ? red[lane] : 0.0f;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  return t;
+}
+
+template <int FMT>
+__device__ __forceinline__ void cast8_sticky(const float (&v)[8], const BlockScale& s, uint32_t sticky, uint32_t& lo,
+                                             uint32_t& hi) {
+  uint32_t p[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = mul_ftz(v[2 * i], s.m1), b = mul_ftz(v[2 * i + 1], s.m1);
+    if (FMT == MX_INT8) { a *= s.m2; b *= s.m2; }
+    // ties away from zero: the last mantissa bit set moves a tie past the half-way point (see cast_pair)
+    a = __uint_as_float(__float_as_uint(a) | sticky);
+    b = __uint_as_float(__float_as_uint(b) | sticky);
+    p[i] = cast_pair<FMT, MX_RNE>(a, b);
+  }
+  pack8<FMT>(p, lo, hi);
+  if (!s.finite) { lo = 0; hi = 0; }
+}
+
+__device__ __forceinline__ size_t scale_at(const NormParams& p, uint32_t row, uint32_t kb) {
+  return p.layout == MX_SCALES_LINEAR ? scale_offset<MX_SCALES_LINEAR>(row, kb, p.kblocks)
+                                      : scale_offset<MX_SCALES_SWIZZLED>(row, kb, p.kblocks);
+}
+
+// The scale words of the rows that pad a swizzled scale tensor to 128 rows, spread over the grid.
+__device__ __forceinline__ void zero_pad_rows(const NormParams& p) {
+  if (p.layout != MX_SCALES_SWIZZLED) return;
+  const uint32_t pad = (0u - p.rows) & 127u, kchunks = (p.kblocks + 3) >> 2;
+  for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < pad * kchunks; i += gridDim.x * blockDim.x) {
+    const uint32_t r = i / kchunks, c = i - r * kchunks;
+    *reinterpret_cast<uint32_t*>(p.scales + scale_offset<MX_SCALES_SWIZZLED>(p.rows + r, 4 * c, p.kblocks)) = 0u;
+  }
+}
+
+// dim % 8 == 0 and dim <= 8 * V * blockDim: the row in registers.
+template <int DTYPE, int FMT, int V>
+__global__ void __launch_bounds__(V == 4 ? 512 : 1024) rmsnorm_kernel(const NormParams p) {
+  constexpr uint32_t bits = FmtTraits<FMT>::bits;
+  __shared__ float red[32];
+  pdl_prologue();
+  const uint32_t T = blockDim.x, row = blockIdx.x, lane = threadIdx.x & 31;
+  const size_t base = (size_t)row * p.dim;
+  const uint32_t groups = p.dim >> 3;                 // of 8 elements that exist
+  const uint32_t groups_stored = p.kblocks * 4;       // whole blocks: the last one padded with zeros
+  float v[V][8];
+  float ss = 0.0f;
+  {
+    Raw8<DTYPE> a[V], b[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * T + threadIdx.x;
+      if (g < groups) {
+        a[i] = load_raw8<DTYPE>(p.x, base + 8 * (size_t)g);
+        if (p.residual) b[i] = load_raw8<DTYPE>(p.residual, base + 8 * (size_t)g);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * T + threadIdx.x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+      if (g < groups) {
+        widen<DTYPE>(a[i], v[i]);
+        if (p.residual) {
+          float r[8];
+          widen<DTYPE>(b[i], r);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[i][e] += r[e];
+        }
+        if (p.h_out) store8<DTYPE>(p.h_out, base + 8 * (size_t)g, v[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
+      }
+    }
+  }
+  const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);
+  uint8_t* out_row = p.elems + (size_t)row * p.kblocks * (4 * bits);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t g = i * T + threadIdx.x;
+    if (i * T + (threadIdx.x & ~31u) >= ((groups_stored + 15) & ~15u)) break;  // warp-uniform
+    if (g < groups) {
+      float w[8];
+      load_weight8(p.weight, p.w_bf16, 8 * g, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * s * w[e];
+      if (p.y_out) store8<DTYPE>(p.y_out, base + 8 * (size_t)g, v[i]);
+    }
+    float m[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[e] = absmax_nan(v[i][2 * e], v[i][2 * e + 1]);
+    float am = absmax_nan(absmax_nan(m[0], m[1]), absmax_nan(m[2], m[3]));
+    am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 1));
+    am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 2));
+    const BlockScale bs = block_scale<FMT>(am);
+    uint32_t lo, hi;
+    cast8_sticky<FMT>(v[i], bs, p.sticky, lo, hi);
+    if constexpr (bits == 6) {  // two lanes' 48 bits each fill three words
+      const uint32_t lo_next = __shfl_down_sync(0xffffffffu, lo, 1);
+      if (g < groups_stored) {
+        uint32_t* d = reinterpret_cast<uint32_t*>(out_row + 12 * (size_t)(g >> 1));
+        if ((lane & 1) == 0) {
+          d[0] = lo;
+          d[1] = __byte_perm(hi, lo_next, 0x5410);
+        } else {
+          d[2] = __byte_perm(lo, hi, 0x5432);
+        }
+      }
+    } else if (g < groups_stored) {
+      if constexpr (bits == 8) *reinterpret_cast<uint2*>(out_row + 8 * (size_t)g) = make_uint2(lo, hi);
+      else *reinterpret_cast<uint32_t*>(out_row + 4 * (size_t)g) = lo;
+    }
+    const uint32_t kb = g >> 2;
+    if ((lane & 3) == 0) {
+      if (kb < p.kblocks) p.scales[scale_at(p, row, kb)] = (uint8_t)bs.byte;
+      else if (p.layout == MX_SCALES_SWIZZLED && kb < ((p.kblocks + 3) & ~3u)) p.scales[scale_at(p, row, kb)] = 0;
+    }
+  }
+  zero_pad_rows(p);
+}
+
+// Any dim: one element per lane, one MX block per warp and step.  The row is read twice, the second
+// time out of the caches.
+template <int DTYPE, int FMT>
+__global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
+  constexpr uint32_t bits = FmtTraits<FMT>::bits;
+  __shared__ float red[32];
+  pdl_prologue();
+  const uint32_t row = blockIdx.x, lane = threadIdx.x & 31;
+  const size_t base = (size_t)row * p.dim;
+  float ss = 0.0f;
+  for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {
+    float v = load1<DTYPE>(p.x, base + c);
+    if (p.residual) v += load1<DTYPE>(p.residual, base + c);
+    ss = fmaf(v, v, ss);
+  }
+  const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);  // (its barrier also orders pass 1 before the stores below)
+  uint8_t* out_row = p.elems + (size_t)row * p.kblocks * (4 * bits);
+  for (uint32_t kb = threadIdx.x >> 5; kb < ((p.kblocks + 3) & ~3u); kb += blockDim.x >> 5) {
+    const uint32_t c = kb * 32 + lane;
+    float y = 0.0f;
+    if (c < p.dim) {
+      float v = load1<DTYPE>(p.x, base + c);
+      if (p.residual) v += load1<DTYPE>(p.residual, base + c);
+      if (p.h_out) store1<DTYPE>(p.h_out, base + c, v);
+      y = v * s * weight1(p.weight, p.w_bf16, c);
+      if (p.y_out) store1<DTYPE>(p.y_out, base + c, y);
+    }
+    if (kb >= p.kblocks) {
+      if (p.layout == MX_SCALES_SWIZZLED && lane == 0) p.scales[scale_at(p, row, kb)] = 0;
+      continue;
+    }
+    float am = absmax_nan(y, 0.0f);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, o));
+    const BlockScale bs = block_scale<FMT>(am);
+    float a = mul_ftz(y, bs.m1);
+    if (FMT == MX_INT8) a *= bs.m2;
+    a = __uint_as_float(__float_as_uint(a) | p.sticky);
+    uint32_t code = cast_pair<FMT, MX_RNE>(a, 0.0f) & ((1u << bits) - 1u);
+    if (!bs.finite) code = 0;
+    // four lanes' codes are 32, 24 or 16 bits of the row's stream
+    uint32_t w = code | (__shfl_down_sync(0xffffffffu, code, 1) << bits);
+    w |= __shfl_down_sync(0xffffffffu, w, 2) << (2 * bits);
+    if ((lane & 3) == 0) {
+      uint8_t* d = out_row + (size_t)kb * (4 * bits) + (lane >> 2) * (bits / 2);
+#pragma unroll
+      for (uint32_t i = 0; i < bits / 2; ++i) d[i] = (uint8_t)(w >> (8 * i));
+    }
+    if (lane == 0) p.scales[scale_at(p, row, kb)] = (uint8_t)bs.byte;
+  }
+  zero_pad_rows(p);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Backward.  Both row sums are taken over what is read anyway,
+//   s1 = sum h^2,  s2 = sum dy w h,   s = rsqrt(s1 / D + eps),   dh = s (dy w - h s^2 s2 / D) + dres,
+// so a row is read once and needs one reduction.  The grid stays resident; a thread keeps its columns
+// from row to row and sums its share of the weight gradient, dy h s, in registers.  Every CTA writes
+// one row of partial sums and a second kernel adds those in a fixed order.
+// ---------------------------------------------------------------------------------------------------
+struct NormBackParams {
+  const void *dy, *h, *weight, *dres;
+  void* dh;
+  float* partial;
+  float2* stats;
+  uint32_t rows, dim, w_bf16, row_chunk;
+  float eps, inv_dim;
+};
+
+template <int DTYPE, int V>
+__global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackParams p) {
+  __shared__ float2 red[2][16];
+  pdl_prologue();
+  const uint32_t T = blockDim.x, lane = threadIdx.x & 31, warps = T >> 5, groups = p.dim >> 3;
+  float dw[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+  Raw8<DTYPE> h[V], d[V], q[V];
+  auto fetch = [&](uint32_t row) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * T + threadIdx.x;
+      if (g < groups) {
+        h[i] = load_raw8<DTYPE>(p.h, (size_t)row * p.dim + 8 * (size_t)g);
+        d[i] = load_raw8<DTYPE>(p.dy, (size_t)row * p.dim + 8 * (size_t)g);
+        if (p.dres) q[i] = load_raw8<DTYPE>(p.dres, (size_t)row * p.dim + 8 * (size_t)g);
+      } else {
+        h[i] = {}; d[i] = {}; q[i] = {};
+      }
+    }
+  };
+  uint32_t row = blockIdx.x, side = 0;
+  if (row < p.rows) fetch(row);
+  for (; row < p.rows; row += gridDim.x, side ^= 1) {
+    float s1 = 0.0f, s2 = 0.0f;
+    float hf[V][8], gf[V][8];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * T + threadIdx.x;
+      float w[8] = {};
+      if (g < groups) load_weight8(p.weight, p.w_bf16, 8 * g, w);
+      widen<DTYPE>(h[i], hf[i]);
+      widen<DTYPE>(d[i], gf[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s1 = fmaf(hf[i][e], hf[i][e], s1);
+        s2 = fmaf(gf[i][e] * w[e], hf[i][e], s2);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (lane == 0) red[side][threadIdx.x >> 5] = make_float2(s1, s2);
+    __syncthreads();
+    float2 t = lane < warps ? red[side][lane] : make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+      t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+      t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+    }
+    t.x = __shfl_sync(0xffffffffu, t.x, 0);
+    t.y = __shfl_sync(0xffffffffu, t.y, 0);
+    const float s = rsqrtf(t.x * p.inv_dim + p.eps), c = s * s * (t.y * p.inv_dim);
+    float qf[V][8];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (p.dres) widen<DTYPE>(q[i], qf[i]);
+    }
+    const size_t base = (size_t)row * p.dim;
+    if (row + gridDim.x < p.rows) fetch(row + gridDim.x);  // the next row is on its way while this one is finished
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * T + threadIdx.x;
+      if (g < groups) {
+        float w[8], o[8];
+        load_weight8(p.weight, p.w_bf16, 8 * g, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          o[e] = s * (gf[i][e] * w[e] - hf[i][e] * c);
+          if (p.dres) o[e] += qf[i][e];
+          dw[i][e] = fmaf(gf[i][e], hf[i][e] * s, dw[i][e]);
+        }
+        store8<DTYPE>(p.dh, base + 8 * (size_t)g, o);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t g = i * T + threadIdx.x;
+    if (g < groups) store8<MX_F32>(p.partial, (size_t)blockIdx.x * p.dim + 8 * (size_t)g, dw[i]);
+  }
+}
+
+// Any dim, in two kernels: the row sums first (a CTA per row), then a thread per column goes down a chunk
+// of rows, writes dh and sums the column's weight gradient.  h and dy are read twice; dh may lie on dy.
+template <int DTYPE>
+__global__ void __launch_bounds__(256) rmsnorm_row_sums_kernel(const NormBackParams p) {
+  __shared__ float red[2][32];
+  pdl_prologue();
+  const uint32_t row = blockIdx.x;
+  const size_t base = (size_t)row * p.dim;
+  float s1 = 0.0f, s2 = 0.0f;
+  for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {
+    const float h = load1<DTYPE>(p.h, base + c);
+    s1 = fmaf(h, h, s1);
+    s2 = fmaf(load1<DTYPE>(p.dy, base + c) * weight1(p.weight, p.w_bf16, c), h, s2);
+  }
+  s1 = cta_sum(s1, red[0]);
+  s2 = cta_sum(s2, red[1]);
+  if (threadIdx.x == 0) {
+    const float s = rsqrtf(s1 * p.inv_dim + p.eps);
+    p.stats[row] = make_float2(s, s * s * (s2 * p.inv_dim));
+  }
+}
+
+template <int DTYPE>
+__global__ void __launch_bounds__(256) rmsnorm_columns_kernel(const NormBackParams p) {
+  pdl_prologue();
+  const uint32_t c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= p.dim) return;
+  const uint32_t r0 = blockIdx.y * p.row_chunk, r1 = min(p.rows, r0 + p.row_chunk);
+  const float w = weight1(p.weight, p.w_bf16, c);
+  float dw = 0.0f;
+#pragma unroll 4
+  for (uint32_t r = r0; r < r1; ++r) {
+    const size_t at = (size_t)r * p.dim + c;
+    const float2 st = __ldg(p.stats + r);
+    const float h = load1<DTYPE>(p.h, at), d = load1<DTYPE>(p.dy, at);
+    float o = st.x * (d * w - h * st.y);
+    if (p.dres) o += load1<DTYPE>(p.dres, at);
+    dw = fmaf(d, h * st.x, dw);
+    store1<DTYPE>(p.dh, at, o);
+  }
+  p.partial[(size_t)blockIdx.y * p.dim + c] = dw;
+}
+
+// dweight[c] = sum over the partial rows, always in the same order: 8 strands of rows per column.
+__global__ void __launch_bounds__(256) rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight,
+                                                              uint32_t parts, uint32_t dim) {
+  __shared__ float sum[8][33];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, strand = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  float t = 0.0f;
+  if (c < dim) {
+#pragma unroll 4
+    for (uint32_t r = strand; r < parts; r += 8) t += partial[(size_t)r * dim + c];
+  }
+  sum[strand][lane] = t;
+  __syncthreads();
+  if (strand == 0 && c < dim) {
+    t = sum[0][lane];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += sum[i][lane];
+    dweight[c] = t;
+  }
+}
+
+// ---- host side ---------------------------------------------------------------
+
+struct Shape {
+  uint32_t threads;
+  int v;  // groups of 8 per thread; 0: the kernel for any dim
+};
+
+template <int DTYPE, int FMT>
+cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
+  const dim3 grid(p.rows);
+  switch (s.v) {
+    case 1: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 1>, grid, dim3(s.threads), 0, stream, p);
+    case 2: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 2>, grid, dim3(s.threads), 0, stream, p);
+    case 4: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 4>, grid, dim3(s.threads), 0, stream, p);
+    default: return launch_pdl(rmsnorm_any_kernel<DTYPE, FMT>, grid, dim3(256), 0, stream, p);
+  }
+}
+
+template <int DTYPE>
+cudaError_t launch_forward_fmt(int fmt, const NormParams& p, Shape s, cudaStream_t stream) {
+  switch (fmt) {
+    case MX_E4M3: return launch_forward<DTYPE, MX_E4M3>(p, s, stream);
+    case MX_E5M2: return launch_forward<DTYPE, MX_E5M2>(p, s, stream);
+    case MX_E3M2: return launch_forward<DTYPE, MX_E3M2>(p, s, stream);
+    case MX_E2M3: return launch_forward<DTYPE, MX_E2M3>(p, s, stream);
+    case MX_E2M1: return launch_forward<DTYPE, MX_E2M1>(p, s, stream);
+    default: return launch_forward<DTYPE, MX_INT8>(p, s, stream);
+  }
+}
+
+template <int DTYPE>
+cudaError_t launch_backward(const NormBackParams& p, uint32_t grid, Shape s, cudaStream_t stream) {
+  return s.v == 1 ? launch_pdl(rmsnorm_backward_kernel<DTYPE, 1>, dim3(grid), dim3(s.threads), 0, stream, p)
+                  : launch_pdl(rmsnorm_backward_kernel<DTYPE, 2>, dim3(grid), dim3(s.threads), 0, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_rmsnorm_quantize(const RmsnormArgs& a) {
+  NormParams p;
+  p.x = a.x; p.residual = a.residual; p.weight = a.weight; p.h_out = a.h_out; p.y_out = a.y_out;
+  p.elems = a.elems; p.scales = a.scales;
+  p.rows = (uint32_t)a.rows; p.dim = (uint32_t)a.dim; p.kblocks = (uint32_t)((a.dim + 31) / 32);
+  p.eps = a.eps; p.inv_dim = 1.0f / (float)a.dim;
+  p.w_bf16 = (uint32_t)a.w_bf16; p.sticky = a.rounding == MX_RHAZ ? 1u : 0u; p.layout = (uint32_t)a.layout;
+  // Groups of 8 that a row stores, whole 16-group runs (the four scale bytes of a swizzled word).
+  const uint32_t groups = (p.kblocks + 3) / 4 * 16;
+  Shape s = {256, 0};
+  if (a.dim % 8 == 0 && groups <= 2048) {
+    if (a.rows <= a.sm_count) {  // a row per SM: as many threads as the row has groups, the shortest chain
+      s.threads = groups < 1024 ? (groups + 31) / 32 * 32 : 1024;
+    } else {
+      s.threads = (groups / 4 + 31) / 32 * 32;
+      if (s.threads < 64) s.threads = 64;
+    }
+    const uint32_t v = (groups + s.threads - 1) / s.threads;
+    s.v = v <= 1 ? 1 : v <= 2 ? 2 : 4;
+  }
+  return a.dtype == MX_BF16 ? launch_forward_fmt<MX_BF16>(a.fmt, p, s, a.stream)
+                            : launch_forward_fmt<MX_F32>(a.fmt, p, s, a.stream);
+}
+
+cudaError_t launch_rmsnorm_backward(const RmsnormBackwardArgs& a) {
+  NormBackParams p;
+  p.dy = a.dy; p.h = a.h; p.weight = a.weight; p.dres = a.dres; p.dh = a.dh; p.partial = a.partial; p.stats = a.stats;
+  p.rows = (uint32_t)a.rows; p.dim = (uint32_t)a.dim; p.w_bf16 = (uint32_t)a.w_bf16;
+  p.eps = a.eps; p.inv_dim = 1.0f / (float)a.dim; p.row_chunk = 0;
+  const uint32_t groups = p.dim / 8;
+  uint32_t parts;
+  cudaError_t e;
+  if (a.dim % 8 == 0 && groups <= 1024) {  // two groups of 8 a thread are what the registers hold
+    Shape s;
+    s.threads = groups < 512 ? (groups + 31) / 32 * 32 : 512;
+    s.v = groups <= s.threads ? 1 : 2;
+    parts = p.rows < (uint32_t)kNormPartials ? p.rows : (uint32_t)kNormPartials;
+    e = a.dtype == MX_BF16 ? launch_backward<MX_BF16>(p, parts, s, a.stream) : launch_backward<MX_F32>(p, parts, s, a.stream);
+  } else {
+    e = a.dtype == MX_BF16 ? launch_pdl(rmsnorm_row_sums_kernel<MX_BF16>, dim3(p.rows), dim3(256), 0, a.stream, p)
+                           : launch_pdl(rmsnorm_row_sums_kernel<MX_F32>, dim3(p.rows), dim3(256), 0, a.stream, p);
+    if (e != cudaSuccess) return e;
+    p.row_chunk = (p.rows + 63) / 64;
+    parts = (p.rows + p.row_chunk - 1) / p.row_chunk;
+    const dim3 grid((p.dim + 255) / 256, parts);
+    e = a.dtype == MX_BF16 ? launch_pdl(rmsnorm_columns_kernel<MX_BF16>, grid, dim3(256), 0, a.stream, p)
+                           : launch_pdl(rmsnorm_columns_kernel<MX_F32>, grid, dim3(256), 0, a.stream, p);
+  }
+  if (e != cudaSuccess) return e;
+  return launch_pdl(rmsnorm_dweight_kernel, dim3((p.dim + 31) / 32), dim3(256), 0, a.stream, (const float*)a.partial,
+                    a.dweight, parts, p.dim);
+}
+
+}  // namespace mx

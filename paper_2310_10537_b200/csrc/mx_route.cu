@@ -1,0 +1,349 @@
+// Routing to experts: scores, group choice, top-k and weights of each token, and the gradient of the
+// weights.  One warp per token; a lane holds NV consecutive experts in registers (read as vectors), so
+// that a lower lane always means a lower expert and ties fall to the lowest index by themselves.
+#include <cuda_runtime.h>
+
+#include "mx.h"
+#include "mx_device.cuh"
+#include "mx_launch.h"
+
+namespace mx {
+namespace {
+
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr int kRouteWarps = 4;  // tokens per CTA
+
+struct RouteParams {
+  const void* logits;
+  const float *bias, *dweights;
+  int32_t* ids;
+  float* weights;
+  void* dlogits;
+  uint32_t tokens, experts, topk, score, groups, topk_groups, group_score, renormalize, group_size;
+  float scale;
+};
+
+// Floats as unsigned integers of the same order; -0 counts as +0 and NaN ranks above everything.
+// 0 is below the key of every float: "not a candidate".
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return x != x ? 0xffffffffu : k;
+}
+__device__ __forceinline__ float from_key(uint32_t k) {
+  return k == 0u ? -INFINITY : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+// The lane's NV logits; experts past the end read as -Inf.
+template <int DTYPE, int NV>
+__device__ __forceinline__ void load_logits(const RouteParams& p, uint32_t token, uint32_t lane, float (&x)[NV]) {
+  const uint32_t e0 = lane * NV;
+  const size_t at = (size_t)token * p.experts + e0;
+  // vectors where every row starts on one and the lane's experts all exist
+  if constexpr (DTYPE == MX_F32 && NV % 4 == 0) {
+    if ((p.experts & 3u) == 0 && e0 + NV <= p.experts) {
+      const float4* q = reinterpret_cast<const float4*>((const float*)p.logits + at);
+#pragma unroll
+      for (int i = 0; i < NV / 4; ++i) {
+        const float4 v = __ldg(q + i);
+        x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+      }
+      return;
+    }
+  }
+  if constexpr (DTYPE == MX_BF16 && NV % 4 == 0) {
+    if ((p.experts & 3u) == 0 && e0 + NV <= p.experts) {
+      const uint2* q = reinterpret_cast<const uint2*>((const uint16_t*)p.logits + at);
+#pragma unroll
+      for (int i = 0; i < NV / 4; ++i) {
+        const uint2 v = __ldg(q + i);
+        x[4 * i] = __uint_as_float(v.x << 16); x[4 * i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[4 * i + 2] = __uint_as_float(v.y << 16); x[4 * i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    x[j] = -INFINITY;
+    if (e0 + j < p.experts)
+      x[j] = DTYPE == MX_BF16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)p.logits + at + j) << 16)
+                              : __ldg((const float*)p.logits + at + j);
+  }
+}
+
+__device__ __forceinline__ float warp_max(float v) {  // NaN wins
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float w = __shfl_xor_sync(kFull, v, o);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(v), "f"(w));
+  }
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  return v;
+}
+
+// Maximum and sum of exponentials of a row of logits (softmax).
+template <int NV>
+__device__ __forceinline__ void softmax_stats(const float (&x)[NV], float& m, float& sum) {
+  m = x[0];
+#pragma unroll
+  for (int j = 1; j < NV; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(x[j]));
+  m = warp_max(m);
+  if (m == -INFINITY) m = 0.0f;  // nothing to choose: every exponential is 0, and the sum
+  sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) sum += expf(x[j] - m);
+  sum = warp_sum(sum);
+}
+__device__ __forceinline__ float softmax_of(float x, float m, float sum) {
+  const float e = expf(x - m);
+  return sum == 0.0f ? 0.0f : e / sum;
+}
+
+// The two largest keys of a set, a >= b.
+__device__ __forceinline__ void top2_add(uint32_t& a, uint32_t& b, uint32_t k) {
+  b = max(b, min(a, k));
+  a = max(a, k);
+}
+
+template <int DTYPE, int NV>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteParams p) {
+  extern __shared__ uint32_t keys_smem[];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t token = blockIdx.x * kRouteWarps + warp;
+  if (token >= p.tokens) return;
+  const uint32_t e0 = lane * NV;
+  float x[NV];
+  load_logits<DTYPE, NV>(p, token, lane, x);
+  float m = 0.0f, sum = 1.0f;
+  const bool soft = p.score == MX_SCORE_SOFTMAX;
+  if (soft) softmax_stats<NV>(x, m, sum);
+  uint32_t key[NV];
+  const bool by_score = !soft || p.bias != nullptr;
+  // a group's two best values are added: softmax without a bias needs the scores there too
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float c = x[j];
+    if (by_score) {
+      c = soft ? softmax_of(x[j], m, sum) : sigmoid(x[j]);
+      if (p.bias && e0 + j < p.experts) c += __ldg(p.bias + e0 + j);
+    }
+    key[j] = e0 + j < p.experts ? order_key(c) : 0u;
+  }
+  if (p.groups > 1) {
+    const bool two = p.group_score == MX_GROUP_TOP2;
+    // the value a group is ranked by, from its two largest keys
+    auto group_value = [&](uint32_t a, uint32_t b) -> float {
+      if (!two) return from_key(a);
+      float va = from_key(a), vb = from_key(b);
+      if (!by_score) { va = softmax_of(va, m, sum); vb = b ? softmax_of(vb, m, sum) : 0.0f; }
+      return b ? va + vb : va;  // (a group of one expert has one score)
+    };
+    uint32_t rank_key = 0;  // of group `lane`
+    const uint32_t lanes_per_group = p.group_size / NV;
+    const bool aligned = p.group_size % NV == 0 && (lanes_per_group & (lanes_per_group - 1)) == 0;
+    if (aligned) {  // a group is a power of two of whole lanes
+      uint32_t a = 0, b = 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) top2_add(a, b, key[j]);
+      for (uint32_t o = 1; o < lanes_per_group; o <<= 1) {
+        const uint32_t a2 = __shfl_xor_sync(kFull, a, o), b2 = __shfl_xor_sync(kFull, b, o);
+        b = max(max(b, b2), min(a, a2));
+        a = max(a, a2);
+      }
+      const uint32_t k = order_key(group_value(a, b));
+      rank_key = __shfl_sync(kFull, k, (lane * lanes_per_group) & 31);
+    } else {        // through shared memory, a lane per group
+      uint32_t* mine = keys_smem + warp * (NV * 32);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) mine[e0 + j] = key[j];
+      __syncwarp();
+      if (lane < p.groups) {
+        uint32_t a = 0, b = 0;
+        for (uint32_t i = 0; i < p.group_size; ++i) top2_add(a, b, mine[lane * p.group_size + i]);
+        rank_key = order_key(group_value(a, b));
+      }
+    }
+    // the topk_groups best groups: fewer than that many are better, or equal and earlier
+    uint32_t better = 0;
+    for (uint32_t g = 0; g < p.groups; ++g) {
+      const uint32_t k = __shfl_sync(kFull, rank_key, g);
+      better += (k > rank_key || (k == rank_key && g < lane)) ? 1u : 0u;
+    }
+    const uint32_t kept = __ballot_sync(kFull, lane < p.groups && better < p.topk_groups);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (e0 + j < p.experts && !((kept >> ((e0 + j) / p.group_size)) & 1u)) key[j] = 0u;
+  }
+  // top-k: the best key of the warp, the first lane that has it, that lane's first expert with it
+  uint32_t best = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) best = max(best, key[j]);
+  uint32_t my_id = 0;
+  float my_s = 0.0f;
+  for (uint32_t i = 0; i < p.topk; ++i) {
+    const uint32_t top = __reduce_max_sync(kFull, best);
+    const uint32_t winner = __ffs(__ballot_sync(kFull, best == top)) - 1;
+    uint32_t at = 0;
+    float xv = 0.0f;
+    if (lane == winner) {
+      best = 0;
+      bool found = false;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool hit = !found && key[j] == top;
+        if (hit) { at = e0 + j; xv = x[j]; key[j] = 0u; found = true; }
+        best = max(best, key[j]);
+      }
+    }
+    at = __shfl_sync(kFull, at, winner);
+    xv = __shfl_sync(kFull, xv, winner);
+    if (lane == i) { my_id = at; my_s = xv; }
+  }
+  const bool live = lane < p.topk;
+  my_s = live ? (soft ? softmax_of(my_s, m, sum) : sigmoid(my_s)) : 0.0f;
+  float w = my_s;
+  if (p.renormalize) {
+    const float total = warp_sum(my_s);
+    w = total == 0.0f ? 0.0f : my_s / total;
+  }
+  if (live) {
+    p.ids[(size_t)token * p.topk + lane] = (int32_t)my_id;
+    p.weights[(size_t)token * p.topk + lane] = w * p.scale;
+  }
+}
+
+// With S = sum of the chosen scores and d = dweights: renormalised weights w_j = scale s_j / S give
+// ds_j = scale (d_j - sum_i d_i s_i / S) / S, others ds_j = scale d_j; then
+//   softmax: dx_e = s_e (ds_e - sum_i ds_i s_i),   sigmoid: dx_e = ds_e s_e (1 - s_e).
+template <int DTYPE, int NV>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const RouteParams p) {
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t token = blockIdx.x * kRouteWarps + warp;
+  if (token >= p.tokens) return;
+  const uint32_t e0 = lane * NV;
+  const bool soft = p.score == MX_SCORE_SOFTMAX;
+  float x[NV];
+  load_logits<DTYPE, NV>(p, token, lane, x);
+  float m = 0.0f, sum = 1.0f;
+  if (soft) softmax_stats<NV>(x, m, sum);
+  int32_t id = -1;
+  float d = 0.0f, s = 0.0f;
+  if (lane < p.topk) {
+    id = __ldg(p.ids + (size_t)token * p.topk + lane);
+    d = __ldg(p.dweights + (size_t)token * p.topk + lane);
+    if ((uint32_t)id < p.experts) {
+      const size_t at = (size_t)token * p.experts + (uint32_t)id;
+      const float xs = DTYPE == MX_BF16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)p.logits + at) << 16)
+                                        : __ldg((const float*)p.logits + at);
+      s = soft ? softmax_of(xs, m, sum) : sigmoid(xs);
+    } else {
+      id = -1;
+      d = 0.0f;
+    }
+  }
+  float ds = p.scale * d;
+  if (p.renormalize) {
+    const float total = warp_sum(s), dot = warp_sum(d * s);
+    ds = total == 0.0f || id < 0 ? 0.0f : p.scale * (d - dot / total) / total;
+  }
+  const float inner = soft ? warp_sum(ds * s) : 0.0f;
+  float o[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) o[j] = 0.0f;
+  for (uint32_t i = 0; i < p.topk; ++i) {
+    const int32_t e = __shfl_sync(kFull, id, i);
+    const float v = __shfl_sync(kFull, ds, i);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (e == (int32_t)(e0 + j)) o[j] += v;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (soft) {
+      o[j] = softmax_of(x[j], m, sum) * (o[j] - inner);
+    } else {
+      const float t = expf(-fabsf(x[j]));  // s (1 - s) without the difference: t / (1 + t)^2
+      o[j] = o[j] == 0.0f ? 0.0f : o[j] * (t / ((1.0f + t) * (1.0f + t)));
+    }
+  }
+  const size_t at = (size_t)token * p.experts + e0;
+  if constexpr (NV % 4 == 0) {
+    if ((p.experts & 3u) == 0 && e0 + NV <= p.experts) {
+#pragma unroll
+      for (int i = 0; i < NV / 4; ++i) {
+        if constexpr (DTYPE == MX_F32) {
+          reinterpret_cast<float4*>((float*)p.dlogits + at)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+          uint2 v;
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o[4 * i + 1]), "f"(o[4 * i]));
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[4 * i + 3]), "f"(o[4 * i + 2]));
+          reinterpret_cast<uint2*>((uint16_t*)p.dlogits + at)[i] = v;
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (e0 + j < p.experts) {
+      if constexpr (DTYPE == MX_F32) {
+        ((float*)p.dlogits)[at + j] = o[j];
+      } else {
+        uint32_t v;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(0.0f), "f"(o[j]));
+        ((uint16_t*)p.dlogits)[at + j] = (uint16_t)v;
+      }
+    }
+  }
+}
+
+RouteParams route_params(const RouteArgs& a) {
+  RouteParams p;
+  p.logits = a.logits; p.bias = a.bias; p.dweights = a.dweights; p.ids = a.ids; p.weights = a.weights;
+  p.dlogits = a.dlogits; p.tokens = (uint32_t)a.tokens; p.experts = (uint32_t)a.experts;
+  p.topk = (uint32_t)a.route.topk; p.score = (uint32_t)a.route.score; p.groups = (uint32_t)a.route.groups;
+  p.topk_groups = (uint32_t)a.route.topk_groups; p.group_score = (uint32_t)a.route.group_score;
+  p.renormalize = a.route.renormalize ? 1u : 0u; p.scale = a.route.scale;
+  p.group_size = p.groups ? p.experts / p.groups : p.experts;
+  return p;
+}
+
+template <int DTYPE, int NV>
+cudaError_t launch_nv(const RouteParams& p, bool backward, cudaStream_t stream) {
+  const dim3 grid((p.tokens + kRouteWarps - 1) / kRouteWarps), block(32 * kRouteWarps);
+  if (backward) return launch_pdl(route_backward_kernel<DTYPE, NV>, grid, block, 0, stream, p);
+  return launch_pdl(route_kernel<DTYPE, NV>, grid, block, p.groups > 1 ? sizeof(uint32_t) * 32 * NV * kRouteWarps : 0, stream, p);
+}
+
+template <int DTYPE>
+cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t stream) {
+  if (p.experts <= 32) return launch_nv<DTYPE, 1>(p, backward, stream);
+  if (p.experts <= 64) return launch_nv<DTYPE, 2>(p, backward, stream);
+  if (p.experts <= 128) return launch_nv<DTYPE, 4>(p, backward, stream);
+  if (p.experts <= 256) return launch_nv<DTYPE, 8>(p, backward, stream);
+  if (p.experts <= 512) return launch_nv<DTYPE, 16>(p, backward, stream);
+  return launch_nv<DTYPE, 32>(p, backward, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_route(const RouteArgs& a) {
+  const RouteParams p = route_params(a);
+  return a.dtype == MX_BF16 ? launch_dtype<MX_BF16>(p, false, a.stream) : launch_dtype<MX_F32>(p, false, a.stream);
+}
+
+cudaError_t launch_route_backward(const RouteArgs& a) {
+  const RouteParams p = route_params(a);
+  return a.dtype == MX_BF16 ? launch_dtype<MX_BF16>(p, true, a.stream) : launch_dtype<MX_F32>(p, true, a.stream);
+}
+
+}  // namespace mx
