@@ -13,11 +13,15 @@
 // One pair of CTAs per two SMs, persistent over the items (group, W tile, X tile) in that order, which
 // every role of the kernel walks by itself from a table of the groups' first items that each CTA
 // makes in shared memory.  Per CTA:
-//   warp 0     copies: 128 rows of W, its half of the X rows, the stage's scale chunks -> one
-//              barrier per stage (the leader's)
-//   warp 1     (leader) scale chunks shared -> tensor memory, then four MMAs, from the same thread:
-//              copies and MMAs of one thread execute in order, so no hand-over lies between them
-//   warps 2-9  epilogue; two accumulators, so that it runs under the next item's MMAs
+//   warp 0      copies 128 rows of W and its half of the X rows -> the stage's barrier (the leader's)
+//   warp 1      (leader) four MMAs per stage
+//   warp 2      (leader) scale chunks shared -> tensor memory, ahead of the MMAs
+//   warp 3      copies the stage's scale chunks -> a barrier of their own
+//   warps 4-11  epilogue, under the next item's MMAs: tiles of up to 128 columns have two accumulators;
+//               wider ones alternate between columns 0..255 and 128..383 of tensor memory (two
+//               whole ones and the scales do not fit), and the half both use is drained first
+// (Scale copies issued by the MMA thread right before their MMAs wait in line behind the MMAs of the
+// stage before and then hold up their own: 65536 x 4096 x 4096 over 32 groups took 1155 us that way.)
 // Every wait is bounded (see mbar_wait); on expiry a status word is set and all roles fall through to
 // the common exit.
 #include <cuda.h>
@@ -33,7 +37,7 @@ namespace mx {
 namespace {
 
 constexpr int kBK = 128;               // K elements per stage: 4 MX blocks, 4 MMAs
-constexpr uint32_t kThreads = 320;     // 10 warps
+constexpr uint32_t kThreads = 384;     // 12 warps
 constexpr uint32_t kTmemCols = 512;
 constexpr long long kSpinLimit = 2000000000LL;  // budget of a wait in cycles (~1 s)
 constexpr uint32_t kMaxStages = 10;
@@ -45,6 +49,7 @@ enum : unsigned int {
   ST_MMA_WAIT_FULL = 2,   // a stage never became full
   ST_MMA_WAIT_ACC = 3,    // an accumulator was never drained
   ST_EPILOGUE_WAIT = 4,   // an accumulator never became full
+  ST_SCALE_WAIT = 5,      // a stage's scales never landed
 };
 __device__ unsigned int g_grouped_status;
 
@@ -52,7 +57,7 @@ struct GroupedParams {
   const int32_t* offsets;
   void* C;
   uint32_t c_bf16, groups, w_rows, x_rows, k_chunks;  // k_chunks: of the whole K axis
-  uint32_t max_n, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
+  uint32_t max_n, acc_step, shared_half, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
   long long spin_limit;
 };
 
@@ -115,20 +120,22 @@ __device__ __forceinline__ void raise_abort(volatile uint32_t* abort_flag, unsig
 template <bool KG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
-                       const __grid_constant__ CUtensorMap tmap_sw, const __grid_constant__ CUtensorMap tmap_sx,
-                       const GroupedParams p) {
+                       const __grid_constant__ CUtensorMap tmap_xf, const __grid_constant__ CUtensorMap tmap_sw,
+                       const __grid_constant__ CUtensorMap tmap_sx, const GroupedParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
   const uint32_t stage_bytes = kWBytes + p.x_stage_bytes;   // operands; a multiple of 1024
   const uint32_t sf_bytes = 512u * p.sf_per_stage;
   const uint32_t off_sf = p.stages * stage_bytes, off_bar = off_sf + p.stages * sf_bytes;
-  constexpr uint32_t kBars = 2 * kMaxStages + 4;
+  constexpr uint32_t kBars = 4 * kMaxStages + 4;
   const uint32_t bar0 = smem_base + off_bar;
   auto full_bar = [&](uint32_t s) { return bar0 + 8 * s; };
   auto empty_bar = [&](uint32_t s) { return bar0 + 8 * (kMaxStages + s); };
-  auto acc_full_bar = [&](uint32_t a) { return bar0 + 8 * (2 * kMaxStages + a); };
-  auto acc_empty_bar = [&](uint32_t a) { return bar0 + 8 * (2 * kMaxStages + 2 + a); };
+  auto sf_full_bar = [&](uint32_t s) { return bar0 + 8 * (2 * kMaxStages + s); };
+  auto sf_ready_bar = [&](uint32_t s) { return bar0 + 8 * (3 * kMaxStages + s); };
+  auto acc_full_bar = [&](uint32_t a) { return bar0 + 8 * (4 * kMaxStages + a); };
+  auto acc_empty_bar = [&](uint32_t a) { return bar0 + 8 * (4 * kMaxStages + 2 + a); };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + off_bar + kBars * 8);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* offset = reinterpret_cast<uint32_t*>(smem_gen + off_bar + kBars * 8 + 16);
@@ -143,8 +150,10 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < p.stages; ++s) {
-      mbar_init(full_bar(s), 1);   // used in the leader: its producer's arrive + the bytes of both CTAs
-      mbar_init(empty_bar(s), 1);  // a tcgen05.commit, delivered to both
+      mbar_init(full_bar(s), 1);      // used in the leader: its producer's arrive + the bytes of both CTAs
+      mbar_init(empty_bar(s), 1);     // a tcgen05.commit, delivered to both
+      mbar_init(sf_full_bar(s), 1);   // as full
+      mbar_init(sf_ready_bar(s), 1);  // used in the leader: the copier's tcgen05.commit
     }
     for (uint32_t a = 0; a < 2; ++a) {
       mbar_init(acc_full_bar(a), 1);
@@ -194,18 +203,25 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const Tables tb = {offset, first};
-  const uint32_t sf_col0 = 2 * p.max_n;
+  const uint32_t sf_col0 = p.acc_step + p.max_n;
+  // The accumulator of a pair's i-th item lies at column acc_step * (i & 1).  Two separate ones: the item
+  // waits until the one before the last is drained, each with a barrier of its own.  Overlapping ones
+  // (shared_half): until the last item's part of columns 128..255 is; one barrier, a phase per item.
+  auto acc_bar_index = [&](uint32_t i) { return p.shared_half ? 0u : i & 1u; };
+  auto acc_parity = [&](uint32_t i) { return (p.shared_half ? i : i >> 1) & 1u; };
 
-  if (warp == 0) {
-    // ------------------------------ copies (both CTAs) ------------------------------
+  if (warp == 0 || warp == 3) {
+    // ------------------- copies (both CTAs): warp 0 operands, warp 3 scale chunks -------------------
+    const bool scales = warp == 3;
     uint32_t stage = 0, phase = 0, g = 0;
     bool ok = true;
     Item it;
     for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
       const uint32_t wrow = (KG ? 0u : it.group * p.w_rows) + it.w0 + rank * 128u;
       const uint32_t half = it.n >> 1, xrow = it.x0 + rank * half, boxes = half / kXBoxRows;
+      const bool whole = it.n == p.max_n;  // a full tile's X rows are one copy
       const uint32_t sx0 = it.x0 >> 7, sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
-      const uint32_t tx = 2u * (p.w_box_bytes + boxes * p.x_box_bytes + 512u * (1u + sx_n));
+      const uint32_t tx = scales ? 2u * 512u * (1u + sx_n) : 2u * (p.w_box_bytes + boxes * p.x_box_bytes);
       for (uint32_t kc = 0; kc < it.nk; ++kc) {
         ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit));
         if (!ok) {
@@ -213,16 +229,23 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
           break;
         }
         if (elect_one()) {
-          const uint32_t fb = leader_bar(full_bar(stage));
-          if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), tx);
+          const uint32_t bar = scales ? sf_full_bar(stage) : full_bar(stage), fb = leader_bar(bar);
+          if (rank == 0) mbar_arrive_expect_tx(bar, tx);
           const int kx = (int)((it.k0 + kc) * kBK), kz = (int)(it.k0 + kc);
-          const uint32_t dw = smem_base + stage * stage_bytes, dx = dw + kWBytes;
-          tma_load_3d_pair(dw, &tmap_w, kx, (int)wrow, 0, fb);
-          for (uint32_t b = 0; b < boxes; ++b)
-            tma_load_3d_pair(dx + b * (kXBoxRows * 128u), &tmap_x, kx, (int)(xrow + b * kXBoxRows), 0, fb);
-          const uint32_t ds = smem_base + off_sf + stage * sf_bytes;
-          tma_load_3d_pair(ds, &tmap_sw, 0, kz, (int)(wrow >> 7), fb);
-          for (uint32_t c = 0; c < sx_n; ++c) tma_load_3d_pair(ds + 512u * (1u + c), &tmap_sx, 0, kz, (int)(sx0 + c), fb);
+          if (scales) {
+            const uint32_t ds = smem_base + off_sf + stage * sf_bytes;
+            tma_load_3d_pair(ds, &tmap_sw, 0, kz, (int)(wrow >> 7), fb);
+            for (uint32_t c = 0; c < sx_n; ++c) tma_load_3d_pair(ds + 512u * (1u + c), &tmap_sx, 0, kz, (int)(sx0 + c), fb);
+          } else {
+            const uint32_t dw = smem_base + stage * stage_bytes, dx = dw + kWBytes;
+            tma_load_3d_pair(dw, &tmap_w, kx, (int)wrow, 0, fb);
+            if (whole) {
+              tma_load_3d_pair(dx, &tmap_xf, kx, (int)xrow, 0, fb);
+            } else {
+              for (uint32_t b = 0; b < boxes; ++b)
+                tma_load_3d_pair(dx + b * (kXBoxRows * 128u), &tmap_x, kx, (int)(xrow + b * kXBoxRows), 0, fb);
+            }
+          }
         }
         __syncwarp();
         if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -232,35 +255,60 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       const long long t0 = clock64();
       while (clock64() - t0 < 2000000LL) {}
     }
-  } else if (warp == 1) {
-    // ------------------------------ MMA issuer (leader) ------------------------------
+  } else if (warp == 2) {
+    // ------------------------------ scale copier (leader) ------------------------------
     if (rank == 0) {
-      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, g = 0;
+      uint32_t stage = 0, phase = 0, g = 0;
       bool ok = true;
       Item it;
       for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_empty_bar(acc), acc_phase ^ 1u, abort_flag, 4 * p.spin_limit))) {
-          raise_abort(abort_flag, ST_MMA_WAIT_ACC);
-          break;
-        }
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * p.max_n;
         const uint32_t sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
-        const uint32_t sx_col = 4 + ((it.x0 & 127u) >> 5);  // a tile starts on row 0 or 64 of a scale chunk
-        const uint32_t idesc0 = p.idesc | ((it.n >> 3) << 17);
         for (uint32_t kc = 0; kc < it.nk; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(full_bar(stage), phase, abort_flag, p.spin_limit));
+          ok = __all_sync(0xffffffffu, mbar_wait(sf_full_bar(stage), phase, abort_flag, p.spin_limit));
           if (!ok) {
-            raise_abort(abort_flag, ST_MMA_WAIT_FULL);
+            raise_abort(abort_flag, ST_SCALE_WAIT);
             break;
           }
           tc_fence_after();
           const uint32_t sf_smem = smem_base + off_sf + stage * sf_bytes;
           const uint32_t sf_tmem = tmem_base + sf_col0 + stage * (4u * p.sf_per_stage);
+          if (elect_one()) {
+            for (uint32_t c = 0; c <= sx_n; ++c) tc_cp_scales_pair(sf_tmem + 4 * c, scale_desc(sf_smem + 512 * c));
+            tc_commit_leader(sf_ready_bar(stage));  // arrives when the copies have completed in both CTAs
+          }
+          __syncwarp();
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------ MMA issuer (leader) ------------------------------
+    if (rank == 0) {
+      uint32_t stage = 0, phase = 0, i = 0, g = 0;
+      bool ok = true;
+      Item it;
+      for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs, ++i) {
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_empty_bar(acc_bar_index(i)), acc_parity(i) ^ 1u, abort_flag,
+                                               4 * p.spin_limit))) {
+          raise_abort(abort_flag, ST_MMA_WAIT_ACC);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (i & 1u) * p.acc_step;
+        const uint32_t sx_col = 4 + ((it.x0 & 127u) >> 5);  // a tile starts on row 0 or 64 of a scale chunk
+        const uint32_t idesc0 = p.idesc | ((it.n >> 3) << 17);
+        for (uint32_t kc = 0; kc < it.nk; ++kc) {
+          ok = __all_sync(0xffffffffu, mbar_wait(sf_ready_bar(stage), phase, abort_flag, p.spin_limit) &&
+                                           mbar_wait(full_bar(stage), phase, abort_flag, p.spin_limit));
+          if (!ok) {
+            raise_abort(abort_flag, ST_MMA_WAIT_FULL);
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sf_tmem = tmem_base + sf_col0 + stage * (4u * p.sf_per_stage);
           const uint64_t wdesc = operand_desc(smem_base + stage * stage_bytes);
           const uint64_t xdesc = operand_desc(smem_base + stage * stage_bytes + kWBytes);
           if (elect_one()) {
-            for (uint32_t c = 0; c <= sx_n; ++c) tc_cp_scales_pair(sf_tmem + 4 * c, scale_desc(sf_smem + 512 * c));
 #pragma unroll
             for (uint32_t k = 0; k < 4; ++k)  // byte k of each scale column belongs to MX block k of the stage
               tc_mma_pair(d_tmem, wdesc + 2 * k, xdesc + 2 * k, idesc0 | (k << 4) | (k << 29), sf_tmem, sf_tmem + sx_col,
@@ -270,58 +318,75 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
           __syncwarp();
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
-        if (ok && elect_one()) tc_commit_pair(acc_full_bar(acc));
+        if (ok && elect_one()) tc_commit_pair(acc_full_bar(i & 1u));
         __syncwarp();
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
     }
   } else {
     // ------------------------------ epilogue (both CTAs) ------------------------------
     // Warps q and q + 4 share the TMEM lanes 32 q .. 32 q + 31 and take alternate steps of 32 X rows.
-    const uint32_t quarter = warp & 3u, odd = (warp - 2u) >> 2;
-    uint32_t acc = 0, acc_phase = 0, g = 0;
+    const uint32_t quarter = warp & 3u, odd = (warp - 4u) >> 2;
+    uint32_t i = 0, g = 0;
     Item it;
-    for (uint32_t t = pair; next_item<KG>(p, tb, t, g, it); t += num_pairs) {
-      if (!mbar_wait(acc_full_bar(acc), acc_phase, abort_flag, 4 * p.spin_limit)) {
+    for (uint32_t t = pair; next_item<KG>(p, tb, t, g, it); t += num_pairs, ++i) {
+      if (!mbar_wait(acc_full_bar(i & 1u), (i >> 1) & 1u, abort_flag, 4 * p.spin_limit)) {
         if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
         break;
       }
       tc_fence_after();
       const uint32_t n = it.w0 + rank * 128u + quarter * 32u + lane;  // this thread's column of C
       const size_t row_base = KG ? (size_t)it.group * p.x_rows : 0;
-      const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + acc * p.max_n;
-      for (uint32_t c = 32 * odd; c < it.n; c += 64) {
-        uint32_t r[32];
-        if (it.nk != 0) {
-          tc_ld32(taddr + c, r);
-          tc_wait_ld();
-        } else {  // an empty K group: no MMA has written the accumulator
+      const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + (i & 1u) * p.acc_step;
+      // up to two steps (64 columns of the tile) from column c on, 64 apart, into registers
+      auto load = [&](uint32_t c, uint32_t (&r)[2][32]) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = 0u;
+        for (uint32_t h = 0; h < 2; ++h) {
+          if (c + 64 * h < it.n && it.nk != 0) {
+            tc_ld32(taddr + c + 64 * h, r[h]);
+          } else {  // an empty K group: no MMA has written the accumulator
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[h][j] = 0u;
+          }
         }
-        if (n < p.w_rows) {
-          const uint32_t r0 = it.x0 + c, live = it.x_end > r0 ? it.x_end - r0 : 0u;
+        tc_wait_ld();
+      };
+      auto store = [&](uint32_t c, const uint32_t (&r)[2][32]) {
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+          const uint32_t r0 = it.x0 + c + 64 * h, live = it.x_end > r0 ? it.x_end - r0 : 0u;
+          if (n >= p.w_rows || live == 0) continue;
           const size_t at = (row_base + r0) * p.w_rows + n;
           if (p.c_bf16) {
             uint16_t* dst = reinterpret_cast<uint16_t*>(p.C) + at;
 #pragma unroll
             for (uint32_t j = 0; j < 32; ++j) {
-              uint16_t h;
-              asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(__uint_as_float(r[j])));
-              if (j < live) dst[(size_t)j * p.w_rows] = h;
+              uint16_t v;
+              asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(v) : "f"(__uint_as_float(r[h][j])));
+              if (j < live) dst[(size_t)j * p.w_rows] = v;
             }
           } else {
             float* dst = reinterpret_cast<float*>(p.C) + at;
 #pragma unroll
             for (uint32_t j = 0; j < 32; ++j)
-              if (j < live) dst[(size_t)j * p.w_rows] = __uint_as_float(r[j]);
+              if (j < live) dst[(size_t)j * p.w_rows] = __uint_as_float(r[h][j]);
           }
         }
+      };
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(leader_bar(acc_empty_bar(acc_bar_index(i))));
+      };
+      // columns 128..255 of tensor memory first where the next item uses them too
+      const uint32_t c0 = (p.shared_half && !(i & 1u)) ? 128u : 0u, c1 = 128u - c0;
+      uint32_t r[2][32];
+      load(c0 + 32 * odd, r);
+      release();
+      store(c0 + 32 * odd, r);
+      if (p.shared_half) {
+        load(c1 + 32 * odd, r);
+        store(c1 + 32 * odd, r);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(leader_bar(acc_empty_bar(acc)));
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
   }
 
@@ -377,7 +442,7 @@ bool scale_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, uint64_t row
 
 template <bool KG>
 cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
-  CUtensorMap mw, mx_, msw, msx;
+  CUtensorMap mw, mx_, mxf, msw, msx;
   const uint64_t w_all = (uint64_t)a.w_rows * (KG ? 1u : (uint64_t)a.groups);
   if (!operand_map(fn, &mw, a.W, a.fmtW, w_all, (uint64_t)a.K, 128) ||
       !operand_map(fn, &mx_, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, kXBoxRows) ||
@@ -386,18 +451,22 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
   GroupedParams p;
   p.offsets = a.offsets; p.C = a.C; p.c_bf16 = (uint32_t)a.c_bf16; p.groups = (uint32_t)a.groups;
   p.w_rows = (uint32_t)a.w_rows; p.x_rows = (uint32_t)a.x_rows; p.k_chunks = (uint32_t)((a.K + kBK - 1) / kBK);
-  // The widest tile: 192 columns, twice (two accumulators), leave 128 TMEM columns for the scales of
-  // seven stages.  Groups that hold 64 rows on average take tiles of 64: a stage is then smaller and
-  // more stages of W are in flight, which is what bounds a product with few rows.
+  // The widest tile.  256 columns move the fewest operand bytes per MAC, which is what bounds large groups
+  // (65536 x 4096 x 4096 over 32 groups: 943 us with 192, see the measurements below).  Groups that hold 64
+  // rows on average take tiles of 64: a stage is then smaller and more stages of W are in flight, which is what
+  // bounds a product with few rows.
   const int64_t avg = KG ? a.x_rows : a.x_rows / (a.groups ? a.groups : 1);
-  p.max_n = avg <= 64 ? 64 : avg <= 128 ? 128 : 192;
+  p.max_n = avg <= 64 ? 64 : avg <= 128 ? 128 : 256;
+  p.shared_half = p.max_n == 256 ? 1u : 0u;
+  p.acc_step = p.shared_half ? 128 : p.max_n;
+  if (!operand_map(fn, &mxf, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, p.max_n / 2)) return cudaErrorInvalidValue;
   // scale chunks per stage: one of W, and X rows 64 .. 64 + max_n - 1 of a chunk grid of 128
-  p.sf_per_stage = 1 + (p.max_n == 64 ? 1 : 2);
+  p.sf_per_stage = 1 + (p.max_n == 64 ? 1 : p.max_n == 128 ? 2 : 3);
   p.x_stage_bytes = p.max_n / 2 * 128;
-  const uint32_t fixed = 1024 + (2 * kMaxStages + 4) * 8 + 16 + 2 * (p.groups + 1) * 4;
+  const uint32_t fixed = 1024 + (4 * kMaxStages + 4) * 8 + 16 + 2 * (p.groups + 1) * 4;
   const uint32_t per_stage = kWBytes + p.x_stage_bytes + 512 * p.sf_per_stage;
   p.stages = (232448u - fixed) / per_stage;
-  const uint32_t tmem_stages = (kTmemCols - 2 * p.max_n) / (4 * p.sf_per_stage);
+  const uint32_t tmem_stages = (kTmemCols - p.acc_step - p.max_n) / (4 * p.sf_per_stage);
   if (p.stages > tmem_stages) p.stages = tmem_stages;
   if (p.stages > kMaxStages) p.stages = kMaxStages;
   const uint32_t smem = fixed + p.stages * per_stage;
@@ -421,7 +490,7 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
   const int64_t most = KG ? a.groups * w_tiles * ((a.x_rows + p.max_n - 1) / p.max_n)
                           : w_tiles * (a.groups + a.x_rows / p.max_n);
   const uint32_t pairs = most < a.sm_count / 2 ? (uint32_t)most : (uint32_t)(a.sm_count / 2);
-  return launch_pdl(mx_gemm_grouped_kernel<KG>, dim3(2 * pairs), dim3(kThreads), smem, a.stream, mw, mx_, msw, msx, p);
+  return launch_pdl(mx_gemm_grouped_kernel<KG>, dim3(2 * pairs), dim3(kThreads), smem, a.stream, mw, mx_, mxf, msw, msx, p);
 }
 
 }  // namespace
