@@ -410,30 +410,60 @@ def mx_conv2d(x_elems: torch.Tensor, x_scales: torch.Tensor, w_elems: torch.Tens
 
 # ---- RMS norm, routing, moving rows, the experts' products ----------------------------
 
-def _on_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
-    """Every given tensor is contiguous and on ``device``, which is the current CUDA device (the
-    library launches there)."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors have to be on the current CUDA device, not on {device}")
-    for name, t in tensors.items():
-        if t is not None and (t.device != device or not t.is_contiguous()):
-            raise ValueError(f"{name} has to be a contiguous tensor on {device}")
+# These calls run in loops of a few microseconds per step: their checks ask the tensors directly and
+# sizes of 2-D MX tensors are computed here (they are those of mx_elems_bytes and mx_scales_bytes).
+_DTYPES = {torch.float32: MX_F32, torch.bfloat16: MX_BF16}
+_BITS = {MX_E4M3: 8, MX_E5M2: 8, MX_E3M2: 6, MX_E2M3: 6, MX_E2M1: 4, MX_INT8: 8}
 
 
-def _typed(dtype: torch.dtype, shape: Sequence[int], **tensors: Optional[torch.Tensor]) -> None:
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape)):
-            raise ValueError(f"{name} has to be {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+def _device_of(t: torch.Tensor) -> int:
+    """The index of the tensor's device, which has to be the current CUDA device (the library
+    launches there)."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors have to be on the current CUDA device, not on {t.device}")
+    return dev
 
 
-def _holds(nbytes: int, **tensors: torch.Tensor) -> None:
-    for name, t in tensors.items():
-        if t.numel() * t.element_size() < nbytes:
-            raise ValueError(f"{name} holds {t.numel() * t.element_size()} bytes, {nbytes} are needed")
+def _wrong(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Sequence[int]) -> ValueError:
+    return ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on the current CUDA "
+                      f"device, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _need(name: str, t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
+    """The address of a tensor of this type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise _wrong(name, t, dtype, shape)
+    return t.data_ptr()
+
+
+def _bytes(name: str, t: torch.Tensor, dev: int, nbytes: int) -> int:
+    """The address of a contiguous tensor of at least this many bytes."""
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous tensor on the current CUDA device")
+    if t.numel() * t.element_size() < nbytes:
+        raise ValueError(f"{name} holds {t.numel() * t.element_size()} bytes, {nbytes} are needed")
+    return t.data_ptr()
+
+
+def _mx_sizes(rows: int, dim: int, fmt: int, layout: int) -> Tuple[int, int]:
+    """Bytes of the codes and scales of an MX tensor [rows, dim]; 0 where the library refuses the call anyway."""
+    kb = (dim + 31) // 32
+    scales = rows * kb if layout == MX_SCALES_LINEAR else (rows + 127) // 128 * ((kb + 3) // 4) * 512
+    return rows * kb * 4 * _BITS.get(fmt, 0), scales
+
+
+def _call_opts(dev: int, dtype: int, layout: int = MX_SCALES_SWIZZLED, check: bool = False):
+    return ctypes.byref(mx_opts_t(dtype, layout, torch._C._cuda_getCurrentRawStream(dev), 1 if check else 0, 0))
+
+
+def _float_code(t: torch.Tensor) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported float dtype {t.dtype}")
+    return code
 
 
 def mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int, eps: float = 1e-6,
@@ -448,25 +478,22 @@ def mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int, eps: fl
     be ``x`` or ``residual``).  ``y_out`` also receives the norm itself."""
     if x.dim() != 2:
         raise ValueError("x has to be [rows, dim]")
-    rows, dim = x.shape
-    _on_device(x.device, x=x, weight=weight, residual=residual, y_out=y_out, h_out=h_out)
-    _typed(x.dtype, x.shape, residual=residual, y_out=y_out, h_out=h_out)
-    _typed(weight.dtype, (dim,), weight=weight)
+    shape, dt = x.shape, x.dtype
+    rows, dim = shape
+    dev = _device_of(x)
     if residual is not None and h_out is None:
         h_out = torch.empty_like(x)
-    ne, ns = mx_elems_bytes((rows, dim), 1, fmt), mx_scales_bytes((rows, dim), 1, layout)
+    ne, ns = _mx_sizes(rows, dim, fmt, layout)
     if out is None:
-        elems = torch.empty(ne, dtype=torch.uint8, device=x.device)
-        scales = torch.empty(ns, dtype=torch.uint8, device=x.device)
+        elems, scales = x.new_empty(ne, dtype=torch.uint8), x.new_empty(ns, dtype=torch.uint8)
+        pe, ps = elems.data_ptr(), scales.data_ptr()
     else:
         elems, scales = out
-        _on_device(x.device, elems=elems, scales=scales)
-        _holds(ne, elems=elems)
-        _holds(ns, scales=scales)
-    o = _opts(_dtype_code(x.dtype), layout)
-    _check(_lib.mx_rmsnorm_quantize(x.data_ptr(), _ptr(residual), weight.data_ptr(), _dtype_code(weight.dtype), eps,
-                                    rows, dim, _ptr(h_out), _ptr(y_out), elems.data_ptr(), scales.data_ptr(), fmt,
-                                    rounding, ctypes.byref(o)), "mx_rmsnorm_quantize")
+        pe, ps = _bytes("elems", elems, dev, ne), _bytes("scales", scales, dev, ns)
+    _check(_lib.mx_rmsnorm_quantize(_need("x", x, dev, dt, shape), _need("residual", residual, dev, dt, shape),
+                                    _need("weight", weight, dev, weight.dtype, (dim,)), _float_code(weight), eps, rows, dim,
+                                    _need("h_out", h_out, dev, dt, shape), _need("y_out", y_out, dev, dt, shape), pe, ps,
+                                    fmt, rounding, _call_opts(dev, _float_code(x), layout)), "mx_rmsnorm_quantize")
     return elems, scales, h_out
 
 
@@ -477,20 +504,18 @@ def mx_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
     receives dh and may be ``dy`` or ``dres``."""
     if h.dim() != 2:
         raise ValueError("h has to be [rows, dim]")
-    rows, dim = h.shape
-    _on_device(h.device, dy=dy, h=h, weight=weight, dres=dres, out=out, workspace=workspace)
-    _typed(h.dtype, h.shape, dy=dy, dres=dres, out=out)
-    _typed(weight.dtype, (dim,), weight=weight)
-    need = int(_lib.mx_rmsnorm_backward_workspace_bytes(rows, dim))
+    shape, dt = h.shape, h.dtype
+    rows, dim = shape
+    dev = _device_of(h)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=h.device)
+        workspace = h.new_empty(_lib.mx_rmsnorm_backward_workspace_bytes(rows, dim), dtype=torch.uint8)
     dh = torch.empty_like(h) if out is None else out
-    dweight = torch.empty(dim, dtype=torch.float32, device=h.device)
-    o = _opts(_dtype_code(h.dtype), MX_SCALES_SWIZZLED)
-    _check(_lib.mx_rmsnorm_backward(dy.data_ptr(), h.data_ptr(), weight.data_ptr(), _dtype_code(weight.dtype), eps,
-                                    _ptr(dres), rows, dim, dh.data_ptr(), dweight.data_ptr(), ctypes.byref(o),
-                                    workspace.data_ptr(), workspace.numel() * workspace.element_size()),
-           "mx_rmsnorm_backward")
+    dweight = h.new_empty(dim, dtype=torch.float32)
+    _check(_lib.mx_rmsnorm_backward(_need("dy", dy, dev, dt, shape), _need("h", h, dev, dt, shape),
+                                    _need("weight", weight, dev, weight.dtype, (dim,)), _float_code(weight), eps,
+                                    _need("dres", dres, dev, dt, shape), rows, dim, _need("out", dh, dev, dt, shape),
+                                    dweight.data_ptr(), _call_opts(dev, _float_code(h)), _bytes("workspace", workspace, dev, 0),
+                                    workspace.numel() * workspace.element_size()), "mx_rmsnorm_backward")
     return dh, dweight
 
 
@@ -502,14 +527,14 @@ def mx_route(logits: torch.Tensor, topk: int, score: int = MX_SCORE_SOFTMAX, bia
     if logits.dim() != 2:
         raise ValueError("logits has to be [tokens, experts]")
     tokens, experts = logits.shape
-    _on_device(logits.device, logits=logits, bias=bias)
-    _typed(torch.float32, (experts,), bias=bias)
-    ids = torch.empty((tokens, topk), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((tokens, topk), dtype=torch.float32, device=logits.device)
+    dev = _device_of(logits)
+    width = topk if topk > 0 else 0  # (the library refuses the rest)
+    ids = logits.new_empty((tokens, width), dtype=torch.int32)
+    weights = logits.new_empty((tokens, width), dtype=torch.float32)
     r = mx_route_t(topk, score, groups, topk_groups, group_score, 1 if renormalize else 0, scale)
-    o = _opts(_dtype_code(logits.dtype), MX_SCALES_SWIZZLED)
-    _check(_lib.mx_route(logits.data_ptr(), _ptr(bias), tokens, experts, ctypes.byref(r), ids.data_ptr(),
-                         weights.data_ptr(), ctypes.byref(o)), "mx_route")
+    _check(_lib.mx_route(_need("logits", logits, dev, logits.dtype, logits.shape), _need("bias", bias, dev, torch.float32, (experts,)),
+                         tokens, experts, ctypes.byref(r), ids.data_ptr(), weights.data_ptr(),
+                         _call_opts(dev, _float_code(logits))), "mx_route")
     return ids, weights
 
 
@@ -519,14 +544,14 @@ def mx_route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.T
     if logits.dim() != 2 or ids.dim() != 2:
         raise ValueError("logits has to be [tokens, experts], ids [tokens, topk]")
     tokens, experts = logits.shape
-    _on_device(logits.device, dweights=dweights, logits=logits, ids=ids)
-    _typed(torch.int32, (tokens, ids.shape[1]), ids=ids)
-    _typed(torch.float32, ids.shape, dweights=dweights)
+    topk = ids.shape[1]
+    dev = _device_of(logits)
     dlogits = torch.empty_like(logits)
-    r = mx_route_t(ids.shape[1], score, 1, 1, MX_GROUP_MAX, 1 if renormalize else 0, scale)
-    o = _opts(_dtype_code(logits.dtype), MX_SCALES_SWIZZLED)
-    _check(_lib.mx_route_backward(dweights.data_ptr(), logits.data_ptr(), ids.data_ptr(), tokens, experts,
-                                  ctypes.byref(r), dlogits.data_ptr(), ctypes.byref(o)), "mx_route_backward")
+    r = mx_route_t(topk, score, 1, 1, MX_GROUP_MAX, 1 if renormalize else 0, scale)
+    _check(_lib.mx_route_backward(_need("dweights", dweights, dev, torch.float32, (tokens, topk)),
+                                  _need("logits", logits, dev, logits.dtype, logits.shape),
+                                  _need("ids", ids, dev, torch.int32, (tokens, topk)), tokens, experts, ctypes.byref(r),
+                                  dlogits.data_ptr(), _call_opts(dev, _float_code(logits))), "mx_route_backward")
     return dlogits
 
 
@@ -551,29 +576,26 @@ def mx_moe_plan(ids: torch.Tensor, experts: int, align: int = 64,
     if ids.dim() != 2:
         raise ValueError("ids has to be [tokens, topk]")
     tokens, topk = ids.shape
-    _on_device(ids.device, ids=ids, workspace=workspace)
-    _typed(torch.int32, ids.shape, ids=ids)
-    need = int(_lib.mx_moe_plan_workspace_bytes(tokens, topk, experts))
+    dev = _device_of(ids)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=ids.device)
-    i32 = dict(dtype=torch.int32, device=ids.device)
-    plan = MoePlan(torch.empty(max(experts, 0) + 1, **i32), torch.empty(max(experts, 0), **i32), torch.empty_like(ids),
-                   mx_moe_rows(tokens, topk, experts, align))
-    o = _opts(MX_F32, MX_SCALES_SWIZZLED)
-    _check(_lib.mx_moe_plan(ids.data_ptr(), tokens, topk, experts, align, plan.offsets.data_ptr(),
-                            plan.counts.data_ptr(), plan.row_of.data_ptr(), ctypes.byref(o), workspace.data_ptr(),
-                            workspace.numel() * workspace.element_size()), "mx_moe_plan")
+        workspace = ids.new_empty(_lib.mx_moe_plan_workspace_bytes(tokens, topk, experts), dtype=torch.uint8)
+    plan = MoePlan(ids.new_empty(max(experts, 0) + 1), ids.new_empty(max(experts, 0)), torch.empty_like(ids),
+                   _lib.mx_moe_rows(tokens, topk, experts, align))
+    _check(_lib.mx_moe_plan(_need("ids", ids, dev, torch.int32, ids.shape), tokens, topk, experts, align,
+                            plan.offsets.data_ptr(), plan.counts.data_ptr(), plan.row_of.data_ptr(), _call_opts(dev, MX_F32),
+                            _bytes("workspace", workspace, dev, 0), workspace.numel() * workspace.element_size()), "mx_moe_plan")
     return plan
 
 
-def _check_plan(device: torch.device, plan: MoePlan) -> Tuple[int, int, int]:
-    _on_device(device, offsets=plan.offsets, counts=plan.counts, row_of=plan.row_of)
+def _plan_args(plan: MoePlan, dev: int):
+    """tokens, topk, experts and the addresses of offsets, counts and row_of."""
+    if plan.row_of.dim() != 2:
+        raise ValueError("row_of has to be [tokens, topk]")
     tokens, topk = plan.row_of.shape
     experts = plan.counts.numel()
-    _typed(torch.int32, (experts + 1,), offsets=plan.offsets)
-    _typed(torch.int32, (experts,), counts=plan.counts)
-    _typed(torch.int32, (tokens, topk), row_of=plan.row_of)
-    return tokens, topk, experts
+    return (tokens, topk, experts, _need("offsets", plan.offsets, dev, torch.int32, (experts + 1,)),
+            _need("counts", plan.counts, dev, torch.int32, (experts,)),
+            _need("row_of", plan.row_of, dev, torch.int32, (tokens, topk)))
 
 
 def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int, plan: MoePlan,
@@ -581,39 +603,31 @@ def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int,
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The rows of an MX tensor [tokens, dim] in the order of ``plan``: (elems, scales) of an MX tensor
     [plan.rows, dim], rows without a choice zero."""
-    tokens, topk, experts = _check_plan(elems.device, plan)
-    _on_device(elems.device, elems=elems, scales=scales)
-    _holds(mx_elems_bytes((tokens, dim), 1, fmt), elems=elems)
-    _holds(mx_scales_bytes((tokens, dim), 1, layout), scales=scales)
-    ne, ns = mx_elems_bytes((plan.rows, dim), 1, fmt), mx_scales_bytes((plan.rows, dim), 1, layout)
+    dev = _device_of(elems)
+    tokens, topk, experts, offsets, counts, row_of = _plan_args(plan, dev)
+    ni, nsi = _mx_sizes(tokens, dim, fmt, layout)
+    ne, ns = _mx_sizes(plan.rows, dim, fmt, layout)
     if out is None:
-        out = (torch.empty(ne, dtype=torch.uint8, device=elems.device),
-               torch.empty(ns, dtype=torch.uint8, device=elems.device))
-    else:
-        _on_device(elems.device, out_elems=out[0], out_scales=out[1])
-        _holds(ne, out_elems=out[0])
-        _holds(ns, out_scales=out[1])
-    o = _opts(MX_F32, layout)
-    _check(_lib.mx_moe_gather(elems.data_ptr(), scales.data_ptr(), tokens, topk, dim, fmt, plan.offsets.data_ptr(),
-                              plan.counts.data_ptr(), plan.row_of.data_ptr(), experts, plan.rows,
-                              out[0].data_ptr(), out[1].data_ptr(), ctypes.byref(o)), "mx_moe_gather")
+        out = (elems.new_empty(ne, dtype=torch.uint8), elems.new_empty(ns, dtype=torch.uint8))
+    _check(_lib.mx_moe_gather(_bytes("elems", elems, dev, ni), _bytes("scales", scales, dev, nsi), tokens, topk, dim, fmt,
+                              offsets, counts, row_of, experts, plan.rows, _bytes("out elems", out[0], dev, ne),
+                              _bytes("out scales", out[1], dev, ns), _call_opts(dev, MX_F32, layout)), "mx_moe_gather")
     return out
 
 
 def mx_moe_combine(y: torch.Tensor, weights: Optional[torch.Tensor], plan: MoePlan,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[t] = sum over j of weights[t, j] * y[row_of[t, j]] (``weights`` None: all 1); y [plan.rows, dim]."""
-    tokens, topk, _ = _check_plan(y.device, plan)
-    if y.dim() != 2 or y.shape[0] != plan.rows:
+    dev = _device_of(y)
+    tokens, topk, _, _, _, row_of = _plan_args(plan, dev)
+    if y.dim() != 2:
         raise ValueError(f"y has to be [{plan.rows}, dim]")
-    _on_device(y.device, y=y, weights=weights, out=out)
-    _typed(torch.float32, (tokens, topk), weights=weights)
-    _typed(y.dtype, (tokens, y.shape[1]), out=out)
+    dim = y.shape[1]
     if out is None:
-        out = torch.empty((tokens, y.shape[1]), dtype=y.dtype, device=y.device)
-    o = _opts(_dtype_code(y.dtype), MX_SCALES_SWIZZLED)
-    _check(_lib.mx_moe_combine(y.data_ptr(), _ptr(weights), plan.row_of.data_ptr(), tokens, topk, y.shape[1],
-                               plan.rows, out.data_ptr(), ctypes.byref(o)), "mx_moe_combine")
+        out = y.new_empty((tokens, dim))
+    _check(_lib.mx_moe_combine(_need("y", y, dev, y.dtype, (plan.rows, dim)), _need("weights", weights, dev, torch.float32, (tokens, topk)),
+                               row_of, tokens, topk, dim, plan.rows, _need("out", out, dev, y.dtype, (tokens, dim)),
+                               _call_opts(dev, _float_code(y))), "mx_moe_combine")
     return out
 
 
@@ -621,27 +635,23 @@ def mx_moe_combine_backward(dout: torch.Tensor, y: Optional[torch.Tensor], weigh
                             plan: MoePlan) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Gradients of mx_moe_combine: (dy [plan.rows, dim], dweights FP32 [tokens, topk]).  Without ``y``
     only dy; without ``weights`` as well it is the gather of the rows of a float tensor."""
-    tokens, topk, experts = _check_plan(dout.device, plan)
-    if dout.dim() != 2 or dout.shape[0] != tokens:
+    dev = _device_of(dout)
+    tokens, topk, experts, offsets, counts, row_of = _plan_args(plan, dev)
+    if dout.dim() != 2:
         raise ValueError(f"dout has to be [{tokens}, dim]")
-    dim = dout.shape[1]
-    _on_device(dout.device, dout=dout, y=y, weights=weights)
-    _typed(dout.dtype, (plan.rows, dim), y=y)
-    _typed(torch.float32, (tokens, topk), weights=weights)
-    dy = torch.empty((plan.rows, dim), dtype=dout.dtype, device=dout.device)
-    dw = None if y is None else torch.empty((tokens, topk), dtype=torch.float32, device=dout.device)
-    o = _opts(_dtype_code(dout.dtype), MX_SCALES_SWIZZLED)
-    _check(_lib.mx_moe_combine_backward(dout.data_ptr(), _ptr(y), _ptr(weights), plan.offsets.data_ptr(),
-                                        plan.counts.data_ptr(), plan.row_of.data_ptr(), tokens, topk, dim, experts,
-                                        plan.rows, dy.data_ptr(), _ptr(dw), ctypes.byref(o)),
-           "mx_moe_combine_backward")
+    dim, dt = dout.shape[1], dout.dtype
+    dy = dout.new_empty((plan.rows, dim))
+    dw = None if y is None else dout.new_empty((tokens, topk), dtype=torch.float32)
+    _check(_lib.mx_moe_combine_backward(_need("dout", dout, dev, dt, (tokens, dim)), _need("y", y, dev, dt, (plan.rows, dim)),
+                                        _need("weights", weights, dev, torch.float32, (tokens, topk)), offsets, counts, row_of,
+                                        tokens, topk, dim, experts, plan.rows, dy.data_ptr(), None if dw is None else dw.data_ptr(),
+                                        _call_opts(dev, _float_code(dout))), "mx_moe_combine_backward")
     return dy, dw
 
 
-def _check_operand(elems: torch.Tensor, scales: torch.Tensor, rows: int, K: int, fmt: int, name: str) -> None:
-    _on_device(elems.device, **{name: elems, "s" + name: scales})
-    _holds(mx_elems_bytes((rows, K), 1, fmt), **{name: elems})
-    _holds(mx_scales_bytes((rows, K), 1), **{"s" + name: scales})
+def _operand(name: str, elems: torch.Tensor, scales: torch.Tensor, dev: int, rows: int, K: int, fmt: int):
+    ne, ns = _mx_sizes(rows, K, fmt, MX_SCALES_SWIZZLED)
+    return _bytes(name, elems, dev, ne), _bytes("s" + name, scales, dev, ns)
 
 
 def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
@@ -651,17 +661,14 @@ def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torc
     multiples of 64): A is the MX tensor [rows, K], B that of [groups, N, K]; rows in no group are not
     written."""
     groups = offsets.numel() - 1
-    _on_device(A.device, offsets=offsets, out=out)
-    _typed(torch.int32, (groups + 1,), offsets=offsets)
-    _check_operand(A, sA, rows, K, fmtA, "A")
-    _check_operand(B, sB, groups * N, K, fmtB, "B")
+    dev = _device_of(A)
     if out is None:
         out = torch.empty((rows, N), dtype=out_dtype, device=A.device)
-    _typed(out.dtype, (rows, N), out=out)
-    o = _opts(MX_F32, MX_SCALES_SWIZZLED, check=check_status)
-    _check(_lib.mx_gemm_grouped(A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), offsets.data_ptr(),
-                                out.data_ptr(), _dtype_code(out.dtype), groups, rows, N, K, fmtA, fmtB,
-                                ctypes.byref(o)), "mx_gemm_grouped")
+    pa, psa = _operand("A", A, sA, dev, rows, K, fmtA)
+    pb, psb = _operand("B", B, sB, dev, groups * N, K, fmtB)
+    _check(_lib.mx_gemm_grouped(pa, psa, pb, psb, _need("offsets", offsets, dev, torch.int32, (groups + 1,)),
+                                _need("out", out, dev, out.dtype, (rows, N)), _float_code(out), groups, rows, N, K, fmtA, fmtB,
+                                _call_opts(dev, MX_F32, check=check_status)), "mx_gemm_grouped")
     return out
 
 
@@ -671,17 +678,14 @@ def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: to
     """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128): A is the
     MX tensor [M, rows], B [N, rows], both quantized along the rows; C [groups, M, N]."""
     groups = offsets.numel() - 1
-    _on_device(A.device, offsets=offsets, out=out)
-    _typed(torch.int32, (groups + 1,), offsets=offsets)
-    _check_operand(A, sA, M, rows, fmtA, "A")
-    _check_operand(B, sB, N, rows, fmtB, "B")
+    dev = _device_of(A)
     if out is None:
         out = torch.empty((groups, M, N), dtype=out_dtype, device=A.device)
-    _typed(out.dtype, (groups, M, N), out=out)
-    o = _opts(MX_F32, MX_SCALES_SWIZZLED, check=check_status)
-    _check(_lib.mx_gemm_grouped_k(A.data_ptr(), sA.data_ptr(), B.data_ptr(), sB.data_ptr(), offsets.data_ptr(),
-                                  out.data_ptr(), _dtype_code(out.dtype), groups, M, N, rows, fmtA, fmtB,
-                                  ctypes.byref(o)), "mx_gemm_grouped_k")
+    pa, psa = _operand("A", A, sA, dev, M, rows, fmtA)
+    pb, psb = _operand("B", B, sB, dev, N, rows, fmtB)
+    _check(_lib.mx_gemm_grouped_k(pa, psa, pb, psb, _need("offsets", offsets, dev, torch.int32, (groups + 1,)),
+                                  _need("out", out, dev, out.dtype, (groups, M, N)), _float_code(out), groups, M, N, rows, fmtA,
+                                  fmtB, _call_opts(dev, MX_F32, check=check_status)), "mx_gemm_grouped_k")
     return out
 
 

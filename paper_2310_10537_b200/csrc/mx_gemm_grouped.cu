@@ -56,13 +56,13 @@ __device__ unsigned int g_grouped_status;
 struct GroupedParams {
   const int32_t* offsets;
   void* C;
-  uint32_t c_bf16, groups, w_rows, x_rows, k_chunks;  // k_chunks: of the whole K axis
-  uint32_t max_n, acc_step, shared_half, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
+  uint32_t c_bf16, groups, w_rows, x_rows, k_chunks, k_stages;  // the whole K axis in chunks, in stages
+  uint32_t max_n, acc_step, shared_half, band, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
   long long spin_limit;
 };
 
 // One tile of C for a pair: W rows w0 .. w0 + 255, X rows x0 .. x0 + n - 1 (n a multiple of 32, those
-// from x_end on are not stored), K chunks k0 .. k0 + nk - 1.
+// from x_end on are not stored), nk stages from K chunk k0 on.
 struct Item {
   uint32_t group, w0, x0, n, x_end, k0, nk;
 };
@@ -85,7 +85,11 @@ __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& 
   const uint32_t o = tb.offset[g], len = tb.offset[g + 1] > o ? tb.offset[g + 1] - o : 0u;
   const uint32_t rows = KG ? p.x_rows : len;
   const uint32_t tiles = x_tiles(rows, p.max_n), step = x_step(rows, tiles);
-  const uint32_t j = t - tb.first[g], wt = j / tiles, xt = j - wt * tiles;
+  // bands of X tiles: every W tile meets a band before the next band begins, so that the tiles which
+  // all pairs work on at a time share both operands in the L2
+  const uint32_t j = t - tb.first[g], w_tiles = (p.w_rows + 255) / 256, per_band = p.band * w_tiles;
+  const uint32_t b = j / per_band, in_band = j - b * per_band, bx = min(p.band, tiles - b * p.band);
+  const uint32_t wt = in_band / bx, xt = b * p.band + (in_band - wt * bx);
   it.group = g;
   it.w0 = wt * 256;
   it.x0 = xt * step;
@@ -99,8 +103,15 @@ __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& 
     it.x0 += o;
     it.x_end += o;
     it.k0 = 0;
-    it.nk = p.k_chunks;
+    it.nk = p.k_stages;
   }
+  // Every lane holds the same item, but it comes out of shared memory and the compiler does not know: a
+  // broadcast says so.  Without it each copy and MMA has its operands moved to uniform registers first,
+  // at 70 to 150 clocks an instruction, and the issuing warps set the pace (628 clocks per stage of a 256 x 256
+  // tile, whose MMAs take 512).
+  auto same = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
+  it.group = same(it.group); it.w0 = same(it.w0); it.x0 = same(it.x0); it.n = same(it.n);
+  it.x_end = same(it.x_end); it.k0 = same(it.k0); it.nk = same(it.nk);
   return true;
 }
 
@@ -117,7 +128,7 @@ __device__ __forceinline__ void raise_abort(volatile uint32_t* abort_flag, unsig
   *abort_flag = 1u;
 }
 
-template <bool KG>
+template <bool KG, uint32_t KCH>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x,
                        const __grid_constant__ CUtensorMap tmap_xf, const __grid_constant__ CUtensorMap tmap_sw,
@@ -125,8 +136,9 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t stage_bytes = kWBytes + p.x_stage_bytes;   // operands; a multiple of 1024
-  const uint32_t sf_bytes = 512u * p.sf_per_stage;
+  // a stage holds kch K chunks of 128 elements, each with its W, X and scale bytes
+  const uint32_t chunk_bytes = kWBytes + p.x_stage_bytes, stage_bytes = KCH * chunk_bytes;  // multiples of 1024
+  const uint32_t sf_chunk = 512u * p.sf_per_stage, sf_bytes = KCH * sf_chunk;
   const uint32_t off_sf = p.stages * stage_bytes, off_bar = off_sf + p.stages * sf_bytes;
   constexpr uint32_t kBars = 4 * kMaxStages + 4;
   const uint32_t bar0 = smem_base + off_bar;
@@ -220,8 +232,8 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       const uint32_t wrow = (KG ? 0u : it.group * p.w_rows) + it.w0 + rank * 128u;
       const uint32_t half = it.n >> 1, xrow = it.x0 + rank * half, boxes = half / kXBoxRows;
       const bool whole = it.n == p.max_n;  // a full tile's X rows are one copy
-      const uint32_t sx0 = it.x0 >> 7, sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
-      const uint32_t tx = scales ? 2u * 512u * (1u + sx_n) : 2u * (p.w_box_bytes + boxes * p.x_box_bytes);
+      const uint32_t sx0 = it.x0 >> 7;
+      const uint32_t tx = 2u * KCH * (scales ? sf_chunk : p.w_box_bytes + boxes * p.x_box_bytes);
       for (uint32_t kc = 0; kc < it.nk; ++kc) {
         ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit));
         if (!ok) {
@@ -231,19 +243,23 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         if (elect_one()) {
           const uint32_t bar = scales ? sf_full_bar(stage) : full_bar(stage), fb = leader_bar(bar);
           if (rank == 0) mbar_arrive_expect_tx(bar, tx);
-          const int kx = (int)((it.k0 + kc) * kBK), kz = (int)(it.k0 + kc);
-          if (scales) {
-            const uint32_t ds = smem_base + off_sf + stage * sf_bytes;
-            tma_load_3d_pair(ds, &tmap_sw, 0, kz, (int)(wrow >> 7), fb);
-            for (uint32_t c = 0; c < sx_n; ++c) tma_load_3d_pair(ds + 512u * (1u + c), &tmap_sx, 0, kz, (int)(sx0 + c), fb);
-          } else {
-            const uint32_t dw = smem_base + stage * stage_bytes, dx = dw + kWBytes;
-            tma_load_3d_pair(dw, &tmap_w, kx, (int)wrow, 0, fb);
-            if (whole) {
-              tma_load_3d_pair(dx, &tmap_xf, kx, (int)xrow, 0, fb);
+#pragma unroll
+          for (uint32_t c = 0; c < KCH; ++c) {  // (a chunk past the end of K is filled with zeros)
+            const uint32_t chunk = it.k0 + kc * KCH + c;
+            const int kx = (int)(chunk * kBK), kz = (int)chunk;
+            if (scales) {
+              const uint32_t ds = smem_base + off_sf + stage * sf_bytes + c * sf_chunk;
+              tma_load_3d_pair(ds, &tmap_sw, 0, kz, (int)(wrow >> 7), fb);
+              tma_load_3d_pair(ds + 512u, &tmap_sx, 0, kz, (int)sx0, fb);
             } else {
-              for (uint32_t b = 0; b < boxes; ++b)
-                tma_load_3d_pair(dx + b * (kXBoxRows * 128u), &tmap_x, kx, (int)(xrow + b * kXBoxRows), 0, fb);
+              const uint32_t dw = smem_base + stage * stage_bytes + c * chunk_bytes, dx = dw + kWBytes;
+              tma_load_3d_pair(dw, &tmap_w, kx, (int)wrow, 0, fb);
+              if (whole) {
+                tma_load_3d_pair(dx, &tmap_xf, kx, (int)xrow, 0, fb);
+              } else {
+                for (uint32_t j = 0; j < boxes; ++j)
+                  tma_load_3d_pair(dx + j * (kXBoxRows * 128u), &tmap_x, kx, (int)(xrow + j * kXBoxRows), 0, fb);
+              }
             }
           }
         }
@@ -262,7 +278,6 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       bool ok = true;
       Item it;
       for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
-        const uint32_t sx_n = ((it.x0 & 127u) + it.n + 127u) >> 7;
         for (uint32_t kc = 0; kc < it.nk; ++kc) {
           ok = __all_sync(0xffffffffu, mbar_wait(sf_full_bar(stage), phase, abort_flag, p.spin_limit));
           if (!ok) {
@@ -270,10 +285,13 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             break;
           }
           tc_fence_after();
-          const uint32_t sf_smem = smem_base + off_sf + stage * sf_bytes;
-          const uint32_t sf_tmem = tmem_base + sf_col0 + stage * (4u * p.sf_per_stage);
           if (elect_one()) {
-            for (uint32_t c = 0; c <= sx_n; ++c) tc_cp_scales_pair(sf_tmem + 4 * c, scale_desc(sf_smem + 512 * c));
+#pragma unroll
+            for (uint32_t c = 0; c < KCH; ++c) {
+              const uint32_t sf_smem = smem_base + off_sf + stage * sf_bytes + c * sf_chunk;
+              const uint32_t sf_tmem = tmem_base + sf_col0 + (stage * KCH + c) * (4u * p.sf_per_stage);
+              for (uint32_t j = 0; j < p.sf_per_stage; ++j) tc_cp_scales_pair(sf_tmem + 4 * j, scale_desc(sf_smem + 512 * j));
+            }
             tc_commit_leader(sf_ready_bar(stage));  // arrives when the copies have completed in both CTAs
           }
           __syncwarp();
@@ -305,14 +323,17 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             break;
           }
           tc_fence_after();
-          const uint32_t sf_tmem = tmem_base + sf_col0 + stage * (4u * p.sf_per_stage);
-          const uint64_t wdesc = operand_desc(smem_base + stage * stage_bytes);
-          const uint64_t xdesc = operand_desc(smem_base + stage * stage_bytes + kWBytes);
           if (elect_one()) {
 #pragma unroll
-            for (uint32_t k = 0; k < 4; ++k)  // byte k of each scale column belongs to MX block k of the stage
-              tc_mma_pair(d_tmem, wdesc + 2 * k, xdesc + 2 * k, idesc0 | (k << 4) | (k << 29), sf_tmem, sf_tmem + sx_col,
-                          (kc | k) != 0 ? 1u : 0u);
+            for (uint32_t c = 0; c < KCH; ++c) {
+              const uint32_t sf_tmem = tmem_base + sf_col0 + (stage * KCH + c) * (4u * p.sf_per_stage);
+              const uint64_t wdesc = operand_desc(smem_base + stage * stage_bytes + c * chunk_bytes);
+              const uint64_t xdesc = operand_desc(smem_base + stage * stage_bytes + c * chunk_bytes + kWBytes);
+#pragma unroll
+              for (uint32_t k = 0; k < 4; ++k)  // byte k of each scale column belongs to MX block k of the chunk
+                tc_mma_pair(d_tmem, wdesc + 2 * k, xdesc + 2 * k, idesc0 | (k << 4) | (k << 29), sf_tmem, sf_tmem + sx_col,
+                            (kc | c | k) != 0 ? 1u : 0u);
+            }
             tc_commit_pair(empty_bar(stage));
           }
           __syncwarp();
@@ -433,40 +454,40 @@ bool operand_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, int fmt, u
                 CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// Swizzled scale tensor as [groups of 128 rows][K chunks][128 words], a box per 512-byte chunk.
-bool scale_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K) {
+// Swizzled scale tensor as [groups of 128 rows][K chunks][128 words], a box `chunks` 512-byte chunks of
+// consecutive row groups.
+bool scale_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t K, uint32_t chunks) {
   const uint64_t k_chunks = (K + kBK - 1) / kBK;
   return encode(fn, map, CU_TENSOR_MAP_DATA_TYPE_UINT32, ptr, {128, k_chunks, (rows + 127) / 128},
-                {512, 512 * k_chunks}, {128, 1, 1}, CU_TENSOR_MAP_SWIZZLE_NONE);
+                {512, 512 * k_chunks}, {128, 1, chunks}, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <bool KG>
-cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
+template <bool KG, uint32_t KCH>
+cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn, uint32_t max_n) {
   CUtensorMap mw, mx_, mxf, msw, msx;
   const uint64_t w_all = (uint64_t)a.w_rows * (KG ? 1u : (uint64_t)a.groups);
   if (!operand_map(fn, &mw, a.W, a.fmtW, w_all, (uint64_t)a.K, 128) ||
       !operand_map(fn, &mx_, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, kXBoxRows) ||
-      !scale_map(fn, &msw, a.sW, w_all, (uint64_t)a.K) || !scale_map(fn, &msx, a.sX, (uint64_t)a.x_rows, (uint64_t)a.K))
+      !scale_map(fn, &msw, a.sW, w_all, (uint64_t)a.K, 1))
     return cudaErrorInvalidValue;
   GroupedParams p;
   p.offsets = a.offsets; p.C = a.C; p.c_bf16 = (uint32_t)a.c_bf16; p.groups = (uint32_t)a.groups;
   p.w_rows = (uint32_t)a.w_rows; p.x_rows = (uint32_t)a.x_rows; p.k_chunks = (uint32_t)((a.K + kBK - 1) / kBK);
-  // The widest tile.  256 columns move the fewest operand bytes per MAC, which is what bounds large groups
-  // (65536 x 4096 x 4096 over 32 groups: 943 us with 192, see the measurements below).  Groups that hold 64
-  // rows on average take tiles of 64: a stage is then smaller and more stages of W are in flight, which is what
-  // bounds a product with few rows.
-  const int64_t avg = KG ? a.x_rows : a.x_rows / (a.groups ? a.groups : 1);
-  p.max_n = avg <= 64 ? 64 : avg <= 128 ? 128 : 256;
+  p.max_n = max_n;
   p.shared_half = p.max_n == 256 ? 1u : 0u;
   p.acc_step = p.shared_half ? 128 : p.max_n;
-  if (!operand_map(fn, &mxf, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, p.max_n / 2)) return cudaErrorInvalidValue;
   // scale chunks per stage: one of W, and X rows 64 .. 64 + max_n - 1 of a chunk grid of 128
   p.sf_per_stage = 1 + (p.max_n == 64 ? 1 : p.max_n == 128 ? 2 : 3);
+  if (!operand_map(fn, &mxf, a.X, a.fmtX, (uint64_t)a.x_rows, (uint64_t)a.K, p.max_n / 2) ||
+      !scale_map(fn, &msx, a.sX, (uint64_t)a.x_rows, (uint64_t)a.K, p.sf_per_stage - 1))
+    return cudaErrorInvalidValue;
   p.x_stage_bytes = p.max_n / 2 * 128;
+  p.k_stages = (p.k_chunks + KCH - 1) / KCH;
+  p.band = 16;
   const uint32_t fixed = 1024 + (4 * kMaxStages + 4) * 8 + 16 + 2 * (p.groups + 1) * 4;
-  const uint32_t per_stage = kWBytes + p.x_stage_bytes + 512 * p.sf_per_stage;
+  const uint32_t per_stage = KCH * (kWBytes + p.x_stage_bytes + 512 * p.sf_per_stage);
   p.stages = (232448u - fixed) / per_stage;
-  const uint32_t tmem_stages = (kTmemCols - p.acc_step - p.max_n) / (4 * p.sf_per_stage);
+  const uint32_t tmem_stages = (kTmemCols - p.acc_step - p.max_n) / (4 * p.sf_per_stage * KCH);
   if (p.stages > tmem_stages) p.stages = tmem_stages;
   if (p.stages > kMaxStages) p.stages = kMaxStages;
   const uint32_t smem = fixed + p.stages * per_stage;
@@ -481,7 +502,7 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(mx_gemm_grouped_kernel<KG>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+    e = cudaFuncSetAttribute(mx_gemm_grouped_kernel<KG, KCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) attr_set[dev] = true;
   }
@@ -490,7 +511,7 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn) {
   const int64_t most = KG ? a.groups * w_tiles * ((a.x_rows + p.max_n - 1) / p.max_n)
                           : w_tiles * (a.groups + a.x_rows / p.max_n);
   const uint32_t pairs = most < a.sm_count / 2 ? (uint32_t)most : (uint32_t)(a.sm_count / 2);
-  return launch_pdl(mx_gemm_grouped_kernel<KG>, dim3(2 * pairs), dim3(kThreads), smem, a.stream, mw, mx_, mxf, msw, msx, p);
+  return launch_pdl(mx_gemm_grouped_kernel<KG, KCH>, dim3(2 * pairs), dim3(kThreads), smem, a.stream, mw, mx_, mxf, msw, msx, p);
 }
 
 }  // namespace
@@ -499,7 +520,16 @@ int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err) {
   *cuda_err = cudaSuccess;
   EncodeTiledFn fn = encode_fn(cuda_err);
   if (!fn) return MX_ERR_CUDA;
-  *cuda_err = a.k_groups ? launch_kernel<true>(a, fn) : launch_kernel<false>(a, fn);
+  // The widest tile.  256 columns move the fewest operand bytes per MAC, which is what bounds large groups
+  // (65536 x 4096 x 4096 over 32 groups: 943 us with 192, 835 with 256).  Groups that hold 64
+  // rows on average take tiles of 64: a stage is then smaller and more of W is in flight, which is what
+  // bounds a product with few rows; two K chunks share a stage there, since the hand-overs of a stage of
+  // one chunk take as long as its copies (128 rows on 56 experts of 2048 x 4096: FP4 weights 66.9 -> 57.1 us
+  // with two, FP8 88.9 -> 85.3).  A plan's row bound holds up to 63 rows of padding a group: hence 96 and 192.
+  const int64_t avg = a.k_groups ? a.x_rows : a.x_rows / a.groups;
+  const uint32_t max_n = avg <= 96 ? 64 : avg <= 192 ? 128 : 256;
+  *cuda_err = a.k_groups ? launch_kernel<true, 1>(a, fn, max_n)
+                         : max_n == 64 ? launch_kernel<false, 2>(a, fn, max_n) : launch_kernel<false, 1>(a, fn, max_n);
   return *cuda_err == cudaSuccess ? MX_OK : MX_ERR_CUDA;
 }
 
