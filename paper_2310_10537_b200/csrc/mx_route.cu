@@ -20,6 +20,7 @@ struct RouteParams {
   float* weights;
   void* dlogits;
   uint32_t tokens, experts, topk, score, groups, topk_groups, group_score, renormalize, group_size;
+  FastDiv by_group_size;
   float scale;
 };
 
@@ -74,6 +75,23 @@ __device__ __forceinline__ void load_logits(const RouteParams& p, uint32_t token
   }
 }
 
+// The lane's NV biases.
+template <int NV>
+__device__ __forceinline__ void load_bias(const RouteParams& p, uint32_t e0, float (&b)[NV]) {
+  if constexpr (NV % 4 == 0) {
+    if ((reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0 && e0 + NV <= p.experts) {
+#pragma unroll
+      for (int i = 0; i < NV / 4; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(p.bias + e0) + i);
+        b[4 * i] = v.x; b[4 * i + 1] = v.y; b[4 * i + 2] = v.z; b[4 * i + 3] = v.w;
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) b[j] = e0 + j < p.experts ? __ldg(p.bias + e0 + j) : 0.0f;
+}
+
 __device__ __forceinline__ float warp_max(float v) {  // NaN wins
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
@@ -112,6 +130,92 @@ __device__ __forceinline__ void top2_add(uint32_t& a, uint32_t& b, uint32_t k) {
   a = max(a, k);
 }
 
+// The topk best keys of the warp, in descending order, equal ones in the order of the experts: lane i gets
+// the i-th one's expert and logit.  `smem`: 64 words of the warp.
+//
+// Taking the best of all keys topk times costs a pass over a lane's NV keys each time.  So the field is cut down
+// first: the topk-th largest of the lanes' own maxima is a floor under the topk-th largest key, and what is not
+// below it -- little more than topk keys -- is laid out one per lane, where taking the best is a reduction and
+// a vote.  More than 32 of them (many equal keys), or fewer lanes with candidates than topk: key by key.
+// (16384 tokens, 8 of 256 experts in groups: 1432 instructions per token key by key.)
+template <int NV>
+__device__ __forceinline__ void top_k(const RouteParams& p, uint32_t (&key)[NV], const float (&x)[NV], uint32_t e0,
+                                      uint32_t lane, uint32_t* smem, uint32_t& my_id, float& my_x) {
+  uint32_t best = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) best = max(best, key[j]);
+  if constexpr (NV > 1) {
+    uint32_t floor_key = 0, rest = best;
+    for (uint32_t i = 0; i < p.topk; ++i) {
+      floor_key = __reduce_max_sync(kFull, rest);
+      if (lane == __ffs(__ballot_sync(kFull, rest == floor_key)) - 1) rest = 0;
+    }
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) n += key[j] >= floor_key ? 1u : 0u;
+    uint32_t upto = n;
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(kFull, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const uint32_t all = __shfl_sync(kFull, upto, 31);
+    if (floor_key != 0 && all <= 32) {
+      uint32_t at = upto - n;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (key[j] >= floor_key) {
+          smem[at] = key[j];
+          smem[32 + at] = e0 + j;
+          ++at;
+        }
+      }
+      __syncwarp();
+      uint32_t k = lane < all ? smem[lane] : 0u;
+      const uint32_t id = lane < all ? smem[32 + lane] : 0u;
+      uint32_t place = 32;  // of this lane's key in the order
+      for (uint32_t i = 0; i < p.topk; ++i) {
+        const uint32_t top = __reduce_max_sync(kFull, k);
+        if (lane == __ffs(__ballot_sync(kFull, k == top)) - 1) {
+          place = i;
+          k = 0;
+        }
+      }
+      __syncwarp();
+      if (place < 32) smem[place] = id;
+      __syncwarp();
+      my_id = lane < p.topk ? smem[lane] : 0u;
+      // its logit, from the lane that holds it
+      my_x = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const float v = __shfl_sync(kFull, x[j], my_id / NV);
+        if (my_id % NV == (uint32_t)j) my_x = v;
+      }
+      return;
+    }
+  }
+  for (uint32_t i = 0; i < p.topk; ++i) {
+    const uint32_t top = __reduce_max_sync(kFull, best);
+    const uint32_t winner = __ffs(__ballot_sync(kFull, best == top)) - 1;
+    uint32_t at = 0;
+    float xv = 0.0f;
+    if (lane == winner) {
+      best = 0;
+      bool found = false;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool hit = !found && key[j] == top;
+        if (hit) { at = e0 + j; xv = x[j]; key[j] = 0u; found = true; }
+        best = max(best, key[j]);
+      }
+    }
+    at = __shfl_sync(kFull, at, winner);
+    xv = __shfl_sync(kFull, xv, winner);
+    if (lane == i) { my_id = at; my_x = xv; }
+  }
+}
+
 template <int DTYPE, int NV>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RouteParams p) {
   extern __shared__ uint32_t keys_smem[];
@@ -128,14 +232,24 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
   uint32_t key[NV];
   const bool by_score = !soft || p.bias != nullptr;
   // a group's two best values are added: softmax without a bias needs the scores there too
+  if (by_score) {
+    float b[NV];
+    if (p.bias) {
+      load_bias<NV>(p, e0, b);
+    } else {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    float c = x[j];
-    if (by_score) {
-      c = soft ? softmax_of(x[j], m, sum) : sigmoid(x[j]);
-      if (p.bias && e0 + j < p.experts) c += __ldg(p.bias + e0 + j);
+      for (int j = 0; j < NV; ++j) b[j] = 0.0f;
     }
-    key[j] = e0 + j < p.experts ? order_key(c) : 0u;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) key[j] = order_key((soft ? softmax_of(x[j], m, sum) : sigmoid(x[j])) + b[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) key[j] = order_key(x[j]);
+  }
+  if (e0 + NV > p.experts) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (e0 + j >= p.experts) key[j] = 0u;
   }
   if (p.groups > 1) {
     const bool two = p.group_score == MX_GROUP_TOP2;
@@ -161,7 +275,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
       const uint32_t k = order_key(group_value(a, b));
       rank_key = __shfl_sync(kFull, k, (lane * lanes_per_group) & 31);
     } else {        // through shared memory, a lane per group
-      uint32_t* mine = keys_smem + warp * (NV * 32);
+      uint32_t* mine = keys_smem + warp * (64 + NV * 32) + 64;
 #pragma unroll
       for (int j = 0; j < NV; ++j) mine[e0 + j] = key[j];
       __syncwarp();
@@ -178,37 +292,23 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
       better += (k > rank_key || (k == rank_key && g < lane)) ? 1u : 0u;
     }
     const uint32_t kept = __ballot_sync(kFull, lane < p.groups && better < p.topk_groups);
+    if (aligned) {
+      const bool mine_kept = e0 < p.experts && ((kept >> fastdiv(e0, p.by_group_size)) & 1u);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (e0 + j < p.experts && !((kept >> ((e0 + j) / p.group_size)) & 1u)) key[j] = 0u;
-  }
-  // top-k: the best key of the warp, the first lane that has it, that lane's first expert with it
-  uint32_t best = 0;
+      for (int j = 0; j < NV; ++j) key[j] = mine_kept ? key[j] : 0u;
+    } else {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) best = max(best, key[j]);
-  uint32_t my_id = 0;
-  float my_s = 0.0f;
-  for (uint32_t i = 0; i < p.topk; ++i) {
-    const uint32_t top = __reduce_max_sync(kFull, best);
-    const uint32_t winner = __ffs(__ballot_sync(kFull, best == top)) - 1;
-    uint32_t at = 0;
-    float xv = 0.0f;
-    if (lane == winner) {
-      best = 0;
-      bool found = false;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const bool hit = !found && key[j] == top;
-        if (hit) { at = e0 + j; xv = x[j]; key[j] = 0u; found = true; }
-        best = max(best, key[j]);
-      }
+      for (int j = 0; j < NV; ++j)
+        if (e0 + j < p.experts && !((kept >> fastdiv(e0 + j, p.by_group_size)) & 1u)) key[j] = 0u;
+      __syncwarp();  // the keys in shared memory have been read
     }
-    at = __shfl_sync(kFull, at, winner);
-    xv = __shfl_sync(kFull, xv, winner);
-    if (lane == i) { my_id = at; my_s = xv; }
   }
+  uint32_t my_id = 0;
+  float my_x = 0.0f;
+  top_k<NV>(p, key, x, e0, lane, keys_smem + warp * (64 + NV * 32), my_id, my_x);
+  float my_s;
   const bool live = lane < p.topk;
-  my_s = live ? (soft ? softmax_of(my_s, m, sum) : sigmoid(my_s)) : 0.0f;
+  my_s = live ? (soft ? softmax_of(my_x, m, sum) : sigmoid(my_x)) : 0.0f;
   float w = my_s;
   if (p.renormalize) {
     const float total = warp_sum(my_s);
@@ -256,23 +356,24 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const 
     ds = total == 0.0f || id < 0 ? 0.0f : p.scale * (d - dot / total) / total;
   }
   const float inner = soft ? warp_sum(ds * s) : 0.0f;
+  // ds spread over the experts by way of shared memory
+  extern __shared__ float ds_smem[];
+  float* mine = ds_smem + warp * (NV * 32);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) mine[j * 32 + lane] = 0.0f;
+  __syncwarp();
+  if (id >= 0) atomicAdd(mine + ((uint32_t)id % NV) * 32 + (uint32_t)id / NV, ds);
+  __syncwarp();
   float o[NV];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) o[j] = 0.0f;
-  for (uint32_t i = 0; i < p.topk; ++i) {
-    const int32_t e = __shfl_sync(kFull, id, i);
-    const float v = __shfl_sync(kFull, ds, i);
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (e == (int32_t)(e0 + j)) o[j] += v;
-  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
+    o[j] = mine[j * 32 + lane];
     if (soft) {
-      o[j] = softmax_of(x[j], m, sum) * (o[j] - inner);
-    } else {
+      o[j] = expf(x[j] - m) * inv * (o[j] - inner);
+    } else if (o[j] != 0.0f) {
       const float t = expf(-fabsf(x[j]));  // s (1 - s) without the difference: t / (1 + t)^2
-      o[j] = o[j] == 0.0f ? 0.0f : o[j] * (t / ((1.0f + t) * (1.0f + t)));
+      o[j] *= t / ((1.0f + t) * (1.0f + t));
     }
   }
   const size_t at = (size_t)token * p.experts + e0;
@@ -314,14 +415,15 @@ RouteParams route_params(const RouteArgs& a) {
   p.topk_groups = (uint32_t)a.route.topk_groups; p.group_score = (uint32_t)a.route.group_score;
   p.renormalize = a.route.renormalize ? 1u : 0u; p.scale = a.route.scale;
   p.group_size = p.groups ? p.experts / p.groups : p.experts;
+  p.by_group_size = make_fastdiv(p.group_size);
   return p;
 }
 
 template <int DTYPE, int NV>
 cudaError_t launch_nv(const RouteParams& p, bool backward, cudaStream_t stream) {
   const dim3 grid((p.tokens + kRouteWarps - 1) / kRouteWarps), block(32 * kRouteWarps);
-  if (backward) return launch_pdl(route_backward_kernel<DTYPE, NV>, grid, block, 0, stream, p);
-  return launch_pdl(route_kernel<DTYPE, NV>, grid, block, p.groups > 1 ? sizeof(uint32_t) * 32 * NV * kRouteWarps : 0, stream, p);
+  if (backward) return launch_pdl(route_backward_kernel<DTYPE, NV>, grid, block, sizeof(float) * 32 * NV * kRouteWarps, stream, p);
+  return launch_pdl(route_kernel<DTYPE, NV>, grid, block, sizeof(uint32_t) * (64 + NV * 32) * kRouteWarps, stream, p);
 }
 
 template <int DTYPE>
