@@ -37,6 +37,12 @@ __device__ __forceinline__ float from_key(uint32_t k) {
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
 
+template <int DTYPE>
+__device__ __forceinline__ float load_logit(const RouteParams& p, size_t at) {
+  return DTYPE == MX_BF16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)p.logits + at) << 16)
+                          : __ldg((const float*)p.logits + at);
+}
+
 // The lane's NV logits; experts past the end read as -Inf.
 template <int DTYPE, int NV>
 __device__ __forceinline__ void load_logits(const RouteParams& p, uint32_t token, uint32_t lane, float (&x)[NV]) {
@@ -69,9 +75,7 @@ __device__ __forceinline__ void load_logits(const RouteParams& p, uint32_t token
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     x[j] = -INFINITY;
-    if (e0 + j < p.experts)
-      x[j] = DTYPE == MX_BF16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)p.logits + at + j) << 16)
-                              : __ldg((const float*)p.logits + at + j);
+    if (e0 + j < p.experts) x[j] = load_logit<DTYPE>(p, at + j);
   }
 }
 
@@ -131,7 +135,7 @@ __device__ __forceinline__ void top2_add(uint32_t& a, uint32_t& b, uint32_t k) {
 }
 
 // The topk best keys of the warp, in descending order, equal ones in the order of the experts: lane i gets
-// the i-th one's expert and logit.  `smem`: 64 words of the warp.
+// the i-th one's expert.  `smem`: 64 words of the warp.
 //
 // Taking the best of all keys topk times costs a pass over a lane's NV keys each time.  So the field is cut down
 // first: the topk-th largest of the lanes' own maxima is a floor under the topk-th largest key, and what is not
@@ -139,8 +143,8 @@ __device__ __forceinline__ void top2_add(uint32_t& a, uint32_t& b, uint32_t k) {
 // a vote.  More than 32 of them (many equal keys), or fewer lanes with candidates than topk: key by key.
 // (16384 tokens, 8 of 256 experts in groups: 1432 instructions per token key by key.)
 template <int NV>
-__device__ __forceinline__ void top_k(const RouteParams& p, uint32_t (&key)[NV], const float (&x)[NV], uint32_t e0,
-                                      uint32_t lane, uint32_t* smem, uint32_t& my_id, float& my_x) {
+__device__ __forceinline__ void top_k(const RouteParams& p, uint32_t (&key)[NV], uint32_t e0, uint32_t lane,
+                                      uint32_t* smem, uint32_t& my_id) {
   uint32_t best = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) best = max(best, key[j]);
@@ -185,13 +189,6 @@ __device__ __forceinline__ void top_k(const RouteParams& p, uint32_t (&key)[NV],
       if (place < 32) smem[place] = id;
       __syncwarp();
       my_id = lane < p.topk ? smem[lane] : 0u;
-      // its logit, from the lane that holds it
-      my_x = 0.0f;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const float v = __shfl_sync(kFull, x[j], my_id / NV);
-        if (my_id % NV == (uint32_t)j) my_x = v;
-      }
       return;
     }
   }
@@ -199,20 +196,18 @@ __device__ __forceinline__ void top_k(const RouteParams& p, uint32_t (&key)[NV],
     const uint32_t top = __reduce_max_sync(kFull, best);
     const uint32_t winner = __ffs(__ballot_sync(kFull, best == top)) - 1;
     uint32_t at = 0;
-    float xv = 0.0f;
     if (lane == winner) {
       best = 0;
       bool found = false;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const bool hit = !found && key[j] == top;
-        if (hit) { at = e0 + j; xv = x[j]; key[j] = 0u; found = true; }
+        if (hit) { at = e0 + j; key[j] = 0u; found = true; }
         best = max(best, key[j]);
       }
     }
     at = __shfl_sync(kFull, at, winner);
-    xv = __shfl_sync(kFull, xv, winner);
-    if (lane == i) { my_id = at; my_x = xv; }
+    if (lane == i) my_id = at;
   }
 }
 
@@ -224,10 +219,10 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
   const uint32_t token = blockIdx.x * kRouteWarps + warp;
   if (token >= p.tokens) return;
   const uint32_t e0 = lane * NV;
+  const bool soft = p.score == MX_SCORE_SOFTMAX;
   float x[NV];
   load_logits<DTYPE, NV>(p, token, lane, x);
   float m = 0.0f, sum = 1.0f;
-  const bool soft = p.score == MX_SCORE_SOFTMAX;
   if (soft) softmax_stats<NV>(x, m, sum);
   uint32_t key[NV];
   const bool by_score = !soft || p.bias != nullptr;
@@ -285,13 +280,14 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
         rank_key = order_key(group_value(a, b));
       }
     }
-    // the topk_groups best groups: fewer than that many are better, or equal and earlier
-    uint32_t better = 0;
-    for (uint32_t g = 0; g < p.groups; ++g) {
-      const uint32_t k = __shfl_sync(kFull, rank_key, g);
-      better += (k > rank_key || (k == rank_key && g < lane)) ? 1u : 0u;
+    // the topk_groups best groups, the lower one among equals (every group has a key above 0)
+    uint32_t kept = 0, rest = lane < p.groups ? rank_key : 0u;
+    for (uint32_t i = 0; i < p.topk_groups; ++i) {
+      const uint32_t top = __reduce_max_sync(kFull, rest);
+      const uint32_t who = __ffs(__ballot_sync(kFull, rest == top)) - 1;
+      kept |= 1u << who;
+      if (lane == who) rest = 0u;
     }
-    const uint32_t kept = __ballot_sync(kFull, lane < p.groups && better < p.topk_groups);
     if (aligned) {
       const bool mine_kept = e0 < p.experts && ((kept >> fastdiv(e0, p.by_group_size)) & 1u);
 #pragma unroll
@@ -304,10 +300,10 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
     }
   }
   uint32_t my_id = 0;
-  float my_x = 0.0f;
-  top_k<NV>(p, key, x, e0, lane, keys_smem + warp * (64 + NV * 32), my_id, my_x);
+  top_k<NV>(p, key, e0, lane, keys_smem + warp * (64 + NV * 32), my_id);
   float my_s;
   const bool live = lane < p.topk;
+  const float my_x = live ? load_logit<DTYPE>(p, (size_t)token * p.experts + my_id) : 0.0f;
   my_s = live ? (soft ? softmax_of(my_x, m, sum) : sigmoid(my_x)) : 0.0f;
   float w = my_s;
   if (p.renormalize) {
@@ -342,8 +338,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const 
     d = __ldg(p.dweights + (size_t)token * p.topk + lane);
     if ((uint32_t)id < p.experts) {
       const size_t at = (size_t)token * p.experts + (uint32_t)id;
-      const float xs = DTYPE == MX_BF16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)p.logits + at) << 16)
-                                        : __ldg((const float*)p.logits + at);
+      const float xs = load_logit<DTYPE>(p, at);
       s = soft ? softmax_of(xs, m, sum) : sigmoid(xs);
     } else {
       id = -1;
