@@ -499,6 +499,7 @@ int mx_route_backward(const float* dweights, const void* logits, const int32_t* 
  *   offsets  int32 [experts + 1]
  *   counts   int32 [experts]: rows of each group that hold a choice (the rest is padding)
  *   row_of   int32 [tokens x topk]: the row of a choice, -1 for a dropped one
+ *   src_of   int32 [mx_moe_rows(...)]: the choice (t * topk + j) of a row, -1 for a row without one
  *   workspace  mx_moe_plan_workspace_bytes(tokens, topk, experts) bytes, 16-byte aligned
  * mx_moe_rows(tokens, topk, experts, align) is the largest offsets[experts] can become: the rows
  * to allocate without asking the device (0 on bad arguments).  experts <= 1024, 1 <= align <= 1024,
@@ -508,7 +509,7 @@ int mx_route_backward(const float* dweights, const void* logits, const int32_t* 
 int64_t mx_moe_rows(int64_t tokens, int64_t topk, int64_t experts, int64_t align);
 size_t mx_moe_plan_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts);
 int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t experts, int64_t align,
-                int32_t* offsets, int32_t* counts, int32_t* row_of, const mx_opts_t* opts,
+                int32_t* offsets, int32_t* counts, int32_t* row_of, int32_t* src_of, const mx_opts_t* opts,
                 void* workspace, size_t workspace_bytes);
 
 /*
@@ -516,13 +517,13 @@ int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t expert
  * of the MX tensor [tokens x dim] (codes and scale bytes moved, nothing requantized).  Rows
  * 0 .. rows-1 that no choice maps to are zero blocks (codes 0, scale byte 0), so that products with
  * them are zero.  scales_in and scales_out in opts->scale_layout; every byte of both outputs is
- * written.  dim % 32 == 0; tensors 16-byte aligned; rows as allocated for the plan (a row_of outside
- * [0, rows) is skipped).  Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN,
+ * written.  dim % 32 == 0; tensors 16-byte aligned; rows = mx_moe_rows() of the plan (a row_of outside
+ * [0, rows) or a src_of outside the choices is skipped).  Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN,
  * MX_ERR_UNSUPPORTED (pad_k128, more than 1024 experts), MX_ERR_CUDA.
  */
 int mx_moe_gather(const void* elems_in, const uint8_t* scales_in, int64_t tokens, int64_t topk, int64_t dim,
                   mx_fmt_t fmt, const int32_t* offsets, const int32_t* counts, const int32_t* row_of,
-                  int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts);
+                  const int32_t* src_of, int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts);
 
 /*
  * mx_moe_combine -- out[t,:] = sum over j (ascending) of weights[t,j] * y[row_of[t,j],:], FP32,

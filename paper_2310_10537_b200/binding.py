@@ -142,8 +142,8 @@ def _load() -> ctypes.CDLL:
     lib.mx_moe_rows.restype = i64
     lib.mx_moe_plan_workspace_bytes.argtypes = [i64, i64, i64]
     lib.mx_moe_plan_workspace_bytes.restype = sz
-    lib.mx_moe_plan.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, op, vp, sz]
-    lib.mx_moe_gather.argtypes = [vp, u8p, i64, i64, i64, ci, vp, vp, vp, i64, i64, vp, u8p, op]
+    lib.mx_moe_plan.argtypes = [vp, i64, i64, i64, i64, vp, vp, vp, vp, op, vp, sz]
+    lib.mx_moe_gather.argtypes = [vp, u8p, i64, i64, i64, ci, vp, vp, vp, vp, i64, i64, vp, u8p, op]
     lib.mx_moe_combine.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, op]
     lib.mx_moe_combine_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, op]
     lib.mx_gemm_grouped.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
@@ -558,11 +558,13 @@ def mx_route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.T
 class MoePlan(NamedTuple):
     """Where the rows of a batch go: group e holds rows offsets[e] .. offsets[e + 1], the first counts[e]
     of them choices; row_of [tokens, topk] is the row of a choice (-1: dropped); ``rows`` bounds
-    offsets[-1] and is what row tensors are allocated with."""
+    offsets[-1] and is what row tensors are allocated with; src_of [rows] is the choice of a row (-1: none),
+    which mx_moe_gather needs."""
     offsets: torch.Tensor
     counts: torch.Tensor
     row_of: torch.Tensor
     rows: int
+    src_of: Optional[torch.Tensor] = None
 
 
 def mx_moe_rows(tokens: int, topk: int, experts: int, align: int = 64) -> int:
@@ -579,10 +581,11 @@ def mx_moe_plan(ids: torch.Tensor, experts: int, align: int = 64,
     dev = _device_of(ids)
     if workspace is None:
         workspace = ids.new_empty(_lib.mx_moe_plan_workspace_bytes(tokens, topk, experts), dtype=torch.uint8)
-    plan = MoePlan(ids.new_empty(max(experts, 0) + 1), ids.new_empty(max(experts, 0)), torch.empty_like(ids),
-                   _lib.mx_moe_rows(tokens, topk, experts, align))
+    rows = _lib.mx_moe_rows(tokens, topk, experts, align)
+    plan = MoePlan(ids.new_empty(max(experts, 0) + 1), ids.new_empty(max(experts, 0)), torch.empty_like(ids), rows,
+                   ids.new_empty(rows))
     _check(_lib.mx_moe_plan(_need("ids", ids, dev, torch.int32, ids.shape), tokens, topk, experts, align,
-                            plan.offsets.data_ptr(), plan.counts.data_ptr(), plan.row_of.data_ptr(), _call_opts(dev, MX_F32),
+                            plan.offsets.data_ptr(), plan.counts.data_ptr(), plan.row_of.data_ptr(), plan.src_of.data_ptr(), _call_opts(dev, MX_F32),
                             _bytes("workspace", workspace, dev, 0), workspace.numel() * workspace.element_size()), "mx_moe_plan")
     return plan
 
@@ -605,12 +608,15 @@ def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int,
     [plan.rows, dim], rows without a choice zero."""
     dev = _device_of(elems)
     tokens, topk, experts, offsets, counts, row_of = _plan_args(plan, dev)
+    if plan.src_of is None:
+        raise ValueError("the plan has no src_of")
     ni, nsi = _mx_sizes(tokens, dim, fmt, layout)
     ne, ns = _mx_sizes(plan.rows, dim, fmt, layout)
     if out is None:
         out = (elems.new_empty(ne, dtype=torch.uint8), elems.new_empty(ns, dtype=torch.uint8))
     _check(_lib.mx_moe_gather(_bytes("elems", elems, dev, ni), _bytes("scales", scales, dev, nsi), tokens, topk, dim, fmt,
-                              offsets, counts, row_of, experts, plan.rows, _bytes("out elems", out[0], dev, ne),
+                              offsets, counts, row_of, _need("src_of", plan.src_of, dev, torch.int32, (plan.rows,)), experts,
+                              plan.rows, _bytes("out elems", out[0], dev, ne),
                               _bytes("out scales", out[1], dev, ns), _call_opts(dev, MX_F32, layout)), "mx_moe_gather")
     return out
 

@@ -1009,21 +1009,22 @@ size_t mx_moe_plan_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts
 }
 
 int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t experts, int64_t align,
-                int32_t* offsets, int32_t* counts, int32_t* row_of, const mx_opts_t* opts,
+                int32_t* offsets, int32_t* counts, int32_t* row_of, int32_t* src_of, const mx_opts_t* opts,
                 void* workspace, size_t workspace_bytes) {
   Opts o;
   if (!read_opts(opts, &o)) return MX_ERR_FMT;
   if (!plan_ok(tokens, topk, experts, align)) return MX_ERR_SHAPE;
   if (experts > 1024 || o.pad128) return MX_ERR_UNSUPPORTED;
   const int64_t n = tokens * topk;
-  if (!offsets || !counts || !workspace || (n > 0 && (!ids || !row_of))) return MX_ERR_NULL;
+  if (!offsets || !counts || !workspace || (n > 0 && (!ids || !row_of || !src_of))) return MX_ERR_NULL;
   if ((uintptr_t)ids % 4 || (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4 ||
-      misaligned16(workspace))
+      (uintptr_t)src_of % 4 || misaligned16(workspace))
     return MX_ERR_ALIGN;
   if (workspace_bytes < mx_moe_plan_workspace_bytes(tokens, topk, experts)) return MX_ERR_WORKSPACE;
   mx::MoePlanArgs a;
-  a.ids = ids; a.offsets = offsets; a.counts = counts; a.row_of = row_of; a.hist = (int32_t*)workspace;
-  a.n = n; a.experts = experts; a.align = align; a.sm_count = 0; a.stream = o.stream;
+  a.ids = ids; a.offsets = offsets; a.counts = counts; a.row_of = row_of; a.src_of = src_of;
+  a.hist = (int32_t*)workspace; a.n = n; a.experts = experts; a.align = align;
+  a.rows = mx_moe_rows(tokens, topk, experts, align); a.sm_count = 0; a.stream = o.stream;
   const cudaError_t e = mx::launch_moe_plan(a);
   return e == cudaSuccess ? MX_OK : fail_cuda(e);
 }
@@ -1039,7 +1040,7 @@ static int move_validate(int64_t tokens, int64_t topk, int64_t dim, int64_t rows
 
 int mx_moe_gather(const void* elems_in, const uint8_t* scales_in, int64_t tokens, int64_t topk, int64_t dim,
                   mx_fmt_t fmt, const int32_t* offsets, const int32_t* counts, const int32_t* row_of,
-                  int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts) {
+                  const int32_t* src_of, int64_t experts, int64_t rows, void* elems_out, uint8_t* scales_out, const mx_opts_t* opts) {
   Opts o;
   if (!fmt_ok((int)fmt) || !read_opts(opts, &o)) return MX_ERR_FMT;
   const int rc = move_validate(tokens, topk, dim, rows, o);
@@ -1047,12 +1048,13 @@ int mx_moe_gather(const void* elems_in, const uint8_t* scales_in, int64_t tokens
   if (dim % 32 || experts < 1) return MX_ERR_SHAPE;
   if (experts > 1024) return MX_ERR_UNSUPPORTED;
   if (rows == 0) return MX_OK;
-  if (!offsets || !counts || !elems_out || !scales_out || (tokens > 0 && (!elems_in || !scales_in || !row_of)))
+  if (!offsets || !counts || !src_of || !elems_out || !scales_out || (tokens > 0 && (!elems_in || !scales_in || !row_of)))
     return MX_ERR_NULL;
   if (misaligned16(elems_in) || misaligned16(scales_in) || misaligned16(elems_out) || misaligned16(scales_out) ||
-      (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4)
+      (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4 || (uintptr_t)src_of % 4)
     return MX_ERR_ALIGN;
   mx::MoeMoveArgs a = {};
+  a.src_of = src_of;
   a.src = elems_in; a.scales_in = scales_in; a.offsets = offsets; a.counts = counts; a.row_of = row_of;
   a.dst = elems_out; a.scales_out = scales_out; a.tokens = tokens; a.topk = topk; a.dim = dim; a.experts = experts;
   a.rows = rows; a.bits = fmt_bits((int)fmt); a.layout = o.layout; a.stream = o.stream;

@@ -163,8 +163,8 @@ cudaError_t launch_route_backward(const RouteArgs& a);
 constexpr int kPlanChunk = 2048;  // choices that one CTA of the plan sorts
 struct MoePlanArgs {
   const int32_t* ids;
-  int32_t *offsets, *counts, *row_of, *hist;  // hist: [chunks x experts]
-  int64_t n, experts, align;
+  int32_t *offsets, *counts, *row_of, *src_of, *hist;  // hist: [chunks x experts]
+  int64_t n, experts, align, rows;
   int sm_count;
   cudaStream_t stream;
 };
@@ -174,7 +174,7 @@ struct MoeMoveArgs {
   const void *src, *y;       // rows of the tokens (MX codes or floats); combine: src unused
   const uint8_t* scales_in;
   const float* weights;
-  const int32_t *offsets, *counts, *row_of;
+  const int32_t *offsets, *counts, *row_of, *src_of;
   void* dst;
   uint8_t* scales_out;
   float* dweights;

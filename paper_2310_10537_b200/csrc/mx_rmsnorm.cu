@@ -241,48 +241,95 @@ struct NormBackParams {
   float eps, inv_dim;
 };
 
-template <int DTYPE, int V>
+// The second half of a row: dh, and the row's share of the weight gradient.
+template <int DTYPE>
+__device__ __forceinline__ void finish_group(const NormBackParams& p, size_t at, uint32_t elem, const float (&h)[8],
+                                             const float (&g)[8], const float (&q)[8], float s, float c, float (&dw)[8]) {
+  float w[8], o[8];
+  load_weight8(p.weight, p.w_bf16, elem, w);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    o[e] = s * (g[e] * w[e] - h[e] * c);
+    if (p.dres) o[e] += q[e];
+    dw[e] = fmaf(g[e], h[e] * s, dw[e]);
+  }
+  store8<DTYPE>(p.dh, at, o);
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// dim % 8 == 0, 1024 < dim <= 8 V blockDim: a row per CTA at a time.  The next NS rows are on their way to shared memory
+// meanwhile -- a thread copies just the elements that it will take itself, so the ring needs no
+// barrier.  (One row ahead in registers left 48 KB an SM in flight: 8192 x 4096 BF16 52.7 us.)
+template <int DTYPE, int V, int NS>
 __global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackParams p) {
+  constexpr uint32_t kGroup = DTYPE == MX_BF16 ? 16 : 32;  // bytes of 8 elements
+  extern __shared__ uint4 ring[];
   __shared__ float2 red[2][16];
   pdl_prologue();
   const uint32_t T = blockDim.x, lane = threadIdx.x & 31, warps = T >> 5, groups = p.dim >> 3;
+  const uint32_t slot = V * T * kGroup, stage_bytes = 3 * slot;  // h, dy, dres
+  const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
   float dw[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
-  Raw8<DTYPE> h[V], d[V], q[V];
-  auto fetch = [&](uint32_t row) {
+  auto request = [&](uint32_t row, uint32_t stage) {
+    if (row < p.rows) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t g = i * T + threadIdx.x;
-      if (g < groups) {
-        h[i] = load_raw8<DTYPE>(p.h, (size_t)row * p.dim + 8 * (size_t)g);
-        d[i] = load_raw8<DTYPE>(p.dy, (size_t)row * p.dim + 8 * (size_t)g);
-        if (p.dres) q[i] = load_raw8<DTYPE>(p.dres, (size_t)row * p.dim + 8 * (size_t)g);
-      } else {
-        h[i] = {}; d[i] = {}; q[i] = {};
+      for (int i = 0; i < V; ++i) {
+        const uint32_t g = i * T + threadIdx.x;
+        if (g < groups) {
+          const size_t at = ((size_t)row * p.dim + 8 * (size_t)g) * (kGroup / 8);
+          const uint32_t dst = ring0 + stage * stage_bytes + g * kGroup;
+#pragma unroll
+          for (uint32_t k = 0; k < kGroup; k += 16) {
+            cp_async16(dst + k, (const char*)p.h + at + k);
+            cp_async16(dst + slot + k, (const char*)p.dy + at + k);
+            if (p.dres) cp_async16(dst + 2 * slot + k, (const char*)p.dres + at + k);
+          }
+        }
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  uint32_t row = blockIdx.x, side = 0;
-  if (row < p.rows) fetch(row);
-  for (; row < p.rows; row += gridDim.x, side ^= 1) {
+  auto take = [&](uint32_t stage, uint32_t tensor, uint32_t g) {
+    Raw8<DTYPE> r;
+    const uint4* q = ring + (stage * stage_bytes + tensor * slot + g * kGroup) / 16;
+    r.v[0] = q[0];
+    if constexpr (DTYPE == MX_F32) r.v[1] = q[1];
+    return r;
+  };
+#pragma unroll
+  for (int i = 0; i < NS; ++i) request(blockIdx.x + i * gridDim.x, i);
+  uint32_t side = 0, stage = 0;
+  for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
     float s1 = 0.0f, s2 = 0.0f;
-    float hf[V][8], gf[V][8];
+    float h[V][8], g8[V][8], q[V][8];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const uint32_t g = i * T + threadIdx.x;
-      float w[8] = {};
-      if (g < groups) load_weight8(p.weight, p.w_bf16, 8 * g, w);
-      widen<DTYPE>(h[i], hf[i]);
-      widen<DTYPE>(d[i], gf[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s1 = fmaf(hf[i][e], hf[i][e], s1);
-        s2 = fmaf(gf[i][e] * w[e], hf[i][e], s2);
+      for (int e = 0; e < 8; ++e) { h[i][e] = 0.0f; g8[i][e] = 0.0f; q[i][e] = 0.0f; }
+      if (g < groups) {
+        float w[8];
+        load_weight8(p.weight, p.w_bf16, 8 * g, w);
+        widen<DTYPE>(take(stage, 0, g), h[i]);
+        widen<DTYPE>(take(stage, 1, g), g8[i]);
+        if (p.dres) widen<DTYPE>(take(stage, 2, g), q[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s1 = fmaf(h[i][e], h[i][e], s1);
+          s2 = fmaf(g8[i][e] * w[e], h[i][e], s2);
+        }
       }
     }
+    request(row + NS * gridDim.x, stage);  // into the slots just read
+    if (++stage == NS) stage = 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
       s1 += __shfl_xor_sync(0xffffffffu, s1, o);
@@ -290,42 +337,98 @@ __global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackPar
     }
     if (lane == 0) red[side][threadIdx.x >> 5] = make_float2(s1, s2);
     __syncthreads();
-    float2 t = lane < warps ? red[side][lane] : make_float2(0.0f, 0.0f);
+    float2 t = red[side][lane & 15];
+    if ((lane & 15) >= warps) t = make_float2(0.0f, 0.0f);
 #pragma unroll
     for (int o = 8; o; o >>= 1) {
       t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
       t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
     }
-    t.x = __shfl_sync(0xffffffffu, t.x, 0);
-    t.y = __shfl_sync(0xffffffffu, t.y, 0);
     const float s = rsqrtf(t.x * p.inv_dim + p.eps), c = s * s * (t.y * p.inv_dim);
-    float qf[V][8];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (p.dres) widen<DTYPE>(q[i], qf[i]);
-    }
-    const size_t base = (size_t)row * p.dim;
-    if (row + gridDim.x < p.rows) fetch(row + gridDim.x);  // the next row is on its way while this one is finished
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const uint32_t g = i * T + threadIdx.x;
+      if (g < groups) finish_group<DTYPE>(p, (size_t)row * p.dim + 8 * (size_t)g, 8 * g, h[i], g8[i], q[i], s, c, dw[i]);
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t g = i * T + threadIdx.x;
+    if (g < groups) store8<MX_F32>(p.partial, (size_t)blockIdx.x * p.dim + 8 * (size_t)g, dw[i]);
+  }
+}
+
+// dim % 8 == 0, dim <= 256 V <= 1024: a row per warp, so that a reduction is five shuffles and eight rows are under way
+// in a CTA; the warps' weight gradients meet in shared memory at the end, in warp order.
+constexpr uint32_t kRowWarps = 8;
+template <int DTYPE, int V>
+__global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(const NormBackParams p) {
+  extern __shared__ float sums[];  // [warps][dim]
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = p.dim >> 3;
+  float dw[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+  for (uint32_t row = blockIdx.x * kRowWarps + warp; row < p.rows; row += gridDim.x * kRowWarps) {
+    Raw8<DTYPE> h[V], d[V], q[V];
+    const size_t base = (size_t)row * p.dim;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * 32 + lane;
       if (g < groups) {
-        float w[8], o[8];
+        h[i] = load_raw8<DTYPE>(p.h, base + 8 * (size_t)g);
+        d[i] = load_raw8<DTYPE>(p.dy, base + 8 * (size_t)g);
+        if (p.dres) q[i] = load_raw8<DTYPE>(p.dres, base + 8 * (size_t)g);
+      }
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * 32 + lane;
+      if (g < groups) {
+        float w[8], hf[8], gf[8];
         load_weight8(p.weight, p.w_bf16, 8 * g, w);
+        widen<DTYPE>(h[i], hf);
+        widen<DTYPE>(d[i], gf);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          o[e] = s * (gf[i][e] * w[e] - hf[i][e] * c);
-          if (p.dres) o[e] += qf[i][e];
-          dw[i][e] = fmaf(gf[i][e], hf[i][e] * s, dw[i][e]);
+          s1 = fmaf(hf[e], hf[e], s1);
+          s2 = fmaf(gf[e] * w[e], hf[e], s2);
         }
-        store8<DTYPE>(p.dh, base + 8 * (size_t)g, o);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    const float s = rsqrtf(s1 * p.inv_dim + p.eps), c = s * s * (s2 * p.inv_dim);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t g = i * 32 + lane;
+      if (g < groups) {
+        float hf[8], gf[8], qf[8] = {};
+        widen<DTYPE>(h[i], hf);
+        widen<DTYPE>(d[i], gf);
+        if (p.dres) widen<DTYPE>(q[i], qf);
+        finish_group<DTYPE>(p, base + 8 * (size_t)g, 8 * g, hf, gf, qf, s, c, dw[i]);
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const uint32_t g = i * T + threadIdx.x;
-    if (g < groups) store8<MX_F32>(p.partial, (size_t)blockIdx.x * p.dim + 8 * (size_t)g, dw[i]);
+    const uint32_t g = i * 32 + lane;
+    if (g < groups) store8<MX_F32>(sums, (size_t)warp * p.dim + 8 * (size_t)g, dw[i]);
+  }
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {
+    float t = sums[c];
+#pragma unroll
+    for (uint32_t w = 1; w < kRowWarps; ++w) t += sums[w * p.dim + c];
+    p.partial[(size_t)blockIdx.x * p.dim + c] = t;
   }
 }
 
@@ -372,25 +475,26 @@ __global__ void __launch_bounds__(256) rmsnorm_columns_kernel(const NormBackPara
   p.partial[(size_t)blockIdx.y * p.dim + c] = dw;
 }
 
-// dweight[c] = sum over the partial rows, always in the same order: 8 strands of rows per column.
-__global__ void __launch_bounds__(256) rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight,
-                                                              uint32_t parts, uint32_t dim) {
-  __shared__ float sum[8][33];
+// dweight[c] = sum over the partial rows, always in the same order: 32 strands of rows per column, so that
+// all of a thread's loads are in flight at once (with 8 strands the chain of loads took 8 us).
+__global__ void __launch_bounds__(1024) rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight,
+                                                               uint32_t parts, uint32_t dim) {
+  __shared__ float sum[32][33];
   pdl_prologue();
   const uint32_t lane = threadIdx.x & 31, strand = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float t = 0.0f;
   if (c < dim) {
-#pragma unroll 4
-    for (uint32_t r = strand; r < parts; r += 8) t += partial[(size_t)r * dim + c];
+#pragma unroll 10
+    for (uint32_t r = strand; r < parts; r += 32) t += partial[(size_t)r * dim + c];
   }
   sum[strand][lane] = t;
   __syncthreads();
-  if (strand == 0 && c < dim) {
-    t = sum[0][lane];
+  // warp w sums column w's strands
+  t = sum[lane][strand];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t += sum[i][lane];
-    dweight[c] = t;
-  }
+  for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  const uint32_t col = blockIdx.x * 32 + strand;
+  if (lane == 0 && col < dim) dweight[col] = t;
 }
 
 // ---- host side ---------------------------------------------------------------
@@ -423,10 +527,46 @@ cudaError_t launch_forward_fmt(int fmt, const NormParams& p, Shape s, cudaStream
   }
 }
 
+template <int DTYPE, int V, int NS>
+cudaError_t launch_ring(const NormBackParams& p, uint32_t threads, uint32_t grid, cudaStream_t stream) {
+  const uint32_t smem = NS * 3 * V * threads * (DTYPE == MX_BF16 ? 16 : 32);
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(rmsnorm_backward_kernel<DTYPE, V, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             NS * 3 * V * 512 * (DTYPE == MX_BF16 ? 16 : 32));
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  return launch_pdl(rmsnorm_backward_kernel<DTYPE, V, NS>, dim3(grid), dim3(threads), smem, stream, p);
+}
+
+// Writes *parts rows of partial sums.
 template <int DTYPE>
-cudaError_t launch_backward(const NormBackParams& p, uint32_t grid, Shape s, cudaStream_t stream) {
-  return s.v == 1 ? launch_pdl(rmsnorm_backward_kernel<DTYPE, 1>, dim3(grid), dim3(s.threads), 0, stream, p)
-                  : launch_pdl(rmsnorm_backward_kernel<DTYPE, 2>, dim3(grid), dim3(s.threads), 0, stream, p);
+cudaError_t launch_backward(const NormBackParams& p, int sms, uint32_t* parts, cudaStream_t stream) {
+  const uint32_t groups = p.dim / 8;
+  auto at_most = [&](uint32_t ctas, uint32_t rows_each) {
+    const uint32_t need = (p.rows + rows_each - 1) / rows_each;
+    const uint32_t cap = ctas < (uint32_t)kNormPartials ? ctas : (uint32_t)kNormPartials;
+    return need < cap ? need : cap;
+  };
+  if (groups <= 128) {
+    *parts = at_most(2u * (uint32_t)sms, kRowWarps);
+    const dim3 grid(*parts), block(32 * kRowWarps);
+    const size_t smem = kRowWarps * (size_t)p.dim * 4;
+    if (groups <= 32) return launch_pdl(rmsnorm_backward_warp_kernel<DTYPE, 1>, grid, block, smem, stream, p);
+    if (groups <= 64) return launch_pdl(rmsnorm_backward_warp_kernel<DTYPE, 2>, grid, block, smem, stream, p);
+    return launch_pdl(rmsnorm_backward_warp_kernel<DTYPE, 4>, grid, block, smem, stream, p);
+  }
+  const uint32_t threads = groups < 512 ? (groups + 31) / 32 * 32 : 512;
+  if (groups <= threads) {  // up to 4096 elements: two CTAs an SM, 96 KB of rows each (FP32: two rows)
+    *parts = at_most(2u * (uint32_t)sms, 1);
+    return launch_ring<DTYPE, 1, DTYPE == MX_BF16 ? 4 : 2>(p, threads, *parts, stream);
+  }
+  *parts = at_most((uint32_t)sms, 1);  // up to 8192: one CTA, 192 KB
+  return launch_ring<DTYPE, 2, DTYPE == MX_BF16 ? 4 : 2>(p, threads, *parts, stream);
 }
 
 }  // namespace
@@ -460,15 +600,11 @@ cudaError_t launch_rmsnorm_backward(const RmsnormBackwardArgs& a) {
   p.dy = a.dy; p.h = a.h; p.weight = a.weight; p.dres = a.dres; p.dh = a.dh; p.partial = a.partial; p.stats = a.stats;
   p.rows = (uint32_t)a.rows; p.dim = (uint32_t)a.dim; p.w_bf16 = (uint32_t)a.w_bf16;
   p.eps = a.eps; p.inv_dim = 1.0f / (float)a.dim; p.row_chunk = 0;
-  const uint32_t groups = p.dim / 8;
   uint32_t parts;
   cudaError_t e;
-  if (a.dim % 8 == 0 && groups <= 1024) {  // two groups of 8 a thread are what the registers hold
-    Shape s;
-    s.threads = groups < 512 ? (groups + 31) / 32 * 32 : 512;
-    s.v = groups <= s.threads ? 1 : 2;
-    parts = p.rows < (uint32_t)kNormPartials ? p.rows : (uint32_t)kNormPartials;
-    e = a.dtype == MX_BF16 ? launch_backward<MX_BF16>(p, parts, s, a.stream) : launch_backward<MX_F32>(p, parts, s, a.stream);
+  if (a.dim % 8 == 0 && a.dim <= 8192) {
+    e = a.dtype == MX_BF16 ? launch_backward<MX_BF16>(p, a.sm_count, &parts, a.stream)
+                           : launch_backward<MX_F32>(p, a.sm_count, &parts, a.stream);
   } else {
     e = a.dtype == MX_BF16 ? launch_pdl(rmsnorm_row_sums_kernel<MX_BF16>, dim3(p.rows), dim3(256), 0, a.stream, p)
                            : launch_pdl(rmsnorm_row_sums_kernel<MX_F32>, dim3(p.rows), dim3(256), 0, a.stream, p);
@@ -480,7 +616,7 @@ cudaError_t launch_rmsnorm_backward(const RmsnormBackwardArgs& a) {
                            : launch_pdl(rmsnorm_columns_kernel<MX_F32>, grid, dim3(256), 0, a.stream, p);
   }
   if (e != cudaSuccess) return e;
-  return launch_pdl(rmsnorm_dweight_kernel, dim3((p.dim + 31) / 32), dim3(256), 0, a.stream, (const float*)a.partial,
+  return launch_pdl(rmsnorm_dweight_kernel, dim3((p.dim + 31) / 32), dim3(1024), 0, a.stream, (const float*)a.partial,
                     a.dweight, parts, p.dim);
 }
 

@@ -76,23 +76,23 @@ def test_moe_rows_and_plan():
     assert lib.mx_moe_rows(1, 0, 4, 64) == 0 and lib.mx_moe_rows(1 << 40, 1 << 40, 4, 64) == 0 and lib.mx_moe_rows(4, 2, 4, 2000) == 0
     need = lib.mx_moe_plan_workspace_bytes(4, 2, 8)
     assert need > 0 and lib.mx_moe_plan_workspace_bytes(4, 2, 1025) == 0
-    # ids tokens topk experts align offsets counts row_of opts workspace bytes
-    base = [P, 4, 2, 8, 64, P, P, P, ctypes.byref(O), P, need]
+    # ids tokens topk experts align offsets counts row_of src_of opts workspace bytes
+    base = [P, 4, 2, 8, 64, P, P, P, P, ctypes.byref(O), P, need]
     _calls(lib.mx_moe_plan, base, [
-        ({0: None}, mx.MX_ERR_NULL), ({5: None}, mx.MX_ERR_NULL), ({6: None}, mx.MX_ERR_NULL), ({7: None}, mx.MX_ERR_NULL), ({9: None}, mx.MX_ERR_NULL),
+        ({0: None}, mx.MX_ERR_NULL), ({5: None}, mx.MX_ERR_NULL), ({6: None}, mx.MX_ERR_NULL), ({7: None}, mx.MX_ERR_NULL), ({8: None}, mx.MX_ERR_NULL), ({10: None}, mx.MX_ERR_NULL),
         ({1: -1}, mx.MX_ERR_SHAPE), ({2: 0}, mx.MX_ERR_SHAPE), ({3: 0}, mx.MX_ERR_SHAPE), ({4: 0}, mx.MX_ERR_SHAPE), ({4: 1025}, mx.MX_ERR_SHAPE),
-        ({1: 1 << 31}, mx.MX_ERR_SHAPE), ({3: 1025}, mx.MX_ERR_UNSUPPORTED), ({8: BAD}, mx.MX_ERR_FMT), ({0: P + 2}, mx.MX_ERR_ALIGN), ({9: P + 8}, mx.MX_ERR_ALIGN),
-        ({10: need - 1}, mx.MX_ERR_WORKSPACE)])
+        ({1: 1 << 31}, mx.MX_ERR_SHAPE), ({3: 1025}, mx.MX_ERR_UNSUPPORTED), ({9: BAD}, mx.MX_ERR_FMT), ({0: P + 2}, mx.MX_ERR_ALIGN), ({10: P + 8}, mx.MX_ERR_ALIGN),
+        ({11: need - 1}, mx.MX_ERR_WORKSPACE)])
 
 
 def test_moe_moves():
-    # elems scales tokens topk dim fmt offsets counts row_of experts rows elems_out scales_out opts
-    base = [P, P, 4, 2, 64, 0, P, P, P, 8, 64, P, P, ctypes.byref(O)]
+    # elems scales tokens topk dim fmt offsets counts row_of src_of experts rows elems_out scales_out opts
+    base = [P, P, 4, 2, 64, 0, P, P, P, P, 8, 64, P, P, ctypes.byref(O)]
     _calls(lib.mx_moe_gather, base, [
-        ({0: None}, mx.MX_ERR_NULL), ({6: None}, mx.MX_ERR_NULL), ({8: None}, mx.MX_ERR_NULL), ({12: None}, mx.MX_ERR_NULL), ({5: 6}, mx.MX_ERR_FMT),
-        ({4: 33}, mx.MX_ERR_SHAPE), ({3: 0}, mx.MX_ERR_SHAPE), ({10: -1}, mx.MX_ERR_SHAPE), ({9: 0}, mx.MX_ERR_SHAPE), ({9: 1025}, mx.MX_ERR_UNSUPPORTED),
-        ({13: PAD}, mx.MX_ERR_UNSUPPORTED), ({10: 1 << 31}, mx.MX_ERR_UNSUPPORTED), ({4: 1 << 30, 10: 1 << 30}, mx.MX_ERR_UNSUPPORTED), ({11: P + 8}, mx.MX_ERR_ALIGN),
-        ({10: 0}, mx.MX_OK)])
+        ({0: None}, mx.MX_ERR_NULL), ({6: None}, mx.MX_ERR_NULL), ({8: None}, mx.MX_ERR_NULL), ({9: None}, mx.MX_ERR_NULL), ({13: None}, mx.MX_ERR_NULL),
+        ({5: 6}, mx.MX_ERR_FMT), ({4: 33}, mx.MX_ERR_SHAPE), ({3: 0}, mx.MX_ERR_SHAPE), ({11: -1}, mx.MX_ERR_SHAPE), ({10: 0}, mx.MX_ERR_SHAPE),
+        ({10: 1025}, mx.MX_ERR_UNSUPPORTED), ({14: PAD}, mx.MX_ERR_UNSUPPORTED), ({11: 1 << 31}, mx.MX_ERR_UNSUPPORTED),
+        ({4: 1 << 30, 11: 1 << 30}, mx.MX_ERR_UNSUPPORTED), ({12: P + 8}, mx.MX_ERR_ALIGN), ({11: 0}, mx.MX_OK)])
     # y weights row_of tokens topk dim rows out opts
     base = [P, None, P, 4, 2, 64, 64, P, ctypes.byref(O)]
     _calls(lib.mx_moe_combine, base, [

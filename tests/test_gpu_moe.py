@@ -49,6 +49,9 @@ def test_plan(T, k, E, align):
         assert np.array_equal(plan.counts.cpu().numpy(), counts)
         assert np.array_equal(plan.row_of.cpu().numpy(), row)
         assert plan.rows >= off[-1] and plan.rows % align == 0
+        src = np.full(plan.rows, -1)
+        src[row.reshape(-1)[row.reshape(-1) >= 0]] = np.flatnonzero(row.reshape(-1) >= 0)
+        assert np.array_equal(plan.src_of.cpu().numpy(), src)
 
 
 @pytest.mark.parametrize("layout", [mx.MX_SCALES_SWIZZLED, mx.MX_SCALES_LINEAR])
