@@ -136,13 +136,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanPara
 // ---- rows that no choice maps to ---------------------------------------------------------------------
 // The blocks behind the tokens' blocks of a launch write them as zeros: `split` blocks per expert for
 // the rows that pad its group, then kTailBlocks blocks for the rows behind the last group.
-constexpr uint32_t kTailBlocks = 64;
+constexpr uint32_t kTailBlocks = 256;
 
 struct ZeroRows {
   const int32_t *offsets, *counts;
   uint32_t experts, rows, split;
 };
-inline uint32_t zero_split(int64_t experts) { return experts >= 256 ? 1u : (uint32_t)(256 / experts); }
+inline uint32_t zero_split(int64_t experts) { return experts >= 1024 ? 1u : experts <= 32 ? 32u : (uint32_t)(1024 / experts); }
 inline uint32_t zero_blocks(int64_t experts) { return (uint32_t)experts * zero_split(experts) + kTailBlocks; }
 
 // Calls f(row) for the rows that block `z` of the zero blocks owns.

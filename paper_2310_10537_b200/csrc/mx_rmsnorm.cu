@@ -421,7 +421,11 @@ __global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(c
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const uint32_t g = i * 32 + lane;
-    if (g < groups) store8<MX_F32>(sums, (size_t)warp * p.dim + 8 * (size_t)g, dw[i]);
+    if (g < groups) {
+      float4* d = reinterpret_cast<float4*>(sums + (size_t)warp * p.dim + 8 * g);
+      d[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
+      d[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+    }
   }
   __syncthreads();
   for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {

@@ -19,8 +19,16 @@ template <int DTYPE>
 __device__ __forceinline__ Raw8<DTYPE> load_raw8(const void* base, size_t elem) {
   Raw8<DTYPE> r;
   const char* p = (const char*)base + elem * (DTYPE == MX_BF16 ? 2 : 4);
+  if constexpr (DTYPE == MX_F32) {
+    if (((uintptr_t)p & 31u) == 0) {
+      asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(r.v[0].x), "=r"(r.v[0].y), "=r"(r.v[0].z), "=r"(r.v[0].w), "=r"(r.v[1].x), "=r"(r.v[1].y),
+                     "=r"(r.v[1].z), "=r"(r.v[1].w) : "l"(p));
+      return r;
+    }
+    r.v[1] = ld_16(p + 16);
+  }
   r.v[0] = ld_16(p);
-  if constexpr (DTYPE == MX_F32) r.v[1] = ld_16(p + 16);
   return r;
 }
 __device__ __forceinline__ void widen4(const uint4& u, float (&f)[8]) {
@@ -53,7 +61,14 @@ __device__ __forceinline__ void store8(void* base, size_t elem, const float (&f)
     *reinterpret_cast<uint4*>((char*)base + elem * 2) =
         make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
   } else {
+    // whole sectors: two 16-byte stores would each write half of every sector they touch
     float4* p = reinterpret_cast<float4*>((char*)base + elem * 4);
+    if (((uintptr_t)p & 31u) == 0) {
+      const uint32_t w[8] = {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]),
+                             __float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])};
+      st_32(p, w);
+      return;
+    }
     p[0] = make_float4(f[0], f[1], f[2], f[3]);
     p[1] = make_float4(f[4], f[5], f[6], f[7]);
   }
