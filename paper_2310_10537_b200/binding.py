@@ -153,6 +153,10 @@ def _load() -> ctypes.CDLL:
 
 _lib = _load()
 
+from . import _py_call  # noqa: E402  (it links against the library loaded above)
+
+_py_call.set_error_type(MxError)
+
 
 def lib() -> ctypes.CDLL:
     """The loaded C library (for callers that pass raw pointers)."""
@@ -410,61 +414,8 @@ def mx_conv2d(x_elems: torch.Tensor, x_scales: torch.Tensor, w_elems: torch.Tens
 
 # ---- RMS norm, routing, moving rows, the experts' products ----------------------------
 
-# These calls run in loops of a few microseconds per step: their checks ask the tensors directly and
-# sizes of 2-D MX tensors are computed here (they are those of mx_elems_bytes and mx_scales_bytes).
-_DTYPES = {torch.float32: MX_F32, torch.bfloat16: MX_BF16}
-_BITS = {MX_E4M3: 8, MX_E5M2: 8, MX_E3M2: 6, MX_E2M3: 6, MX_E2M1: 4, MX_INT8: 8}
-
-
-def _device_of(t: torch.Tensor) -> int:
-    """The index of the tensor's device, which has to be the current CUDA device (the library
-    launches there)."""
-    dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors have to be on the current CUDA device, not on {t.device}")
-    return dev
-
-
-def _wrong(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Sequence[int]) -> ValueError:
-    return ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on the current CUDA "
-                      f"device, not {t.dtype} {tuple(t.shape)} on {t.device}")
-
-
-def _need(name: str, t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
-    """The address of a tensor of this type and shape (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        raise _wrong(name, t, dtype, shape)
-    return t.data_ptr()
-
-
-def _bytes(name: str, t: torch.Tensor, dev: int, nbytes: int) -> int:
-    """The address of a contiguous tensor of at least this many bytes."""
-    if t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{name} has to be a contiguous tensor on the current CUDA device")
-    if t.numel() * t.element_size() < nbytes:
-        raise ValueError(f"{name} holds {t.numel() * t.element_size()} bytes, {nbytes} are needed")
-    return t.data_ptr()
-
-
-def _mx_sizes(rows: int, dim: int, fmt: int, layout: int) -> Tuple[int, int]:
-    """Bytes of the codes and scales of an MX tensor [rows, dim]; 0 where the library refuses the call anyway."""
-    kb = (dim + 31) // 32
-    scales = rows * kb if layout == MX_SCALES_LINEAR else (rows + 127) // 128 * ((kb + 3) // 4) * 512
-    return rows * kb * 4 * _BITS.get(fmt, 0), scales
-
-
-def _call_opts(dev: int, dtype: int, layout: int = MX_SCALES_SWIZZLED, check: bool = False):
-    return ctypes.byref(mx_opts_t(dtype, layout, torch._C._cuda_getCurrentRawStream(dev), 1 if check else 0, 0))
-
-
-def _float_code(t: torch.Tensor) -> int:
-    code = _DTYPES.get(t.dtype)
-    if code is None:
-        raise TypeError(f"unsupported float dtype {t.dtype}")
-    return code
-
+# These calls stand in loops of a few microseconds per step, so csrc/py_call.cpp checks their tensors, allocates
+# their results and calls the C entry point: the functions here name and document the arguments.
 
 def mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int, eps: float = 1e-6,
                         residual: Optional[torch.Tensor] = None, rounding: int = MX_RNE,
@@ -476,25 +427,8 @@ def mx_rmsnorm_quantize(x: torch.Tensor, weight: torch.Tensor, fmt: int, eps: fl
 
     ``h`` is the new residual stream (None without a residual, unless ``h_out`` is given; ``h_out`` may
     be ``x`` or ``residual``).  ``y_out`` also receives the norm itself."""
-    if x.dim() != 2:
-        raise ValueError("x has to be [rows, dim]")
-    shape, dt = x.shape, x.dtype
-    rows, dim = shape
-    dev = _device_of(x)
-    if residual is not None and h_out is None:
-        h_out = torch.empty_like(x)
-    ne, ns = _mx_sizes(rows, dim, fmt, layout)
-    if out is None:
-        elems, scales = x.new_empty(ne, dtype=torch.uint8), x.new_empty(ns, dtype=torch.uint8)
-        pe, ps = elems.data_ptr(), scales.data_ptr()
-    else:
-        elems, scales = out
-        pe, ps = _bytes("elems", elems, dev, ne), _bytes("scales", scales, dev, ns)
-    _check(_lib.mx_rmsnorm_quantize(_need("x", x, dev, dt, shape), _need("residual", residual, dev, dt, shape),
-                                    _need("weight", weight, dev, weight.dtype, (dim,)), _float_code(weight), eps, rows, dim,
-                                    _need("h_out", h_out, dev, dt, shape), _need("y_out", y_out, dev, dt, shape), pe, ps,
-                                    fmt, rounding, _call_opts(dev, _float_code(x), layout)), "mx_rmsnorm_quantize")
-    return elems, scales, h_out
+    elems, scales = (None, None) if out is None else out
+    return _py_call.rmsnorm_quantize(x, weight, fmt, eps, residual, rounding, layout, y_out, h_out, elems, scales)
 
 
 def mx_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6,
@@ -502,21 +436,7 @@ def mx_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor,
                         workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradients of the norm: (dh [rows, dim], dweight FP32 [dim]).  ``dres`` is added to dh; ``out``
     receives dh and may be ``dy`` or ``dres``."""
-    if h.dim() != 2:
-        raise ValueError("h has to be [rows, dim]")
-    shape, dt = h.shape, h.dtype
-    rows, dim = shape
-    dev = _device_of(h)
-    if workspace is None:
-        workspace = h.new_empty(_lib.mx_rmsnorm_backward_workspace_bytes(rows, dim), dtype=torch.uint8)
-    dh = torch.empty_like(h) if out is None else out
-    dweight = h.new_empty(dim, dtype=torch.float32)
-    _check(_lib.mx_rmsnorm_backward(_need("dy", dy, dev, dt, shape), _need("h", h, dev, dt, shape),
-                                    _need("weight", weight, dev, weight.dtype, (dim,)), _float_code(weight), eps,
-                                    _need("dres", dres, dev, dt, shape), rows, dim, _need("out", dh, dev, dt, shape),
-                                    dweight.data_ptr(), _call_opts(dev, _float_code(h)), _bytes("workspace", workspace, dev, 0),
-                                    workspace.numel() * workspace.element_size()), "mx_rmsnorm_backward")
-    return dh, dweight
+    return _py_call.rmsnorm_backward(dy, h, weight, eps, dres, out, workspace)
 
 
 def mx_route(logits: torch.Tensor, topk: int, score: int = MX_SCORE_SOFTMAX, bias: Optional[torch.Tensor] = None,
@@ -524,35 +444,13 @@ def mx_route(logits: torch.Tensor, topk: int, score: int = MX_SCORE_SOFTMAX, bia
              scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
     """Experts of every token of ``logits`` [tokens, experts] and their weights: (ids int32, weights
     FP32), both [tokens, topk], the best first."""
-    if logits.dim() != 2:
-        raise ValueError("logits has to be [tokens, experts]")
-    tokens, experts = logits.shape
-    dev = _device_of(logits)
-    width = topk if topk > 0 else 0  # (the library refuses the rest)
-    ids = logits.new_empty((tokens, width), dtype=torch.int32)
-    weights = logits.new_empty((tokens, width), dtype=torch.float32)
-    r = mx_route_t(topk, score, groups, topk_groups, group_score, 1 if renormalize else 0, scale)
-    _check(_lib.mx_route(_need("logits", logits, dev, logits.dtype, logits.shape), _need("bias", bias, dev, torch.float32, (experts,)),
-                         tokens, experts, ctypes.byref(r), ids.data_ptr(), weights.data_ptr(),
-                         _call_opts(dev, _float_code(logits))), "mx_route")
-    return ids, weights
+    return _py_call.route(logits, topk, score, bias, groups, topk_groups, group_score, renormalize, scale)
 
 
 def mx_route_backward(dweights: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor,
                       score: int = MX_SCORE_SOFTMAX, renormalize: bool = True, scale: float = 1.0) -> torch.Tensor:
     """Gradient of mx_route's weights with respect to the logits (the choice ``ids`` held fixed)."""
-    if logits.dim() != 2 or ids.dim() != 2:
-        raise ValueError("logits has to be [tokens, experts], ids [tokens, topk]")
-    tokens, experts = logits.shape
-    topk = ids.shape[1]
-    dev = _device_of(logits)
-    dlogits = torch.empty_like(logits)
-    r = mx_route_t(topk, score, 1, 1, MX_GROUP_MAX, 1 if renormalize else 0, scale)
-    _check(_lib.mx_route_backward(_need("dweights", dweights, dev, torch.float32, (tokens, topk)),
-                                  _need("logits", logits, dev, logits.dtype, logits.shape),
-                                  _need("ids", ids, dev, torch.int32, (tokens, topk)), tokens, experts, ctypes.byref(r),
-                                  dlogits.data_ptr(), _call_opts(dev, _float_code(logits))), "mx_route_backward")
-    return dlogits
+    return _py_call.route_backward(dweights, logits, ids, score, renormalize, scale)
 
 
 class MoePlan(NamedTuple):
@@ -575,30 +473,7 @@ def mx_moe_plan(ids: torch.Tensor, experts: int, align: int = 64,
                 workspace: Optional[torch.Tensor] = None) -> MoePlan:
     """Sort the choices ``ids`` [tokens, topk] by expert, groups padded to ``align`` rows: a multiple of
     64 for mx_gemm_grouped, of 128 for mx_gemm_grouped_k."""
-    if ids.dim() != 2:
-        raise ValueError("ids has to be [tokens, topk]")
-    tokens, topk = ids.shape
-    dev = _device_of(ids)
-    if workspace is None:
-        workspace = ids.new_empty(_lib.mx_moe_plan_workspace_bytes(tokens, topk, experts), dtype=torch.uint8)
-    rows = _lib.mx_moe_rows(tokens, topk, experts, align)
-    plan = MoePlan(ids.new_empty(max(experts, 0) + 1), ids.new_empty(max(experts, 0)), torch.empty_like(ids), rows,
-                   ids.new_empty(rows))
-    _check(_lib.mx_moe_plan(_need("ids", ids, dev, torch.int32, ids.shape), tokens, topk, experts, align,
-                            plan.offsets.data_ptr(), plan.counts.data_ptr(), plan.row_of.data_ptr(), plan.src_of.data_ptr(), _call_opts(dev, MX_F32),
-                            _bytes("workspace", workspace, dev, 0), workspace.numel() * workspace.element_size()), "mx_moe_plan")
-    return plan
-
-
-def _plan_args(plan: MoePlan, dev: int):
-    """tokens, topk, experts and the addresses of offsets, counts and row_of."""
-    if plan.row_of.dim() != 2:
-        raise ValueError("row_of has to be [tokens, topk]")
-    tokens, topk = plan.row_of.shape
-    experts = plan.counts.numel()
-    return (tokens, topk, experts, _need("offsets", plan.offsets, dev, torch.int32, (experts + 1,)),
-            _need("counts", plan.counts, dev, torch.int32, (experts,)),
-            _need("row_of", plan.row_of, dev, torch.int32, (tokens, topk)))
+    return MoePlan._make(_py_call.moe_plan(ids, experts, align, workspace))
 
 
 def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int, plan: MoePlan,
@@ -606,58 +481,21 @@ def mx_moe_gather(elems: torch.Tensor, scales: torch.Tensor, dim: int, fmt: int,
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The rows of an MX tensor [tokens, dim] in the order of ``plan``: (elems, scales) of an MX tensor
     [plan.rows, dim], rows without a choice zero."""
-    dev = _device_of(elems)
-    tokens, topk, experts, offsets, counts, row_of = _plan_args(plan, dev)
-    if plan.src_of is None:
-        raise ValueError("the plan has no src_of")
-    ni, nsi = _mx_sizes(tokens, dim, fmt, layout)
-    ne, ns = _mx_sizes(plan.rows, dim, fmt, layout)
-    if out is None:
-        out = (elems.new_empty(ne, dtype=torch.uint8), elems.new_empty(ns, dtype=torch.uint8))
-    _check(_lib.mx_moe_gather(_bytes("elems", elems, dev, ni), _bytes("scales", scales, dev, nsi), tokens, topk, dim, fmt,
-                              offsets, counts, row_of, _need("src_of", plan.src_of, dev, torch.int32, (plan.rows,)), experts,
-                              plan.rows, _bytes("out elems", out[0], dev, ne),
-                              _bytes("out scales", out[1], dev, ns), _call_opts(dev, MX_F32, layout)), "mx_moe_gather")
-    return out
+    out_elems, out_scales = (None, None) if out is None else out
+    return _py_call.moe_gather(elems, scales, dim, fmt, plan, layout, out_elems, out_scales)
 
 
 def mx_moe_combine(y: torch.Tensor, weights: Optional[torch.Tensor], plan: MoePlan,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[t] = sum over j of weights[t, j] * y[row_of[t, j]] (``weights`` None: all 1); y [plan.rows, dim]."""
-    dev = _device_of(y)
-    tokens, topk, _, _, _, row_of = _plan_args(plan, dev)
-    if y.dim() != 2:
-        raise ValueError(f"y has to be [{plan.rows}, dim]")
-    dim = y.shape[1]
-    if out is None:
-        out = y.new_empty((tokens, dim))
-    _check(_lib.mx_moe_combine(_need("y", y, dev, y.dtype, (plan.rows, dim)), _need("weights", weights, dev, torch.float32, (tokens, topk)),
-                               row_of, tokens, topk, dim, plan.rows, _need("out", out, dev, y.dtype, (tokens, dim)),
-                               _call_opts(dev, _float_code(y))), "mx_moe_combine")
-    return out
+    return _py_call.moe_combine(y, weights, plan, out)
 
 
 def mx_moe_combine_backward(dout: torch.Tensor, y: Optional[torch.Tensor], weights: Optional[torch.Tensor],
                             plan: MoePlan) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Gradients of mx_moe_combine: (dy [plan.rows, dim], dweights FP32 [tokens, topk]).  Without ``y``
     only dy; without ``weights`` as well it is the gather of the rows of a float tensor."""
-    dev = _device_of(dout)
-    tokens, topk, experts, offsets, counts, row_of = _plan_args(plan, dev)
-    if dout.dim() != 2:
-        raise ValueError(f"dout has to be [{tokens}, dim]")
-    dim, dt = dout.shape[1], dout.dtype
-    dy = dout.new_empty((plan.rows, dim))
-    dw = None if y is None else dout.new_empty((tokens, topk), dtype=torch.float32)
-    _check(_lib.mx_moe_combine_backward(_need("dout", dout, dev, dt, (tokens, dim)), _need("y", y, dev, dt, (plan.rows, dim)),
-                                        _need("weights", weights, dev, torch.float32, (tokens, topk)), offsets, counts, row_of,
-                                        tokens, topk, dim, experts, plan.rows, dy.data_ptr(), None if dw is None else dw.data_ptr(),
-                                        _call_opts(dev, _float_code(dout))), "mx_moe_combine_backward")
-    return dy, dw
-
-
-def _operand(name: str, elems: torch.Tensor, scales: torch.Tensor, dev: int, rows: int, K: int, fmt: int):
-    ne, ns = _mx_sizes(rows, K, fmt, MX_SCALES_SWIZZLED)
-    return _bytes(name, elems, dev, ne), _bytes("s" + name, scales, dev, ns)
+    return _py_call.moe_combine_backward(dout, y, weights, plan)
 
 
 def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
@@ -666,16 +504,7 @@ def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torc
     """C[r] = A[r] . B[g]^T for the rows r of group g, offsets[g] .. offsets[g + 1] (int32, on the device,
     multiples of 64): A is the MX tensor [rows, K], B that of [groups, N, K]; rows in no group are not
     written."""
-    groups = offsets.numel() - 1
-    dev = _device_of(A)
-    if out is None:
-        out = torch.empty((rows, N), dtype=out_dtype, device=A.device)
-    pa, psa = _operand("A", A, sA, dev, rows, K, fmtA)
-    pb, psb = _operand("B", B, sB, dev, groups * N, K, fmtB)
-    _check(_lib.mx_gemm_grouped(pa, psa, pb, psb, _need("offsets", offsets, dev, torch.int32, (groups + 1,)),
-                                _need("out", out, dev, out.dtype, (rows, N)), _float_code(out), groups, rows, N, K, fmtA, fmtB,
-                                _call_opts(dev, MX_F32, check=check_status)), "mx_gemm_grouped")
-    return out
+    return _py_call.gemm_grouped(A, sA, B, sB, offsets, rows, N, K, fmtA, fmtB, out, out_dtype, check_status)
 
 
 def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
@@ -683,16 +512,7 @@ def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: to
                       out_dtype: torch.dtype = torch.float32, check_status: bool = False) -> torch.Tensor:
     """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128): A is the
     MX tensor [M, rows], B [N, rows], both quantized along the rows; C [groups, M, N]."""
-    groups = offsets.numel() - 1
-    dev = _device_of(A)
-    if out is None:
-        out = torch.empty((groups, M, N), dtype=out_dtype, device=A.device)
-    pa, psa = _operand("A", A, sA, dev, M, rows, fmtA)
-    pb, psb = _operand("B", B, sB, dev, N, rows, fmtB)
-    _check(_lib.mx_gemm_grouped_k(pa, psa, pb, psb, _need("offsets", offsets, dev, torch.int32, (groups + 1,)),
-                                  _need("out", out, dev, out.dtype, (groups, M, N)), _float_code(out), groups, M, N, rows, fmtA,
-                                  fmtB, _call_opts(dev, MX_F32, check=check_status)), "mx_gemm_grouped_k")
-    return out
+    return _py_call.gemm_grouped_k(A, sA, B, sB, offsets, M, N, rows, fmtA, fmtB, out, out_dtype, check_status)
 
 
 # ---- host-buffer variants: tensors live in (pinned) host memory ----------------

@@ -11,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmx_b200.so")
+PY_CALL = os.path.join(HERE, "_py_call.so")  # the Python side's marshalling module (csrc/py_call.cpp)
 BUILD = os.path.join(HERE, "build")
 SOURCES = ["mx_api.cu", "mx_quantize.cu", "mx_quantize_dual.cu", "mx_quantize_tile.cu", "mx_dequantize.cu",
            "mx_gemm.cu", "mx_im2col.cu", "mx_rmsnorm.cu", "mx_route.cu", "mx_moe.cu", "mx_gemm_grouped.cu"]
@@ -36,11 +37,31 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _build_py_call() -> None:
+    """Compile the marshalling module with g++ against torch's headers.  Its torch libraries are those of
+    the process that imports it; the C library is found next to it."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cuda_inc = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc")))), "include")
+    inc = [*include_paths(), sysconfig.get_paths()["include"], cuda_inc, os.path.join(ROOT, "include")]
+    tmp = PY_CALL + f".tmp{os.getpid()}"
+    subprocess.check_call(["g++", "-std=c++20", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
+                           os.path.join(CSRC, "py_call.cpp"), "-o", tmp,
+                           *[f for i in inc for f in ("-isystem", i)], "-L", lib_dir, "-L", HERE, "-Wl,-rpath,$ORIGIN",
+                           "-lmx_b200", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, PY_CALL)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every kernel file and link ``libmx_b200.so`` next to this module."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
+    """Compile every kernel file, link ``libmx_b200.so`` next to this module and compile the marshalling
+    module against it."""
+    built = os.path.exists(LIB) and os.path.exists(PY_CALL)
+    if not force and built and min(os.path.getmtime(LIB), os.path.getmtime(PY_CALL)) >= _newest_source():
         return LIB
-    if not force and os.path.exists(LIB) and shutil.which("nvcc") is None:
+    if not force and built and shutil.which("nvcc") is None:
         return LIB  # no compiler on this machine: use the library that was shipped
     os.makedirs(BUILD, exist_ok=True)
     if force:
@@ -53,6 +74,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call(["nvcc", "-shared", "-cudart", "static", "-gencode",
                            "arch=compute_100a,code=sm_100a", "-o", tmp, *objs])
     os.replace(tmp, LIB)
+    _build_py_call()
     return LIB
 
 

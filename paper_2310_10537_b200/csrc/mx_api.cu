@@ -1090,7 +1090,7 @@ int mx_moe_combine_backward(const void* dout, const void* y, const float* weight
   if (experts > 1024) return MX_ERR_UNSUPPORTED;
   if (tokens == 0 && rows == 0) return MX_OK;
   if (!offsets || !counts || (rows > 0 && !dy) || (tokens > 0 && (!dout || !row_of))) return MX_ERR_NULL;
-  if (rows > 0 && (y == nullptr) != (dweights == nullptr)) return MX_ERR_NULL;
+  if (rows > 0 && tokens > 0 && (y == nullptr) != (dweights == nullptr)) return MX_ERR_NULL;
   if (misaligned16(dout) || misaligned16(y) || misaligned16(dy) || (uintptr_t)weights % 4 || (uintptr_t)dweights % 4 ||
       (uintptr_t)offsets % 4 || (uintptr_t)counts % 4 || (uintptr_t)row_of % 4)
     return MX_ERR_ALIGN;

@@ -87,7 +87,7 @@ def test_gather_moves_bytes(T, k, E, align, dim, fmt, layout):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("T,k,E,align,dim", [(1, 1, 1, 64, 1), (16, 8, 64, 64, 256), (300, 2, 5, 128, 1001), (33, 3, 7, 1, 96), (70, 4, 40, 64, 4096),
-                                             (5, 40, 64, 64, 104), (9, 9, 16, 64, 8192)])
+                                             (5, 40, 64, 64, 104), (9, 9, 16, 64, 8192), (0, 2, 4, 64, 64)])
 def test_combine_and_its_gradients(T, k, E, align, dim, dtype):
     ids = _ids(T, k, E, 8, True)
     plan = mx.mx_moe_plan(torch.from_numpy(ids).cuda(), E, align)
