@@ -290,7 +290,9 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
             for (uint32_t c = 0; c < KCH; ++c) {
               const uint32_t sf_smem = smem_base + off_sf + stage * sf_bytes + c * sf_chunk;
               const uint32_t sf_tmem = tmem_base + sf_col0 + (stage * KCH + c) * (4u * p.sf_per_stage);
-              for (uint32_t j = 0; j < p.sf_per_stage; ++j) tc_cp_scales_pair(sf_tmem + 4 * j, scale_desc(sf_smem + 512 * j));
+#pragma unroll
+              for (uint32_t j = 0; j < 4; ++j)
+                if (j < p.sf_per_stage) tc_cp_scales_pair(sf_tmem + 4 * j, scale_desc(sf_smem + 512 * j));
             }
             tc_commit_leader(sf_ready_bar(stage));  // arrives when the copies have completed in both CTAs
           }
@@ -316,8 +318,9 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         const uint32_t sx_col = 4 + ((it.x0 & 127u) >> 5);  // a tile starts on row 0 or 64 of a scale chunk
         const uint32_t idesc0 = p.idesc | ((it.n >> 3) << 17);
         for (uint32_t kc = 0; kc < it.nk; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(sf_ready_bar(stage), phase, abort_flag, p.spin_limit) &&
-                                           mbar_wait(full_bar(stage), phase, abort_flag, p.spin_limit));
+          // half of the lanes wait for the scales, half for the operands: one wait's time for both
+          ok = __all_sync(0xffffffffu, mbar_wait((lane & 1u) ? full_bar(stage) : sf_ready_bar(stage), phase, abort_flag,
+                                                 p.spin_limit));
           if (!ok) {
             raise_abort(abort_flag, ST_MMA_WAIT_FULL);
             break;
