@@ -1005,7 +1005,7 @@ int64_t mx_moe_rows(int64_t tokens, int64_t topk, int64_t experts, int64_t align
 size_t mx_moe_plan_workspace_bytes(int64_t tokens, int64_t topk, int64_t experts) {
   if (!plan_ok(tokens, topk, experts, 1) || experts > 1024) return 0;
   const int64_t chunks = (tokens * topk + mx::kPlanChunk - 1) / mx::kPlanChunk;
-  return align_up((size_t)(chunks < 1 ? 1 : chunks) * (size_t)experts * 4, 256);
+  return align_up((size_t)(chunks + 1) * (size_t)experts * 4, 256);  // the chunks' histograms, and the totals
 }
 
 int mx_moe_plan(const int32_t* ids, int64_t tokens, int64_t topk, int64_t experts, int64_t align,

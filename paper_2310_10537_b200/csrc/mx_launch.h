@@ -163,7 +163,7 @@ cudaError_t launch_route_backward(const RouteArgs& a);
 constexpr int kPlanChunk = 2048;  // choices that one CTA of the plan sorts
 struct MoePlanArgs {
   const int32_t* ids;
-  int32_t *offsets, *counts, *row_of, *src_of, *hist;  // hist: [chunks x experts]
+  int32_t *offsets, *counts, *row_of, *src_of, *hist;  // hist: [chunks + 1 x experts]
   int64_t n, experts, align, rows;
   int sm_count;
   cudaStream_t stream;

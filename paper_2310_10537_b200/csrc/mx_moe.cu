@@ -18,13 +18,15 @@ constexpr uint32_t kPlanThreads = 1024, kPlanWarps = 32, kPlanPerWarp = kPlanChu
 // A CTA sorts a chunk of kPlanChunk choices.  Ranks are exact and independent of timing: a warp takes
 // 64 consecutive choices, lanes with the same expert find each other with match_any, and the warps'
 // counts are added up in warp order.  With more than one chunk the chunks' histograms come first, in
-// a launch of their own, and every CTA adds up those before its own.
+// a launch of their own, and every CTA adds up those before its own; with more than kPlanScan chunks a
+// third launch does that once for all of them.
 
 struct PlanParams {
   const int32_t* ids;
   int32_t *offsets, *counts, *row_of, *src_of, *hist;
-  uint32_t n, experts, align, chunks, rows;
+  uint32_t n, experts, align, chunks, rows, scanned;
 };
+constexpr uint32_t kPlanScan = 64;
 
 __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const PlanParams p) {
   extern __shared__ uint32_t count[];
@@ -41,71 +43,121 @@ __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const PlanPara
     p.hist[(size_t)blockIdx.x * p.experts + e] = (int32_t)count[e];
 }
 
+__device__ __forceinline__ uint32_t warp_prefix(uint32_t v, uint32_t lane) {  // inclusive
+#pragma unroll
+  for (uint32_t o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(kFull, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+// hist[c][e] becomes the choices of expert e before chunk c; row `chunks` the totals.  A block per 32
+// experts (lanes), the chunks in 32 runs (warps).
+__global__ void __launch_bounds__(1024) plan_scan_kernel(const PlanParams p) {
+  __shared__ uint32_t run[32][33];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+  const uint32_t per = (p.chunks + 31) / 32, c0 = min(p.chunks, warp * per), c1 = min(p.chunks, c0 + per);
+  uint32_t t = 0;
+  if (e < p.experts) {
+#pragma unroll 8
+    for (uint32_t c = c0; c < c1; ++c) t += (uint32_t)p.hist[(size_t)c * p.experts + e];
+  }
+  run[warp][lane] = t;
+  __syncthreads();
+  // warp w: the runs of expert w
+  const uint32_t v = run[lane][warp], upto = warp_prefix(v, lane);
+  run[lane][warp] = upto - v;
+  if (lane == 31 && blockIdx.x * 32 + warp < p.experts)
+    p.hist[(size_t)p.chunks * p.experts + blockIdx.x * 32 + warp] = (int32_t)upto;
+  __syncthreads();
+  t = run[warp][lane];
+  if (e < p.experts) {
+    for (uint32_t c = c0; c < c1; ++c) {
+      int32_t* h = p.hist + (size_t)c * p.experts + e;
+      const uint32_t x = (uint32_t)*h;
+      *h = (int32_t)t;
+      t += x;
+    }
+  }
+}
+
+// Shared memory of plan_place_kernel per expert: first row, end of the group, its rows without a choice and
+// the warps' counts (rows of `stride` shorts: odd, so that a column's 32 counts lie in different banks).
+__host__ __device__ inline uint32_t plan_stride(uint32_t experts) { return experts | 1u; }
+__host__ __device__ inline size_t plan_smem(uint32_t experts) {
+  return (size_t)experts * 12 + (size_t)kPlanWarps * plan_stride(experts) * 2;
+}
+
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanParams p) {
   extern __shared__ uint32_t smem[];
-  uint32_t* first = smem;                                           // [experts] row of the chunk's first choice
-  uint32_t* pad_end = smem + p.experts;                             // [experts] end of the group
-  uint16_t* pad_rows = reinterpret_cast<uint16_t*>(smem + 2 * p.experts);  // [experts] its rows without a choice
-  uint16_t* count = pad_rows + p.experts;                           // [warps][experts]
+  const uint32_t E = p.experts, stride = plan_stride(E);
+  uint32_t* first = smem;               // [E] row of the chunk's first choice
+  uint32_t* total_of = smem + E;        // [E] choices of the expert; then the end of its group
+  uint32_t* pad_rows = smem + 2 * E;    // [E]
+  uint16_t* count = reinterpret_cast<uint16_t*>(smem + 3 * E);  // [warps][stride]
   __shared__ uint32_t warp_total[33];
   pdl_prologue();
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, E = p.experts;
-  for (uint32_t i = threadIdx.x; i < kPlanWarps * E; i += kPlanThreads) count[i] = 0;
-  __syncthreads();
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (uint32_t i = threadIdx.x; i < kPlanWarps * stride; i += kPlanThreads) count[i] = 0;
   uint32_t expert[kPlanPerWarp / 32], rank[kPlanPerWarp / 32];
-  uint16_t* mine = count + warp * E;
   const uint32_t i0 = blockIdx.x * kPlanChunk + warp * kPlanPerWarp + lane;
 #pragma unroll
   for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
-    const uint32_t i = i0 + 32 * k;
-    const uint32_t e = i < p.n ? (uint32_t)__ldg(p.ids + i) : 0xffffffffu;
-    const bool live = e < E;
-    const uint32_t peers = __match_any_sync(kFull, live ? e : 0xffffffffu);
-    const uint32_t before = live ? mine[e] : 0u;
+    const uint32_t e = i0 + 32 * k < p.n ? (uint32_t)__ldg(p.ids + i0 + 32 * k) : 0xffffffffu;
+    expert[k] = e < E ? e : 0xffffffffu;
+  }
+  __syncthreads();
+  uint16_t* mine = count + warp * stride;
+#pragma unroll
+  for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
+    const bool live = expert[k] < E;
+    const uint32_t peers = __match_any_sync(kFull, expert[k]);
+    const uint32_t before = live ? mine[expert[k]] : 0u;
     __syncwarp();
-    if (live && (peers & ((1u << lane) - 1u)) == 0) mine[e] = (uint16_t)(before + __popc(peers));
+    if (live && (peers & ((1u << lane) - 1u)) == 0) mine[expert[k]] = (uint16_t)(before + __popc(peers));
     __syncwarp();
-    expert[k] = live ? e : 0xffffffffu;
     rank[k] = before + __popc(peers & ((1u << lane) - 1u));
   }
   __syncthreads();
-  // thread e: the warps' counts become ranks, the chunks' counts the chunk's start and the group's size
-  const uint32_t e = threadIdx.x;
-  uint32_t total = 0, base = 0;
-  if (e < E) {
-    for (uint32_t w = 0; w < kPlanWarps; ++w) {
-      const uint32_t c = count[w * E + e];
-      count[w * E + e] = (uint16_t)total;
-      total += c;
-    }
-    if (p.chunks > 1) {
-      total = 0;
-#pragma unroll 8
-      for (uint32_t c = 0; c < p.chunks; ++c) {
-        const uint32_t h = (uint32_t)p.hist[(size_t)c * E + e];
-        if (c < blockIdx.x) base += h;
-        total += h;
-      }
-    }
-  }
-  const uint32_t padded = (total + p.align - 1) / p.align * p.align;
-  uint32_t scan = padded;  // inclusive, over the experts
+  // A warp per expert: the warps' counts (one per lane) become ranks; the chunks' counts the chunk's start
+  // in the group and the group's size.
+  for (uint32_t e = warp; e < E; e += kPlanWarps) {
+    const uint32_t c = count[lane * stride + e], upto = warp_prefix(c, lane);
+    count[lane * stride + e] = (uint16_t)(upto - c);
+    uint32_t total = __shfl_sync(kFull, upto, 31), base = 0;
+    if (p.scanned) {
+      base = (uint32_t)p.hist[(size_t)blockIdx.x * E + e];
+      total = (uint32_t)p.hist[(size_t)p.chunks * E + e];
+    } else if (p.chunks > 1) {
+      uint32_t t = 0, u = 0;
 #pragma unroll
-  for (uint32_t o = 1; o < 32; o <<= 1) {
-    const uint32_t v = __shfl_up_sync(kFull, scan, o);
-    if (lane >= o) scan += v;
+      for (uint32_t k = 0; k < kPlanScan; k += 32) {
+        const uint32_t ch = k + lane;
+        const uint32_t h = ch < p.chunks ? (uint32_t)p.hist[(size_t)ch * E + e] : 0u;
+        t += h;
+        if (ch < blockIdx.x) u += h;
+      }
+      total = __reduce_add_sync(kFull, t);
+      base = __reduce_add_sync(kFull, u);
+    }
+    if (lane == 0) {
+      first[e] = base;
+      total_of[e] = total;
+    }
   }
+  __syncthreads();
+  const uint32_t e = threadIdx.x, total = e < E ? total_of[e] : 0u;
+  const uint32_t padded = (total + p.align - 1) / p.align * p.align;
+  uint32_t scan = warp_prefix(padded, lane);  // over the experts
   if (lane == 31) warp_total[warp] = scan;
   __syncthreads();
-  uint32_t w = lane < warp ? warp_total[lane] : 0u;
-#pragma unroll
-  for (uint32_t o = 16; o; o >>= 1) w += __shfl_xor_sync(kFull, w, o);
-  scan += w;
+  scan += __reduce_add_sync(kFull, lane < warp ? warp_total[lane] : 0u);
   if (e < E) {
-    first[e] = scan - padded + base;
-    pad_end[e] = scan;
-    pad_rows[e] = (uint16_t)(padded - total);
-    if (e == E - 1) warp_total[32] = scan;
+    first[e] += scan - padded;
+    total_of[e] = scan;
+    pad_rows[e] = padded - total;
     if (blockIdx.x == 0) {
       p.counts[e] = (int32_t)total;
       p.offsets[e] = (int32_t)(scan - padded);
@@ -116,8 +168,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanPara
 #pragma unroll
   for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
     const uint32_t i = i0 + 32 * k;
-    if (i < p.n)
-    {
+    if (i < p.n) {
       const int32_t row = expert[k] < E ? (int32_t)(first[expert[k]] + mine[expert[k]] + rank[k]) : -1;
       p.row_of[i] = row;
       if (row >= 0) p.src_of[row] = (int32_t)i;
@@ -125,12 +176,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanPara
   }
   // rows without a choice: the last ones of every group (a warp per group, spread over the blocks), and
   // those behind the last group
-  const uint32_t all = warp_total[32];
   for (uint32_t g = blockIdx.x * kPlanWarps + warp; g < E; g += gridDim.x * kPlanWarps) {
-    const uint32_t r1 = pad_end[g], n_pad = pad_rows[g];
+    const uint32_t r1 = total_of[g], n_pad = pad_rows[g];
     for (uint32_t r = r1 - n_pad + lane; r < r1; r += 32) p.src_of[r] = -1;
   }
-  for (uint32_t r = all + blockIdx.x * kPlanThreads + threadIdx.x; r < p.rows; r += gridDim.x * kPlanThreads) p.src_of[r] = -1;
+  for (uint32_t r = total_of[E - 1] + blockIdx.x * kPlanThreads + threadIdx.x; r < p.rows; r += gridDim.x * kPlanThreads)
+    p.src_of[r] = -1;
 }
 
 // ---- rows that no choice maps to ---------------------------------------------------------------------
@@ -406,14 +457,13 @@ cudaError_t launch_moe_plan(const MoePlanArgs& a) {
   p.ids = a.ids; p.offsets = a.offsets; p.counts = a.counts; p.row_of = a.row_of; p.src_of = a.src_of; p.hist = a.hist; p.rows = (uint32_t)a.rows;
   p.n = (uint32_t)a.n; p.experts = (uint32_t)a.experts; p.align = (uint32_t)a.align;
   p.chunks = (uint32_t)((a.n + kPlanChunk - 1) / kPlanChunk);
-  const size_t smem = (size_t)a.experts * (2 * sizeof(uint32_t) + (kPlanWarps + 1) * sizeof(uint16_t));
+  p.scanned = p.chunks > kPlanScan ? 1u : 0u;
   static bool attr_set[64] = {false};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             1024 * (int)(2 * sizeof(uint32_t) + (kPlanWarps + 1) * sizeof(uint16_t)));
+    e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)plan_smem(1024));
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) attr_set[dev] = true;
   }
@@ -421,7 +471,11 @@ cudaError_t launch_moe_plan(const MoePlanArgs& a) {
     e = launch_pdl(plan_count_kernel, dim3(p.chunks), dim3(kPlanThreads), sizeof(uint32_t) * a.experts, a.stream, p);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(plan_place_kernel, dim3(p.chunks ? p.chunks : 1), dim3(kPlanThreads), smem, a.stream, p);
+  if (p.scanned) {
+    e = launch_pdl(plan_scan_kernel, dim3((p.experts + 31) / 32), dim3(1024), 0, a.stream, p);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(plan_place_kernel, dim3(p.chunks ? p.chunks : 1), dim3(kPlanThreads), plan_smem(p.experts), a.stream, p);
 }
 
 cudaError_t launch_moe_gather(const MoeMoveArgs& a) {

@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
 
 // ---------------------------------------------------------------------------------------------------
 // Backward.  Both row sums are taken over what is read anyway,
-//   s1 = sum h^2,  s2 = sum dy w h,   s = rsqrt(s1 / D + eps),   dh = s (dy w - h s^2 s2 / D) + dres,
+//   s1 = sum h^2,  s2 = sum dy h w,   s = rsqrt(s1 / D + eps),   dh = s (dy w - h s^2 s2 / D) + dres,
 // so a row is read once and needs one reduction.  The grid stays resident; a thread keeps its columns
 // from row to row and sums its share of the weight gradient, dy h s, in registers.  Every CTA writes
 // one row of partial sums and a second kernel adds those in a fixed order.
@@ -241,19 +241,86 @@ struct NormBackParams {
   float eps, inv_dim;
 };
 
-// The second half of a row: dh, and the row's share of the weight gradient.
+// Pairs of FP32 numbers: one instruction for both.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 template <int DTYPE>
-__device__ __forceinline__ void finish_group(const NormBackParams& p, size_t at, uint32_t elem, const float (&h)[8],
-                                             const float (&g)[8], const float (&q)[8], float s, float c, float (&dw)[8]) {
-  float w[8], o[8];
-  load_weight8(p.weight, p.w_bf16, elem, w);
+__device__ __forceinline__ void widen2(const Raw8<DTYPE>& r, uint64_t (&v)[4]) {
+  float f[8];
+  widen<DTYPE>(r, f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    o[e] = s * (g[e] * w[e] - h[e] * c);
-    if (p.dres) o[e] += q[e];
-    dw[e] = fmaf(g[e], h[e] * s, dw[e]);
+  for (int i = 0; i < 4; ++i) v[i] = pack2(f[2 * i], f[2 * i + 1]);
+}
+
+// A group's share of the row sums: s1 += h^2, s2 += (dy h) w.
+template <int DTYPE>
+__device__ __forceinline__ void sum_group(const Raw8<DTYPE>& hr, const Raw8<DTYPE>& gr, const uint64_t (&w)[4],
+                                          uint64_t& s1, uint64_t& s2) {
+  uint64_t h[4], g[4];
+  widen2<DTYPE>(hr, h);
+  widen2<DTYPE>(gr, g);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s1 = fma2(h[i], h[i], s1);
+    s2 = fma2(mul2(g[i], h[i]), w[i], s2);
+  }
+}
+
+// The second half of a row, with k = s c: dh = s dy w + dres - h k, and dw += s dy h.
+template <int DTYPE>
+__device__ __forceinline__ void finish_group(const NormBackParams& p, size_t at, const Raw8<DTYPE>& hr, const Raw8<DTYPE>& gr,
+                                             const Raw8<DTYPE>& qr, const uint64_t (&w)[4], float s, float k,
+                                             uint64_t (&dw)[4]) {
+  uint64_t h[4], g[4], q[4];
+  widen2<DTYPE>(hr, h);
+  widen2<DTYPE>(gr, g);
+  if (p.dres) {
+    widen2<DTYPE>(qr, q);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = 0;
+  }
+  const uint64_t ss = pack2(s, s), kk = pack2(-k, -k);
+  float o[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t gs = mul2(g[i], ss);
+    unpack2(fma2(h[i], kk, fma2(gs, w[i], q[i])), o[2 * i], o[2 * i + 1]);
+    dw[i] = fma2(gs, h[i], dw[i]);
   }
   store8<DTYPE>(p.dh, at, o);
+}
+
+__device__ __forceinline__ void load_weight2(const NormBackParams& p, uint32_t elem, uint64_t (&w)[4]) {
+  float f[8];
+  load_weight8(p.weight, p.w_bf16, elem, f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = pack2(f[2 * i], f[2 * i + 1]);
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+  float lo, hi;
+  unpack2(v, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ void spread2(const uint64_t (&v)[4], float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -272,11 +339,14 @@ __global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackPar
   const uint32_t T = blockDim.x, lane = threadIdx.x & 31, warps = T >> 5, groups = p.dim >> 3;
   const uint32_t slot = V * T * kGroup, stage_bytes = 3 * slot;  // h, dy, dres
   const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
-  float dw[V][8];
+  uint64_t dw[V][4], w[V][4];  // a thread's columns, and so its weights, are the same in every row
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int i = 0; i < V; ++i) {
+    const uint32_t g = i * T + threadIdx.x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+    for (int e = 0; e < 4; ++e) { dw[i][e] = 0; w[i][e] = 0; }
+    if (g < groups) load_weight2(p, 8 * g, w[i]);
+  }
   auto request = [&](uint32_t row, uint32_t stage) {
     if (row < p.rows) {
 #pragma unroll
@@ -308,26 +378,19 @@ __global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackPar
   uint32_t side = 0, stage = 0;
   for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
     asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
-    float s1 = 0.0f, s2 = 0.0f;
-    float h[V][8], g8[V][8], q[V][8];
+    uint64_t a1 = 0, a2 = 0;
+    Raw8<DTYPE> h[V], d[V], q[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const uint32_t g = i * T + threadIdx.x;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) { h[i][e] = 0.0f; g8[i][e] = 0.0f; q[i][e] = 0.0f; }
       if (g < groups) {
-        float w[8];
-        load_weight8(p.weight, p.w_bf16, 8 * g, w);
-        widen<DTYPE>(take(stage, 0, g), h[i]);
-        widen<DTYPE>(take(stage, 1, g), g8[i]);
-        if (p.dres) widen<DTYPE>(take(stage, 2, g), q[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s1 = fmaf(h[i][e], h[i][e], s1);
-          s2 = fmaf(g8[i][e] * w[e], h[i][e], s2);
-        }
+        h[i] = take(stage, 0, g);
+        d[i] = take(stage, 1, g);
+        if (p.dres) q[i] = take(stage, 2, g);
+        sum_group<DTYPE>(h[i], d[i], w[i], a1, a2);
       }
     }
+    float s1 = sum2(a1), s2 = sum2(a2);
     request(row + NS * gridDim.x, stage);  // into the slots just read
     if (++stage == NS) stage = 0;
 #pragma unroll
@@ -344,18 +407,22 @@ __global__ void __launch_bounds__(512) rmsnorm_backward_kernel(const NormBackPar
       t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
       t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
     }
-    const float s = rsqrtf(t.x * p.inv_dim + p.eps), c = s * s * (t.y * p.inv_dim);
+    const float s = rsqrtf(t.x * p.inv_dim + p.eps), k = s * (s * s * (t.y * p.inv_dim));
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const uint32_t g = i * T + threadIdx.x;
-      if (g < groups) finish_group<DTYPE>(p, (size_t)row * p.dim + 8 * (size_t)g, 8 * g, h[i], g8[i], q[i], s, c, dw[i]);
+      if (g < groups) finish_group<DTYPE>(p, (size_t)row * p.dim + 8 * (size_t)g, h[i], d[i], q[i], w[i], s, k, dw[i]);
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const uint32_t g = i * T + threadIdx.x;
-    if (g < groups) store8<MX_F32>(p.partial, (size_t)blockIdx.x * p.dim + 8 * (size_t)g, dw[i]);
+    if (g < groups) {
+      float f[8];
+      spread2(dw[i], f);
+      store8<MX_F32>(p.partial, (size_t)blockIdx.x * p.dim + 8 * (size_t)g, f);
+    }
   }
 }
 
@@ -367,11 +434,14 @@ __global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(c
   extern __shared__ float sums[];  // [warps][dim]
   pdl_prologue();
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = p.dim >> 3;
-  float dw[V][8];
+  uint64_t dw[V][4], w[V][4];
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int i = 0; i < V; ++i) {
+    const uint32_t g = i * 32 + lane;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+    for (int e = 0; e < 4; ++e) { dw[i][e] = 0; w[i][e] = 0; }
+    if (g < groups) load_weight2(p, 8 * g, w[i]);
+  }
   for (uint32_t row = blockIdx.x * kRowWarps + warp; row < p.rows; row += gridDim.x * kRowWarps) {
     Raw8<DTYPE> h[V], d[V], q[V];
     const size_t base = (size_t)row * p.dim;
@@ -384,47 +454,32 @@ __global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(c
         if (p.dres) q[i] = load_raw8<DTYPE>(p.dres, base + 8 * (size_t)g);
       }
     }
-    float s1 = 0.0f, s2 = 0.0f;
+    uint64_t a1 = 0, a2 = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t g = i * 32 + lane;
-      if (g < groups) {
-        float w[8], hf[8], gf[8];
-        load_weight8(p.weight, p.w_bf16, 8 * g, w);
-        widen<DTYPE>(h[i], hf);
-        widen<DTYPE>(d[i], gf);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s1 = fmaf(hf[e], hf[e], s1);
-          s2 = fmaf(gf[e] * w[e], hf[e], s2);
-        }
-      }
-    }
+    for (int i = 0; i < V; ++i)
+      if (i * 32 + lane < groups) sum_group<DTYPE>(h[i], d[i], w[i], a1, a2);
+    float s1 = sum2(a1), s2 = sum2(a2);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
       s1 += __shfl_xor_sync(0xffffffffu, s1, o);
       s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
-    const float s = rsqrtf(s1 * p.inv_dim + p.eps), c = s * s * (s2 * p.inv_dim);
+    const float s = rsqrtf(s1 * p.inv_dim + p.eps), k = s * (s * s * (s2 * p.inv_dim));
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const uint32_t g = i * 32 + lane;
-      if (g < groups) {
-        float hf[8], gf[8], qf[8] = {};
-        widen<DTYPE>(h[i], hf);
-        widen<DTYPE>(d[i], gf);
-        if (p.dres) widen<DTYPE>(q[i], qf);
-        finish_group<DTYPE>(p, base + 8 * (size_t)g, 8 * g, hf, gf, qf, s, c, dw[i]);
-      }
+      if (g < groups) finish_group<DTYPE>(p, base + 8 * (size_t)g, h[i], d[i], q[i], w[i], s, k, dw[i]);
     }
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const uint32_t g = i * 32 + lane;
     if (g < groups) {
+      float f[8];
+      spread2(dw[i], f);
       float4* d = reinterpret_cast<float4*>(sums + (size_t)warp * p.dim + 8 * g);
-      d[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
-      d[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+      d[0] = make_float4(f[0], f[1], f[2], f[3]);
+      d[1] = make_float4(f[4], f[5], f[6], f[7]);
     }
   }
   __syncthreads();
