@@ -160,7 +160,7 @@ struct RouteArgs {
 cudaError_t launch_route(const RouteArgs& a);
 cudaError_t launch_route_backward(const RouteArgs& a);
 
-constexpr int kPlanChunk = 2048;  // choices that one CTA of the plan sorts
+constexpr int kPlanChunk = 1024;  // choices that one CTA of the plan sorts
 struct MoePlanArgs {
   const int32_t* ids;
   int32_t *offsets, *counts, *row_of, *src_of, *hist;  // hist: [chunks + 1 x experts]

@@ -12,21 +12,22 @@ namespace mx {
 namespace {
 
 constexpr uint32_t kFull = 0xffffffffu;
-constexpr uint32_t kPlanThreads = 1024, kPlanWarps = 32, kPlanPerWarp = kPlanChunk / kPlanWarps;
+constexpr uint32_t kPlanThreads = 512, kPlanWarps = 16, kPlanPerWarp = kPlanChunk / kPlanWarps;
 
 // ---- plan ------------------------------------------------------------------------------------------
 // A CTA sorts a chunk of kPlanChunk choices.  Ranks are exact and independent of timing: a warp takes
-// 64 consecutive choices, lanes with the same expert find each other with match_any, and the warps'
-// counts are added up in warp order.  With more than one chunk the chunks' histograms come first, in
-// a launch of their own, and every CTA adds up those before its own; with more than kPlanScan chunks a
-// third launch does that once for all of them.
+// 64 consecutive choices, lanes with the same expert find each other by a vote per bit of its number
+// (match.any takes 45 clocks of a unit that the SM's warps share), and the warps' counts are added up in warp
+// order.  With more than one chunk the chunks' histograms come first, in a launch of their own, and every
+// CTA adds up those before its own; where that is more than kPlanDirect numbers a third launch does it once
+// for all of them.  (65536 choices of 64 experts: 10.1 us with chunks of 2048, match.any and a warp per expert.)
 
 struct PlanParams {
   const int32_t* ids;
   int32_t *offsets, *counts, *row_of, *src_of, *hist;
   uint32_t n, experts, align, chunks, rows, scanned;
 };
-constexpr uint32_t kPlanScan = 64;
+constexpr uint32_t kPlanDirect = 64 * kPlanThreads;  // histogram entries a CTA adds up by itself
 
 __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const PlanParams p) {
   extern __shared__ uint32_t count[];
@@ -83,24 +84,20 @@ __global__ void __launch_bounds__(1024) plan_scan_kernel(const PlanParams p) {
   }
 }
 
-// Shared memory of plan_place_kernel per expert: first row, end of the group, its rows without a choice and
-// the warps' counts (rows of `stride` shorts: odd, so that a column's 32 counts lie in different banks).
-__host__ __device__ inline uint32_t plan_stride(uint32_t experts) { return experts | 1u; }
-__host__ __device__ inline size_t plan_smem(uint32_t experts) {
-  return (size_t)experts * 12 + (size_t)kPlanWarps * plan_stride(experts) * 2;
-}
+// Shared memory of plan_place_kernel per expert: first row, choices (then the end of its group), rows without
+// a choice, and the warps' counts.
+inline size_t plan_smem(uint32_t experts) { return (size_t)experts * (3 * sizeof(uint32_t) + kPlanWarps * sizeof(uint16_t)); }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanParams p) {
   extern __shared__ uint32_t smem[];
-  const uint32_t E = p.experts, stride = plan_stride(E);
+  const uint32_t E = p.experts;
   uint32_t* first = smem;               // [E] row of the chunk's first choice
   uint32_t* total_of = smem + E;        // [E] choices of the expert; then the end of its group
   uint32_t* pad_rows = smem + 2 * E;    // [E]
-  uint16_t* count = reinterpret_cast<uint16_t*>(smem + 3 * E);  // [warps][stride]
-  __shared__ uint32_t warp_total[33];
+  uint16_t* count = reinterpret_cast<uint16_t*>(smem + 3 * E);  // [warps][E]
+  __shared__ uint32_t warp_total[kPlanWarps];
   pdl_prologue();
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (uint32_t i = threadIdx.x; i < kPlanWarps * stride; i += kPlanThreads) count[i] = 0;
   uint32_t expert[kPlanPerWarp / 32], rank[kPlanPerWarp / 32];
   const uint32_t i0 = blockIdx.x * kPlanChunk + warp * kPlanPerWarp + lane;
 #pragma unroll
@@ -108,63 +105,82 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanPara
     const uint32_t e = i0 + 32 * k < p.n ? (uint32_t)__ldg(p.ids + i0 + 32 * k) : 0xffffffffu;
     expert[k] = e < E ? e : 0xffffffffu;
   }
+  for (uint32_t i = threadIdx.x; i < kPlanWarps * E; i += kPlanThreads) count[i] = 0;
+  for (uint32_t i = threadIdx.x; i < E; i += kPlanThreads) { first[i] = 0; total_of[i] = 0; }
   __syncthreads();
-  uint16_t* mine = count + warp * stride;
+  uint16_t* mine = count + warp * E;
 #pragma unroll
   for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
     const bool live = expert[k] < E;
-    const uint32_t peers = __match_any_sync(kFull, expert[k]);
+    uint32_t peers = __ballot_sync(kFull, live);
+    for (uint32_t b = 1; b < E; b <<= 1) {
+      const uint32_t set = __ballot_sync(kFull, expert[k] & b);
+      peers &= expert[k] & b ? set : ~set;
+    }
     const uint32_t before = live ? mine[expert[k]] : 0u;
     __syncwarp();
     if (live && (peers & ((1u << lane) - 1u)) == 0) mine[expert[k]] = (uint16_t)(before + __popc(peers));
     __syncwarp();
     rank[k] = before + __popc(peers & ((1u << lane) - 1u));
   }
-  __syncthreads();
-  // A warp per expert: the warps' counts (one per lane) become ranks; the chunks' counts the chunk's start
-  // in the group and the group's size.
-  for (uint32_t e = warp; e < E; e += kPlanWarps) {
-    const uint32_t c = count[lane * stride + e], upto = warp_prefix(c, lane);
-    count[lane * stride + e] = (uint16_t)(upto - c);
-    uint32_t total = __shfl_sync(kFull, upto, 31), base = 0;
-    if (p.scanned) {
-      base = (uint32_t)p.hist[(size_t)blockIdx.x * E + e];
-      total = (uint32_t)p.hist[(size_t)p.chunks * E + e];
-    } else if (p.chunks > 1) {
-      uint32_t t = 0, u = 0;
-#pragma unroll
-      for (uint32_t k = 0; k < kPlanScan; k += 32) {
-        const uint32_t ch = k + lane;
-        const uint32_t h = ch < p.chunks ? (uint32_t)p.hist[(size_t)ch * E + e] : 0u;
-        t += h;
-        if (ch < blockIdx.x) u += h;
+  // the chunks before this one, and all of them (integers: the order of the additions does not matter)
+  if (p.scanned) {
+    for (uint32_t e = threadIdx.x; e < E; e += kPlanThreads) {
+      first[e] = (uint32_t)p.hist[(size_t)blockIdx.x * E + e];
+      total_of[e] = (uint32_t)p.hist[(size_t)p.chunks * E + e];
+    }
+  } else if (p.chunks > 1) {
+    const uint32_t strands = E < kPlanThreads ? kPlanThreads / E : 1u, strand = threadIdx.x / E;
+    if (strand < strands) {
+      for (uint32_t e = threadIdx.x - strand * E; e < E; e += kPlanThreads) {
+        uint32_t all = 0, before = 0;
+#pragma unroll 8
+        for (uint32_t c = strand; c < p.chunks; c += strands) {
+          const uint32_t h = (uint32_t)p.hist[(size_t)c * E + e];
+          all += h;
+          before += c < blockIdx.x ? h : 0u;
+        }
+        atomicAdd(&total_of[e], all);
+        atomicAdd(&first[e], before);
       }
-      total = __reduce_add_sync(kFull, t);
-      base = __reduce_add_sync(kFull, u);
-    }
-    if (lane == 0) {
-      first[e] = base;
-      total_of[e] = total;
     }
   }
   __syncthreads();
-  const uint32_t e = threadIdx.x, total = e < E ? total_of[e] : 0u;
-  const uint32_t padded = (total + p.align - 1) / p.align * p.align;
-  uint32_t scan = warp_prefix(padded, lane);  // over the experts
-  if (lane == 31) warp_total[warp] = scan;
-  __syncthreads();
-  scan += __reduce_add_sync(kFull, lane < warp ? warp_total[lane] : 0u);
-  if (e < E) {
-    first[e] += scan - padded;
-    total_of[e] = scan;
-    pad_rows[e] = padded - total;
-    if (blockIdx.x == 0) {
-      p.counts[e] = (int32_t)total;
-      p.offsets[e] = (int32_t)(scan - padded);
-      if (e == E - 1) p.offsets[E] = (int32_t)scan;
+  // the warps' counts become ranks
+  for (uint32_t e = threadIdx.x; e < E; e += kPlanThreads) {
+    uint32_t c[kPlanWarps], t = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kPlanWarps; ++w) c[w] = count[w * E + e];
+#pragma unroll
+    for (uint32_t w = 0; w < kPlanWarps; ++w) {
+      count[w * E + e] = (uint16_t)t;
+      t += c[w];
     }
+    if (p.chunks <= 1) total_of[e] = t;
   }
-  __syncthreads();
+  // groups one after the other, kPlanThreads experts at a time
+  uint32_t start = 0;
+  for (uint32_t e0 = 0; e0 < E; e0 += kPlanThreads) {
+    const uint32_t e = e0 + threadIdx.x, total = e < E ? total_of[e] : 0u;  // (written by this thread, or before the barrier)
+    const uint32_t padded = (total + p.align - 1) / p.align * p.align;
+    uint32_t scan = warp_prefix(padded, lane);
+    if (lane == 31) warp_total[warp] = scan;
+    __syncthreads();
+    const uint32_t w = lane < kPlanWarps ? warp_total[lane] : 0u;
+    scan += start + __reduce_add_sync(kFull, lane < warp ? w : 0u);
+    start += __reduce_add_sync(kFull, w);
+    if (e < E) {
+      first[e] += scan - padded;
+      total_of[e] = scan;
+      pad_rows[e] = padded - total;
+      if (blockIdx.x == 0) {
+        p.counts[e] = (int32_t)total;
+        p.offsets[e] = (int32_t)(scan - padded);
+      }
+    }
+    __syncthreads();
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[E] = (int32_t)start;
 #pragma unroll
   for (uint32_t k = 0; k < kPlanPerWarp / 32; ++k) {
     const uint32_t i = i0 + 32 * k;
@@ -180,7 +196,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const PlanPara
     const uint32_t r1 = total_of[g], n_pad = pad_rows[g];
     for (uint32_t r = r1 - n_pad + lane; r < r1; r += 32) p.src_of[r] = -1;
   }
-  for (uint32_t r = total_of[E - 1] + blockIdx.x * kPlanThreads + threadIdx.x; r < p.rows; r += gridDim.x * kPlanThreads)
+  for (uint32_t r = start + blockIdx.x * kPlanThreads + threadIdx.x; r < p.rows; r += gridDim.x * kPlanThreads)
     p.src_of[r] = -1;
 }
 
@@ -457,7 +473,7 @@ cudaError_t launch_moe_plan(const MoePlanArgs& a) {
   p.ids = a.ids; p.offsets = a.offsets; p.counts = a.counts; p.row_of = a.row_of; p.src_of = a.src_of; p.hist = a.hist; p.rows = (uint32_t)a.rows;
   p.n = (uint32_t)a.n; p.experts = (uint32_t)a.experts; p.align = (uint32_t)a.align;
   p.chunks = (uint32_t)((a.n + kPlanChunk - 1) / kPlanChunk);
-  p.scanned = p.chunks > kPlanScan ? 1u : 0u;
+  p.scanned = p.chunks > 1 && (uint64_t)p.chunks * p.experts > kPlanDirect ? 1u : 0u;
   static bool attr_set[64] = {false};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
