@@ -534,18 +534,23 @@ __global__ void __launch_bounds__(256) rmsnorm_columns_kernel(const NormBackPara
   p.partial[(size_t)blockIdx.y * p.dim + c] = dw;
 }
 
-// dweight[c] = sum over the partial rows, always in the same order: 32 strands of rows per column, so that
-// all of a thread's loads are in flight at once (with 8 strands the chain of loads took 8 us).
+// dweight[c] = sum over the partial rows, always in the same order: 32 strands of rows per column, all of a
+// thread's loads in flight at once (as chains of dependent batches they took 8 us).
 __global__ void __launch_bounds__(1024) rmsnorm_dweight_kernel(const float* __restrict__ partial, float* __restrict__ dweight,
                                                                uint32_t parts, uint32_t dim) {
   __shared__ float sum[32][33];
   pdl_prologue();
   const uint32_t lane = threadIdx.x & 31, strand = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float t = 0.0f;
-  if (c < dim) {
-#pragma unroll 10
-    for (uint32_t r = strand; r < parts; r += 32) t += partial[(size_t)r * dim + c];
+  constexpr uint32_t kEach = (kNormPartials + 31) / 32;
+  float v[kEach];
+#pragma unroll
+  for (uint32_t k = 0; k < kEach; ++k) {
+    const uint32_t r = strand + 32 * k;
+    v[k] = c < dim && r < parts ? partial[(size_t)r * dim + c] : 0.0f;
   }
+#pragma unroll
+  for (uint32_t k = 0; k < kEach; ++k) t += v[k];
   sum[strand][lane] = t;
   __syncthreads();
   // warp w sums column w's strands
