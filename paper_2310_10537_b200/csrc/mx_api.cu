@@ -1074,7 +1074,10 @@ int mx_moe_combine(const void* y, const float* weights, const int32_t* row_of, i
   mx::MoeMoveArgs a = {};
   a.y = y; a.weights = weights; a.row_of = row_of; a.dst = out; a.tokens = tokens; a.topk = topk; a.dim = dim;
   a.rows = rows; a.dtype = o.dtype; a.stream = o.stream;
-  const cudaError_t e = mx::launch_moe_combine(a);
+  cudaError_t e;
+  a.sm_count = sm_count(&e);
+  if (e != cudaSuccess) return fail_cuda(e);
+  e = mx::launch_moe_combine(a);
   return e == cudaSuccess ? MX_OK : fail_cuda(e);
 }
 

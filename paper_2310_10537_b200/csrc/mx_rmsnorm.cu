@@ -85,13 +85,51 @@ __device__ __forceinline__ void zero_pad_rows(const NormParams& p) {
   }
 }
 
+// Quantizes the group g of 8 values of a row whose blocks are four neighbouring lanes' groups, and stores its codes
+// and the block's scale (with the swizzled layout also the zero bytes up to whole words).
+template <int FMT>
+__device__ __forceinline__ void store_group(const NormParams& p, uint32_t row, uint8_t* out_row, uint32_t g,
+                                            const float (&v)[8]) {
+  constexpr uint32_t bits = FmtTraits<FMT>::bits;
+  const uint32_t lane = threadIdx.x & 31, groups_stored = p.kblocks * 4;
+  float m[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[e] = absmax_nan(v[2 * e], v[2 * e + 1]);
+  float am = absmax_nan(absmax_nan(m[0], m[1]), absmax_nan(m[2], m[3]));
+  am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 1));
+  am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 2));
+  const BlockScale bs = block_scale<FMT>(am);
+  uint32_t lo, hi;
+  cast8_sticky<FMT>(v, bs, p.sticky, lo, hi);
+  if constexpr (bits == 6) {  // two lanes' 48 bits each fill three words
+    const uint32_t lo_next = __shfl_down_sync(0xffffffffu, lo, 1);
+    if (g < groups_stored) {
+      uint32_t* d = reinterpret_cast<uint32_t*>(out_row + 12 * (size_t)(g >> 1));
+      if ((lane & 1) == 0) {
+        d[0] = lo;
+        d[1] = __byte_perm(hi, lo_next, 0x5410);
+      } else {
+        d[2] = __byte_perm(lo, hi, 0x5432);
+      }
+    }
+  } else if (g < groups_stored) {
+    if constexpr (bits == 8) *reinterpret_cast<uint2*>(out_row + 8 * (size_t)g) = make_uint2(lo, hi);
+    else *reinterpret_cast<uint32_t*>(out_row + 4 * (size_t)g) = lo;
+  }
+  const uint32_t kb = g >> 2;
+  if ((lane & 3) == 0) {
+    if (kb < p.kblocks) p.scales[scale_at(p, row, kb)] = (uint8_t)bs.byte;
+    else if (p.layout == MX_SCALES_SWIZZLED && kb < ((p.kblocks + 3) & ~3u)) p.scales[scale_at(p, row, kb)] = 0;
+  }
+}
+
 // dim % 8 == 0 and dim <= 8 * V * blockDim: the row in registers.
 template <int DTYPE, int FMT, int V>
 __global__ void __launch_bounds__(V == 4 ? 512 : 1024) rmsnorm_kernel(const NormParams p) {
   constexpr uint32_t bits = FmtTraits<FMT>::bits;
   __shared__ float red[32];
   pdl_prologue();
-  const uint32_t T = blockDim.x, row = blockIdx.x, lane = threadIdx.x & 31;
+  const uint32_t T = blockDim.x, row = blockIdx.x;
   const size_t base = (size_t)row * p.dim;
   const uint32_t groups = p.dim >> 3;                 // of 8 elements that exist
   const uint32_t groups_stored = p.kblocks * 4;       // whole blocks: the last one padded with zeros
@@ -139,43 +177,86 @@ __global__ void __launch_bounds__(V == 4 ? 512 : 1024) rmsnorm_kernel(const Norm
       for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * s * w[e];
       if (p.y_out) store8<DTYPE>(p.y_out, base + 8 * (size_t)g, v[i]);
     }
-    float m[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) m[e] = absmax_nan(v[i][2 * e], v[i][2 * e + 1]);
-    float am = absmax_nan(absmax_nan(m[0], m[1]), absmax_nan(m[2], m[3]));
-    am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 1));
-    am = absmax_nan(am, __shfl_xor_sync(0xffffffffu, am, 2));
-    const BlockScale bs = block_scale<FMT>(am);
-    uint32_t lo, hi;
-    cast8_sticky<FMT>(v[i], bs, p.sticky, lo, hi);
-    if constexpr (bits == 6) {  // two lanes' 48 bits each fill three words
-      const uint32_t lo_next = __shfl_down_sync(0xffffffffu, lo, 1);
-      if (g < groups_stored) {
-        uint32_t* d = reinterpret_cast<uint32_t*>(out_row + 12 * (size_t)(g >> 1));
-        if ((lane & 1) == 0) {
-          d[0] = lo;
-          d[1] = __byte_perm(hi, lo_next, 0x5410);
-        } else {
-          d[2] = __byte_perm(lo, hi, 0x5432);
-        }
-      }
-    } else if (g < groups_stored) {
-      if constexpr (bits == 8) *reinterpret_cast<uint2*>(out_row + 8 * (size_t)g) = make_uint2(lo, hi);
-      else *reinterpret_cast<uint32_t*>(out_row + 4 * (size_t)g) = lo;
-    }
-    const uint32_t kb = g >> 2;
-    if ((lane & 3) == 0) {
-      if (kb < p.kblocks) p.scales[scale_at(p, row, kb)] = (uint8_t)bs.byte;
-      else if (p.layout == MX_SCALES_SWIZZLED && kb < ((p.kblocks + 3) & ~3u)) p.scales[scale_at(p, row, kb)] = 0;
-    }
+    store_group<FMT>(p, row, out_row, g, v[i]);
   }
   zero_pad_rows(p);
 }
 
-// Any dim: one element per lane, one MX block per warp and step.  The row is read twice, the second
-// time out of the caches.
+// Any dim that fits shared memory: rows start anywhere, so h is read (once) and stored an element per lane; it waits in
+// shared memory as FP32 and is quantized from there in groups of 8 like the rows above.
+// (8192 x 4001 BF16: 165 us with an element per lane throughout and the row read twice.)
 template <int DTYPE, int FMT>
 __global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
+  constexpr uint32_t bits = FmtTraits<FMT>::bits;
+  extern __shared__ float4 row_smem[];
+  __shared__ float red[32];
+  float* h = reinterpret_cast<float*>(row_smem);  // [dim rounded up to 128]
+  pdl_prologue();
+  const uint32_t row = blockIdx.x, groups = (p.kblocks + 3) / 4 * 16;
+  const size_t base = (size_t)row * p.dim;
+  float ss = 0.0f;
+  for (uint32_t c0 = threadIdx.x; c0 < p.dim; c0 += 8 * 256) {
+    float v[8], r[8];  // (loads first: h_out may be x or residual, so they cannot move past the stores)
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t c = c0 + 256 * k;
+      v[k] = c < p.dim ? load1<DTYPE>(p.x, base + c) : 0.0f;
+      r[k] = c < p.dim && p.residual ? load1<DTYPE>(p.residual, base + c) : 0.0f;
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+      const uint32_t c = c0 + 256 * k;
+      if (c < p.dim) {
+        if (p.residual) v[k] += r[k];
+        if (p.h_out) store1<DTYPE>(p.h_out, base + c, v[k]);
+        h[c] = v[k];
+        ss = fmaf(v[k], v[k], ss);
+      }
+    }
+  }
+  for (uint32_t c = p.dim + threadIdx.x; c < 8 * groups; c += 256) h[c] = 0.0f;
+  const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);  // (its barrier: the row is in shared memory)
+  uint8_t* out_row = p.elems + (size_t)row * p.kblocks * (4 * bits);
+  for (uint32_t g0 = threadIdx.x & ~31u; g0 < groups; g0 += 256) {  // (warps stay whole for the shuffles)
+    const uint32_t g = g0 + (threadIdx.x & 31);
+    float v[8] = {}, w[8] = {};
+    if (g < groups) {
+      const float4 a = reinterpret_cast<const float4*>(h)[2 * g], b = reinterpret_cast<const float4*>(h)[2 * g + 1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    if (8 * g + 8 <= p.dim) {
+      load_weight8(p.weight, p.w_bf16, 8 * g, w);
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (8 * g + e < p.dim) w[e] = weight1(p.weight, p.w_bf16, 8 * g + e);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * s * w[e];
+    if (8 * g >= p.dim) {  // padding stays zero whatever s is
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    } else if (8 * g + 8 > p.dim) {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (8 * g + e >= p.dim) v[e] = 0.0f;
+    }
+    if (p.y_out && g < groups) {
+      reinterpret_cast<float4*>(h)[2 * g] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(h)[2 * g + 1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    store_group<FMT>(p, row, out_row, g, v);
+  }
+  if (p.y_out) {
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < p.dim; c += 256) store1<DTYPE>(p.y_out, base + c, h[c]);
+  }
+  zero_pad_rows(p);
+}
+
+// Rows longer than shared memory: an element per lane, an MX block per warp and step; the row is read twice.
+template <int DTYPE, int FMT>
+__global__ void __launch_bounds__(1024) rmsnorm_long_kernel(const NormParams p) {
   constexpr uint32_t bits = FmtTraits<FMT>::bits;
   __shared__ float red[32];
   pdl_prologue();
@@ -187,7 +268,7 @@ __global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
     if (p.residual) v += load1<DTYPE>(p.residual, base + c);
     ss = fmaf(v, v, ss);
   }
-  const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);  // (its barrier also orders pass 1 before the stores below)
+  const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);  // (its barrier also orders the reads above before the stores below)
   uint8_t* out_row = p.elems + (size_t)row * p.kblocks * (4 * bits);
   for (uint32_t kb = threadIdx.x >> 5; kb < ((p.kblocks + 3) & ~3u); kb += blockDim.x >> 5) {
     const uint32_t c = kb * 32 + lane;
@@ -491,7 +572,102 @@ __global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(c
   }
 }
 
-// Any dim, in two kernels: the row sums first (a CTA per row), then a thread per column goes down a chunk
+// Any dim up to 512 V: the ring above for rows that start anywhere.  The 16-byte vectors that cover a row are copied
+// by whichever thread comes to them, so a barrier stands between copy and use; a thread takes every 512th
+// element, twice from shared memory.  (8192 x 4001 BF16: 150 us with the two kernels below.)
+__device__ __forceinline__ void cp_async16_part(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+template <int DTYPE> __host__ __device__ constexpr uint32_t elem_bytes() { return DTYPE == MX_BF16 ? 2u : 4u; }
+// bytes of a tensor's slot: a row, up to 15 bytes before it, whole vectors
+template <int DTYPE>
+__host__ __device__ inline uint32_t any_slot(uint32_t dim) { return (dim * elem_bytes<DTYPE>() + 15 + 15) / 16 * 16; }
+
+template <int DTYPE, int V, int NS>
+__global__ void __launch_bounds__(512) rmsnorm_backward_any_kernel(const NormBackParams p) {
+  constexpr uint32_t esz = elem_bytes<DTYPE>();
+  extern __shared__ uint4 ring[];
+  __shared__ float2 red[2][16];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, slot = any_slot<DTYPE>(p.dim), stage_bytes = 3 * slot;
+  const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+  const size_t row_bytes = (size_t)p.dim * esz, all_bytes = row_bytes * p.rows;
+  float dw[V], w[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t c = i * 512 + threadIdx.x;
+    dw[i] = 0.0f;
+    w[i] = c < p.dim ? weight1(p.weight, p.w_bf16, c) : 0.0f;
+  }
+  auto request = [&](uint32_t row, uint32_t stage) {
+    if (row < p.rows) {
+      const size_t b0 = row * row_bytes, a0 = b0 & ~(size_t)15;
+      const uint32_t vecs = (uint32_t)((b0 + row_bytes - a0 + 15) / 16);
+      for (uint32_t j = threadIdx.x; j < vecs; j += 512) {
+        const size_t at = a0 + 16 * (size_t)j;
+        const uint32_t n = all_bytes - at < 16 ? (uint32_t)(all_bytes - at) : 16u;  // nothing behind the tensor is read
+        const uint32_t dst = ring0 + stage * stage_bytes + 16 * j;
+        cp_async16_part(dst, (const char*)p.h + at, n);
+        cp_async16_part(dst + slot, (const char*)p.dy + at, n);
+        if (p.dres) cp_async16_part(dst + 2 * slot, (const char*)p.dres + at, n);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i) request(blockIdx.x + i * gridDim.x, i);
+  uint32_t side = 0, stage = 0;
+  for (uint32_t row = blockIdx.x; row < p.rows; row += gridDim.x, side ^= 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
+    __syncthreads();  // the row has landed, and everybody is done with the row before: its stage is free
+    request(row + (NS - 1) * gridDim.x, stage == 0 ? NS - 1 : stage - 1);
+    const size_t base = (size_t)row * p.dim;
+    const char* at = (const char*)ring + stage * stage_bytes + (uint32_t)(row * row_bytes & 15);
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t c = i * 512 + threadIdx.x;
+      if (c < p.dim) {
+        const float h = load1<DTYPE>(at, c), g = load1<DTYPE>(at + slot, c);
+        s1 = fmaf(h, h, s1);
+        s2 = fmaf(g * h, w[i], s2);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (lane == 0) red[side][threadIdx.x >> 5] = make_float2(s1, s2);
+    __syncthreads();
+    float2 t = red[side][lane & 15];
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+      t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+      t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+    }
+    const float s = rsqrtf(t.x * p.inv_dim + p.eps), k = s * (s * s * (t.y * p.inv_dim));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t c = i * 512 + threadIdx.x;
+      if (c < p.dim) {
+        const float h = load1<DTYPE>(at, c), gs = load1<DTYPE>(at + slot, c) * s;
+        const float q = p.dres ? load1<DTYPE>(at + 2 * slot, c) : 0.0f;
+        dw[i] = fmaf(gs, h, dw[i]);
+        store1<DTYPE>(p.dh, base + c, fmaf(-k, h, fmaf(gs, w[i], q)));
+      }
+    }
+    if (++stage == NS) stage = 0;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t c = i * 512 + threadIdx.x;
+    if (c < p.dim) p.partial[(size_t)blockIdx.x * p.dim + c] = dw[i];
+  }
+}
+
+// Longer rows, in two kernels: the row sums first (a CTA per row), then a thread per column goes down a chunk
 // of rows, writes dh and sums the column's weight gradient.  h and dy are read twice; dh may lie on dy.
 template <int DTYPE>
 __global__ void __launch_bounds__(256) rmsnorm_row_sums_kernel(const NormBackParams p) {
@@ -565,8 +741,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_dweight_kernel(const float* __re
 
 struct Shape {
   uint32_t threads;
-  int v;  // groups of 8 per thread; 0: the kernel for any dim
+  int v;  // groups of 8 per thread; 0: the kernels for any dim
 };
+constexpr uint32_t kAnyBytes = 200 * 1024;  // a row of FP32 in shared memory
 
 template <int DTYPE, int FMT>
 cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
@@ -575,8 +752,20 @@ cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
     case 1: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 1>, grid, dim3(s.threads), 0, stream, p);
     case 2: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 2>, grid, dim3(s.threads), 0, stream, p);
     case 4: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 4>, grid, dim3(s.threads), 0, stream, p);
-    default: return launch_pdl(rmsnorm_any_kernel<DTYPE, FMT>, grid, dim3(256), 0, stream, p);
+    default: break;
   }
+  const uint32_t smem = (p.kblocks + 3) / 4 * 512;
+  if (smem > kAnyBytes) return launch_pdl(rmsnorm_long_kernel<DTYPE, FMT>, grid, dim3(1024), 0, stream, p);
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(rmsnorm_any_kernel<DTYPE, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAnyBytes);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  return launch_pdl(rmsnorm_any_kernel<DTYPE, FMT>, grid, dim3(256), smem, stream, p);
 }
 
 template <int DTYPE>
@@ -605,6 +794,33 @@ cudaError_t launch_ring(const NormBackParams& p, uint32_t threads, uint32_t grid
     if (dev >= 0 && dev < 64) attr_set[dev] = true;
   }
   return launch_pdl(rmsnorm_backward_kernel<DTYPE, V, NS>, dim3(grid), dim3(threads), smem, stream, p);
+}
+
+template <int DTYPE, int V, int NS>
+cudaError_t launch_any(const NormBackParams& p, uint32_t smem, int sms, uint32_t* parts, cudaStream_t stream) {
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(rmsnorm_backward_any_kernel<DTYPE, V, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  uint32_t grid = (smem <= 112 * 1024 ? 2u : 1u) * (uint32_t)sms;
+  if (grid > (uint32_t)kNormPartials) grid = (uint32_t)kNormPartials;
+  *parts = p.rows < grid ? p.rows : grid;
+  return launch_pdl(rmsnorm_backward_any_kernel<DTYPE, V, NS>, dim3(*parts), dim3(512), smem, stream, p);
+}
+// Rows of any length up to 8192, three of them in the ring (two where three do not fit).
+template <int DTYPE>
+cudaError_t launch_backward_any(const NormBackParams& p, int sms, uint32_t* parts, cudaStream_t stream) {
+  const uint32_t stage = 3 * any_slot<DTYPE>(p.dim);
+  if (3 * stage > 220 * 1024) return launch_any<DTYPE, 16, 2>(p, 2 * stage, sms, parts, stream);
+  if (p.dim <= 1024) return launch_any<DTYPE, 2, 3>(p, 3 * stage, sms, parts, stream);
+  if (p.dim <= 2048) return launch_any<DTYPE, 4, 3>(p, 3 * stage, sms, parts, stream);
+  if (p.dim <= 4096) return launch_any<DTYPE, 8, 3>(p, 3 * stage, sms, parts, stream);
+  return launch_any<DTYPE, 16, 3>(p, 3 * stage, sms, parts, stream);
 }
 
 // Writes *parts rows of partial sums.
@@ -666,9 +882,13 @@ cudaError_t launch_rmsnorm_backward(const RmsnormBackwardArgs& a) {
   p.eps = a.eps; p.inv_dim = 1.0f / (float)a.dim; p.row_chunk = 0;
   uint32_t parts;
   cudaError_t e;
-  if (a.dim % 8 == 0 && a.dim <= 8192) {
-    e = a.dtype == MX_BF16 ? launch_backward<MX_BF16>(p, a.sm_count, &parts, a.stream)
-                           : launch_backward<MX_F32>(p, a.sm_count, &parts, a.stream);
+  if (a.dim <= 8192) {
+    if (a.dim % 8 == 0)
+      e = a.dtype == MX_BF16 ? launch_backward<MX_BF16>(p, a.sm_count, &parts, a.stream)
+                             : launch_backward<MX_F32>(p, a.sm_count, &parts, a.stream);
+    else
+      e = a.dtype == MX_BF16 ? launch_backward_any<MX_BF16>(p, a.sm_count, &parts, a.stream)
+                             : launch_backward_any<MX_F32>(p, a.sm_count, &parts, a.stream);
   } else {
     e = a.dtype == MX_BF16 ? launch_pdl(rmsnorm_row_sums_kernel<MX_BF16>, dim3(p.rows), dim3(256), 0, a.stream, p)
                            : launch_pdl(rmsnorm_row_sums_kernel<MX_F32>, dim3(p.rows), dim3(256), 0, a.stream, p);

@@ -40,7 +40,7 @@ def _norm64(h, w):
 @pytest.mark.parametrize("layout", [mx.MX_SCALES_SWIZZLED, mx.MX_SCALES_LINEAR])
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("rows,dim", [(1, 32), (3, 64), (1, 1), (5, 31), (7, 1000), (130, 4096), (129, 160), (2, 8192), (200, 1001),
-                                      (300, 16384), (3, 20000), (257, 8)])
+                                      (300, 16384), (3, 20000), (257, 8), (2, 60001), (310, 4001)])
 def test_mx_output_is_the_quantized_norm(rows, dim, fmt, layout):
     x, r, w = _inputs(rows, dim, 1)
     for residual in (None, r):
@@ -112,7 +112,7 @@ def _backward64(dy, h, w, dres):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,dim", [(1, 1), (1, 32), (4, 7), (300, 8), (1023, 1000), (130, 1001), (297, 4096), (64, 8192), (40, 8200), (700, 513)])
+@pytest.mark.parametrize("rows,dim", [(1, 1), (1, 32), (4, 7), (300, 8), (1023, 1000), (130, 1001), (297, 4096), (64, 8192), (40, 8200), (700, 513), (600, 4001), (300, 8191), (5, 9000)])
 def test_backward_against_the_formula(rows, dim, dtype):
     h, r, w = _inputs(rows, dim, 4, dtype)
     g = torch.Generator(device="cuda").manual_seed(5)
