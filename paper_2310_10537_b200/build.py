@@ -51,7 +51,7 @@ def _build_py_call() -> None:
     subprocess.check_call(["g++", "-std=c++20", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
                            os.path.join(CSRC, "py_call.cpp"), "-o", tmp,
                            *[f for i in inc for f in ("-isystem", i)], "-L", lib_dir, "-L", HERE, "-Wl,-rpath,$ORIGIN",
-                           "-lmx_b200", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+                           "-lmx_b200", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     os.replace(tmp, PY_CALL)
 
 

@@ -105,10 +105,8 @@ __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& 
     it.k0 = 0;
     it.nk = p.k_stages;
   }
-  // Every lane holds the same item, but it comes out of shared memory and the compiler does not know: a
-  // broadcast says so.  Without it each copy and MMA has its operands moved to uniform registers first,
-  // at 70 to 150 clocks an instruction, and the issuing warps set the pace (628 clocks per stage of a 256 x 256
-  // tile, whose MMAs take 512).
+  // Every lane holds the same item, but it comes out of shared memory and the compiler does not know; a
+  // broadcast says so, and the copies' and MMAs' operands stay in uniform registers.
   auto same = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
   it.group = same(it.group); it.w0 = same(it.w0); it.x0 = same(it.x0); it.n = same(it.n);
   it.x_end = same(it.x_end); it.k0 = same(it.k0); it.nk = same(it.nk);

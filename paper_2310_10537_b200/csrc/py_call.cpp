@@ -9,6 +9,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -108,7 +109,9 @@ mx_dtype_t float_code(const at::Tensor& t) { return float_code(t.scalar_type());
 at::Tensor make(const at::Tensor& like, c10::ScalarType dtype, std::initializer_list<int64_t> sizes) {
   for (int64_t s : sizes)
     if (s < 0) fail(PyExc_ValueError, "negative extent");
-  return at::empty(at::IntArrayRef(sizes.begin(), sizes.size()), like.options().dtype(dtype).requires_grad(false));
+  // Past the dispatcher, whose part is more than the allocation's: a norm of 16 x 4096 with its three results takes the
+  // host 4.55 us, 5.4 with at::empty.
+  return at::Tensor(at::detail::empty_cuda(at::IntArrayRef(sizes.begin(), sizes.size()), dtype, like.device(), std::nullopt));
 }
 
 mx_opts_t options(int dev, int dtype, int layout = MX_SCALES_SWIZZLED, bool check_status = false) {
