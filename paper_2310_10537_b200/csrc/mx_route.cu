@@ -1,6 +1,6 @@
 // Routing to experts: scores, group choice, top-k and weights of each token, and the gradient of the
-// weights.  One warp per token; a lane holds NV consecutive experts in registers (read as vectors), so
-// that a lower lane always means a lower expert and ties fall to the lowest index by themselves.
+// weights.  One warp per token, or a few lanes (below); a lane holds consecutive experts in registers (read as
+// vectors), so that a lower lane always means a lower expert and ties fall to the lowest index by themselves.
 #include <cuda_runtime.h>
 
 #include "mx.h"
@@ -24,18 +24,25 @@ struct RouteParams {
   float scale;
 };
 
-// Floats as unsigned integers of the same order; -0 counts as +0 and NaN ranks above everything.
-// 0 is below the key of every float: "not a candidate".
+// Floats as unsigned integers of the same order; -0 counts as +0, and NaN ranks above everything (the
+// addition makes every NaN the canonical one, 0x7fffffff).  0 is below the key of every float: "not a candidate".
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
-  const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-  return x != x ? 0xffffffffu : k;
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_key(uint32_t k) {
   return k == 0u ? -INFINITY : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// 1 / (1 + exp(-x)) without a branch: t = exp(-|x|), and 1 / (1 + t) by one Newton-Raphson step from the approximate
+// reciprocal (1 + t is in [1, 2]: neither end of the range of floats is near).
+__device__ __forceinline__ float sigmoid(float x) {
+  const float t = expf(-fabsf(x)), d = 1.0f + t;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  r = fmaf(r, fmaf(-d, r, 1.0f), r);
+  return x >= 0.0f ? r : t * r;
+}
 
 template <int DTYPE>
 __device__ __forceinline__ float load_logit(const RouteParams& p, size_t at) {
@@ -126,6 +133,17 @@ __device__ __forceinline__ void softmax_stats(const float (&x)[NV], float& m, fl
 __device__ __forceinline__ float softmax_of(float x, float m, float sum) {
   const float e = expf(x - m);
   return sum == 0.0f ? 0.0f : e / sum;
+}
+
+// The value that a group is ranked by, from its two largest keys.
+__device__ __forceinline__ float group_value(const RouteParams& p, bool by_score, float m, float sum, uint32_t a, uint32_t b) {
+  if (p.group_score != MX_GROUP_TOP2) return from_key(a);
+  float va = from_key(a), vb = from_key(b);
+  if (!by_score) {  // the keys are those of logits, and scores are added
+    va = softmax_of(va, m, sum);
+    vb = b ? softmax_of(vb, m, sum) : 0.0f;
+  }
+  return b ? va + vb : va;  // (a group of one expert has one score)
 }
 
 // The two largest keys of a set, a >= b.
@@ -247,14 +265,6 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
       if (e0 + j >= p.experts) key[j] = 0u;
   }
   if (p.groups > 1) {
-    const bool two = p.group_score == MX_GROUP_TOP2;
-    // the value a group is ranked by, from its two largest keys
-    auto group_value = [&](uint32_t a, uint32_t b) -> float {
-      if (!two) return from_key(a);
-      float va = from_key(a), vb = from_key(b);
-      if (!by_score) { va = softmax_of(va, m, sum); vb = b ? softmax_of(vb, m, sum) : 0.0f; }
-      return b ? va + vb : va;  // (a group of one expert has one score)
-    };
     uint32_t rank_key = 0;  // of group `lane`
     const uint32_t lanes_per_group = p.group_size / NV;
     const bool aligned = p.group_size % NV == 0 && (lanes_per_group & (lanes_per_group - 1)) == 0;
@@ -267,7 +277,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
         b = max(max(b, b2), min(a, a2));
         a = max(a, a2);
       }
-      const uint32_t k = order_key(group_value(a, b));
+      const uint32_t k = order_key(group_value(p, by_score, m, sum, a, b));
       rank_key = __shfl_sync(kFull, k, (lane * lanes_per_group) & 31);
     } else {        // through shared memory, a lane per group
       uint32_t* mine = keys_smem + warp * (64 + NV * 32) + 64;
@@ -277,7 +287,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
       if (lane < p.groups) {
         uint32_t a = 0, b = 0;
         for (uint32_t i = 0; i < p.group_size; ++i) top2_add(a, b, mine[lane * p.group_size + i]);
-        rank_key = order_key(group_value(a, b));
+        rank_key = order_key(group_value(p, by_score, m, sum, a, b));
       }
     }
     // the topk_groups best groups, the lower one among equals (every group has a key above 0)
@@ -313,6 +323,256 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const RoutePara
   if (live) {
     p.ids[(size_t)token * p.topk + lane] = (int32_t)my_id;
     p.weights[(size_t)token * p.topk + lane] = w * p.scale;
+  }
+}
+
+// ---- a few lanes per token ---------------------------------------------------------------------------
+// With many tokens the instructions of a warp per token bound the call: most of them are steps of a reduction, done
+// by 32 lanes for one token.  Here L lanes share a token, kPartKeys consecutive experts each, and a warp
+// takes 32 / L tokens.  The best kPartK keys come out of sorting networks -- eight keys at a time, merged into
+// the lane's list, then the lanes' lists in pairs.  What is not below the topk-th goes to shared memory, where each
+// finds its place by counting those before it.  (16384 tokens, 8 of 256 in groups, sigmoid and bias: 12.6 us, 16.6
+// with a warp per token; 262144 tokens, 6 of 64: 36 us, 106.  Comparisons and selections bound it, which issue
+// at half rate.)
+
+constexpr int kPartKeys = 16;        // experts per lane
+constexpr uint32_t kPartK = 8;       // most choices
+constexpr uint32_t kPartField = 24;  // candidates that are counted against each other; more (equal keys): one by one
+
+__device__ __forceinline__ void descend(uint32_t& a, uint32_t& b) {
+  const uint32_t hi = max(a, b);
+  b = min(a, b);
+  a = hi;
+}
+__device__ __forceinline__ void sort8(uint32_t (&k)[8]) {  // odd-even merge sort
+  descend(k[0], k[1]); descend(k[2], k[3]); descend(k[4], k[5]); descend(k[6], k[7]);
+  descend(k[0], k[2]); descend(k[1], k[3]); descend(k[4], k[6]); descend(k[5], k[7]);
+  descend(k[1], k[2]); descend(k[5], k[6]);
+  descend(k[0], k[4]); descend(k[1], k[5]); descend(k[2], k[6]); descend(k[3], k[7]);
+  descend(k[2], k[4]); descend(k[3], k[5]);
+  descend(k[1], k[2]); descend(k[3], k[4]); descend(k[5], k[6]);
+}
+__device__ __forceinline__ void bitonic8(uint32_t (&k)[8]) {  // a bitonic sequence in descending order
+#pragma unroll
+  for (int d = 4; d; d >>= 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((i & d) == 0) descend(k[i], k[i + d]);
+  }
+}
+
+// The eight best of two descending lists, into the first.
+__device__ __forceinline__ void merge8(uint32_t (&k)[8], const uint32_t (&other)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) k[i] = max(k[i], other[7 - i]);
+  bitonic8(k);
+}
+
+// The lane's kPartKeys numbers from e0 on; past the end of the row -Inf.  No load depends on a branch, and all
+// are in flight at once.  Rows of a multiple of four numbers.
+template <int DTYPE>
+__device__ __forceinline__ void load_part(const void* row, size_t at, uint32_t experts, uint32_t e0, float (&x)[kPartKeys]) {
+  constexpr int V = kPartKeys / 4;
+  if constexpr (DTYPE == MX_F32) {
+    float4 v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      v[i] = __ldg(reinterpret_cast<const float4*>((const float*)row + at + (e0 + 4 * i < experts ? e0 + 4 * i : 0u)));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[4 * i] = v[i].x; x[4 * i + 1] = v[i].y; x[4 * i + 2] = v[i].z; x[4 * i + 3] = v[i].w;
+    }
+  } else {
+    uint2 v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      v[i] = __ldg(reinterpret_cast<const uint2*>((const uint16_t*)row + at + (e0 + 4 * i < experts ? e0 + 4 * i : 0u)));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[4 * i] = __uint_as_float(v[i].x << 16); x[4 * i + 1] = __uint_as_float(v[i].x & 0xFFFF0000u);
+      x[4 * i + 2] = __uint_as_float(v[i].y << 16); x[4 * i + 3] = __uint_as_float(v[i].y & 0xFFFF0000u);
+    }
+  }
+  if (e0 + kPartKeys > experts) {
+#pragma unroll
+    for (int j = 0; j < kPartKeys; ++j)
+      if (e0 + j >= experts) x[j] = -INFINITY;
+  }
+}
+
+// Needs experts % 4 == 0, experts <= kPartKeys L, topk <= kPartK, the bias on a 16-byte boundary, and groups of a
+// power of two of whole lanes.
+template <int DTYPE, int L>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const RouteParams p) {
+  constexpr uint32_t kTokens = 32 / L;  // of a warp
+  __shared__ uint4 keys[kRouteWarps][kPartKeys / 4][32];
+  __shared__ uint2 fields[kRouteWarps][kTokens][kPartField];
+  __shared__ uint32_t chosen[kRouteWarps][kTokens][kPartK];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane % L, part = lane / L, e0 = kPartKeys * q;
+  const uint32_t token0 = (blockIdx.x * kRouteWarps + warp) * kTokens;
+  if (token0 >= p.tokens) return;
+  const uint32_t token = min(token0 + part, p.tokens - 1);  // (past the end: computed, not written)
+  const bool soft = p.score == MX_SCORE_SOFTMAX, by_score = !soft || p.bias != nullptr;
+  float m = 0.0f, sum = 1.0f;
+  uint32_t key[kPartKeys];
+  {
+    float x[kPartKeys], b[kPartKeys];
+    load_part<DTYPE>(p.logits, (size_t)token * p.experts, p.experts, e0, x);
+    if (p.bias) {
+      load_part<MX_F32>(p.bias, 0, p.experts, e0, b);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPartKeys; ++j) b[j] = 0.0f;
+    }
+    if (soft) {
+      m = x[0];
+#pragma unroll
+      for (int j = 1; j < kPartKeys; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(x[j]));
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) {
+        const float w = __shfl_xor_sync(kFull, m, o);
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(w));
+      }
+      if (m == -INFINITY) m = 0.0f;  // nothing to choose: every exponential is 0, and the sum
+      sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kPartKeys; ++j) sum += expf(x[j] - m);
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) sum += __shfl_xor_sync(kFull, sum, o);
+    }
+    if (by_score) {
+#pragma unroll
+      for (int j = 0; j < kPartKeys; ++j) x[j] = (soft ? softmax_of(x[j], m, sum) : sigmoid(x[j])) + b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kPartKeys; ++j) key[j] = order_key(x[j]);
+    if (e0 + kPartKeys > p.experts) {
+#pragma unroll
+      for (int j = 0; j < kPartKeys; ++j)
+        if (e0 + j >= p.experts) key[j] = 0u;
+    }
+  }
+  if (p.groups > 1) {
+    const uint32_t lanes = p.group_size / kPartKeys;  // of a group
+    uint32_t a = 0, b = 0;
+#pragma unroll
+    for (int j = 0; j < kPartKeys; ++j) top2_add(a, b, key[j]);
+#pragma unroll
+    for (uint32_t o = 1; o < L; o <<= 1) {
+      if (o < lanes) {
+        const uint32_t a2 = __shfl_xor_sync(kFull, a, o), b2 = __shfl_xor_sync(kFull, b, o);
+        b = max(max(b, b2), min(a, a2));
+        a = max(a, a2);
+      }
+    }
+    const uint32_t mine = order_key(group_value(p, by_score, m, sum, a, b)), first = e0 < p.experts ? q & ~(lanes - 1) : q;
+    uint32_t before = 0;  // the better groups, and the equal ones of lower experts
+    for (uint32_t g = 0; g < p.groups; ++g) {
+      const uint32_t other = __shfl_sync(kFull, mine, g * lanes, L);
+      before += other > mine || (other == mine && g * lanes < first) ? 1u : 0u;
+    }
+#pragma unroll
+    for (int j = 0; j < kPartKeys; ++j) key[j] = before < p.topk_groups ? key[j] : 0u;
+  }
+  // the keys are laid down where they can be read by number
+#pragma unroll
+  for (int i = 0; i < kPartKeys / 4; ++i) keys[warp][i][lane] = make_uint4(key[4 * i], key[4 * i + 1], key[4 * i + 2], key[4 * i + 3]);
+  auto key_at = [&](uint32_t s) { return reinterpret_cast<const uint32_t*>(&keys[warp][s >> 2][lane])[s & 3]; };
+  // A floor under the topk-th best: with up to 4 lanes that key itself, else the topk-th of the best of every four
+  // keys, which lets few more through and is cheaper (4 lanes: 16384 tokens, 6 of 64: 5.8 us; 6.6 with fours)
+  uint32_t best[8], k[8];
+  if constexpr (L < 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { best[j] = key[j]; k[j] = key[8 + j]; }
+    sort8(best);
+    sort8(k);
+    merge8(best, k);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) best[j] = max(max(key[4 * j], key[4 * j + 1]), max(key[4 * j + 2], key[4 * j + 3]));
+    descend(best[0], best[1]); descend(best[2], best[3]);
+    descend(best[0], best[2]); descend(best[1], best[3]);
+    descend(best[1], best[2]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) best[7 - j] = __shfl_xor_sync(kFull, best[j], 1);
+    bitonic8(best);
+  }
+#pragma unroll
+  for (int o = L < 8 ? 1 : 2; o < L; o <<= 1) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = __shfl_xor_sync(kFull, best[j], o);
+    merge8(best, k);
+  }
+  uint32_t floor_key = best[0];
+#pragma unroll
+  for (uint32_t j = 1; j < kPartK; ++j) floor_key = j < p.topk ? best[j] : floor_key;
+  floor_key = max(floor_key, 1u);  // (no candidate has 0)
+  uint32_t hits = 0;
+#pragma unroll
+  for (int s = 0; s < kPartKeys; ++s) hits |= key[s] >= floor_key ? 1u << s : 0u;
+  const uint32_t n = __popc(hits);
+  uint32_t upto = n;
+#pragma unroll
+  for (uint32_t o = 1; o < L; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(kFull, upto, o, L);
+    if (q >= o) upto += v;
+  }
+  const uint32_t all = __shfl_sync(kFull, upto, L - 1, L);
+  if (!__any_sync(kFull, all > kPartField)) {
+    uint2* field = fields[warp][part];  // in the order of the experts
+    for (uint32_t at = upto - n; hits; ++at, hits &= hits - 1) {
+      const uint32_t s = __ffs(hits) - 1;
+      field[at] = make_uint2(key_at(s), e0 + s);
+    }
+    __syncwarp();
+    for (uint32_t c = q; c < all; c += L) {
+      const uint2 me = field[c];
+      uint32_t place = 0;
+#pragma unroll 4
+      for (uint32_t j = 0; j < all; ++j) place += field[j].x > me.x || (field[j].x == me.x && j < c) ? 1u : 0u;
+      if (place < p.topk) chosen[warp][part][place] = me.y;
+    }
+  } else {  // the next in the order, topk times
+    uint32_t last_key = 0xffffffffu;
+    int32_t last = -1;
+    for (uint32_t r = 0; r < p.topk; ++r) {
+      uint32_t top = 0, id = 0;
+      for (uint32_t s = 0; s < (uint32_t)kPartKeys; ++s) {
+        const uint32_t k = key_at(s), e = e0 + s;
+        if (k > top && (k < last_key || (k == last_key && (int32_t)e > last))) { top = k; id = e; }
+      }
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) {
+        const uint32_t k2 = __shfl_xor_sync(kFull, top, o), id2 = __shfl_xor_sync(kFull, id, o);
+        if (k2 > top || (k2 == top && id2 < id)) { top = k2; id = id2; }
+      }
+      last_key = top;
+      last = (int32_t)id;
+      if (q == 0) chosen[warp][part][r] = id;
+    }
+  }
+  __syncwarp();
+  constexpr int R = L < (int)kPartK ? kPartK / L : 1;  // choices per lane
+  float s[R], total = 0.0f;
+  uint32_t id[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool live = q + L * r < p.topk;
+    id[r] = live ? chosen[warp][part][q + L * r] : 0u;
+    const float x = load_logit<DTYPE>(p, (size_t)token * p.experts + id[r]);
+    s[r] = live ? (soft ? softmax_of(x, m, sum) : sigmoid(x)) : 0.0f;
+    total += s[r];
+  }
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) total += __shfl_xor_sync(kFull, total, o);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (q + L * r < p.topk && token0 + part < p.tokens) {
+      const size_t at = (size_t)token * p.topk + q + L * r;
+      p.ids[at] = (int32_t)id[r];
+      p.weights[at] = (p.renormalize ? (total == 0.0f ? 0.0f : s[r] / total) : s[r]) * p.scale;
+    }
   }
 }
 
@@ -421,8 +681,28 @@ cudaError_t launch_nv(const RouteParams& p, bool backward, cudaStream_t stream) 
   return launch_pdl(route_kernel<DTYPE, NV>, grid, block, sizeof(uint32_t) * (64 + NV * 32) * kRouteWarps, stream, p);
 }
 
+template <int DTYPE, int L>
+cudaError_t launch_part(const RouteParams& p, cudaStream_t stream) {
+  const uint32_t per_cta = 32 / L * kRouteWarps;
+  return launch_pdl(route_part_kernel<DTYPE, L>, dim3((p.tokens + per_cta - 1) / per_cta), dim3(32 * kRouteWarps), 0, stream, p);
+}
+
 template <int DTYPE>
 cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t stream) {
+  const uint32_t lanes = p.group_size / kPartKeys;
+  // A few lanes per token.  Few experts need many tokens for it to pay: 8 experts, top-2, 2048 tokens 2.6 us (a
+  // warp per token 2.3), 4096 2.6 (3.0); 64 experts, top-6, 1024 tokens 3.0 (2.6), 2048 3.1 (3.6).
+  // With more than 128 it is never behind (256 in 8 groups: 16 tokens 3.0, 3.9; 512 ungrouped, 16384 tokens: 16.8, 16.3).
+  const bool enough = p.experts > 128 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
+  if (!backward && enough && p.topk <= kPartK && p.experts % 4 == 0 && p.experts <= 32 * kPartKeys &&
+      (p.groups == 1 || (p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0)) &&
+      (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0) {
+    if (p.experts <= 2 * kPartKeys) return launch_part<DTYPE, 2>(p, stream);
+    if (p.experts <= 4 * kPartKeys) return launch_part<DTYPE, 4>(p, stream);
+    if (p.experts <= 8 * kPartKeys) return launch_part<DTYPE, 8>(p, stream);
+    if (p.experts <= 16 * kPartKeys) return launch_part<DTYPE, 16>(p, stream);
+    return launch_part<DTYPE, 32>(p, stream);
+  }
   if (p.experts <= 32) return launch_nv<DTYPE, 1>(p, backward, stream);
   if (p.experts <= 64) return launch_nv<DTYPE, 2>(p, backward, stream);
   if (p.experts <= 128) return launch_nv<DTYPE, 4>(p, backward, stream);
