@@ -368,16 +368,18 @@ __device__ __forceinline__ void merge8(uint32_t (&k)[8], const uint32_t (&other)
   bitonic8(k);
 }
 
-// The lane's kPartKeys numbers from e0 on; past the end of the row -Inf.  No load depends on a branch, and all
-// are in flight at once.  Rows of a multiple of four numbers.
-template <int DTYPE>
+// The lane's kPartKeys numbers, in fours: number e0 and the next three, then those `step` fours further on; past the
+// end of the row -Inf.  No load depends on a branch, and all are in flight at once.  Rows of a multiple of four numbers.
+template <int DTYPE, int step = 1>
 __device__ __forceinline__ void load_part(const void* row, size_t at, uint32_t experts, uint32_t e0, float (&x)[kPartKeys]) {
   constexpr int V = kPartKeys / 4;
   if constexpr (DTYPE == MX_F32) {
     float4 v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      v[i] = __ldg(reinterpret_cast<const float4*>((const float*)row + at + (e0 + 4 * i < experts ? e0 + 4 * i : 0u)));
+    for (int i = 0; i < V; ++i) {
+      const uint32_t e = e0 + 4 * step * i;
+      v[i] = __ldg(reinterpret_cast<const float4*>((const float*)row + at + (e < experts ? e : 0u)));
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       x[4 * i] = v[i].x; x[4 * i + 1] = v[i].y; x[4 * i + 2] = v[i].z; x[4 * i + 3] = v[i].w;
@@ -385,19 +387,44 @@ __device__ __forceinline__ void load_part(const void* row, size_t at, uint32_t e
   } else {
     uint2 v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      v[i] = __ldg(reinterpret_cast<const uint2*>((const uint16_t*)row + at + (e0 + 4 * i < experts ? e0 + 4 * i : 0u)));
+    for (int i = 0; i < V; ++i) {
+      const uint32_t e = e0 + 4 * step * i;
+      v[i] = __ldg(reinterpret_cast<const uint2*>((const uint16_t*)row + at + (e < experts ? e : 0u)));
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       x[4 * i] = __uint_as_float(v[i].x << 16); x[4 * i + 1] = __uint_as_float(v[i].x & 0xFFFF0000u);
       x[4 * i + 2] = __uint_as_float(v[i].y << 16); x[4 * i + 3] = __uint_as_float(v[i].y & 0xFFFF0000u);
     }
   }
-  if (e0 + kPartKeys > experts) {
+  if (e0 + 4 * step * (V - 1) >= experts) {
 #pragma unroll
     for (int j = 0; j < kPartKeys; ++j)
-      if (e0 + j >= experts) x[j] = -INFINITY;
+      if (e0 + 4 * step * (j / 4) >= experts) x[j] = -INFINITY;
   }
+}
+
+// Maximum and sum of exponentials of a token's logits; `keep`: x becomes the exponentials.
+template <int L>
+__device__ __forceinline__ void part_softmax(float (&x)[kPartKeys], float& m, float& sum, bool keep) {
+  m = x[0];
+#pragma unroll
+  for (int j = 1; j < kPartKeys; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(x[j]));
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) {
+    const float w = __shfl_xor_sync(kFull, m, o);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(w));
+  }
+  if (m == -INFINITY) m = 0.0f;  // nothing to choose: every exponential is 0, and the sum
+  sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kPartKeys; ++j) {
+    const float e = expf(x[j] - m);
+    sum += e;
+    if (keep) x[j] = e;
+  }
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) sum += __shfl_xor_sync(kFull, sum, o);
 }
 
 // Needs experts % 4 == 0, experts <= kPartKeys L, topk <= kPartK, the bias on a 16-byte boundary, and groups of a
@@ -425,22 +452,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const Rout
 #pragma unroll
       for (int j = 0; j < kPartKeys; ++j) b[j] = 0.0f;
     }
-    if (soft) {
-      m = x[0];
-#pragma unroll
-      for (int j = 1; j < kPartKeys; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(x[j]));
-#pragma unroll
-      for (int o = 1; o < L; o <<= 1) {
-        const float w = __shfl_xor_sync(kFull, m, o);
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(w));
-      }
-      if (m == -INFINITY) m = 0.0f;  // nothing to choose: every exponential is 0, and the sum
-      sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < kPartKeys; ++j) sum += expf(x[j] - m);
-#pragma unroll
-      for (int o = 1; o < L; o <<= 1) sum += __shfl_xor_sync(kFull, sum, o);
-    }
+    if (soft) part_softmax<L>(x, m, sum, false);
     if (by_score) {
 #pragma unroll
       for (int j = 0; j < kPartKeys; ++j) x[j] = (soft ? softmax_of(x[j], m, sum) : sigmoid(x[j])) + b[j];
@@ -662,6 +674,99 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_kernel(const 
   }
 }
 
+// The same with L lanes per token and up to kPartKeys L experts, for the reason given above route_part_kernel: the
+// reductions of a warp per token.  Order does not matter here, and a lane holds every L-th four experts, so that
+// the lanes' vectors meet in whole sectors.  Needs experts % 4 == 0 and topk <= kPartK.
+template <int DTYPE, int L>
+__global__ void __launch_bounds__(32 * kRouteWarps) route_backward_part_kernel(const RouteParams p) {
+  constexpr uint32_t kTokens = 32 / L;
+  constexpr int V = kPartKeys / 4;
+  __shared__ float4 ds_of[kRouteWarps][V][32];
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane % L, part = lane / L;
+  const uint32_t token0 = (blockIdx.x * kRouteWarps + warp) * kTokens;
+  if (token0 >= p.tokens) return;
+  const bool live = token0 + part < p.tokens;
+  const size_t token = min(token0 + part, p.tokens - 1), row = token * p.experts;
+  const bool soft = p.score == MX_SCORE_SOFTMAX;
+  constexpr int R = L < (int)kPartK ? kPartK / L : 1;  // choices per lane
+  int32_t id[R];
+  float d[R], xs[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const uint32_t c = q + L * r;
+    id[r] = c < p.topk ? __ldg(p.ids + token * p.topk + c) : -1;
+    d[r] = c < p.topk ? __ldg(p.dweights + token * p.topk + c) : 0.0f;
+    if ((uint32_t)id[r] >= p.experts) { id[r] = -1; d[r] = 0.0f; }
+    xs[r] = load_logit<DTYPE>(p, row + (id[r] < 0 ? 0u : (uint32_t)id[r]));
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) ds_of[warp][i][lane] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float x[kPartKeys];  // (a sigmoid's gradient is that of the chosen logits alone)
+  float m = 0.0f, sum = 1.0f;
+  if (soft) {
+    load_part<DTYPE, L>(p.logits, row, p.experts, 4 * q, x);
+    part_softmax<L>(x, m, sum, true);
+  }
+  float s[R], ds[R], total = 0.0f, dot = 0.0f, inner = 0.0f;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    s[r] = id[r] < 0 ? 0.0f : soft ? softmax_of(xs[r], m, sum) : sigmoid(xs[r]);
+    total += s[r];
+    dot += d[r] * s[r];
+  }
+  if (p.renormalize) {
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+      total += __shfl_xor_sync(kFull, total, o);
+      dot += __shfl_xor_sync(kFull, dot, o);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    ds[r] = p.scale * d[r];
+    if (p.renormalize) ds[r] = total == 0.0f || id[r] < 0 ? 0.0f : p.scale * (d[r] - dot / total) / total;
+    inner += ds[r] * s[r];
+    if (!soft && ds[r] != 0.0f) {
+      const float t = expf(-fabsf(xs[r]));  // s (1 - s) without the difference: t / (1 + t)^2
+      ds[r] *= t / ((1.0f + t) * (1.0f + t));
+    }
+  }
+  if (soft) {
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) inner += __shfl_xor_sync(kFull, inner, o);
+  }
+  __syncwarp();
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (id[r] >= 0) {
+      const uint32_t unit = (uint32_t)id[r] >> 2;
+      atomicAdd(reinterpret_cast<float*>(&ds_of[warp][unit / L][part * L + unit % L]) + (id[r] & 3), ds[r]);
+    }
+  }
+  __syncwarp();
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const float4 v = ds_of[warp][i][lane];
+    float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (soft) o[j] = x[4 * i + j] * inv * (o[j] - inner);
+    const uint32_t e0 = 4 * (L * i + q);
+    if (live && e0 < p.experts) {
+      if constexpr (DTYPE == MX_F32) {
+        *reinterpret_cast<float4*>((float*)p.dlogits + row + e0) = make_float4(o[0], o[1], o[2], o[3]);
+      } else {
+        uint2 w;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(o[1]), "f"(o[0]));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(o[3]), "f"(o[2]));
+        *reinterpret_cast<uint2*>((uint16_t*)p.dlogits + row + e0) = w;
+      }
+    }
+  }
+}
+
 RouteParams route_params(const RouteArgs& a) {
   RouteParams p;
   p.logits = a.logits; p.bias = a.bias; p.dweights = a.dweights; p.ids = a.ids; p.weights = a.weights;
@@ -682,9 +787,10 @@ cudaError_t launch_nv(const RouteParams& p, bool backward, cudaStream_t stream) 
 }
 
 template <int DTYPE, int L>
-cudaError_t launch_part(const RouteParams& p, cudaStream_t stream) {
+cudaError_t launch_part(const RouteParams& p, bool backward, cudaStream_t stream) {
   const uint32_t per_cta = 32 / L * kRouteWarps;
-  return launch_pdl(route_part_kernel<DTYPE, L>, dim3((p.tokens + per_cta - 1) / per_cta), dim3(32 * kRouteWarps), 0, stream, p);
+  return launch_pdl(backward ? route_backward_part_kernel<DTYPE, L> : route_part_kernel<DTYPE, L>,
+                    dim3((p.tokens + per_cta - 1) / per_cta), dim3(32 * kRouteWarps), 0, stream, p);
 }
 
 template <int DTYPE>
@@ -693,15 +799,17 @@ cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t strea
   // A few lanes per token.  Few experts need many tokens for it to pay: 8 experts, top-2, 2048 tokens 2.6 us (a
   // warp per token 2.3), 4096 2.6 (3.0); 64 experts, top-6, 1024 tokens 3.0 (2.6), 2048 3.1 (3.6).
   // With more than 128 it is never behind (256 in 8 groups: 16 tokens 3.0, 3.9; 512 ungrouped, 16384 tokens: 16.8, 16.3).
-  const bool enough = p.experts > 128 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
-  if (!backward && enough && p.topk <= kPartK && p.experts % 4 == 0 && p.experts <= 32 * kPartKeys &&
-      (p.groups == 1 || (p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0)) &&
-      (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0) {
-    if (p.experts <= 2 * kPartKeys) return launch_part<DTYPE, 2>(p, stream);
-    if (p.experts <= 4 * kPartKeys) return launch_part<DTYPE, 4>(p, stream);
-    if (p.experts <= 8 * kPartKeys) return launch_part<DTYPE, 8>(p, stream);
-    if (p.experts <= 16 * kPartKeys) return launch_part<DTYPE, 16>(p, stream);
-    return launch_part<DTYPE, 32>(p, stream);
+  // Gradient: 64 experts, 16 tokens 2.4 (2.1), 2048 2.5 (2.6); 128 experts 2.1 (2.2), 16384 tokens 4.7 (6.9).
+  const bool enough = backward ? p.experts > 64 || p.tokens >= 2048u
+                               : p.experts > 128 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
+  const bool groups_fit = p.groups == 1 || (p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0);
+  if (enough && p.topk <= kPartK && p.experts % 4 == 0 && p.experts <= 32 * kPartKeys &&
+      (backward || (groups_fit && (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0))) {
+    if (p.experts <= 2 * kPartKeys) return launch_part<DTYPE, 2>(p, backward, stream);
+    if (p.experts <= 4 * kPartKeys) return launch_part<DTYPE, 4>(p, backward, stream);
+    if (p.experts <= 8 * kPartKeys) return launch_part<DTYPE, 8>(p, backward, stream);
+    if (p.experts <= 16 * kPartKeys) return launch_part<DTYPE, 16>(p, backward, stream);
+    return launch_part<DTYPE, 32>(p, backward, stream);
   }
   if (p.experts <= 32) return launch_nv<DTYPE, 1>(p, backward, stream);
   if (p.experts <= 64) return launch_nv<DTYPE, 2>(p, backward, stream);

@@ -1,6 +1,8 @@
 """Routing of many tokens (a few lanes per token) against the definition in 64 bits, and against calls with few.
 
 Bounds as for few tokens: ids are exact where the choice compares logits, weights are within 64 * 2^-24."""
+import ctypes
+
 import pytest
 import torch
 
@@ -80,3 +82,56 @@ def test_many_tokens_are_routed_like_each_alone():
     for t0 in (0, 1000, 4990):
         i1, w1 = mx.mx_route(x[t0:t0 + 8], 4, SIG, groups=2, topk_groups=1)
         assert torch.equal(ids[t0:t0 + 8], i1) and bool(((w[t0:t0 + 8] - w1).abs() <= 128 * 2.0 ** -24 * w1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score", [SOFT, SIG])
+@pytest.mark.parametrize("T,E,k", [(2049, 4, 2), (2050, 28, 8), (2100, 64, 6), (33, 68, 1), (1, 128, 8), (70, 256, 5), (21, 512, 8)])
+def test_gradient_against_the_formula(T, E, k, score, dtype):
+    x = _logits(T, E, E, dtype, ties=False)
+    for renorm in (True, False):
+        ids, _ = mx.mx_route(x, k, score, renormalize=renorm, scale=2.0)
+        dw = torch.randn(T, k, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+        got = mx.mx_route_backward(dw, x, ids, score, renorm, 2.0)
+        with torch.enable_grad():
+            x64 = x.double().requires_grad_(True)
+            ref = torch.autograd.grad((_weights64(_scores64(x64, score), ids, renorm, 2.0) * dw.double()).sum(), x64)[0]
+        s = _scores64(x, score)
+        big = 4 * dw.double().abs().amax(1, keepdim=True) * (1 / s.gather(1, ids.long()).sum(1, keepdim=True) if renorm else 1.0)
+        half = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+        assert bool(((got.double() - ref).abs() <= 128 * 2.0 ** -24 * big * s + half * ref.abs() + 1e-37).all())
+
+
+@pytest.mark.parametrize("T,E", [(2050, 16), (3, 128)])
+def test_gradient_ignores_ids_outside_and_handles_dead_rows(T, E):
+    x = _logits(T, E, 5, torch.float32)
+    x[2] = -float("inf")
+    ids = torch.zeros(T, 2, dtype=torch.int32, device="cuda")
+    ids[:3] = torch.tensor([[0, -1], [E + 83, 3], [0, 1]])
+    ids[3:, 1] = E - 1
+    dw = torch.ones(T, 2, device="cuda")
+    for score in (SOFT, SIG):
+        got = mx.mx_route_backward(dw, x, ids, score, False, 1.0)
+        s = _scores64(x[:2], score)
+        for t, e in ((0, 0), (1, 3)):
+            ref = -s[t] * s[t, e] if score == SOFT else torch.zeros_like(s[t])
+            ref[e] += s[t, e] if score == SOFT else s[t, e] * (1 - s[t, e])
+            assert torch.allclose(got[t].double(), ref, rtol=1e-5, atol=1e-7)
+        assert bool((mx.mx_route_backward(dw, x, ids, score, True, 1.0)[2] == 0).all())
+
+
+def test_outputs_are_filled_and_nothing_else():
+    T, E, k = 2051, 64, 6
+    x = _logits(T, E, 9, torch.float32)
+    ids, w = mx.mx_route(x, k)
+    d = mx.mx_route_backward(w, x, ids)
+    lib = mx.lib()
+    raw_i = torch.full((T * k + 512,), -7, dtype=torch.int32, device="cuda")
+    raw_w, raw_d = (torch.full((n + 512,), 77.0, device="cuda") for n in (T * k, T * E))
+    route = mx.binding.mx_route_t(k, mx.MX_SCORE_SOFTMAX, 1, 1, mx.MX_GROUP_MAX, 1, 1.0)
+    opts = mx.binding.mx_opts_t(mx.MX_F32, mx.MX_SCALES_SWIZZLED, torch.cuda.current_stream().cuda_stream, 0, 0)
+    assert lib.mx_route(x.data_ptr(), None, T, E, ctypes.byref(route), raw_i[256:].data_ptr(), raw_w[256:].data_ptr(), ctypes.byref(opts)) == 0
+    assert lib.mx_route_backward(w.data_ptr(), x.data_ptr(), ids.data_ptr(), T, E, ctypes.byref(route), raw_d[256:].data_ptr(), ctypes.byref(opts)) == 0
+    for raw, want, n in ((raw_i, ids, T * k), (raw_w, w, T * k), (raw_d, d, T * E)):
+        assert torch.equal(raw[256:256 + n], want.flatten())
+        assert bool((raw[:256] == raw[0]).all()) and bool((raw[256 + n:] == raw[0]).all()) and float(raw[0]) in (-7, 77)
