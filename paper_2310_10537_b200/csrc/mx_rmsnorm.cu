@@ -40,6 +40,15 @@ __device__ __forceinline__ float weight1(const void* w, uint32_t w_bf16, uint32_
   return w_bf16 ? __uint_as_float((uint32_t)__ldg((const uint16_t*)w + c) << 16) : __ldg((const float*)w + c);
 }
 
+// The elements at .. at + 7 of a BF16 tensor of `all` elements; those past its end are zero.
+__device__ __forceinline__ uint4 load_part8(const void* base, size_t at, size_t all) {
+  uint32_t w[4] = {};
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e)
+    if (at + e < all) w[e >> 1] |= (uint32_t)((const uint16_t*)base)[at + e] << (16 * (e & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Sum over the CTA; every thread gets it.  `red` holds a float per warp and is not read again by
 // the caller before its next barrier.
 __device__ __forceinline__ float cta_sum(float v, float* red) {
@@ -183,48 +192,117 @@ __global__ void __launch_bounds__(V == 4 ? 512 : 1024) rmsnorm_kernel(const Norm
   zero_pad_rows(p);
 }
 
-// Any dim that fits shared memory: rows start anywhere, so h is read (once) and stored an element per lane; it waits in
-// shared memory as FP32 and is quantized from there in groups of 8 like the rows above.
-// (8192 x 4001 BF16: 165 us with an element per lane throughout and the row read twice.)
-template <int DTYPE, int FMT>
-__global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
+// Any dim that fits shared memory: rows start anywhere.  h is formed once, stored, and waits in shared memory as FP32,
+// from where it is quantized in groups of 8 like the rows above (both types sum the squares in the same order).  x, residual and h_out lie alike relative to 16 bytes, so BF16 rows move in the
+// aligned vectors that cover them -- only the first and the last of a row go by elements -- and shared memory skips a
+// word after every 8, which keeps both the shifted writes and the groups' reads free of bank conflicts.  FP32 rows move an
+// element per lane, whole sectors (in vectors of 8 the registers leave too few threads: 8192 x 4001 104 us instead of 73).
+// (8192 x 4001 BF16: 69 us; 114 an element per lane, 165 with a second pass over memory.)
+template <int DTYPE> __host__ __device__ constexpr uint32_t any_at(uint32_t c) { return DTYPE == MX_BF16 ? c + (c >> 3) : c; }
+
+template <int DTYPE>
+__device__ __forceinline__ void any_group(const float* h, uint32_t g, float (&v)[8]) {
+  if constexpr (DTYPE == MX_BF16) {
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) v[e] = h[9 * g + e];
+  } else {
+    const float4 a = reinterpret_cast<const float4*>(h)[2 * g], b = reinterpret_cast<const float4*>(h)[2 * g + 1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+
+template <int DTYPE, int FMT, uint32_t T>
+__global__ void __launch_bounds__(T) rmsnorm_any_kernel(const NormParams p) {
   constexpr uint32_t bits = FmtTraits<FMT>::bits;
   extern __shared__ float4 row_smem[];
   __shared__ float red[32];
-  float* h = reinterpret_cast<float*>(row_smem);  // [dim rounded up to 128]
+  float* h = reinterpret_cast<float*>(row_smem);  // element c at any_at(c), up to dim rounded up to 128
   pdl_prologue();
   const uint32_t row = blockIdx.x, groups = (p.kblocks + 3) / 4 * 16;
   const size_t base = (size_t)row * p.dim;
   float ss = 0.0f;
-  for (uint32_t c0 = threadIdx.x; c0 < p.dim; c0 += 8 * 256) {
-    float v[8], r[8];  // (loads first: h_out may be x or residual, so they cannot move past the stores)
+  if constexpr (DTYPE == MX_BF16) {
+    const uint32_t shift = (uint32_t)(base & 7u), vecs = (p.dim + shift + 7) >> 3;
+    const size_t first = base - shift, all = (size_t)p.rows * p.dim;  // element 0 of vector 0; of the tensor
+    constexpr uint32_t U = 4;
+    for (uint32_t j0 = threadIdx.x; j0 < vecs; j0 += U * T) {
+      uint4 v[U], q[U];  // (loads first: h_out may be x or residual)
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-      const uint32_t c = c0 + 256 * k;
-      v[k] = c < p.dim ? load1<DTYPE>(p.x, base + c) : 0.0f;
-      r[k] = c < p.dim && p.residual ? load1<DTYPE>(p.residual, base + c) : 0.0f;
+      for (uint32_t k = 0; k < U; ++k) {
+        const uint32_t j = j0 + T * k;
+        const size_t at = first + 8 * (size_t)j;
+        v[k] = q[k] = make_uint4(0, 0, 0, 0);
+        if (j < vecs && at + 8 <= all) {
+          v[k] = ld_16((const uint16_t*)p.x + at);
+          if (p.residual) q[k] = ld_16((const uint16_t*)p.residual + at);
+        } else if (j < vecs) {  // the last row's end
+          v[k] = load_part8(p.x, at, all);
+          if (p.residual) q[k] = load_part8(p.residual, at, all);
+        }
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < U; ++k) {
+        const uint32_t j = j0 + T * k;
+        if (j >= vecs) break;
+        float f[8], g[8];
+        widen4(v[k], f);
+        if (p.residual) {
+          widen4(q[k], g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] += g[e];
+        }
+        const uint32_t c0 = 8 * j - shift;  // (wraps in vector 0 of a shifted row)
+        if (8 * j >= shift && c0 + 8 <= p.dim) {
+          if (p.h_out) store8<MX_BF16>(p.h_out, base + c0, f);
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) h[any_at<DTYPE>(c0 + e)] = f[e];
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) {
+            const uint32_t c = c0 + e;
+            if (c < p.dim) {  // (a neighbour's element wraps to a large number)
+              if (p.h_out) store1<DTYPE>(p.h_out, base + c, f[e]);
+              h[any_at<DTYPE>(c)] = f[e];
+            }
+          }
+        }
+      }
     }
+  } else {
+    for (uint32_t c0 = threadIdx.x; c0 < p.dim; c0 += 8 * T) {
+      float v[8], r[8];
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-      const uint32_t c = c0 + 256 * k;
-      if (c < p.dim) {
-        if (p.residual) v[k] += r[k];
-        if (p.h_out) store1<DTYPE>(p.h_out, base + c, v[k]);
-        h[c] = v[k];
-        ss = fmaf(v[k], v[k], ss);
+      for (uint32_t k = 0; k < 8; ++k) {
+        const uint32_t c = c0 + T * k;
+        v[k] = c < p.dim ? load1<DTYPE>(p.x, base + c) : 0.0f;
+        r[k] = c < p.dim && p.residual ? load1<DTYPE>(p.residual, base + c) : 0.0f;
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) {
+        const uint32_t c = c0 + T * k;
+        if (c < p.dim) {
+          if (p.residual) v[k] += r[k];
+          if (p.h_out) store1<DTYPE>(p.h_out, base + c, v[k]);
+          h[c] = v[k];
+          ss = fmaf(v[k], v[k], ss);
+        }
       }
     }
   }
-  for (uint32_t c = p.dim + threadIdx.x; c < 8 * groups; c += 256) h[c] = 0.0f;
+  for (uint32_t c = p.dim + threadIdx.x; c < 8 * groups; c += T) h[any_at<DTYPE>(c)] = 0.0f;
+  if constexpr (DTYPE == MX_BF16) {  // the squares in the order of the FP32 rows
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < p.dim; c += T) {
+      const float v = h[any_at<DTYPE>(c)];
+      ss = fmaf(v, v, ss);
+    }
+  }
   const float s = rsqrtf(cta_sum(ss, red) * p.inv_dim + p.eps);  // (its barrier: the row is in shared memory)
   uint8_t* out_row = p.elems + (size_t)row * p.kblocks * (4 * bits);
-  for (uint32_t g0 = threadIdx.x & ~31u; g0 < groups; g0 += 256) {  // (warps stay whole for the shuffles)
+  for (uint32_t g0 = threadIdx.x & ~31u; g0 < groups; g0 += T) {  // (warps stay whole for the shuffles)
     const uint32_t g = g0 + (threadIdx.x & 31);
     float v[8] = {}, w[8] = {};
-    if (g < groups) {
-      const float4 a = reinterpret_cast<const float4*>(h)[2 * g], b = reinterpret_cast<const float4*>(h)[2 * g + 1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
+    if (g < groups) any_group<DTYPE>(h, g, v);
     if (8 * g + 8 <= p.dim) {
       load_weight8(p.weight, p.w_bf16, 8 * g, w);
     } else {
@@ -243,14 +321,14 @@ __global__ void __launch_bounds__(256) rmsnorm_any_kernel(const NormParams p) {
         if (8 * g + e >= p.dim) v[e] = 0.0f;
     }
     if (p.y_out && g < groups) {
-      reinterpret_cast<float4*>(h)[2 * g] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(h)[2 * g + 1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) h[any_at<DTYPE>(8 * g) + e] = v[e];
     }
     store_group<FMT>(p, row, out_row, g, v);
   }
   if (p.y_out) {
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < p.dim; c += 256) store1<DTYPE>(p.y_out, base + c, h[c]);
+    for (uint32_t c = threadIdx.x; c < p.dim; c += T) store1<DTYPE>(p.y_out, base + c, h[any_at<DTYPE>(c)]);
   }
   zero_pad_rows(p);
 }
@@ -575,6 +653,60 @@ __global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_kernel(c
   }
 }
 
+// Rows that start anywhere, dim <= 32 V <= 1024: a row per warp, an element per lane; the weights wait in shared memory.
+template <int DTYPE, int V>
+__global__ void __launch_bounds__(32 * kRowWarps) rmsnorm_backward_warp_any_kernel(const NormBackParams p) {
+  extern __shared__ float sums[];  // [warps][dim], then the weights
+  pdl_prologue();
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float* weight = sums + kRowWarps * p.dim;
+  for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) weight[c] = weight1(p.weight, p.w_bf16, c);
+  __syncthreads();
+  float dw[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) dw[i] = 0.0f;
+  for (uint32_t row = blockIdx.x * kRowWarps + warp; row < p.rows; row += gridDim.x * kRowWarps) {
+    const size_t base = (size_t)row * p.dim + lane;
+    float h[V], g[V], q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const bool live = 32 * i + lane < p.dim;
+      h[i] = live ? load1<DTYPE>(p.h, base + 32 * i) : 0.0f;
+      g[i] = live ? load1<DTYPE>(p.dy, base + 32 * i) : 0.0f;
+      q[i] = live && p.dres ? load1<DTYPE>(p.dres, base + 32 * i) : 0.0f;
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      s1 = fmaf(h[i], h[i], s1);
+      if (32 * i + lane < p.dim) s2 = fmaf(g[i] * weight[32 * i + lane], h[i], s2);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    const float s = rsqrtf(s1 * p.inv_dim + p.eps), k = s * (s * s * (s2 * p.inv_dim));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (32 * i + lane >= p.dim) continue;
+      const float gs = g[i] * s;
+      dw[i] = fmaf(gs, h[i], dw[i]);
+      store1<DTYPE>(p.dh, base + 32 * i, fmaf(gs, weight[32 * i + lane], fmaf(-k, h[i], q[i])));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (32 * i + lane < p.dim) sums[warp * p.dim + 32 * i + lane] = dw[i];
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < p.dim; c += blockDim.x) {
+    float t = sums[c];
+#pragma unroll
+    for (uint32_t w = 1; w < kRowWarps; ++w) t += sums[w * p.dim + c];
+    p.partial[(size_t)blockIdx.x * p.dim + c] = t;
+  }
+}
+
 // Any dim up to 512 V: the ring above for rows that start anywhere.  The 16-byte vectors that cover a row are copied
 // by whichever thread comes to them, so a barrier stands between copy and use; a thread takes every 512th
 // element, twice from shared memory.  (8192 x 4001 BF16: 150 us with the two kernels below.)
@@ -744,9 +876,24 @@ __global__ void __launch_bounds__(1024) rmsnorm_dweight_kernel(const float* __re
 
 struct Shape {
   uint32_t threads;
-  int v;  // groups of 8 per thread; 0: the kernels for any dim
+  int v;     // groups of 8 per thread; 0: the kernels for any dim
+  bool few;  // rows: each has an SM to itself
 };
 constexpr uint32_t kAnyBytes = 200 * 1024;  // a row of FP32 in shared memory
+
+template <int DTYPE, int FMT, uint32_t T>
+cudaError_t launch_any_forward(const NormParams& p, uint32_t smem, cudaStream_t stream) {
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(rmsnorm_any_kernel<DTYPE, FMT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAnyBytes);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
+  return launch_pdl(rmsnorm_any_kernel<DTYPE, FMT, T>, dim3(p.rows), dim3(T), smem, stream, p);
+}
 
 template <int DTYPE, int FMT>
 cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
@@ -757,18 +904,13 @@ cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
     case 4: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 4>, grid, dim3(s.threads), 0, stream, p);
     default: break;
   }
-  const uint32_t smem = (p.kblocks + 3) / 4 * 512;
+  const uint32_t smem = any_at<DTYPE>((p.kblocks + 3) / 4 * 128) * 4;
   if (smem > kAnyBytes) return launch_pdl(rmsnorm_long_kernel<DTYPE, FMT>, grid, dim3(1024), 0, stream, p);
-  static bool attr_set[64] = {false};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(rmsnorm_any_kernel<DTYPE, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAnyBytes);
-    if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64) attr_set[dev] = true;
-  }
-  return launch_pdl(rmsnorm_any_kernel<DTYPE, FMT>, grid, dim3(256), smem, stream, p);
+  // few threads where rows are short, so that more of them are under way (8192 x 257 BF16: 13.6 us with 64, 25 with 256); their
+  // number is a constant of the kernel, which halves its registers (8192 x 4001 FP32: 94 us otherwise, 73)
+  if (!s.few && p.dim <= 768) return launch_any_forward<DTYPE, FMT, 64>(p, smem, stream);
+  if (!s.few && p.dim <= 2048) return launch_any_forward<DTYPE, FMT, 128>(p, smem, stream);
+  return launch_any_forward<DTYPE, FMT, 256>(p, smem, stream);
 }
 
 template <int DTYPE>
@@ -815,11 +957,22 @@ cudaError_t launch_any(const NormBackParams& p, uint32_t smem, int sms, uint32_t
   *parts = p.rows < grid ? p.rows : grid;
   return launch_pdl(rmsnorm_backward_any_kernel<DTYPE, V, NS>, dim3(*parts), dim3(512), smem, stream, p);
 }
-// Rows of any length up to 8192, three of them in the ring (two where three do not fit).
+// Rows of any length up to 8192: many short ones a warp each, else three of them in the ring (two where three do not fit).
 template <int DTYPE>
 cudaError_t launch_backward_any(const NormBackParams& p, int sms, uint32_t* parts, cudaStream_t stream) {
   const uint32_t stage = 3 * any_slot<DTYPE>(p.dim);
   if (3 * stage > 220 * 1024) return launch_any<DTYPE, 16, 2>(p, 2 * stage, sms, parts, stream);
+  if (p.dim <= 1024 && p.rows >= 1024) {
+    // (1001 BF16: 8192 rows 38 us, 55 in the ring; 64 rows 8.4, 4.4; 257: 13, 45)
+    const uint32_t need = (p.rows + kRowWarps - 1) / kRowWarps, most = 2u * (uint32_t)sms;
+    *parts = need < most ? need : most;
+    if (*parts > (uint32_t)kNormPartials) *parts = (uint32_t)kNormPartials;
+    const dim3 grid(*parts), block(32 * kRowWarps);
+    const size_t smem = (kRowWarps + 1) * (size_t)p.dim * 4;
+    if (p.dim <= 256) return launch_pdl(rmsnorm_backward_warp_any_kernel<DTYPE, 8>, grid, block, smem, stream, p);
+    if (p.dim <= 512) return launch_pdl(rmsnorm_backward_warp_any_kernel<DTYPE, 16>, grid, block, smem, stream, p);
+    return launch_pdl(rmsnorm_backward_warp_any_kernel<DTYPE, 32>, grid, block, smem, stream, p);
+  }
   if (p.dim <= 1024) return launch_any<DTYPE, 2, 3>(p, 3 * stage, sms, parts, stream);
   if (p.dim <= 2048) return launch_any<DTYPE, 4, 3>(p, 3 * stage, sms, parts, stream);
   if (p.dim <= 4096) return launch_any<DTYPE, 8, 3>(p, 3 * stage, sms, parts, stream);
@@ -863,9 +1016,9 @@ cudaError_t launch_rmsnorm_quantize(const RmsnormArgs& a) {
   p.w_bf16 = (uint32_t)a.w_bf16; p.sticky = a.rounding == MX_RHAZ ? 1u : 0u; p.layout = (uint32_t)a.layout;
   // Groups of 8 that a row stores, whole 16-group runs (the four scale bytes of a swizzled word).
   const uint32_t groups = (p.kblocks + 3) / 4 * 16;
-  Shape s = {256, 0};
+  Shape s = {256, 0, a.rows <= a.sm_count};
   if (a.dim % 8 == 0 && groups <= 2048) {
-    if (a.rows <= a.sm_count) {  // a row per SM: as many threads as the row has groups, the shortest chain
+    if (s.few) {  // a row per SM: as many threads as the row has groups, the shortest chain
       s.threads = groups < 1024 ? (groups + 31) / 32 * 32 : 1024;
     } else {
       s.threads = (groups / 4 + 31) / 32 * 32;
