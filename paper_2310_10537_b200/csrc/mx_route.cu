@@ -19,7 +19,7 @@ struct RouteParams {
   int32_t* ids;
   float* weights;
   void* dlogits;
-  uint32_t tokens, experts, topk, score, groups, topk_groups, group_score, renormalize, group_size;
+  uint32_t tokens, experts, topk, score, groups, topk_groups, group_score, renormalize, group_size, group_lanes;
   FastDiv by_group_size;
   float scale;
 };
@@ -427,8 +427,7 @@ __device__ __forceinline__ void part_softmax(float (&x)[kPartKeys], float& m, fl
   for (int o = 1; o < L; o <<= 1) sum += __shfl_xor_sync(kFull, sum, o);
 }
 
-// Needs experts % 4 == 0, experts <= kPartKeys L, topk <= kPartK, the bias on a 16-byte boundary, and groups of a
-// power of two of whole lanes.
+// Needs experts % 4 == 0, experts <= kPartKeys L, topk <= kPartK, and the bias on a 16-byte boundary.
 template <int DTYPE, int L>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const RouteParams p) {
   constexpr uint32_t kTokens = 32 / L;  // of a warp
@@ -465,8 +464,12 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const Rout
         if (e0 + j >= p.experts) key[j] = 0u;
     }
   }
-  if (p.groups > 1) {
-    const uint32_t lanes = p.group_size / kPartKeys;  // of a group
+  auto lay_down = [&]() {  // the keys where they can be read by number
+#pragma unroll
+    for (int i = 0; i < kPartKeys / 4; ++i) keys[warp][i][lane] = make_uint4(key[4 * i], key[4 * i + 1], key[4 * i + 2], key[4 * i + 3]);
+  };
+  if (p.groups > 1 && p.group_lanes) {  // a group is a power of two of whole lanes
+    const uint32_t lanes = p.group_lanes;  // of a group
     uint32_t a = 0, b = 0;
 #pragma unroll
     for (int j = 0; j < kPartKeys; ++j) top2_add(a, b, key[j]);
@@ -486,10 +489,33 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const Rout
     }
 #pragma unroll
     for (int j = 0; j < kPartKeys; ++j) key[j] = before < p.topk_groups ? key[j] : 0u;
-  }
-  // the keys are laid down where they can be read by number
+  } else if (p.groups > 1) {  // through shared memory, L groups at a time
+    lay_down();
+    __syncwarp();
+    uint32_t* value = reinterpret_cast<uint32_t*>(fields[warp][part]);  // 32 groups at most
+    for (uint32_t g = q; g < p.groups; g += L) {
+      uint32_t a = 0, b = 0;
+      for (uint32_t e = g * p.group_size; e < (g + 1) * p.group_size; ++e)
+        top2_add(a, b, reinterpret_cast<const uint32_t*>(&keys[warp][(e % kPartKeys) >> 2][part * L + e / kPartKeys])[e & 3]);
+      value[g] = order_key(group_value(p, by_score, m, sum, a, b));
+    }
+    __syncwarp();
+    uint32_t kept = 0;
+    for (uint32_t g = q; g < p.groups; g += L) {
+      uint32_t before = 0;
+      for (uint32_t o = 0; o < p.groups; ++o) before += value[o] > value[g] || (value[o] == value[g] && o < g) ? 1u : 0u;
+      kept |= before < p.topk_groups ? 1u << g : 0u;
+    }
 #pragma unroll
-  for (int i = 0; i < kPartKeys / 4; ++i) keys[warp][i][lane] = make_uint4(key[4 * i], key[4 * i + 1], key[4 * i + 2], key[4 * i + 3]);
+    for (int o = 1; o < L; o <<= 1) kept |= __shfl_xor_sync(kFull, kept, o);
+    uint32_t g = fastdiv(e0, p.by_group_size), at = e0 - g * p.group_size;
+#pragma unroll
+    for (int j = 0; j < kPartKeys; ++j) {
+      key[j] = g < p.groups && ((kept >> g) & 1u) ? key[j] : 0u;
+      if (++at == p.group_size) { at = 0; ++g; }
+    }
+  }
+  lay_down();
   auto key_at = [&](uint32_t s) { return reinterpret_cast<const uint32_t*>(&keys[warp][s >> 2][lane])[s & 3]; };
   // A floor under the topk-th best: with up to 4 lanes that key itself, else the topk-th of the best of every four
   // keys, which lets few more through and is cheaper (4 lanes: 16384 tokens, 6 of 64: 5.8 us; 6.6 with fours)
@@ -776,6 +802,8 @@ RouteParams route_params(const RouteArgs& a) {
   p.renormalize = a.route.renormalize ? 1u : 0u; p.scale = a.route.scale;
   p.group_size = p.groups ? p.experts / p.groups : p.experts;
   p.by_group_size = make_fastdiv(p.group_size);
+  const uint32_t lanes = p.group_size / kPartKeys;
+  p.group_lanes = p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0u;
   return p;
 }
 
@@ -795,16 +823,15 @@ cudaError_t launch_part(const RouteParams& p, bool backward, cudaStream_t stream
 
 template <int DTYPE>
 cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t stream) {
-  const uint32_t lanes = p.group_size / kPartKeys;
   // A few lanes per token.  Few experts need many tokens for it to pay: 8 experts, top-2, 2048 tokens 2.6 us (a
   // warp per token 2.3), 4096 2.6 (3.0); 64 experts, top-6, 1024 tokens 3.0 (2.6), 2048 3.1 (3.6).
-  // With more than 128 it is never behind (256 in 8 groups: 16 tokens 3.0, 3.9; 512 ungrouped, 16384 tokens: 16.8, 16.3).
+  // With more than 128 always: 256 in 8 groups, 16 tokens 3.0 (3.9), 160 in 8 groups, 16384 tokens 14.5 (18.3); with a token
+  // per warp it has little to share and may lose a little (512 ungrouped, 16384 tokens 16.8 (16.3), 384 in 8 groups 34.7 (33.6)).
   // Gradient: 64 experts, 16 tokens 2.4 (2.1), 2048 2.5 (2.6); 128 experts 2.1 (2.2), 16384 tokens 4.7 (6.9).
   const bool enough = backward ? p.experts > 64 || p.tokens >= 2048u
                                : p.experts > 128 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
-  const bool groups_fit = p.groups == 1 || (p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0);
   if (enough && p.topk <= kPartK && p.experts % 4 == 0 && p.experts <= 32 * kPartKeys &&
-      (backward || (groups_fit && (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0))) {
+      (backward || (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0)) {
     if (p.experts <= 2 * kPartKeys) return launch_part<DTYPE, 2>(p, backward, stream);
     if (p.experts <= 4 * kPartKeys) return launch_part<DTYPE, 4>(p, backward, stream);
     if (p.experts <= 8 * kPartKeys) return launch_part<DTYPE, 8>(p, backward, stream);

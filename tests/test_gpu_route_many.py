@@ -135,3 +135,22 @@ def test_outputs_are_filled_and_nothing_else():
     for raw, want, n in ((raw_i, ids, T * k), (raw_w, w, T * k), (raw_d, d, T * E)):
         assert torch.equal(raw[256:256 + n], want.flatten())
         assert bool((raw[:256] == raw[0]).all()) and bool((raw[256 + n:] == raw[0]).all()) and float(raw[0]) in (-7, 77)
+
+
+@pytest.mark.parametrize("score", [SOFT, SIG])
+@pytest.mark.parametrize("T,E,k,groups,kg", [(4100, 8, 2, 4, 2), (4097, 24, 8, 3, 2), (2050, 40, 4, 8, 3), (2048, 64, 6, 32, 7), (2049, 96, 8, 8, 4), (2111, 128, 8, 16, 5),
+                                             (33, 160, 6, 8, 3), (50, 384, 8, 8, 2), (21, 480, 8, 20, 4), (19, 512, 8, 32, 32)])
+def test_groups_of_any_size(T, E, k, groups, kg, score):
+    x = _logits(T, E, E + groups, torch.float32)
+    ids, w = mx.mx_route(x, k, score, groups=groups, topk_groups=kg)
+    c = _choice64(x.double(), groups, kg, mx.MX_GROUP_MAX, None)
+    assert torch.equal(ids.long(), torch.sort(c, dim=1, descending=True, stable=True).indices[:, :k])
+    ref = _weights64(_scores64(x, score), ids, True, 1.0)
+    assert bool(((w.double() - ref).abs() <= 64 * 2.0 ** -24 * ref).all())
+    # sums of two: the same as through the other way (a bias of zeros off the 16-byte boundary), which adds nothing
+    if E // groups > 1:
+        zeros = torch.zeros(E + 4, device="cuda")
+        args = dict(groups=groups, topk_groups=kg, group_score=mx.MX_GROUP_TOP2)
+        ids, w = mx.mx_route(x, k, SIG, bias=zeros[:E], **args)
+        ids2, w2 = mx.mx_route(x, k, SIG, bias=zeros[1:E + 1], **args)
+        assert torch.equal(ids, ids2) and bool(((w - w2).abs() <= 128 * 2.0 ** -24 * w).all())
