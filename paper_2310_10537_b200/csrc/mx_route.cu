@@ -532,19 +532,32 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_part_kernel(const Rout
     descend(best[0], best[1]); descend(best[2], best[3]);
     descend(best[0], best[2]); descend(best[1], best[3]);
     descend(best[1], best[2]);
+    if constexpr (L < 32) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) best[7 - j] = __shfl_xor_sync(kFull, best[j], 1);
-    bitonic8(best);
+      for (int j = 0; j < 4; ++j) best[7 - j] = __shfl_xor_sync(kFull, best[j], 1);
+      bitonic8(best);
+    }
   }
+  uint32_t floor_key;
+  if constexpr (L < 32) {
 #pragma unroll
-  for (int o = L < 8 ? 1 : 2; o < L; o <<= 1) {
+    for (int o = L < 8 ? 1 : 2; o < L; o <<= 1) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) k[j] = __shfl_xor_sync(kFull, best[j], o);
-    merge8(best, k);
+      for (int j = 0; j < 8; ++j) k[j] = __shfl_xor_sync(kFull, best[j], o);
+      merge8(best, k);
+    }
+    floor_key = best[0];
+#pragma unroll
+    for (uint32_t j = 1; j < kPartK; ++j) floor_key = j < p.topk ? best[j] : floor_key;
+  } else {  // the whole warp: its best, taken off the lane that has it, topk times
+    floor_key = 0;
+    for (uint32_t i = 0; i < p.topk; ++i) {
+      floor_key = __reduce_max_sync(kFull, best[0]);
+      if (lane == __ffs(__ballot_sync(kFull, best[0] == floor_key)) - 1) {
+        best[0] = best[1]; best[1] = best[2]; best[2] = best[3]; best[3] = 0;
+      }
+    }
   }
-  uint32_t floor_key = best[0];
-#pragma unroll
-  for (uint32_t j = 1; j < kPartK; ++j) floor_key = j < p.topk ? best[j] : floor_key;
   floor_key = max(floor_key, 1u);  // (no candidate has 0)
   uint32_t hits = 0;
 #pragma unroll
