@@ -329,8 +329,8 @@ struct CombineParams {
   ZeroRows zero;
 };
 
-// A CTA per token -- few tokens: several, each with a part of the columns.  VEC: 8 elements at a time (dim % 8 == 0), else one.
-// Bound by memory: 8192 tokens x 4096 BF16, top-8, 101 us, 5.95 TB/s.
+// Several CTAs per token, each with a part of the columns.  VEC: 8 elements at a time (dim % 8 == 0), else one.
+// Bound by memory: 8192 tokens x 4096 BF16, top-8, 98 us, 6.2 TB/s.
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(128) combine_kernel(const CombineParams p) {
   pdl_prologue();
@@ -525,10 +525,13 @@ static CombineParams combine_params(const MoeMoveArgs& a) {
 
 cudaError_t launch_moe_combine(const MoeMoveArgs& a) {
   const CombineParams p = combine_params(a);
-  // enough CTAs for every SM to hold four: 64 tokens x 4096, top-4: 7.2 us with one CTA per token
-  const uint32_t units = a.dim % 8 == 0 ? p.dim / 8 : p.dim, most = (units + 127) / 128;
-  const uint32_t wanted = (4u * (uint32_t)a.sm_count + p.tokens - 1) / p.tokens;
-  const dim3 grid(p.tokens, wanted < most ? wanted : most), block(128);
+  // Two steps of columns per CTA, so that the last round of CTAs is a small part of all (4817 tokens x 7520, top-4: 66 us,
+  // 77 with a CTA per token; one step: 66, but 8192 x 4096, top-2, 37 instead of 33).  One step where that leaves an SM
+  // less than 16 of them (239 x 6144, top-6: 4.9 us, 6.8; 64 x 4096, top-4: 3.5, 7.2 with a CTA per token).
+  const uint32_t units = a.dim % 8 == 0 ? p.dim / 8 : p.dim, two = (units + 255) / 256;
+  const bool enough = (uint64_t)p.tokens * two >= 16u * (uint64_t)a.sm_count;
+  const uint32_t parts = enough ? two : (units + 127) / 128;
+  const dim3 grid(p.tokens, parts < 65535u ? parts : 65535u), block(128);
   if (a.dtype == MX_BF16)
     return a.dim % 8 == 0 ? launch_pdl(combine_kernel<MX_BF16, true>, grid, block, 0, a.stream, p)
                           : launch_pdl(combine_kernel<MX_BF16, false>, grid, block, 0, a.stream, p);
