@@ -1119,7 +1119,7 @@ static int grouped_run(const mx::GroupedArgs& args, const Opts& o) {
     if (rc != MX_OK) return fail_cuda(e);
     if (st != 0) {
       std::snprintf(g_cuda_error, sizeof(g_cuda_error), "device-side wait %u of a grouped product gave up (1 producer/"
-                    "stage empty, 2 MMA/stage full, 3 MMA/accumulator free, 4 epilogue/accumulator full)", st);
+                    "stage empty, 2 MMA/stage full, 3 MMA/accumulator free, 4 epilogue/accumulator full, 5 scale copier/scales)", st);
       return MX_ERR_TIMEOUT;
     }
   }

@@ -25,7 +25,7 @@
 // What bounds it: large groups the power limit -- 65536 x 4096 x 4096 over 32 groups 827 us, 2.66 PFLOP/s, at
 // 1.29 GHz; of its cycles 86 % are MMAs, 2 % the hand-over of accumulators, and a stage takes 573 clocks instead of 512.
 // Weight gradients 4096 x 2048 over 16 groups of 2048 rows: 207 to 262 us by the clock (1.29 GHz), 81 % MMAs.  128 rows on
-// 56 experts of 2048 x 4096, FP4 weights: 56.7 us, 4.4 TB/s of weights; 448 tiles on 74 pairs are seven rounds of which the
+// 56 experts of 2048 x 4096, FP4 weights: 55.9 us, 4.5 TB/s of weights; 448 tiles on 74 pairs are seven rounds of which the
 // last holds 4, and a stage's copies and hand-overs take longer than its bytes.
 // Every wait is bounded (see mbar_wait); on expiry a status word is set and all roles fall through to
 // the common exit.
