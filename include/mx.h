@@ -486,7 +486,7 @@ int mx_route(const void* logits, const float* bias, int64_t tokens, int64_t expe
  * Gradient of the weights with respect to the logits, the choice held fixed (the bias and the
  * groups have no gradient).  dweights FP32 [tokens x topk], ids as mx_route wrote them (an id outside
  * [0, experts) contributes nothing), dlogits [tokens x experts] of opts->dtype, overwritten.
- * Of `route` topk, score, renormalize and scale are used.  Errors as mx_route.
+ * Of `route` topk, score, renormalize and scale are used; the other fields may hold anything.  Errors as mx_route.
  */
 int mx_route_backward(const float* dweights, const void* logits, const int32_t* ids, int64_t tokens,
                       int64_t experts, const mx_route_t* route, void* dlogits, const mx_opts_t* opts);

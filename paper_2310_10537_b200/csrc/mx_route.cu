@@ -806,14 +806,15 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_backward_part_kernel(c
   }
 }
 
-RouteParams route_params(const RouteArgs& a) {
+RouteParams route_params(const RouteArgs& a, bool backward) {
   RouteParams p;
   p.logits = a.logits; p.bias = a.bias; p.dweights = a.dweights; p.ids = a.ids; p.weights = a.weights;
   p.dlogits = a.dlogits; p.tokens = (uint32_t)a.tokens; p.experts = (uint32_t)a.experts;
-  p.topk = (uint32_t)a.route.topk; p.score = (uint32_t)a.route.score; p.groups = (uint32_t)a.route.groups;
+  p.topk = (uint32_t)a.route.topk; p.score = (uint32_t)a.route.score;
+  p.groups = backward ? 1u : (uint32_t)a.route.groups;  // (the gradient has no groups: nobody has checked that field)
   p.topk_groups = (uint32_t)a.route.topk_groups; p.group_score = (uint32_t)a.route.group_score;
   p.renormalize = a.route.renormalize ? 1u : 0u; p.scale = a.route.scale;
-  p.group_size = p.groups ? p.experts / p.groups : p.experts;
+  p.group_size = p.experts / p.groups;
   p.by_group_size = make_fastdiv(p.group_size);
   const uint32_t lanes = p.group_size / kPartKeys;
   p.group_lanes = p.group_size % kPartKeys == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0u;
@@ -862,12 +863,12 @@ cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t strea
 }  // namespace
 
 cudaError_t launch_route(const RouteArgs& a) {
-  const RouteParams p = route_params(a);
+  const RouteParams p = route_params(a, false);
   return a.dtype == MX_BF16 ? launch_dtype<MX_BF16>(p, false, a.stream) : launch_dtype<MX_F32>(p, false, a.stream);
 }
 
 cudaError_t launch_route_backward(const RouteArgs& a) {
-  const RouteParams p = route_params(a);
+  const RouteParams p = route_params(a, true);
   return a.dtype == MX_BF16 ? launch_dtype<MX_BF16>(p, true, a.stream) : launch_dtype<MX_F32>(p, true, a.stream);
 }
 
