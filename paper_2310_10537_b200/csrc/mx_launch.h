@@ -127,6 +127,14 @@ struct RmsnormArgs {
   cudaStream_t stream;
 };
 cudaError_t launch_rmsnorm_quantize(const RmsnormArgs& a);
+// Shared memory that a row takes in the forward kernel for rows of any length: FP32, whole runs of 128
+// elements, for BF16 rows a word more after every 8.  In 64 bits: a row may have 2^31 - 1 elements.  Rows
+// beyond kNormRowBytes take the kernel that reads them twice.
+constexpr uint64_t kNormRowBytes = 200 * 1024;
+constexpr uint64_t norm_row_bytes(bool bf16, int64_t dim) {
+  const uint64_t padded = ((uint64_t)dim + 127) / 128 * 128;
+  return 4 * (bf16 ? padded + padded / 8 : padded);
+}
 
 // Partial sums of the weight gradient (rows of `partial`) that the backward pass writes at most.
 constexpr int kNormPartials = 296;

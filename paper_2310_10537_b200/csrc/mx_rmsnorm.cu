@@ -879,7 +879,6 @@ struct Shape {
   int v;     // groups of 8 per thread; 0: the kernels for any dim
   bool few;  // rows: each has an SM to itself
 };
-constexpr uint32_t kAnyBytes = 200 * 1024;  // a row of FP32 in shared memory
 
 template <int DTYPE, int FMT, uint32_t T>
 cudaError_t launch_any_forward(const NormParams& p, uint32_t smem, cudaStream_t stream) {
@@ -888,7 +887,8 @@ cudaError_t launch_any_forward(const NormParams& p, uint32_t smem, cudaStream_t 
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(rmsnorm_any_kernel<DTYPE, FMT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAnyBytes);
+    e = cudaFuncSetAttribute(rmsnorm_any_kernel<DTYPE, FMT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)kNormRowBytes);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) attr_set[dev] = true;
   }
@@ -904,8 +904,9 @@ cudaError_t launch_forward(const NormParams& p, Shape s, cudaStream_t stream) {
     case 4: return launch_pdl(rmsnorm_kernel<DTYPE, FMT, 4>, grid, dim3(s.threads), 0, stream, p);
     default: break;
   }
-  const uint32_t smem = any_at<DTYPE>((p.kblocks + 3) / 4 * 128) * 4;
-  if (smem > kAnyBytes) return launch_pdl(rmsnorm_long_kernel<DTYPE, FMT>, grid, dim3(1024), 0, stream, p);
+  const uint64_t row_bytes = norm_row_bytes(DTYPE == MX_BF16, p.dim);
+  if (row_bytes > kNormRowBytes) return launch_pdl(rmsnorm_long_kernel<DTYPE, FMT>, grid, dim3(1024), 0, stream, p);
+  const uint32_t smem = (uint32_t)row_bytes;
   // few threads where rows are short, so that more of them are under way (8192 x 257 BF16: 13.6 us with 64, 25 with 256); their
   // number is a constant of the kernel, which halves its registers (8192 x 4001 FP32: 94 us otherwise, 73)
   if (!s.few && p.dim <= 768) return launch_any_forward<DTYPE, FMT, 64>(p, smem, stream);
