@@ -552,7 +552,7 @@ int mx_moe_combine_backward(const void* dout, const void* y, const float* weight
  * product accumulated in FP32 as in mx_gemm.  offsets: int32 [groups + 1] in DEVICE memory (of
  * mx_moe_plan, or any ascending row numbers that are multiples of 64; the last may also be `rows`).
  * Rows of C before offsets[0] or from offsets[groups] on are not written.  An offset that breaks
- * the rule is clamped to [0, rows] and rounded down to a multiple of 64, a descending pair is an
+ * the rule is clamped to [0, rows] and, below `rows`, rounded down to a multiple of 64, a descending pair is an
  * empty group: nothing outside C is ever touched.
  * The gradient of A is the same call on dC quantized along N and B quantized along N ([groups x K x N]).
  * N % 128 == 0; K as mx_gemm (a multiple of 32, of 128 with 6- or 4-bit codes); groups <= 1024.
@@ -562,8 +562,8 @@ int mx_moe_combine_backward(const void* dout, const void* y, const float* weight
  *   C[g] = A[:, offsets[g] .. offsets[g+1]] . B[:, offsets[g] .. offsets[g+1]]^T
  * A packed [M x rows], B packed [N x rows] (K-major: mx_quantize of dC and of A's float rows along
  * axis 0), SWIZZLED scales; C [groups x M x N], FP32 or BF16, all of it written: zero for an
- * empty group.  offsets multiples of 128 (clamped and rounded down as above); the padding rows of a group
- * have to be zero blocks.  rows % 32 == 0 (% 128 with 6- or 4-bit codes); N a multiple of 8.
+ * empty group.  offsets multiples of 128, the last may also be `rows` (what is not is clamped to [0, rows] and, below
+ * `rows`, rounded down); the padding rows of a group have to be zero blocks.  rows % 32 == 0 (% 128 with 6- or 4-bit codes); N a multiple of 8.
  * Errors of both: as mx_gemm; MX_ERR_UNSUPPORTED for more than 1024 groups or pad_k128.
  */
 int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,

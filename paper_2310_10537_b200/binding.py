@@ -512,7 +512,7 @@ def mx_gemm_grouped(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torc
 def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
                       M: int, N: int, rows: int, fmtA: int, fmtB: int, out: Optional[torch.Tensor] = None,
                       out_dtype: torch.dtype = torch.float32, check_status: bool = False) -> torch.Tensor:
-    """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128): A is the
+    """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128, or `rows`): A is the
     MX tensor [M, rows], B [N, rows], both quantized along the rows; C [groups, M, N]."""
     return _py_call.gemm_grouped_k(A, sA, B, sB, offsets, M, N, rows, fmtA, fmtB, out, out_dtype, check_status)
 

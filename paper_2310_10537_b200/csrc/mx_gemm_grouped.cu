@@ -62,7 +62,7 @@ __device__ unsigned int g_grouped_status;
 struct GroupedParams {
   const int32_t* offsets;
   void* C;
-  uint32_t c_bf16, groups, w_rows, x_rows, k_chunks, k_stages;  // the whole K axis in chunks, in stages
+  uint32_t c_bf16, groups, w_rows, x_rows, k_len, k_chunks, k_stages;  // the whole K axis in elements, chunks, stages
   uint32_t max_n, acc_step, shared_half, band, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
   long long spin_limit;
 };
@@ -121,11 +121,12 @@ __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& 
   return true;
 }
 
-// Offsets as the kernel may use them: clamped to the tensor, on the grid, in units of rows (KG: of K chunks).
+// Offsets as the kernel may use them: the end of the tensor, or on the grid; in units of rows (KG: of K chunks, of which
+// the last one may be a part: the copies fill it up with zeros).
 template <bool KG>
 __device__ __forceinline__ uint32_t sane_offset(const GroupedParams& p, int32_t raw) {
   const uint32_t v = raw > 0 ? (uint32_t)raw : 0u;
-  if (KG) return min(v / (uint32_t)kBK, p.k_chunks);
+  if (KG) return v >= p.k_len ? p.k_chunks : v / (uint32_t)kBK;
   return v >= p.x_rows ? p.x_rows : (v & ~63u);
 }
 
@@ -499,7 +500,8 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn, uint32_t max_n
     return cudaErrorInvalidValue;
   GroupedParams p;
   p.offsets = a.offsets; p.C = a.C; p.c_bf16 = (uint32_t)a.c_bf16; p.groups = (uint32_t)a.groups;
-  p.w_rows = (uint32_t)a.w_rows; p.x_rows = (uint32_t)a.x_rows; p.k_chunks = (uint32_t)((a.K + kBK - 1) / kBK);
+  p.w_rows = (uint32_t)a.w_rows; p.x_rows = (uint32_t)a.x_rows; p.k_len = (uint32_t)a.K;
+  p.k_chunks = (uint32_t)((a.K + kBK - 1) / kBK);
   p.max_n = max_n;
   p.shared_half = p.max_n == 256 ? 1u : 0u;
   p.acc_step = p.shared_half ? 128 : p.max_n;
