@@ -80,10 +80,20 @@ struct Tables {
   const uint32_t* order;
 };
 
-// X rows of a group in tiles of at most max_n, as even as whole steps of 32 allow, starting at
-// multiples of 64 (where the scale bytes of a tile's first row may lie in their TMEM columns).
-__device__ __forceinline__ uint32_t x_tiles(uint32_t rows, uint32_t max_n) { return (rows + max_n - 1) / max_n; }
-__device__ __forceinline__ uint32_t x_step(uint32_t rows, uint32_t tiles) { return ((rows + tiles - 1) / tiles + 63u) & ~63u; }
+// X rows of a group in tiles of at most max_n, as even as whole steps of 64 allow, starting at
+// multiples of 64 (where the scale bytes of a tile's first row may lie in their TMEM columns).  Every tile has rows (an MMA
+// of N = 0 would be a bad one): rows / tiles is at most max_n, a multiple of 64, and so is the step it is rounded up
+// to; the tiles before the last then hold at most (tiles - 1) max_n rows, which is less than all.
+__host__ __device__ constexpr uint32_t x_tiles(uint32_t rows, uint32_t max_n) { return (rows + max_n - 1) / max_n; }
+__host__ __device__ constexpr uint32_t x_step(uint32_t rows, uint32_t tiles) { return ((rows + tiles - 1) / tiles + 63u) & ~63u; }
+constexpr bool tiles_have_rows(uint32_t max_n) {
+  for (uint32_t rows = 1; rows <= 4096; ++rows) {
+    const uint32_t tiles = x_tiles(rows, max_n), step = x_step(rows, tiles);
+    if (step > max_n || (tiles - 1) * step >= rows) return false;
+  }
+  return true;
+}
+static_assert(tiles_have_rows(64) && tiles_have_rows(128) && tiles_have_rows(256), "a tile without rows");
 
 template <bool KG>
 __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& tb, uint32_t t, uint32_t& slot, Item& it) {
@@ -101,8 +111,7 @@ __device__ __forceinline__ bool next_item(const GroupedParams& p, const Tables& 
   it.group = g;
   it.w0 = wt * 256;
   it.x0 = xt * step;
-  const uint32_t left = it.x0 < rows ? rows - it.x0 : 0u;  // (rounding the step up can leave a last tile without rows)
-  it.n = min(step, (left + 31u) & ~31u);
+  it.n = min(step, (rows - it.x0 + 31u) & ~31u);
   it.x_end = min(rows, it.x0 + it.n);
   if (KG) {
     it.k0 = o;
