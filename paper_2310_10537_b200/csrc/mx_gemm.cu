@@ -412,7 +412,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
         cv_w = (int)wo * cg.stride_w - cg.pad_w;
       }
       for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
         if (!ok) {
           raise_abort(abort_flag, ST_PRODUCER_WAIT);
           break;
@@ -492,7 +492,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
       bool ok = true;
       for (uint32_t t = blockIdx.x; t < num_tiles && ok; t += gridDim.x) {
         for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(sf_full_bar(stage), phase, abort_flag, spin_limit));
+          ok = mbar_wait_warp(sf_full_bar(stage), phase, abort_flag, spin_limit);
           if (!ok) {
             raise_abort(abort_flag, ST_SCALE_WAIT);
             break;
@@ -525,7 +525,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
         const TileCoord tc = tile_coord(t, tiles_m, tiles_n, group_m);
         const int cz_a = (int)(tc.b * tiles_m + tc.tm), cz_b = (int)((tc.b * N + tc.tn * BN) / 128);
         for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
           if (!ok) {
             raise_abort(abort_flag, ST_PRODUCER_WAIT);
             break;
@@ -569,7 +569,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
               cvp[j] = m < cg.M ? n0 * cg.H * cg.W : 0xFFFFFFFFu;
             }
             for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-              ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+              ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
               if (!ok) {
                 raise_abort(abort_flag, ST_PRODUCER_WAIT);
                 break;
@@ -689,7 +689,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
         for (uint32_t d = 0; d < kScaleAhead; ++d) {
           const uint32_t kc = kc0 + d;
           if (kc >= k_chunks || !ok) break;
-          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
           if (!ok) {
             raise_abort(abort_flag, ST_PRODUCER_WAIT);
             break;
@@ -744,7 +744,7 @@ gemm_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
     uint32_t acc = 0, acc_phase = 0;
     for (uint32_t t = blockIdx.x; t < num_tiles; t += gridDim.x) {
       const TileCoord tc = tile_coord(t, tiles_m, tiles_n, group_m);
-      if (!mbar_wait(acc_full_bar(acc), acc_phase, abort_flag, 4 * spin_limit)) {
+      if (!mbar_wait_warp(acc_full_bar(acc), acc_phase, abort_flag, 4 * spin_limit)) {
         if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
         break;
       }
@@ -913,7 +913,7 @@ mx_gemm_skinny_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
     bool ok = true;
     for (uint32_t t = blockIdx.x; t < tiles_n && ok; t += gridDim.x) {
       for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
         if (!ok) {
           raise_abort(abort_flag, ST_PRODUCER_WAIT);
           break;
@@ -951,7 +951,7 @@ mx_gemm_skinny_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
     bool ok = true;
     for (uint32_t t = blockIdx.x; t < tiles_n && ok; t += gridDim.x) {
       for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(sf_full_bar(stage), phase, abort_flag, spin_limit));
+        ok = mbar_wait_warp(sf_full_bar(stage), phase, abort_flag, spin_limit);
         if (!ok) {
           raise_abort(abort_flag, ST_SCALE_WAIT);
           break;
@@ -1015,7 +1015,7 @@ mx_gemm_skinny_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_c
     const uint32_t quarter = warp & 3u;  // TMEM lanes this warp may read: 32 * quarter .. + 31
     uint32_t acc = 0, acc_phase = 0;
     for (uint32_t t = blockIdx.x; t < tiles_n; t += gridDim.x) {
-      if (!mbar_wait(acc_full_bar(acc), acc_phase, abort_flag, 4 * spin_limit)) {
+      if (!mbar_wait_warp(acc_full_bar(acc), acc_phase, abort_flag, 4 * spin_limit)) {
         if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
         break;
       }
@@ -1275,7 +1275,7 @@ pair_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
         cv_w = (int)wo * cg.stride_w - cg.pad_w;
       }
       for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
         if (!ok) {
           raise_abort(abort_flag, ST_PRODUCER_WAIT);
           break;
@@ -1501,7 +1501,7 @@ pair_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
         const int cz_a = (int)((tc.b * tiles_m + tc.tm) * 2 + rank);
         const int cz_b = (int)(tc.b * (N / 128) + tc.tn * cfg::kSfbGroups);
         for (uint32_t kc = 0; kc < k_chunks; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit));
+          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, spin_limit);
           if (!ok) {
             raise_abort(abort_flag, ST_PRODUCER_WAIT);
             break;
@@ -1535,7 +1535,7 @@ pair_kernel_body(const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const CUt
     for (uint32_t t = pair; t < num_tiles; t += num_pairs) {
       const PairItem it = pair_item(t, split_from);
       const TileCoord tc = tile_coord(it.tile, tiles_m, tiles_n, group_m);
-      if (!mbar_wait(acc_full_bar, acc_phase, abort_flag, 4 * spin_limit)) {
+      if (!mbar_wait_warp(acc_full_bar, acc_phase, abort_flag, 4 * spin_limit)) {
         if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
         break;
       }

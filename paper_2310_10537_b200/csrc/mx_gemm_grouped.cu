@@ -266,7 +266,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       const uint32_t sx0 = it.x0 >> 7;
       const uint32_t tx = 2u * KCH * (scales ? sf_chunk : p.w_box_bytes + boxes * p.x_box_bytes);
       for (uint32_t kc = 0; kc < it.nk; ++kc) {
-        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit));
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit);
         if (!ok) {
           raise_abort(abort_flag, ST_PRODUCER_WAIT);
           break;
@@ -310,7 +310,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       Item it;
       for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
         for (uint32_t kc = 0; kc < it.nk; ++kc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(sf_full_bar(stage), phase, abort_flag, p.spin_limit));
+          ok = mbar_wait_warp(sf_full_bar(stage), phase, abort_flag, p.spin_limit);
           if (!ok) {
             raise_abort(abort_flag, ST_SCALE_WAIT);
             break;
@@ -384,7 +384,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     uint32_t i = 0, g = 0;
     Item it;
     for (uint32_t t = pair; next_item<KG>(p, tb, t, g, it); t += num_pairs, ++i) {
-      if (!mbar_wait(acc_full_bar(i & 1u), (i >> 1) & 1u, abort_flag, 4 * p.spin_limit)) {
+      if (!mbar_wait_warp(acc_full_bar(i & 1u), (i >> 1) & 1u, abort_flag, 4 * p.spin_limit)) {
         if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
         break;
       }

@@ -46,6 +46,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity,
     }
   }
 }
+// The same for a whole warp: all of its lanes go on, or none does.  Lane by lane a wait that gives up would leave some
+// lanes behind in code (shuffles, tensor-memory loads) that needs the warp whole, and a failure with a limit would
+// become a hang.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const volatile uint32_t* abort_flag, long long limit) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
+}
 // Every copy of a stage (A tile, B tile, A scales, B scales) goes through a rank-3 tensor map.
 // The warps that issue copies, tcgen05.cp, tcgen05.mma and tcgen05.commit run their loops converged
 // and issue from the lane elect_one() picks: issued from inside a `lane == 0` branch each of
