@@ -573,6 +573,19 @@ int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uin
                       void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
                       mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts);
 
+/*
+ * The same products with the device-side wait budget in the caller's hands, for the failure drill: wait_cycles and
+ * drop_fill as in mx_gemm_plan_t (0 and -1: the library's choice, exactly the calls above; a fill is one of the stages that a
+ * CTA pair's products pass through, 128 K elements of an operand tile, 256 where groups hold 64 rows on average).
+ * Errors as above; MX_ERR_SHAPE for wait_cycles < 0 or drop_fill < -1.
+ */
+int mx_gemm_grouped_ex(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                       void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
+                       mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts, int64_t wait_cycles, int32_t drop_fill);
+int mx_gemm_grouped_k_ex(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                         void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
+                         mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts, int64_t wait_cycles, int32_t drop_fill);
+
 /* ------------------------------------------------------------------------- */
 /* Host-buffer variants                                                      */
 /* ------------------------------------------------------------------------- */

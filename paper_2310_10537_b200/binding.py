@@ -45,6 +45,7 @@ EXPORTS = [
     "mx_rmsnorm_quantize", "mx_rmsnorm_backward_workspace_bytes", "mx_rmsnorm_backward", "mx_route",
     "mx_route_backward", "mx_moe_rows", "mx_moe_plan_workspace_bytes", "mx_moe_plan", "mx_moe_gather",
     "mx_moe_combine", "mx_moe_combine_backward", "mx_gemm_grouped", "mx_gemm_grouped_k",
+    "mx_gemm_grouped_ex", "mx_gemm_grouped_k_ex",
 ]
 
 
@@ -150,6 +151,8 @@ def _load() -> ctypes.CDLL:
     lib.mx_moe_combine_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, op]
     lib.mx_gemm_grouped.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
     lib.mx_gemm_grouped_k.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
+    lib.mx_gemm_grouped_ex.argtypes = lib.mx_gemm_grouped.argtypes + [i64, ctypes.c_int32]
+    lib.mx_gemm_grouped_k_ex.argtypes = lib.mx_gemm_grouped_k.argtypes + [i64, ctypes.c_int32]
     return lib
 
 
@@ -515,6 +518,25 @@ def mx_gemm_grouped_k(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: to
     """C[g] = A[:, r0:r1] . B[:, r0:r1]^T with r0, r1 = offsets[g], offsets[g + 1] (multiples of 128, or `rows`): A is the
     MX tensor [M, rows], B [N, rows], both quantized along the rows; C [groups, M, N]."""
     return _py_call.gemm_grouped_k(A, sA, B, sB, offsets, M, N, rows, fmtA, fmtB, out, out_dtype, check_status)
+
+
+def mx_gemm_grouped_ex(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
+                       rows: int, N: int, K: int, fmtA: int, fmtB: int, out: Optional[torch.Tensor] = None,
+                       out_dtype: torch.dtype = torch.float32, check_status: bool = False, wait_cycles: int = 0,
+                       drop_fill: int = -1) -> torch.Tensor:
+    """mx_gemm_grouped with the device-side wait budget (wait_cycles; drop_fill is the failure drill) in the caller's
+    hands."""
+    return _py_call.gemm_grouped_ex(A, sA, B, sB, offsets, rows, N, K, fmtA, fmtB, out, out_dtype, check_status,
+                                    wait_cycles, drop_fill)
+
+
+def mx_gemm_grouped_k_ex(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB: torch.Tensor, offsets: torch.Tensor,
+                         M: int, N: int, rows: int, fmtA: int, fmtB: int, out: Optional[torch.Tensor] = None,
+                         out_dtype: torch.dtype = torch.float32, check_status: bool = False, wait_cycles: int = 0,
+                         drop_fill: int = -1) -> torch.Tensor:
+    """mx_gemm_grouped_k with the device-side wait budget in the caller's hands, as mx_gemm_grouped_ex."""
+    return _py_call.gemm_grouped_k_ex(A, sA, B, sB, offsets, M, N, rows, fmtA, fmtB, out, out_dtype, check_status,
+                                      wait_cycles, drop_fill)
 
 
 # ---- host-buffer variants: tensors live in (pinned) host memory ----------------

@@ -1126,15 +1126,16 @@ static int grouped_run(const mx::GroupedArgs& args, const Opts& o) {
   return MX_OK;
 }
 
-int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
-                    void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
-                    mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+int mx_gemm_grouped_ex(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                       void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
+                       mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts, int64_t wait_cycles, int32_t drop_fill) {
   Opts o;
   if (!fmt_ok((int)fmtA) || !fmt_ok((int)fmtB) || !read_opts(opts, &o) ||
       ((int)c_dtype != MX_F32 && (int)c_dtype != MX_BF16))
     return MX_ERR_FMT;
   if (fmtA == MX_INT8 || fmtB == MX_INT8 || o.pad128 || o.layout != MX_SCALES_SWIZZLED) return MX_ERR_UNSUPPORTED;
   if (groups < 0 || rows < 0 || N < 0 || N % 128 || K < 32 || K % 32) return MX_ERR_SHAPE;
+  if (wait_cycles < 0 || drop_fill < -1) return MX_ERR_SHAPE;
   if ((fmt_bits((int)fmtA) < 8 || fmt_bits((int)fmtB) < 8) && K % 128) return MX_ERR_SHAPE;
   if (big(rows + 1024) || big(N) || big(K)) return MX_ERR_SHAPE;
   if (groups > 1024) return MX_ERR_UNSUPPORTED;
@@ -1147,18 +1148,20 @@ int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8
   mx::GroupedArgs a = {};
   a.W = B; a.sW = sB; a.X = A; a.sX = sA; a.offsets = offsets; a.C = C; a.c_bf16 = (int)c_dtype == MX_BF16;
   a.k_groups = 0; a.groups = groups; a.w_rows = N; a.x_rows = rows; a.K = K; a.fmtW = (int)fmtB; a.fmtX = (int)fmtA;
+  a.wait_cycles = wait_cycles; a.drop_fill = drop_fill;
   return grouped_run(a, o);
 }
 
-int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
-                      void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
-                      mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+int mx_gemm_grouped_k_ex(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                         void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
+                         mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts, int64_t wait_cycles, int32_t drop_fill) {
   Opts o;
   if (!fmt_ok((int)fmtA) || !fmt_ok((int)fmtB) || !read_opts(opts, &o) ||
       ((int)c_dtype != MX_F32 && (int)c_dtype != MX_BF16))
     return MX_ERR_FMT;
   if (fmtA == MX_INT8 || fmtB == MX_INT8 || o.pad128 || o.layout != MX_SCALES_SWIZZLED) return MX_ERR_UNSUPPORTED;
   if (groups < 0 || M < 0 || N < 0 || rows < 0 || N % 8 || rows % 32) return MX_ERR_SHAPE;
+  if (wait_cycles < 0 || drop_fill < -1) return MX_ERR_SHAPE;
   if ((fmt_bits((int)fmtA) < 8 || fmt_bits((int)fmtB) < 8) && rows % 128) return MX_ERR_SHAPE;
   if (big(M + 1024) || big(N) || big(rows)) return MX_ERR_SHAPE;
   if (groups > 1024) return MX_ERR_UNSUPPORTED;
@@ -1175,7 +1178,20 @@ int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uin
   mx::GroupedArgs a = {};
   a.W = B; a.sW = sB; a.X = A; a.sX = sA; a.offsets = offsets; a.C = C; a.c_bf16 = (int)c_dtype == MX_BF16;
   a.k_groups = 1; a.groups = groups; a.w_rows = N; a.x_rows = M; a.K = rows; a.fmtW = (int)fmtB; a.fmtX = (int)fmtA;
+  a.wait_cycles = wait_cycles; a.drop_fill = drop_fill;
   return grouped_run(a, o);
+}
+
+int mx_gemm_grouped(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                    void* C, mx_dtype_t c_dtype, int64_t groups, int64_t rows, int64_t N, int64_t K,
+                    mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+  return mx_gemm_grouped_ex(A, sA, B, sB, offsets, C, c_dtype, groups, rows, N, K, fmtA, fmtB, opts, 0, -1);
+}
+
+int mx_gemm_grouped_k(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
+                      void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
+                      mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts) {
+  return mx_gemm_grouped_k_ex(A, sA, B, sB, offsets, C, c_dtype, groups, M, N, rows, fmtA, fmtB, opts, 0, -1);
 }
 
 size_t mx_gemm_host_workspace_bytes(int64_t M, int64_t N, int64_t K, mx_fmt_t fmtA, mx_fmt_t fmtB) {

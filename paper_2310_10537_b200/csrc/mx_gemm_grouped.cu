@@ -49,6 +49,7 @@ constexpr uint32_t kMaxStages = 10;
 constexpr uint32_t kWBytes = 128 * kBK;         // one byte per element in shared memory
 constexpr uint32_t kSortedGroups = 128;
 constexpr uint32_t kXBoxRows = 16;              // rows of X per copy (half a 32-row step per CTA)
+constexpr uint32_t kNoDrop = 0xFFFFFFFFu;       // failure drill off
 
 enum : unsigned int {
   ST_PRODUCER_WAIT = 1,   // a stage never became empty
@@ -64,6 +65,7 @@ struct GroupedParams {
   void* C;
   uint32_t c_bf16, groups, w_rows, x_rows, k_len, k_chunks, k_stages;  // the whole K axis in elements, chunks, stages
   uint32_t max_n, acc_step, shared_half, band, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
+  uint32_t drop_fill;
   long long spin_limit;
 };
 
@@ -255,8 +257,11 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
 
   if (warp == 0 || warp == 3) {
     // ------------------- copies (both CTAs): warp 0 operands, warp 3 scale chunks -------------------
+    // Failure drill (drop_fill != kNoDrop): the operands' fill with that running number is left out in both CTAs -- no copy
+    // is issued and its barrier is not armed -- so that the MMA issuer's wait for it runs out.
     const bool scales = warp == 3;
-    uint32_t stage = 0, phase = 0, g = 0;
+    const uint32_t drop = scales ? kNoDrop : p.drop_fill;
+    uint32_t stage = 0, phase = 0, g = 0, fill = 0;
     bool ok = true;
     Item it;
     for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs) {
@@ -271,7 +276,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
           raise_abort(abort_flag, ST_PRODUCER_WAIT);
           break;
         }
-        if (elect_one()) {
+        if (fill++ != drop && elect_one()) {
           const uint32_t bar = scales ? sf_full_bar(stage) : full_bar(stage), fb = leader_bar(bar);
           if (rank == 0) mbar_arrive_expect_tx(bar, tx);
 #pragma unroll
@@ -534,7 +539,8 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn, uint32_t max_n
   // bytes a copy reports: packed source bytes, rows past the end included
   p.w_box_bytes = (uint32_t)(128 * kBK * fmt_bits(a.fmtW) / 8);
   p.x_box_bytes = (uint32_t)(kXBoxRows * kBK * fmt_bits(a.fmtX) / 8);
-  p.spin_limit = kSpinLimit;
+  p.spin_limit = a.wait_cycles ? a.wait_cycles : kSpinLimit;
+  p.drop_fill = a.drop_fill < 0 ? kNoDrop : (uint32_t)a.drop_fill;
   static bool attr_set[64] = {false};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -206,6 +206,8 @@ struct GroupedArgs {
   int k_groups;  // 0: groups of X rows, each with w_rows rows of W; 1: groups along K
   int64_t groups, w_rows, x_rows, K;
   int fmtW, fmtX;
+  int64_t wait_cycles;  // budget of a wait in clocks; 0: the library's
+  int drop_fill;        // failure drill: the operand copies leave out this fill of a stage; < 0: off
   int sm_count;
   cudaStream_t stream;
 };

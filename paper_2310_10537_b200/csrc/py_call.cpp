@@ -371,7 +371,8 @@ PyObject* moe_combine_backward(Args a) {
 }
 
 // A sA B sB offsets n0 n1 n2 fmtA fmtB out out_dtype check_status; n0 n1 n2 = rows N K, or M N rows
-template <bool KG>
+// EX: wait_cycles drop_fill
+template <bool KG, bool EX>
 PyObject* gemm_grouped(Args a) {
   const at::Tensor &A = *tensor(a[0], "A"), &sA = *tensor(a[1], "sA"), &B = *tensor(a[2], "B"), &sB = *tensor(a[3], "sB");
   const at::Tensor &off = *tensor(a[4], "offsets"), *out = tensor(a[10], "out", true);
@@ -393,12 +394,14 @@ PyObject* gemm_grouped(Args a) {
   void* pc = KG ? need(&c, "out", dev, c.scalar_type(), {groups, n0, n1}) : need(&c, "out", dev, c.scalar_type(), {n0, n1});
   const mx_dtype_t code = float_code(c);
   const mx_opts_t o = options(dev, MX_F32, MX_SCALES_SWIZZLED, small(a[12]) != 0);
+  const int64_t wait = EX ? integer(a[13]) : 0;
+  const int64_t d = EX ? integer(a[14]) : -1;
+  const int drop = d < -1 || d > 1 << 30 ? -2 : (int)d;  // (-2: the library refuses it)
+  const auto call = KG ? mx_gemm_grouped_k_ex : mx_gemm_grouped_ex;
   check(unlocked([&] {
-          return KG ? mx_gemm_grouped_k(pa, (const uint8_t*)psa, pb, (const uint8_t*)psb, po, pc, code, groups, n0, n1, n2,
-                                        (mx_fmt_t)fa, (mx_fmt_t)fb, &o)
-                    : mx_gemm_grouped(pa, (const uint8_t*)psa, pb, (const uint8_t*)psb, po, pc, code, groups, n0, n1, n2,
-                                      (mx_fmt_t)fa, (mx_fmt_t)fb, &o);
-        }), KG ? "mx_gemm_grouped_k" : "mx_gemm_grouped");
+          return call(pa, (const uint8_t*)psa, pb, (const uint8_t*)psb, po, pc, code, groups, n0, n1, n2, (mx_fmt_t)fa,
+                      (mx_fmt_t)fb, &o, wait, drop);
+        }), KG ? (EX ? "mx_gemm_grouped_k_ex" : "mx_gemm_grouped_k") : (EX ? "mx_gemm_grouped_ex" : "mx_gemm_grouped"));
   return out ? given(a[10]) : wrap(made);
 }
 
@@ -439,7 +442,8 @@ PyMethodDef g_methods[] = {
     ENTRY("route", route, 9), ENTRY("route_backward", route_backward, 6),
     ENTRY("moe_plan", moe_plan, 4), ENTRY("moe_gather", moe_gather, 8),
     ENTRY("moe_combine", moe_combine, 4), ENTRY("moe_combine_backward", moe_combine_backward, 4),
-    ENTRY("gemm_grouped", gemm_grouped<false>, 13), ENTRY("gemm_grouped_k", gemm_grouped<true>, 13),
+    ENTRY("gemm_grouped", (gemm_grouped<false, false>), 13), ENTRY("gemm_grouped_k", (gemm_grouped<true, false>), 13),
+    ENTRY("gemm_grouped_ex", (gemm_grouped<false, true>), 15), ENTRY("gemm_grouped_k_ex", (gemm_grouped<true, true>), 15),
     {"set_error_type", set_error_type, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_py_call", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
