@@ -32,6 +32,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "mx.h"
 #include "mx_device.cuh"
 #include "mx_launch.h"
@@ -58,14 +60,17 @@ enum : unsigned int {
   ST_EPILOGUE_WAIT = 4,   // an accumulator never became full
   ST_SCALE_WAIT = 5,      // a stage's scales never landed
 };
-__device__ unsigned int g_grouped_status;
+// What an expired wait leaves behind: a word per stream (see status_word), so that a checked call learns of its own
+// stream's products alone.
+constexpr uint32_t kStatusWords = 128;
+__device__ unsigned int g_grouped_status[kStatusWords];
 
 struct GroupedParams {
   const int32_t* offsets;
   void* C;
   uint32_t c_bf16, groups, w_rows, x_rows, k_len, k_chunks, k_stages;  // the whole K axis in elements, chunks, stages
   uint32_t max_n, acc_step, shared_half, band, stages, sf_per_stage, x_stage_bytes, idesc, w_box_bytes, x_box_bytes;
-  uint32_t drop_fill;
+  uint32_t drop_fill, status_word;
   long long spin_limit;
 };
 
@@ -141,8 +146,8 @@ __device__ __forceinline__ uint32_t sane_offset(const GroupedParams& p, int32_t 
   return v >= p.x_rows ? p.x_rows : (v & ~63u);
 }
 
-__device__ __forceinline__ void raise_abort(volatile uint32_t* abort_flag, unsigned int code) {
-  atomicCAS(&g_grouped_status, 0u, code);
+__device__ __forceinline__ void raise_abort(const GroupedParams& p, volatile uint32_t* abort_flag, unsigned int code) {
+  atomicCAS(&g_grouped_status[p.status_word], 0u, code);
   *abort_flag = 1u;
 }
 
@@ -273,7 +278,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       for (uint32_t kc = 0; kc < it.nk; ++kc) {
         ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.spin_limit);
         if (!ok) {
-          raise_abort(abort_flag, ST_PRODUCER_WAIT);
+          raise_abort(p, abort_flag, ST_PRODUCER_WAIT);
           break;
         }
         if (fill++ != drop && elect_one()) {
@@ -317,7 +322,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
         for (uint32_t kc = 0; kc < it.nk; ++kc) {
           ok = mbar_wait_warp(sf_full_bar(stage), phase, abort_flag, p.spin_limit);
           if (!ok) {
-            raise_abort(abort_flag, ST_SCALE_WAIT);
+            raise_abort(p, abort_flag, ST_SCALE_WAIT);
             break;
           }
           tc_fence_after();
@@ -346,7 +351,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
       for (uint32_t t = pair; ok && next_item<KG>(p, tb, t, g, it); t += num_pairs, ++i) {
         if (!__all_sync(0xffffffffu, mbar_wait(acc_empty_bar(acc_bar_index(i)), acc_parity(i) ^ 1u, abort_flag,
                                                4 * p.spin_limit))) {
-          raise_abort(abort_flag, ST_MMA_WAIT_ACC);
+          raise_abort(p, abort_flag, ST_MMA_WAIT_ACC);
           break;
         }
         tc_fence_after();
@@ -358,7 +363,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
           ok = __all_sync(0xffffffffu, mbar_wait((lane & 1u) ? full_bar(stage) : sf_ready_bar(stage), phase, abort_flag,
                                                  p.spin_limit));
           if (!ok) {
-            raise_abort(abort_flag, ST_MMA_WAIT_FULL);
+            raise_abort(p, abort_flag, ST_MMA_WAIT_FULL);
             break;
           }
           tc_fence_after();
@@ -390,7 +395,7 @@ mx_gemm_grouped_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_
     Item it;
     for (uint32_t t = pair; next_item<KG>(p, tb, t, g, it); t += num_pairs, ++i) {
       if (!mbar_wait_warp(acc_full_bar(i & 1u), (i >> 1) & 1u, abort_flag, 4 * p.spin_limit)) {
-        if (lane == 0) raise_abort(abort_flag, ST_EPILOGUE_WAIT);
+        if (lane == 0) raise_abort(p, abort_flag, ST_EPILOGUE_WAIT);
         break;
       }
       tc_fence_after();
@@ -504,6 +509,23 @@ bool scale_map(EncodeTiledFn fn, CUtensorMap* map, const void* ptr, uint64_t row
                 {512, 512 * k_chunks}, {128, 1, chunks}, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+// The status word of a stream of device `dev`: a table of stream handles, entered without a lock.  When more streams
+// have come than there are words, a word serves several of them, and a checked call may also report a
+// failure of another of those.
+uint32_t status_word(int dev, cudaStream_t stream) {
+  static std::atomic<uintptr_t> table[64][kStatusWords];
+  const uintptr_t key = (uintptr_t)stream + 1;  // (the default stream is 0)
+  const uint32_t start = (uint32_t)((key >> 4) * 2654435761u >> 16) % kStatusWords;
+  if (dev < 0 || dev >= 64) return start;
+  for (uint32_t i = 0; i < kStatusWords; ++i) {
+    std::atomic<uintptr_t>& slot = table[dev][(start + i) % kStatusWords];
+    uintptr_t have = slot.load(std::memory_order_relaxed);
+    if (have == 0 && slot.compare_exchange_strong(have, key, std::memory_order_relaxed)) have = key;
+    if (have == key) return (start + i) % kStatusWords;
+  }
+  return start;
+}
+
 template <bool KG, uint32_t KCH>
 cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn, uint32_t max_n) {
   CUtensorMap mw, mx_, mxf, msw, msx;
@@ -550,6 +572,7 @@ cudaError_t launch_kernel(const GroupedArgs& a, EncodeTiledFn fn, uint32_t max_n
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) attr_set[dev] = true;
   }
+  p.status_word = status_word(dev, a.stream);
   // no more pairs than items there can be: every group at most one tile more than its share of rows
   const int64_t w_tiles = (a.w_rows + 255) / 256;
   const int64_t most = KG ? a.groups * w_tiles * ((a.x_rows + p.max_n - 1) / p.max_n)
@@ -577,13 +600,18 @@ int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err) {
   return *cuda_err == cudaSuccess ? MX_OK : MX_ERR_CUDA;
 }
 
-// Reads and clears the device status word (synchronises the stream first).
+// Reads and clears the stream's status word, after what has been launched on the stream.
 int gemm_grouped_status(cudaStream_t stream, unsigned int* out, cudaError_t* cuda_err) {
-  *cuda_err = cudaStreamSynchronize(stream);
-  if (*cuda_err == cudaSuccess) *cuda_err = cudaMemcpyFromSymbol(out, g_grouped_status, sizeof(unsigned int));
+  int dev = 0;
+  *cuda_err = cudaGetDevice(&dev);
+  const size_t at = sizeof(unsigned int) * status_word(dev, stream);
+  const unsigned int zero = 0;
+  if (*cuda_err == cudaSuccess)
+    *cuda_err = cudaMemcpyFromSymbolAsync(out, g_grouped_status, sizeof(unsigned int), at, cudaMemcpyDeviceToHost, stream);
+  if (*cuda_err == cudaSuccess) *cuda_err = cudaStreamSynchronize(stream);
   if (*cuda_err == cudaSuccess && *out != 0) {
-    const unsigned int zero = 0;
-    *cuda_err = cudaMemcpyToSymbol(g_grouped_status, &zero, sizeof(unsigned int));
+    *cuda_err = cudaMemcpyToSymbolAsync(g_grouped_status, &zero, sizeof(unsigned int), at, cudaMemcpyHostToDevice, stream);
+    if (*cuda_err == cudaSuccess) *cuda_err = cudaStreamSynchronize(stream);
   }
   return *cuda_err == cudaSuccess ? MX_OK : MX_ERR_CUDA;
 }
