@@ -4,7 +4,7 @@ Argument marshalling only: every function takes torch tensors (or raw
 pointers), passes ``data_ptr()`` and the current CUDA stream to the C entry point
 of the same name and raises :class:`MxError` on a nonzero status.  The norm, routing,
 row-moving and grouped-product calls, whose GPU time may be a few microseconds, are
-marshalled in C++ (``csrc/py_call.cpp``).  PyTorch owns
+marshalled in C++ (``csrc/py_call.cpp``; without that module they raise ImportError).  PyTorch owns
 the memory; all arithmetic runs in the library's CUDA kernels.  If the shared
 library is missing the import of this module fails -- there is no fallback.
 """
@@ -15,6 +15,8 @@ import os
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
+
+from . import build as _build
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmx_b200.so")
@@ -158,9 +160,33 @@ def _load() -> ctypes.CDLL:
 
 _lib = _load()
 
-from . import _py_call  # noqa: E402  (it links against the library loaded above)
 
-_py_call.set_error_type(MxError)
+
+class _NoPyCall:
+    """Stands for the marshalling module where it cannot be used: the calls that need it raise, all others work."""
+
+    def __init__(self, why: str):
+        self._why = why
+
+    def __getattr__(self, name: str):
+        raise ImportError(f"{name} needs {os.path.join(os.path.dirname(LIB_PATH), '_py_call.so')}, {self._why}: build it with "
+                          "`python paper_2310_10537_b200/build.py` (there is no fallback)")
+
+
+def _load_py_call():
+    """csrc/py_call.cpp (it links against the library loaded above, and against the C++ interfaces of one torch)."""
+    try:
+        from . import _py_call as module
+    except ImportError as e:
+        return _NoPyCall(f"which cannot be loaded ({e})")
+    here = _build.py_call_for()
+    if module.compiled_for != here:
+        return _NoPyCall(f"which was compiled for {module.compiled_for}, not for {here}")
+    module.set_error_type(MxError)
+    return module
+
+
+_py_call = _load_py_call()
 
 
 def lib() -> ctypes.CDLL:

@@ -13,6 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmx_b200.so")
 PY_CALL = os.path.join(HERE, "_py_call.so")  # the Python side's marshalling module (csrc/py_call.cpp)
 BUILD = os.path.join(HERE, "build")
+STAMP = os.path.join(BUILD, "py_call.stamp")  # the interpreter and torch that module was compiled for
 SOURCES = ["mx_api.cu", "mx_quantize.cu", "mx_quantize_dual.cu", "mx_quantize_tile.cu", "mx_dequantize.cu",
            "mx_gemm.cu", "mx_im2col.cu", "mx_rmsnorm.cu", "mx_route.cu", "mx_moe.cu", "mx_gemm_grouped.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -22,6 +23,29 @@ NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a",
 def _newest_source() -> float:
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "mx.h")]
     return max(os.path.getmtime(f) for f in files)
+
+
+def py_call_for() -> str:
+    """What the marshalling module depends on beside its sources: the C++ interfaces of this interpreter and torch.
+    Empty without torch."""
+    try:
+        import torch
+    except ImportError:
+        return ""
+    return f"python {sys.version_info[0]}.{sys.version_info[1]}, torch {torch.__version__}"
+
+
+def _stale_py_call() -> bool:
+    """The marshalling module is missing, older than a source or compiled for another interpreter or torch."""
+    want = py_call_for()
+    if not want:
+        return False  # nobody here can call it
+    if not os.path.exists(PY_CALL) or not os.path.exists(STAMP):
+        return True
+    if os.path.getmtime(PY_CALL) < max(os.path.getmtime(f) for f in (os.path.join(CSRC, "py_call.cpp"), os.path.join(ROOT, "include", "mx.h"))):
+        return True
+    with open(STAMP) as f:
+        return f.read() != want
 
 
 def _compile(src: str, verbose: bool) -> str:
@@ -49,32 +73,34 @@ def _build_py_call() -> None:
     inc = [*include_paths(), sysconfig.get_paths()["include"], cuda_inc, os.path.join(ROOT, "include")]
     tmp = PY_CALL + f".tmp{os.getpid()}"
     subprocess.check_call(["g++", "-std=c++20", "-O2", "-fPIC", "-shared", "-fvisibility=hidden",
-                           os.path.join(CSRC, "py_call.cpp"), "-o", tmp,
+                           f'-DMX_PY_CALL_FOR="{py_call_for()}"', os.path.join(CSRC, "py_call.cpp"), "-o", tmp,
                            *[f for i in inc for f in ("-isystem", i)], "-L", lib_dir, "-L", HERE, "-Wl,-rpath,$ORIGIN",
                            "-lmx_b200", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     os.replace(tmp, PY_CALL)
+    with open(STAMP, "w") as f:
+        f.write(py_call_for())
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every kernel file, link ``libmx_b200.so`` next to this module and compile the marshalling
-    module against it."""
-    built = os.path.exists(LIB) and os.path.exists(PY_CALL)
-    if not force and built and min(os.path.getmtime(LIB), os.path.getmtime(PY_CALL)) >= _newest_source():
-        return LIB
-    if not force and built and shutil.which("nvcc") is None:
-        return LIB  # no compiler on this machine: use the library that was shipped
+    """Compile every kernel file and link ``libmx_b200.so`` next to this module; where there is a torch, compile the
+    marshalling module against it (again when torch or the interpreter has changed)."""
+    have_lib = not force and os.path.exists(LIB)
+    if have_lib and shutil.which("nvcc") is None:
+        return LIB  # no compiler on this machine: use what was shipped
     os.makedirs(BUILD, exist_ok=True)
-    if force:
-        for f in os.listdir(BUILD):
-            if f.endswith(".o"):
-                os.remove(os.path.join(BUILD, f))
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-    tmp = LIB + f".tmp{os.getpid()}"
-    subprocess.check_call(["nvcc", "-shared", "-cudart", "static", "-gencode",
-                           "arch=compute_100a,code=sm_100a", "-o", tmp, *objs])
-    os.replace(tmp, LIB)
-    _build_py_call()
+    if not have_lib or os.path.getmtime(LIB) < _newest_source():
+        if force:
+            for f in os.listdir(BUILD):
+                if f.endswith(".o"):
+                    os.remove(os.path.join(BUILD, f))
+        with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+            objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        tmp = LIB + f".tmp{os.getpid()}"
+        subprocess.check_call(["nvcc", "-shared", "-cudart", "static", "-gencode",
+                               "arch=compute_100a,code=sm_100a", "-o", tmp, *objs])
+        os.replace(tmp, LIB)
+    if (force and py_call_for()) or _stale_py_call():
+        _build_py_call()
     return LIB
 
 

@@ -450,4 +450,12 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_py_call", nullptr, -1, g_method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__py_call(void) { return PyModule_Create(&g_module); }
+#ifndef MX_PY_CALL_FOR
+#define MX_PY_CALL_FOR ""
+#endif
+PyMODINIT_FUNC PyInit__py_call(void) {
+  PyObject* m = PyModule_Create(&g_module);
+  // the interpreter and torch whose C++ interfaces this was compiled against: binding.py compares them
+  if (m && PyModule_AddStringConstant(m, "compiled_for", MX_PY_CALL_FOR) < 0) Py_CLEAR(m);
+  return m;
+}
