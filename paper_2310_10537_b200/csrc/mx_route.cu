@@ -837,13 +837,15 @@ cudaError_t launch_part(const RouteParams& p, bool backward, cudaStream_t stream
 
 template <int DTYPE>
 cudaError_t launch_dtype(const RouteParams& p, bool backward, cudaStream_t stream) {
-  // A few lanes per token.  Few experts need many tokens for it to pay: 8 experts, top-2, 2048 tokens 2.6 us (a
-  // warp per token 2.3), 4096 2.6 (3.0); 64 experts, top-6, 1024 tokens 3.0 (2.6), 2048 3.1 (3.6).
-  // With more than 128 always: 256 in 8 groups, 16 tokens 3.0 (3.9), 160 in 8 groups, 16384 tokens 14.5 (18.3); with a token
-  // per warp it has little to share and may lose a little (512 ungrouped, 16384 tokens 16.8 (16.3), 384 in 8 groups 34.7 (33.6)).
-  // Gradient: 64 experts, 16 tokens 2.4 (2.1), 2048 2.5 (2.6); 128 experts 2.1 (2.2), 16384 tokens 4.7 (6.9).
+  // A few lanes per token, or a warp (in parentheses; us).  Few tokens are a matter of one token's latency, which is
+  // the warp's: 8 experts, top-2, 2048 tokens 2.7 (2.3), 4096 2.7 (2.9); 64, top-8, 1024 3.2 (2.8), 2048 3.3 (3.9); 256, top-8,
+  // 16 2.9 (2.8), in 8 groups, sigmoid and bias 1024 3.8 (3.7), 2048 5.5 (6.1), 65536 40 (52).  (Top-2 gains less: 256, sigmoid and bias
+  // 4096 6.4 (5.1), 65536 32.5 (32.8).)  With more than 256 a lane of the warp has 16 keys either way, and what is left is
+  // the sorting networks': 512, top-8, 16 2.8 (3.0), 16384 14.8 (15.7); 384 in 8 groups, 1024 6.2 (8.1); it loses at most 5 % where the
+  // groups are no power of two of whole lanes (320 in 8, 65536 99 (95)).
+  // Gradient: 64 experts, 1024 tokens 2.4 (2.2), 2048 2.4 (2.5); 128, 16 2.1 (2.2), 16384 5.0 (6.8).
   const bool enough = backward ? p.experts > 64 || p.tokens >= 2048u
-                               : p.experts > 128 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
+                               : p.experts > 256 || p.tokens >= (p.experts > 32 ? 2048u : 4096u);
   if (enough && p.topk <= kPartK && p.experts % 4 == 0 && p.experts <= 32 * kPartKeys &&
       (backward || (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0)) {
     if (p.experts <= 2 * kPartKeys) return launch_part<DTYPE, 2>(p, backward, stream);
