@@ -22,10 +22,11 @@
 //               whole ones and the scales do not fit), and the half both use is drained first
 // (Scale copies issued by the MMA thread right before their MMAs wait in line behind the MMAs of the
 // stage before and then hold up their own: 65536 x 4096 x 4096 over 32 groups took 1155 us that way.)
-// What bounds it: large groups the power limit -- 65536 x 4096 x 4096 over 32 groups 827 us, 2.66 PFLOP/s, at
-// 1.29 GHz; of its cycles 86 % are MMAs, 2 % the hand-over of accumulators, and a stage takes 573 clocks instead of 512.
-// Weight gradients 4096 x 2048 over 16 groups of 2048 rows: 207 to 262 us by the clock (1.29 GHz), 81 % MMAs.  128 rows on
-// 56 experts of 2048 x 4096, FP4 weights: 55.9 us, 4.5 TB/s of weights; 448 tiles on 74 pairs are seven rounds of which the
+// What bounds it: large groups the power limit -- 65536 x 4096 x 4096 over 32 groups 820 to 1012 us by the state of the
+// board, 2.2 to 2.7 PFLOP/s, at 1.29 GHz; of its cycles 86 % are MMAs, 2 % the hand-over of accumulators, and a stage takes 573
+// clocks instead of 512.  Weight gradients 4096 x 2048 over 16 groups of 2048 rows, BF16 out: 207 to 273 us; an item has half as many
+// stages, so the hand-overs and the epilogue's stores count twice: 81 % MMAs at the same clock (FP32 out 67 to 69 %, at 1.36).  128 rows on
+// 56 experts of 2048 x 4096, FP4 weights: 55.7 to 60.7 us, 4.1 to 4.5 TB/s of weights; 448 tiles on 74 pairs are seven rounds of which the
 // last holds 4, and a stage's copies and hand-overs take longer than its bytes.
 // Every wait is bounded (see mbar_wait); on expiry a status word is set and all roles fall through to
 // the common exit.
@@ -588,7 +589,7 @@ int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err) {
   EncodeTiledFn fn = encode_fn(cuda_err);
   if (!fn) return MX_ERR_CUDA;
   // The widest tile.  256 columns move the fewest operand bytes per MAC, which is what bounds large groups
-  // (65536 x 4096 x 4096 over 32 groups: 943 us with 192, 835 with 256).  Groups that hold 64
+  // (65536 x 4096 x 4096 over 32 groups: 943 us with 192, 835 with 256 on the same board; 820 to 1012 by the state of the board).  Groups that hold 64
   // rows on average take tiles of 64: a stage is then smaller and more of W is in flight, which is what
   // bounds a product with few rows; two K chunks share a stage there, since the hand-overs of a stage of
   // one chunk take as long as its copies (128 rows on 56 experts of 2048 x 4096: FP4 weights 66.9 -> 57.1 us

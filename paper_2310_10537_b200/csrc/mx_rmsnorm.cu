@@ -5,8 +5,8 @@
 // Forward: one CTA per row.  The row is read once and stays in registers (FP32) while its sum of
 // squares is formed, so that the traffic is x, residual in and h, codes, scales out; a thread holds
 // groups of 8 consecutive elements, four neighbouring lanes an MX block, whose maximum takes two
-// shuffles.  y is never rounded before Algorithm 1.  Bound by memory: 8192 x 8192 BF16 with residual, E4M3 out, 77.7 us,
-// 6.07 TB/s of those bytes (a copy: 6.46); 16 x 4096 2.6 us, of which launch, two barriers and one latency of memory.
+// shuffles.  y is never rounded before Algorithm 1.  Bound by memory: 8192 x 8192 BF16 with residual, E4M3 out, 77.7 to 84.1 us,
+// 5.6 to 6.07 TB/s of those bytes (a copy: 6.46); 8192 x 4096 40.7 us; 16 x 4096 2.6 us, of which launch, two barriers and one latency of memory.
 #include <cuda_runtime.h>
 
 #include "mx.h"
