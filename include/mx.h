@@ -11,7 +11,8 @@
  *
  * and what a mixture-of-experts transformer layer needs between its products: the RMS norm that
  * ends in an MX tensor, routing, moving MX rows to their experts and back, and products over ragged
- * groups of rows -- each with the gradient that training needs.
+ * groups of rows -- each with the gradient that training needs; and for serving a paged key-value cache of
+ * MX rows, written, read back and attended over.
  *
  * An MX block is k = 32 elements P_i that share one E8M0 scale X = 2^(byte-127)
  * (Section 2, Table 1).  Element formats: FP8 E4M3 / E5M2, FP6 E3M2 / E2M3,
@@ -587,6 +588,90 @@ int mx_gemm_grouped_ex(const void* A, const uint8_t* sA, const void* B, const ui
 int mx_gemm_grouped_k_ex(const void* A, const uint8_t* sA, const void* B, const uint8_t* sB, const int32_t* offsets,
                          void* C, mx_dtype_t c_dtype, int64_t groups, int64_t M, int64_t N, int64_t rows,
                          mx_fmt_t fmtA, mx_fmt_t fmtB, const mx_opts_t* opts, int64_t wait_cycles, int32_t drop_fill);
+
+/* ------------------------------------------------------------------------- */
+/* Paged key-value cache in MX format                                        */
+/* ------------------------------------------------------------------------- */
+/*
+ * What attention keeps of every token, quantized as it is written.  A cache is four DEVICE tensors the
+ * caller owns, keys and values alike:
+ *   codes   [pages x heads x page_size] rows of `dim` element codes (dim * bits / 8 bytes)
+ *   scales  [pages x heads x page_size] rows of E8M0 bytes, one per block of 32 elements, filled up with
+ *           zero bytes to whole 32-bit words: 4 * ceil(dim / 128) bytes a row
+ * An MX block lies along a head's row, the axis that the products with the queries reduce over and the
+ * only one a single token fills.  Token `offset` of page p is slot p * page_size + offset.
+ *   dim a nonzero multiple of 32; page_size >= 1 (any, also one that is no power of two); fmt an 8- or 4-bit
+ *   format (6-bit rows are no whole 16-byte units: MX_ERR_UNSUPPORTED); all four tensors 16-byte
+ *   aligned; pages * page_size below 2^31 and pages * page_size * heads below 2^32 - 1.
+ * mx_kv_elems_bytes / mx_kv_scales_bytes: bytes of one codes and one scales tensor (the pointers may be
+ * NULL there); 0 on bad arguments.
+ */
+typedef struct {
+  void* k_elems;
+  uint8_t* k_scales;
+  void* v_elems;
+  uint8_t* v_scales;
+  int64_t pages, page_size, heads, dim;
+  int32_t fmt;   /* mx_fmt_t */
+} mx_kv_t;
+size_t mx_kv_elems_bytes(const mx_kv_t* kv);
+size_t mx_kv_scales_bytes(const mx_kv_t* kv);
+
+/*
+ * mx_kv_append -- quantize the rows of new tokens into their slots.
+ *   k, v     [tokens x heads x dim] of opts->dtype; rows of one token contiguous, tokens k_stride and
+ *            v_stride elements apart (>= heads * dim; a projection's output is read in place).  16-byte
+ *            aligned, strides multiples of 16 bytes
+ *   slots    int32 [tokens]; a slot outside [0, pages * page_size) is a token that is not written
+ * Codes and scale bytes are what mx_quantize writes for those rows along their last axis.  No other slot's
+ * bytes change.  Slots of one call have to differ: what two tokens leave in the same slot is either one's
+ * codes with either one's scales.
+ *
+ * mx_kv_read -- the cached rows as numbers: k_out[i], v_out[i] = rows of slots[i], values as
+ * mx_dequantize gives them, contiguous [tokens x heads x dim] of opts->dtype (16-byte aligned); zeros for a
+ * slot outside the cache.
+ *
+ * Of opts dtype and stream are used.  Errors of both: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN,
+ * MX_ERR_UNSUPPORTED (6-bit formats, pad_k128, a cache beyond the limits above, tokens * heads * dim of
+ * 2^34 or more), MX_ERR_CUDA.  tokens == 0 is a no-op.
+ */
+int mx_kv_append(const mx_kv_t* kv, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                 const int32_t* slots, int64_t tokens, mx_round_t rounding, const mx_opts_t* opts);
+int mx_kv_read(const mx_kv_t* kv, const int32_t* slots, int64_t tokens, void* k_out, void* v_out,
+               const mx_opts_t* opts);
+
+/*
+ * mx_kv_attention -- attention of the newest tokens of every sequence over its cached ones.
+ *   q        queries [batch x new_tokens x q_heads x dim] of opts->dtype; tokens (of all sequences in
+ *            order) q_stride elements apart (>= q_heads * dim), 16-byte aligned, stride a multiple of 16 bytes
+ *   table    int32 [batch x max_pages]: token j of sequence b lies in page table[b][j / page_size], at offset
+ *            j % page_size.  An entry outside [0, pages) is a page whose tokens nobody sees
+ *   lengths  int32 [batch]: cached tokens of each sequence, the new ones counted (they are appended first);
+ *            taken as 0 below 0 and as max_pages * page_size above that
+ *   query i of new_tokens is token lengths[b] - new_tokens + i and sees the tokens up to itself, with
+ *   window > 0 only the last `window` of them.  Query head a reads key-value head a / (q_heads / heads).
+ *     s_j = scale * <q, K_j>;   out = sum_j e^{s_j} V_j / sum_j e^{s_j};   lse = ln sum_j e^{s_j}
+ *   out      [batch x new_tokens x q_heads x dim] of opts->dtype, contiguous, 16-byte aligned
+ *   lse      NULL, or FP32 [batch x new_tokens x q_heads]
+ * A query that sees no token gets out = 0 and lse = -Inf.  K and V are the values mx_dequantize gives; scores,
+ * maxima and sums are FP32.  What lies in slots that no query sees (NaN scales, stale codes) has no influence.
+ *   workspace  mx_kv_attention_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and
+ *              after; two calls that may overlap need one each
+ * dim 64, 96, 128, 192 or 256; q_heads a multiple of heads; scale finite; batch * new_tokens * q_heads below
+ * 2^31, max_pages * page_size below 2^31.
+ * Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN, MX_ERR_UNSUPPORTED (another dim, 6-bit
+ * formats, pad_k128, extents beyond the limits), MX_ERR_WORKSPACE, MX_ERR_CUDA.
+ */
+typedef struct {
+  int64_t batch, new_tokens, q_heads, max_pages;
+  int64_t q_stride;
+  int64_t window;   /* 0: every token up to the query */
+  float scale;
+} mx_kv_attention_t;
+size_t mx_kv_attention_workspace_bytes(const mx_kv_t* kv, const mx_kv_attention_t* attn);
+int mx_kv_attention(const mx_kv_t* kv, const mx_kv_attention_t* attn, const void* q, const int32_t* table,
+                    const int32_t* lengths, void* out, float* lse, const mx_opts_t* opts, void* workspace,
+                    size_t workspace_bytes);
 
 /* ------------------------------------------------------------------------- */
 /* Host-buffer variants                                                      */

@@ -3,7 +3,7 @@
 Argument marshalling only: every function takes torch tensors (or raw
 pointers), passes ``data_ptr()`` and the current CUDA stream to the C entry point
 of the same name and raises :class:`MxError` on a nonzero status.  The norm, routing,
-row-moving and grouped-product calls, whose GPU time may be a few microseconds, are
+row-moving, grouped-product and cache calls, whose GPU time may be a few microseconds, are
 marshalled in C++ (``csrc/py_call.cpp``; without that module they raise ImportError).  PyTorch owns
 the memory; all arithmetic runs in the library's CUDA kernels.  If the shared
 library is missing the import of this module fails -- there is no fallback.
@@ -48,6 +48,8 @@ EXPORTS = [
     "mx_route_backward", "mx_moe_rows", "mx_moe_plan_workspace_bytes", "mx_moe_plan", "mx_moe_gather",
     "mx_moe_combine", "mx_moe_combine_backward", "mx_gemm_grouped", "mx_gemm_grouped_k",
     "mx_gemm_grouped_ex", "mx_gemm_grouped_k_ex",
+    "mx_kv_elems_bytes", "mx_kv_scales_bytes", "mx_kv_append", "mx_kv_read", "mx_kv_attention_workspace_bytes",
+    "mx_kv_attention",
 ]
 
 
@@ -75,6 +77,18 @@ class mx_route_t(ctypes.Structure):
     _fields_ = [("topk", ctypes.c_int32), ("score", ctypes.c_int32), ("groups", ctypes.c_int32),
                 ("topk_groups", ctypes.c_int32), ("group_score", ctypes.c_int32),
                 ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class mx_kv_t(ctypes.Structure):
+    _fields_ = [("k_elems", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_elems", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("heads", ctypes.c_int64), ("dim", ctypes.c_int64), ("fmt", ctypes.c_int32)]
+
+
+class mx_kv_attention_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("new_tokens", ctypes.c_int64), ("q_heads", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("window", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
 
 
 class MxError(RuntimeError):
@@ -155,6 +169,16 @@ def _load() -> ctypes.CDLL:
     lib.mx_gemm_grouped_k.argtypes = [vp, u8p, vp, u8p, vp, vp, ci, i64, i64, i64, i64, ci, ci, op]
     lib.mx_gemm_grouped_ex.argtypes = lib.mx_gemm_grouped.argtypes + [i64, ctypes.c_int32]
     lib.mx_gemm_grouped_k_ex.argtypes = lib.mx_gemm_grouped_k.argtypes + [i64, ctypes.c_int32]
+    kp, ap = ctypes.POINTER(mx_kv_t), ctypes.POINTER(mx_kv_attention_t)
+    lib.mx_kv_elems_bytes.argtypes = [kp]
+    lib.mx_kv_elems_bytes.restype = sz
+    lib.mx_kv_scales_bytes.argtypes = [kp]
+    lib.mx_kv_scales_bytes.restype = sz
+    lib.mx_kv_append.argtypes = [kp, vp, vp, i64, i64, vp, i64, ci, op]
+    lib.mx_kv_read.argtypes = [kp, vp, i64, vp, vp, op]
+    lib.mx_kv_attention_workspace_bytes.argtypes = [kp, ap]
+    lib.mx_kv_attention_workspace_bytes.restype = sz
+    lib.mx_kv_attention.argtypes = [kp, ap, vp, vp, vp, vp, vp, op, vp, sz]
     return lib
 
 
@@ -563,6 +587,54 @@ def mx_gemm_grouped_k_ex(A: torch.Tensor, sA: torch.Tensor, B: torch.Tensor, sB:
     """mx_gemm_grouped_k with the device-side wait budget in the caller's hands, as mx_gemm_grouped_ex."""
     return _py_call.gemm_grouped_k_ex(A, sA, B, sB, offsets, M, N, rows, fmtA, fmtB, out, out_dtype, check_status,
                                       wait_cycles, drop_fill)
+
+
+# ---- paged key-value cache ------------------------------------------------------------
+
+class KvCache(NamedTuple):
+    """A paged cache of keys and values in MX format: codes [pages, heads, page_size, dim * bits / 8] and scale bytes
+    [pages, heads, page_size, 4 * ceil(dim / 128)], uint8, keys and values alike.  Token ``offset`` of page p is slot
+    p * page_size + offset."""
+    k_elems: torch.Tensor
+    k_scales: torch.Tensor
+    v_elems: torch.Tensor
+    v_scales: torch.Tensor
+    dim: int
+    fmt: int
+
+
+def mx_kv_cache(pages: int, page_size: int, heads: int, dim: int, fmt: int, device="cuda") -> KvCache:
+    """An empty cache (all bytes zero) for ``pages`` pages of ``page_size`` tokens."""
+    desc = mx_kv_t(None, None, None, None, pages, page_size, heads, dim, fmt)
+    rows = pages * heads * page_size
+    if rows and not _lib.mx_kv_elems_bytes(ctypes.byref(desc)):
+        raise ValueError(f"no cache of {pages} pages x {heads} heads x {page_size} tokens x {dim} in format {fmt}")
+    code, scale = dim * mx_fmt_bits(fmt) // 8, (dim + 127) // 128 * 4
+    zeros = lambda n: torch.zeros((pages, heads, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
+    return KvCache(zeros(code), zeros(scale), zeros(code), zeros(scale), dim, fmt)
+
+
+def mx_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rounding: int = MX_RNE) -> None:
+    """Quantize the rows ``k``, ``v`` [tokens, heads, dim] into the slots ``slots`` (int32 [tokens], all different; one
+    outside the cache: not written).  Tokens may be evenly spaced parts of a wider tensor."""
+    _py_call.kv_append(cache, k, v, slots, rounding)
+
+
+def mx_kv_read(cache: KvCache, slots: torch.Tensor, dtype: torch.dtype = torch.float32,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values of ``slots`` as numbers, (k, v) [tokens, heads, dim]; zeros for a slot outside the cache."""
+    out_k, out_v = (None, None) if out is None else out
+    return _py_call.kv_read(cache, slots, dtype, out_k, out_v)
+
+
+def mx_kv_attention(q: torch.Tensor, cache: KvCache, table: torch.Tensor, lengths: torch.Tensor,
+                    scale: Optional[float] = None, window: int = 0, return_lse: bool = False,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Attention of the newest tokens ``q`` [batch, heads, dim], or [batch, new tokens, heads, dim], over the cached
+    tokens of their sequences: sequence b has ``lengths[b]`` tokens (the new ones included) in the pages ``table[b]``
+    (int32 [batch, pages of a sequence]).  ``scale`` defaults to dim ** -0.5; ``window`` > 0: a query sees its last
+    ``window`` tokens only.  Returns out, shaped as q, or (out, lse)."""
+    return _py_call.kv_attention(q, cache, table, lengths, scale, window, return_lse, out, workspace)
 
 
 # ---- host-buffer variants: tensors live in (pinned) host memory ----------------

@@ -15,7 +15,8 @@ PY_CALL = os.path.join(HERE, "_py_call.so")  # the Python side's marshalling mod
 BUILD = os.path.join(HERE, "build")
 STAMP = os.path.join(BUILD, "py_call.stamp")  # the interpreter and torch that module was compiled for
 SOURCES = ["mx_api.cu", "mx_quantize.cu", "mx_quantize_dual.cu", "mx_quantize_tile.cu", "mx_dequantize.cu",
-           "mx_gemm.cu", "mx_im2col.cu", "mx_rmsnorm.cu", "mx_route.cu", "mx_moe.cu", "mx_gemm_grouped.cu"]
+           "mx_gemm.cu", "mx_im2col.cu", "mx_rmsnorm.cu", "mx_route.cu", "mx_moe.cu", "mx_gemm_grouped.cu",
+           "mx_kv.cu", "mx_kv_attention.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

@@ -1105,6 +1105,137 @@ int mx_moe_combine_backward(const void* dout, const void* y, const float* weight
   return e == cudaSuccess ? MX_OK : fail_cuda(e);
 }
 
+// The cache's own rules; `pointers`: the tensors have to be there.
+static int kv_validate(const mx_kv_t* kv, bool pointers) {
+  if (!kv) return MX_ERR_NULL;
+  if (!fmt_ok(kv->fmt)) return MX_ERR_FMT;
+  if (kv->pages < 0 || kv->page_size < 1 || kv->heads < 1 || kv->dim < 32 || kv->dim % 32) return MX_ERR_SHAPE;
+  int64_t slots, rows, elems;
+  if (__builtin_mul_overflow(kv->pages, kv->page_size, &slots) || __builtin_mul_overflow(slots, kv->heads, &rows) ||
+      __builtin_mul_overflow(rows, kv->dim, &elems) || elems > kMaxElements)
+    return MX_ERR_SHAPE;
+  if (fmt_bits(kv->fmt) == 6 || big(slots) || rows >= 0xFFFFFFFFll || big(kv->page_size) || big(kv->heads) || big(kv->dim))
+    return MX_ERR_UNSUPPORTED;
+  if (pointers && slots > 0 && (!kv->k_elems || !kv->k_scales || !kv->v_elems || !kv->v_scales)) return MX_ERR_NULL;
+  return MX_OK;
+}
+static bool kv_misaligned(const mx_kv_t* kv) {
+  return misaligned16(kv->k_elems) || misaligned16(kv->v_elems) || misaligned16(kv->k_scales) || misaligned16(kv->v_scales);
+}
+static mx::KvArgs kv_args(const mx_kv_t* kv) {
+  return {(uint8_t*)kv->k_elems, kv->k_scales, (uint8_t*)kv->v_elems, kv->v_scales,
+          kv->pages, kv->page_size, kv->heads, kv->dim, kv->fmt};
+}
+
+size_t mx_kv_elems_bytes(const mx_kv_t* kv) {
+  if (kv_validate(kv, false) != MX_OK) return 0;
+  return (size_t)(kv->pages * kv->heads * kv->page_size) * (size_t)(kv->dim * fmt_bits(kv->fmt) / 8);
+}
+size_t mx_kv_scales_bytes(const mx_kv_t* kv) {
+  if (kv_validate(kv, false) != MX_OK) return 0;
+  return (size_t)(kv->pages * kv->heads * kv->page_size) * (size_t)((kv->dim + 127) / 128 * 4);
+}
+
+// What mx_kv_append and mx_kv_read ask of their extents alike.
+static int kv_move_validate(const mx_kv_t* kv, int64_t tokens, const Opts& o) {
+  const int rc = kv_validate(kv, true);
+  if (rc != MX_OK) return rc;
+  int64_t n;
+  if (tokens < 0 || __builtin_mul_overflow(tokens, kv->heads * kv->dim, &n)) return MX_ERR_SHAPE;
+  if (o.pad128 || n >= (int64_t)1 << 34 || big(tokens)) return MX_ERR_UNSUPPORTED;
+  return MX_OK;
+}
+
+int mx_kv_append(const mx_kv_t* kv, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                 const int32_t* slots, int64_t tokens, mx_round_t rounding, const mx_opts_t* opts) {
+  Opts o;
+  if (!read_opts(opts, &o) || ((int)rounding != MX_RNE && (int)rounding != MX_RHAZ)) return MX_ERR_FMT;
+  const int rc = kv_move_validate(kv, tokens, o);
+  if (rc != MX_OK) return rc;
+  const int64_t row = kv->heads * kv->dim, esz = o.dtype == MX_BF16 ? 2 : 4;
+  int64_t span;
+  if (k_stride < row || v_stride < row || __builtin_mul_overflow(k_stride > v_stride ? k_stride : v_stride, tokens, &span) ||
+      span > kMaxElements)
+    return MX_ERR_SHAPE;
+  if (tokens == 0) return MX_OK;
+  if (!k || !v || !slots) return MX_ERR_NULL;
+  if (misaligned16(k) || misaligned16(v) || k_stride * esz % 16 || v_stride * esz % 16 || (uintptr_t)slots % 4 || kv_misaligned(kv))
+    return MX_ERR_ALIGN;
+  if (kv->pages == 0) return MX_OK;
+  mx::KvMoveArgs a = {};
+  a.kv = kv_args(kv); a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride; a.slots = slots; a.tokens = tokens;
+  a.rounding = (int)rounding; a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_kv_append(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+int mx_kv_read(const mx_kv_t* kv, const int32_t* slots, int64_t tokens, void* k_out, void* v_out,
+               const mx_opts_t* opts) {
+  Opts o;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = kv_move_validate(kv, tokens, o);
+  if (rc != MX_OK) return rc;
+  if (tokens == 0) return MX_OK;
+  if (!slots || !k_out || !v_out) return MX_ERR_NULL;
+  if (misaligned16(k_out) || misaligned16(v_out) || (uintptr_t)slots % 4 || kv_misaligned(kv)) return MX_ERR_ALIGN;
+  mx::KvMoveArgs a = {};
+  a.kv = kv_args(kv); a.k_out = k_out; a.v_out = v_out; a.slots = slots; a.tokens = tokens; a.dtype = o.dtype; a.stream = o.stream;
+  const cudaError_t e = mx::launch_kv_read(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
+static int kv_attention_validate(const mx_kv_t* kv, const mx_kv_attention_t* t, bool pointers) {
+  if (!t) return MX_ERR_NULL;
+  const int rc = kv_validate(kv, pointers);
+  if (rc != MX_OK) return rc;
+  int64_t n, m, e;
+  if (t->batch < 0 || t->new_tokens < 1 || t->q_heads < 1 || t->q_heads % kv->heads || t->max_pages < 0 || t->window < 0 ||
+      !(t->scale > -3.4e38f && t->scale < 3.4e38f))
+    return MX_ERR_SHAPE;
+  if (__builtin_mul_overflow(t->batch, t->new_tokens, &n) || __builtin_mul_overflow(n, t->q_heads, &n) ||
+      __builtin_mul_overflow(t->max_pages, kv->page_size, &m) || __builtin_mul_overflow(n, kv->dim, &e) || e > kMaxElements ||
+      __builtin_mul_overflow(t->batch, t->max_pages, &e) || e > kMaxElements)
+    return MX_ERR_SHAPE;
+  if (kv->dim != 64 && kv->dim != 96 && kv->dim != 128 && kv->dim != 192 && kv->dim != 256) return MX_ERR_UNSUPPORTED;
+  if (big(n) || big(m) || big(t->batch) || big(t->new_tokens) || big(t->q_heads) || big(t->max_pages)) return MX_ERR_UNSUPPORTED;
+  return MX_OK;
+}
+
+size_t mx_kv_attention_workspace_bytes(const mx_kv_t* kv, const mx_kv_attention_t* attn) {
+  if (kv_attention_validate(kv, attn, false) != MX_OK) return 0;
+  return mx::kv_attention_workspace(kv_args(kv), attn->batch, attn->new_tokens, attn->q_heads);
+}
+
+int mx_kv_attention(const mx_kv_t* kv, const mx_kv_attention_t* attn, const void* q, const int32_t* table,
+                    const int32_t* lengths, void* out, float* lse, const mx_opts_t* opts, void* workspace,
+                    size_t workspace_bytes) {
+  Opts o;
+  if (!read_opts(opts, &o)) return MX_ERR_FMT;
+  const int rc = kv_attention_validate(kv, attn, true);
+  if (rc != MX_OK) return rc;
+  if (o.pad128) return MX_ERR_UNSUPPORTED;
+  const int64_t esz = o.dtype == MX_BF16 ? 2 : 4;
+  int64_t span;
+  if (attn->q_stride < attn->q_heads * kv->dim ||
+      __builtin_mul_overflow(attn->q_stride, attn->batch * attn->new_tokens, &span) || span > kMaxElements)
+    return MX_ERR_SHAPE;
+  if (attn->batch == 0) return MX_OK;
+  if (!q || !lengths || !out || !workspace || (attn->max_pages > 0 && !table)) return MX_ERR_NULL;
+  if (misaligned16(q) || attn->q_stride * esz % 16 || misaligned16(out) || (uintptr_t)lse % 4 || (uintptr_t)table % 4 ||
+      (uintptr_t)lengths % 4 || (uintptr_t)workspace % 256 || kv_misaligned(kv))
+    return MX_ERR_ALIGN;
+  if (workspace_bytes < mx_kv_attention_workspace_bytes(kv, attn)) return MX_ERR_WORKSPACE;
+  mx::KvAttentionArgs a = {};
+  a.kv = kv_args(kv); a.q = q; a.table = table; a.lengths = lengths; a.out = out; a.lse = lse; a.workspace = workspace;
+  a.batch = attn->batch; a.new_tokens = attn->new_tokens; a.q_heads = attn->q_heads; a.max_pages = attn->max_pages;
+  a.q_stride = attn->q_stride; a.window = attn->window; a.scale = attn->scale; a.dtype = o.dtype; a.stream = o.stream;
+  cudaError_t e;
+  a.sm_count = sm_count(&e);
+  if (e != cudaSuccess) return fail_cuda(e);
+  e = mx::launch_kv_attention(a);
+  return e == cudaSuccess ? MX_OK : fail_cuda(e);
+}
+
 static int grouped_run(const mx::GroupedArgs& args, const Opts& o) {
   mx::GroupedArgs a = args;
   cudaError_t e;

@@ -214,4 +214,40 @@ struct GroupedArgs {
 int launch_gemm_grouped(const GroupedArgs& a, cudaError_t* cuda_err);
 int gemm_grouped_status(cudaStream_t stream, unsigned int* status, cudaError_t* cuda_err);
 
+// The paged cache (see mx_kv_t).  A row is a token's codes for one head; rows are numbered
+// (page * heads + head) * page_size + offset.
+struct KvArgs {
+  uint8_t *k_elems, *k_scales, *v_elems, *v_scales;
+  int64_t pages, page_size, heads, dim;
+  int fmt;
+};
+struct KvMoveArgs {
+  KvArgs kv;
+  const void *k, *v;       // append: rows to quantize
+  void *k_out, *v_out;     // read: rows as numbers
+  int64_t k_stride, v_stride;
+  const int32_t* slots;
+  int64_t tokens;
+  int rounding, dtype;
+  cudaStream_t stream;
+};
+cudaError_t launch_kv_append(const KvMoveArgs& a);
+cudaError_t launch_kv_read(const KvMoveArgs& a);
+
+struct KvAttentionArgs {
+  KvArgs kv;
+  const void* q;
+  const int32_t *table, *lengths;
+  void* out;
+  float* lse;              // may be null
+  void* workspace;
+  int64_t batch, new_tokens, q_heads, max_pages, q_stride, window;
+  float scale;
+  int dtype;
+  int sm_count;
+  cudaStream_t stream;
+};
+size_t kv_attention_workspace(const KvArgs& kv, int64_t batch, int64_t new_tokens, int64_t q_heads);
+cudaError_t launch_kv_attention(const KvAttentionArgs& a);
+
 }  // namespace mx

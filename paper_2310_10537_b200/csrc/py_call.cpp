@@ -1,4 +1,4 @@
-// Python calls of the norm, routing, row-moving and grouped-product entry points, marshalled in C++.
+// Python calls of the norm, routing, row-moving, grouped-product and cache entry points, marshalled in C++.
 //
 // These calls stand in loops whose GPU time is a few microseconds, where checking the tensors, allocating the
 // results and converting the arguments in Python costs several times that (norm of 16 x 4096: 15 us of host time
@@ -13,6 +13,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <cmath>
 #include <initializer_list>
 #include <string>
 
@@ -405,6 +406,132 @@ PyObject* gemm_grouped(Args a) {
   return out ? given(a[10]) : wrap(made);
 }
 
+// A KvCache: the four tensors [pages, heads, page_size, row bytes], dim, fmt.
+mx_kv_t kv_cache(PyObject* t, int* dev) {
+  if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 6) fail(PyExc_TypeError, "cache has to be a KvCache");
+  const at::Tensor &ke = *tensor(PyTuple_GET_ITEM(t, 0), "k_elems"), &ks = *tensor(PyTuple_GET_ITEM(t, 1), "k_scales");
+  const at::Tensor &ve = *tensor(PyTuple_GET_ITEM(t, 2), "v_elems"), &vs = *tensor(PyTuple_GET_ITEM(t, 3), "v_scales");
+  if (ke.dim() != 4) fail(PyExc_ValueError, "k_elems has to be [pages, heads, page_size, bytes]");
+  *dev = call_device(ke);
+  mx_kv_t kv = {};
+  kv.pages = ke.size(0);
+  kv.heads = ke.size(1);
+  kv.page_size = ke.size(2);
+  kv.dim = integer(PyTuple_GET_ITEM(t, 4));
+  kv.fmt = small(PyTuple_GET_ITEM(t, 5));
+  const int bits = mx_fmt_bits((mx_fmt_t)kv.fmt);
+  const int64_t dim = kv.dim > 0 && kv.dim < 1 << 24 ? kv.dim : 0;  // (the library refuses the rest)
+  const int64_t code = dim * bits / 8, scale = (dim + 127) / 128 * 4;
+  kv.k_elems = need(&ke, "k_elems", *dev, at::kByte, {kv.pages, kv.heads, kv.page_size, code});
+  kv.k_scales = (uint8_t*)need(&ks, "k_scales", *dev, at::kByte, {kv.pages, kv.heads, kv.page_size, scale});
+  kv.v_elems = need(&ve, "v_elems", *dev, at::kByte, {kv.pages, kv.heads, kv.page_size, code});
+  kv.v_scales = (uint8_t*)need(&vs, "v_scales", *dev, at::kByte, {kv.pages, kv.heads, kv.page_size, scale});
+  return kv;
+}
+// Rows of heads of tokens that may lie inside a wider tensor: [.., heads, dim] contiguous within a token, the tokens (all
+// leading axes in order) evenly spaced.  Their spacing in elements.
+int64_t token_stride(const at::Tensor& t, const char* name, int dev, c10::ScalarType dtype, int64_t heads, int64_t dim) {
+  const int64_t n = t.dim();
+  if (!t.is_cuda() || t.get_device() != dev)
+    fail(PyExc_ValueError, std::string(name) + " has to be a tensor on the current CUDA device");
+  if (t.scalar_type() != dtype || t.size(n - 2) != heads || t.size(n - 1) != dim)
+    fail(PyExc_ValueError, std::string(name) + " has to be " + c10::toString(dtype) + " [.., " + std::to_string(heads) + ", " +
+                               std::to_string(dim) + "], not " + describe(t.scalar_type(), t.sizes()));
+  const bool rows = (dim < 2 || t.stride(n - 1) == 1) && (heads < 2 || t.stride(n - 2) == dim);
+  const bool lead = n < 4 || t.size(0) < 2 || t.size(1) == 0 || t.stride(0) == t.size(1) * t.stride(1);
+  if (!rows || !lead) fail(PyExc_ValueError, std::string(name) + " has to have contiguous heads and evenly spaced tokens");
+  // of a single token the stride says nothing
+  if (n == 4 && t.size(1) < 2) return t.size(0) < 2 ? heads * dim : t.stride(0);
+  return t.size(n - 3) < 2 ? heads * dim : t.stride(n - 3);
+}
+
+// cache k v slots rounding
+PyObject* kv_append(Args a) {
+  int dev;
+  const mx_kv_t kv = kv_cache(a[0], &dev);
+  const at::Tensor &k = *tensor(a[1], "k"), &v = *tensor(a[2], "v"), &slots = *tensor(a[3], "slots");
+  if (k.dim() != 3 || v.dim() != 3) fail(PyExc_ValueError, "k and v have to be [tokens, heads, dim]");
+  const int64_t tokens = k.size(0);
+  const mx_dtype_t code = float_code(k);
+  const int64_t ks = token_stride(k, "k", dev, k.scalar_type(), kv.heads, kv.dim), vs = token_stride(v, "v", dev, k.scalar_type(), kv.heads, kv.dim);
+  if (v.size(0) != tokens) fail(PyExc_ValueError, "k and v have to have the same tokens");
+  const int32_t* ps = (const int32_t*)need(&slots, "slots", dev, at::kInt, {tokens});
+  const int rounding = small(a[4]);
+  const mx_opts_t o = options(dev, code);
+  const void *pk = k.data_ptr(), *pv = v.data_ptr();
+  check(unlocked([&] { return mx_kv_append(&kv, pk, pv, ks, vs, ps, tokens, (mx_round_t)rounding, &o); }), "mx_kv_append");
+  return given(Py_None);
+}
+
+// cache slots dtype out_k out_v
+PyObject* kv_read(Args a) {
+  int dev;
+  const mx_kv_t kv = kv_cache(a[0], &dev);
+  const at::Tensor &slots = *tensor(a[1], "slots"), *ok = tensor(a[3], "out k", true), *ov = tensor(a[4], "out v", true);
+  if (slots.dim() != 1) fail(PyExc_ValueError, "slots has to be [tokens]");
+  const int64_t tokens = slots.size(0);
+  if (!THPDtype_Check(a[2])) fail(PyExc_TypeError, "dtype has to be a torch.dtype");
+  const auto dt = reinterpret_cast<THPDtype*>(a[2])->scalar_type;
+  const mx_dtype_t code = float_code(dt);
+  const int32_t* ps = (const int32_t*)need(&slots, "slots", dev, at::kInt, {tokens});
+  at::Tensor mk, mv;
+  void* pk = ok ? need(ok, "out k", dev, dt, {tokens, kv.heads, kv.dim}) : (mk = make(slots, dt, {tokens, kv.heads, kv.dim})).data_ptr();
+  void* pv = ov ? need(ov, "out v", dev, dt, {tokens, kv.heads, kv.dim}) : (mv = make(slots, dt, {tokens, kv.heads, kv.dim})).data_ptr();
+  const mx_opts_t o = options(dev, code);
+  check(unlocked([&] { return mx_kv_read(&kv, ps, tokens, pk, pv, &o); }), "mx_kv_read");
+  return pair(ok ? given(a[3]) : wrap(mk), ov ? given(a[4]) : wrap(mv));
+}
+
+// q cache table lengths scale window return_lse out workspace
+PyObject* kv_attention(Args a) {
+  int dev;
+  const mx_kv_t kv = kv_cache(a[1], &dev);
+  const at::Tensor &q = *tensor(a[0], "q"), &table = *tensor(a[2], "table"), &len = *tensor(a[3], "lengths");
+  const at::Tensor *out = tensor(a[7], "out", true), *ws = tensor(a[8], "workspace", true);
+  const int64_t n = q.dim();
+  if (n != 3 && n != 4) fail(PyExc_ValueError, "q has to be [batch, heads, dim] or [batch, new tokens, heads, dim]");
+  two_dims(table, "table", "[batch, pages of a sequence]");
+  mx_kv_attention_t t = {};
+  t.batch = q.size(0);
+  t.new_tokens = n == 4 ? q.size(1) : 1;
+  t.q_heads = q.size(n - 2);
+  t.max_pages = table.size(1);
+  t.window = integer(a[5]);
+  const auto dt = q.scalar_type();
+  const mx_dtype_t code = float_code(q);
+  t.q_stride = token_stride(q, "q", dev, dt, t.q_heads, kv.dim);
+  const float natural = kv.dim > 0 ? 1.0f / sqrtf((float)kv.dim) : 0.0f;
+  t.scale = a[4] == Py_None ? natural : real(a[4]);
+  const int32_t* pt = (const int32_t*)need(&table, "table", dev, at::kInt, {t.batch, t.max_pages});
+  const int32_t* pl = (const int32_t*)need(&len, "lengths", dev, at::kInt, {t.batch});
+  const int with_lse = PyObject_IsTrue(a[6]);
+  if (with_lse < 0) throw Raised();
+  at::Tensor made, lse, space;
+  if (out) {
+    on_device(*out, "out", dev);
+    if (out->scalar_type() != dt || out->sizes() != q.sizes())
+      fail(PyExc_ValueError, "out has to be " + describe(dt, q.sizes()) + ", not " + describe(out->scalar_type(), out->sizes()));
+  } else {
+    made = n == 4 ? make(q, dt, {t.batch, t.new_tokens, t.q_heads, kv.dim}) : make(q, dt, {t.batch, t.q_heads, kv.dim});
+  }
+  if (with_lse) lse = n == 4 ? make(q, at::kFloat, {t.batch, t.new_tokens, t.q_heads}) : make(q, at::kFloat, {t.batch, t.q_heads});
+  int64_t bytes = (int64_t)mx_kv_attention_workspace_bytes(&kv, &t);
+  void* pws;
+  if (ws) {
+    pws = holds(*ws, "workspace", dev, 0);
+    bytes = (int64_t)ws->nbytes();
+  } else {
+    pws = (space = make(q, at::kByte, {bytes > 0 ? bytes : 1})).data_ptr();
+  }
+  const mx_opts_t o = options(dev, code);
+  const void* pq = q.data_ptr();
+  void* po = out ? out->data_ptr() : made.data_ptr();
+  float* pe = with_lse ? (float*)lse.data_ptr() : nullptr;
+  check(unlocked([&] { return mx_kv_attention(&kv, &t, pq, pt, pl, po, pe, &o, pws, (size_t)bytes); }), "mx_kv_attention");
+  PyObject* r = out ? given(a[7]) : wrap(made);
+  return with_lse ? pair(r, wrap(lse)) : r;
+}
+
 // One entry: the argument count, and no C++ exception leaves.
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject*, Args args, Py_ssize_t n) {
@@ -444,6 +571,7 @@ PyMethodDef g_methods[] = {
     ENTRY("moe_combine", moe_combine, 4), ENTRY("moe_combine_backward", moe_combine_backward, 4),
     ENTRY("gemm_grouped", (gemm_grouped<false, false>), 13), ENTRY("gemm_grouped_k", (gemm_grouped<true, false>), 13),
     ENTRY("gemm_grouped_ex", (gemm_grouped<false, true>), 15), ENTRY("gemm_grouped_k_ex", (gemm_grouped<true, true>), 15),
+    ENTRY("kv_append", kv_append, 5), ENTRY("kv_read", kv_read, 5), ENTRY("kv_attention", kv_attention, 9),
     {"set_error_type", set_error_type, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_py_call", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
