@@ -16,7 +16,8 @@ BUILD = os.path.join(HERE, "build")
 STAMP = os.path.join(BUILD, "py_call.stamp")  # the interpreter and torch that module was compiled for
 SOURCES = ["mx_api.cu", "mx_quantize.cu", "mx_quantize_dual.cu", "mx_quantize_tile.cu", "mx_dequantize.cu",
            "mx_gemm.cu", "mx_im2col.cu", "mx_rmsnorm.cu", "mx_route.cu", "mx_moe.cu", "mx_gemm_grouped.cu",
-           "mx_kv.cu", "mx_kv_attention.cu"]
+           "mx_kv.cu", "mx_kv_attention.cu", "mx_kv_attention_e4m3.cu", "mx_kv_attention_e5m2.cu",
+           "mx_kv_attention_e2m1.cu", "mx_kv_attention_int8.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

@@ -1198,12 +1198,15 @@ static int kv_attention_validate(const mx_kv_t* kv, const mx_kv_attention_t* t, 
     return MX_ERR_SHAPE;
   if (kv->dim != 64 && kv->dim != 96 && kv->dim != 128 && kv->dim != 192 && kv->dim != 256) return MX_ERR_UNSUPPORTED;
   if (big(n) || big(m) || big(t->batch) || big(t->new_tokens) || big(t->q_heads) || big(t->max_pages)) return MX_ERR_UNSUPPORTED;
+  // units of 16 tokens of a sequence for 8 query rows of a key-value head are numbered in 32 bits
+  const int64_t row_tiles = (t->new_tokens * (t->q_heads / kv->heads) + 7) / 8;
+  if (__builtin_mul_overflow(t->batch * kv->heads, row_tiles, &n) || __builtin_mul_overflow(n, m / 16 + 1, &e) || big(e)) return MX_ERR_UNSUPPORTED;
   return MX_OK;
 }
 
 size_t mx_kv_attention_workspace_bytes(const mx_kv_t* kv, const mx_kv_attention_t* attn) {
   if (kv_attention_validate(kv, attn, false) != MX_OK) return 0;
-  return mx::kv_attention_workspace(kv_args(kv), attn->batch, attn->new_tokens, attn->q_heads);
+  return mx::kv_attention_workspace(kv_args(kv));
 }
 
 int mx_kv_attention(const mx_kv_t* kv, const mx_kv_attention_t* attn, const void* q, const int32_t* table,

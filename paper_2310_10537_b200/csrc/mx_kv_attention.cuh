@@ -1,0 +1,694 @@
+// Attention of the newest tokens over a paged cache of MX rows (see mx_kv_attention in mx.h).
+//
+// Mathematics.  For the query rows r of one sequence that share a key-value head, with s in units of log2 e,
+//   s[j, r] = qf[r] * sum_b KX[j, b] * (sum_{d in block b} KP[j, d] * q'[r, d])        q = q' * a power of two
+//   out[r, d] = sum_j 2^{s[j, r]} VX[j, b(d)] VP[j, d] / sum_j 2^{s[j, r]}
+// Both inner sums are tensor-core products of FP16 operands with FP32 accumulators: codes of every format are exact in
+// FP16 (INT8 as the integer), queries are scaled by a power of two into its range.  A key's block scale multiplies the
+// FP32 sum of its block.  A value's scale depends on the token, the axis that its product sums over, so it joins the
+// softmax weight: w[j, r, b] = 2^{s - m[r]} VX[j, b] F[r, b], where m and F are powers of two kept per row (and block) that
+// hold w below 2^15: F follows the largest contribution seen so far, as m follows the largest score.  Both move
+// only when a tile breaks the bound (a vote of the warp), by factors that are exact.
+// Rounded to FP16: w, half a step 2^-11 of a weight (BF16 results, whose own rounding is 2^-8), or two FP16 terms, 2^-22 (FP32
+// results; the queries too).  Scores, maxima, sums and accumulators are FP32.
+//
+// Layout.  A warp takes kTokens tokens at a time: S^T = K Q^T has the tokens on the M side of the MMA and the query rows
+// on its N side, 8 or 16 of them (a group of 4 query heads wastes half of 8, not three quarters of 16), then
+// O^T = V^T W^T with the row's elements on the M side.  W^T comes out of S^T's accumulators by 8 x 8 transposes
+// in registers.  The order of the elements within a block and of the tokens within a tile is free in these sums, and chosen
+// such that a lane's codes are consecutive bytes: no shuffling of codes but the pairing of neighbouring tokens' values.
+// The warps of a block have their own tiles and their own asynchronous copies, kStages tiles deep, and meet only at the
+// end of a sequence.
+//
+// Split.  The tiles of all sequences, heads and groups of rows, one after the other, are dealt out in equal runs to
+// two blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
+// otherwise it leaves a part (its weighted mean and the log of its weight) and a second kernel joins the parts, in the
+// order of the tiles: results do not depend on timing.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "mx_device.cuh"
+#include "mx_kv_attention_args.h"
+#include "mx_rows.cuh"
+
+namespace mx {
+namespace attn {
+
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.4028234663852886e38f;  // the reference before any score
+constexpr float kRoom = 6.0f;                       // a moved m leaves the new maximum this far below it
+constexpr float kTop = 32768.0f;                    // weights stay at or below this
+constexpr int kAim = 8;                             // log2 of the largest weight after F has moved
+constexpr float kMost = 8.507059173023462e37f;      // 2^126, F's largest value
+
+// Shape of a kernel instance.
+template <int FMT, int DIM, bool WIDE>
+struct Cfg {
+  static constexpr int kBits = FmtTraits<FMT>::bits;
+  static constexpr int kBlocks = DIM / 32;
+  static constexpr int kRow = DIM * kBits / 8;             // bytes of a row's codes
+  static constexpr int kGroup = 4 * kBits;                 // bytes of a block's codes
+  // rows in shared memory: whole powers of two, so that the 16-byte units can be permuted within lines of 128 bytes
+  static constexpr int kPitch = kRow <= 32 ? 32 : kRow <= 64 ? 64 : kRow <= 128 ? 128 : 256;
+  static constexpr int kTiles = kPitch <= 128 ? 2 : 1;     // MMA tiles of 16 tokens
+  static constexpr int kTokens = 16 * kTiles;
+  static constexpr int kScale = (kBlocks + 3) / 4 * 4;     // bytes of a row's scales
+  static constexpr int kUnits = kRow / 16;                 // 16-byte units of a row
+  static constexpr int kCopies = kTokens * kUnits / 32;    // of these a lane copies
+  static constexpr int kCodes = kTokens * kPitch;
+  static constexpr int kStage = 2 * kCodes + 2 * kTokens * kScale + 128;  // codes, scales, the mask of seen tokens
+  static constexpr int kJoinDim = DIM < 128 ? DIM : DIM == 192 ? 96 : 128;  // elements of a row joined at a time
+  static constexpr int kJoin = 2 * 8 * kJoinDim * 4 + kWarps * 16 * 4;
+  static constexpr int kFit = (115712 - kJoin) / (kWarps * kStage);       // two blocks per SM
+  static constexpr int kStages = kFit < 4 ? kFit : 4;
+  static constexpr int kShared = kWarps * kStages * kStage + kJoin;
+  static_assert(kStages >= 2 && kTokens * kUnits % 32 == 0, "tiles in flight");
+  // the integer n of an INT8 code stands for n / 64
+  static constexpr float kUnit = FMT == MX_INT8 ? 0.015625f : 1.0f;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+__device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Transpose of an 8 x 8 matrix of 16-bit elements held as two of a row per lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two scale bytes as FP32 (0: 2^-127, 255: NaN).
+__device__ __forceinline__ void scales2(uint32_t two, float& a, float& b) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
+  a = __uint_as_float(d << 16);
+  b = __uint_as_float(d & 0xFFFF0000u);
+}
+
+// Codes as FP16 pairs.  `w` holds four 8-bit codes (4-bit: all eight of the lane's): pair 0 are codes 0, 1.
+template <int FMT>
+__device__ __forceinline__ uint32_t half_pair(uint32_t w, int pair) {
+  uint32_t h;
+  if constexpr (FMT == MX_E4M3) {
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(pair ? w >> 16 : w)));
+  } else if constexpr (FMT == MX_E5M2) {
+    h = __byte_perm(w, 0, pair ? 0x3424 : 0x1404);  // E5M2 is FP16's upper byte
+  } else if constexpr (FMT == MX_E2M1) {
+    // (unpacked from the whole word: taken from a half of it, byte 2 came out as byte 0)
+#define MX_E2M1_PAIR(byte) asm("{ .reg .b8 b0, b1, b2, b3; mov.b32 {b0, b1, b2, b3}, %1; cvt.rn.f16x2.e2m1x2 %0, " byte "; }" : "=r"(h) : "r"(w))
+    if (pair == 0) MX_E2M1_PAIR("b0");
+    else if (pair == 1) MX_E2M1_PAIR("b1");
+    else if (pair == 2) MX_E2M1_PAIR("b2");
+    else MX_E2M1_PAIR("b3");
+#undef MX_E2M1_PAIR
+  } else {  // 0x6400 | u = 1024 + u; u = n + 128
+    const uint32_t u = __byte_perm(w ^ 0x80808080u, 0x64646464u, pair ? 0x4342 : 0x4140);
+    const uint32_t bias = 0x64806480u;  // 1152
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(u), "r"(bias));
+  }
+  return h;
+}
+
+// Byte offset of a row (0 .. kTokens - 1) in a tile's codes, its 16-byte units permuted such that the four or eight rows that a
+// warp reads at a time lie in different banks; byte x of the row is at offset ^ x (+ 128 for the second line of a row of 256).
+template <class C>
+__device__ __forceinline__ uint32_t row_at(uint32_t r) {
+  if (C::kPitch >= 128) return r * C::kPitch + (C::kBits == 8 ? ((r ^ (r >> 2)) & 3) << 5 : (r & 7) << 4);
+  if (C::kPitch == 64) return (r >> 1) * 128 + (((r & 1) << 6) ^ (C::kBits == 8 ? ((r >> 1) & 3) << 5 : ((r >> 1) & 3) << 4));
+  return (r >> 2) * 128 + (((r & 3) << 5) ^ (((r >> 2) & 1) << 4));
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_small(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N), "r"(there ? N : 0) : "memory");
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds2(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+
+// The instance for rows of DIM elements in format FMT, NR times 8 query rows at a time.
+template <int FMT, int DIM, int NR, bool WIDE>
+__global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args a) {
+  using C = Cfg<FMT, DIM, WIDE>;
+  constexpr int B = C::kBlocks, TL = C::kTiles, W = WIDE ? 2 : 1;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (C::kStages * C::kStage);
+  float* join = reinterpret_cast<float*>(smem + kWarps * C::kStages * C::kStage);  // [2][8][kJoinDim]
+  float* join_lse = join + 2 * 8 * C::kJoinDim;                                    // [kWarps][16]
+
+  // The lengths come from the kernels before this one.  The join may be scheduled only after this point, so that it, too,
+  // finds them written.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // sequences without a tile
+  for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    if (a.tiles(a.length(b)) != 0) continue;
+    const uint32_t rows = a.new_tokens * a.q_heads;
+    for (uint32_t i = threadIdx.x; i < rows * (DIM / 8); i += kWarps * 32) {
+      const float zero[8] = {};
+      store8<WIDE ? MX_F32 : MX_BF16>(a.out, ((size_t)b * rows) * DIM + (size_t)i * 8, zero);
+    }
+    if (a.lse)
+      for (uint32_t i = threadIdx.x; i < rows; i += kWarps * 32) a.lse[(size_t)b * rows + i] = -INFINITY;
+  }
+
+  const Share share = a.share(lane);
+  const uint32_t first = blockIdx.x * share.per;
+  if (first >= share.total) return;
+  const uint32_t last = min(first + share.per, share.total);  // this block's tiles are first .. last - 1
+
+  // ---- the copies' side: which tokens the next tile to copy holds -------------------------------------------
+  Segment ls = a.find(share, first, lane);
+  uint32_t lu = first + warp;   // the tile to copy next
+  uint32_t page = 0, off = 0;   // of this lane's token in it
+  bool there = false;
+  auto look_up = [&] {
+    if (lu >= last) return;
+    while (lu >= ls.end) a.next(ls);
+    const uint32_t j = (ls.first_tile + (lu - ls.start)) * C::kTokens + (lane % C::kTokens);
+    there = j < ls.length && j >= ls.begin;
+    if (there) {
+      const uint32_t p = fastdiv(j, a.by_page);
+      off = j - p * a.page_size;
+      page = (uint32_t)__ldg(a.table + (size_t)ls.b * a.max_pages + p);
+    }
+  };
+  uint32_t fill = 0;  // the stage to fill next
+  auto copy_tile = [&] {
+    if (lu < last) {
+      const bool ok = there && page < a.pages;  // (a negative entry is a large one)
+      const uint32_t row = ok ? (page * a.heads + ls.head(a)) * a.page_size + off : 0;
+      const uint32_t seen = __ballot_sync(0xFFFFFFFFu, ok);
+      const uint32_t stage = base + fill * C::kStage, scales = stage + 2 * C::kCodes;
+#pragma unroll
+      for (int i = 0; i < C::kCopies; ++i) {
+        const uint32_t n = lane + 32 * i, r = n / C::kUnits, u = n % C::kUnits;
+        const size_t at = (size_t)__shfl_sync(0xFFFFFFFFu, row, r) * C::kRow + u * 16;
+        const bool has = seen >> r & 1;
+        const uint32_t to = stage + (row_at<C>(r) ^ ((u & 7) << 4)) + (u >> 3) * 128;
+        copy16(to, a.k_elems + at, has);
+        copy16(to + C::kCodes, a.v_elems + at, has);
+      }
+      if (TL == 2) {
+        copy_small<C::kScale>(scales + lane * C::kScale, a.k_scales + (size_t)row * C::kScale, ok);
+        copy_small<C::kScale>(scales + (32 + lane) * C::kScale, a.v_scales + (size_t)row * C::kScale, ok);
+      } else {  // keys' by the lower half of the warp, values' by the upper
+        copy_small<C::kScale>(scales + lane * C::kScale, (lane < 16 ? a.k_scales : a.v_scales) + (size_t)row * C::kScale, ok);
+      }
+      if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + 2 * C::kTokens * C::kScale), "r"(seen) : "memory");
+      lu += kWarps;
+      fill = fill + 1 == C::kStages ? 0 : fill + 1;
+      look_up();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  look_up();
+#pragma unroll
+  for (int i = 0; i < C::kStages - 1; ++i) copy_tile();
+
+  // lane offsets of the codes: keys of tokens g, g + 8; values of tokens 2 t, 2 t + 1 (and 8 further on)
+  const uint32_t k_at[2] = {row_at<C>(g) + t * (C::kGroup / 4), row_at<C>(g + 8) + t * (C::kGroup / 4)};
+  uint32_t v_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v_at[i] = row_at<C>(2 * t + (i & 1) + (i & 2) * 4) + g * (C::kGroup / 8);
+
+  uint32_t use = 0, unit = first + warp;
+  Segment s = a.find(share, first, lane);
+  for (;;) {
+    // ---- one sequence and head: the queries ------------------------------------------------------------------
+    const uint32_t seg_end = min(s.end, last);
+    const uint32_t group0 = s.row_tile(a) * (8 * NR);  // first query row of this tile of rows
+    uint32_t q[W][B][2][NR][2];
+    float qf[NR][2];
+    int lo[NR][2], hi[NR][2];  // tokens that the lane's rows 2 t, 2 t + 1 see
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const uint32_t r = group0 + n * 8 + g;
+      float x[B][8];
+      float amax = 0.0f;
+      if (r < a.rows) {
+        const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
+        const size_t at = ((size_t)s.b * a.new_tokens + i) * a.q_stride + (size_t)head * DIM + t * 8;
+#pragma unroll
+        for (int b = 0; b < B; ++b) widen(load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32), x[b]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[b][j] = 0.0f;
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax = absmax_nan(amax, x[b][j]);
+      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+      // q' = q * 2^-e with the largest element in [2^7, 2^8): FP16 then holds what is 2^-22 of it to full precision.
+      // Inf or NaN make the row NaN.
+      const uint32_t ab = __float_as_uint(amax) & 0x7FFFFFFFu;
+      const int e = ab == 0 ? 0 : (int)(ab >> 23) - 134;  // -134 .. 120
+      const float half1 = ab >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - e / 2) << 23);
+      const float half2 = __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float u = x[b][4 * k + 2 * j] * half1 * half2, v = x[b][4 * k + 2 * j + 1] * half1 * half2;
+            q[0][b][k][n][j] = pack_half(u, v);
+            if (WIDE) {
+              const float2 h = unpack_half(q[0][b][k][n][j]);
+              q[W - 1][b][k][n][j] = pack_half(u - h.x, v - h.y);
+            }
+          }
+      const float f = a.scale_log2 * C::kUnit / half2 / half1;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        qf[n][j] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + j) * 4);
+        const uint32_t row = group0 + n * 8 + 2 * t + j;
+        const int i = row < a.rows ? (int)fastdiv(row, a.by_group) : (int)a.new_tokens - 1;
+        hi[n][j] = (int)s.length - ((int)a.new_tokens - 1 - i);
+        lo[n][j] = a.window ? max(hi[n][j] - (int)a.window, 0) : 0;
+      }
+    }
+    // tiles between these are seen by all rows
+    const int all_lo = a.window ? max((int)s.length - (int)a.window, 0) : 0, all_hi = (int)s.length - ((int)a.new_tokens - 1);
+
+    float m[NR][2], l[NR][2], F[B][NR][2], acc[B][2][NR][4];
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        m[n][j] = kLowest;
+        l[n][j] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < B; ++b) F[b][n][j] = kMost;
+      }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[b][h][n][i] = 0.0f;
+
+    // ---- its tiles ----------------------------------------------------------------------------------------
+    for (; unit < seg_end; unit += kWarps) {
+      copy_tile();
+      asm volatile("cp.async.wait_group %0;" ::"n"(C::kStages - 1) : "memory");
+      __syncwarp();
+      const uint32_t stage = base + use * C::kStage, scales = stage + 2 * C::kCodes;
+      use = use + 1 == C::kStages ? 0 : use + 1;
+      const uint32_t seen = lds4(scales + 2 * C::kTokens * C::kScale);
+      const int j0 = (int)(s.first_tile + (unit - s.start)) * C::kTokens;
+      const bool edge = seen != 0xFFFFFFFFu || j0 < all_lo || j0 + C::kTokens > all_hi;
+
+      // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1
+      float p[TL][NR][4];
+#pragma unroll
+      for (int x = 0; x < TL; ++x) {
+        float ks[2][C::kScale];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < C::kScale; c += 4) {
+            const uint32_t w = lds4(scales + (16 * x + 8 * h + g) * C::kScale + c);
+            scales2(w, ks[h][c], ks[h][c + 1]);
+            scales2(w >> 16, ks[h][c + 2], ks[h][c + 3]);
+          }
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[x][n][i] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          uint32_t ka[2][4];  // two steps of 16 elements
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t at = stage + x * 16 * C::kPitch + (k_at[h] ^ ((b * C::kGroup) & 127)) + (b * C::kGroup) / 128 * 128;
+            if (C::kBits == 8) {
+              const uint2 c = lds8(at);
+              ka[0][h] = half_pair<FMT>(c.x, 0);
+              ka[0][2 + h] = half_pair<FMT>(c.x, 1);
+              ka[1][h] = half_pair<FMT>(c.y, 0);
+              ka[1][2 + h] = half_pair<FMT>(c.y, 1);
+            } else {
+              const uint32_t c = lds4(at);
+              ka[0][h] = half_pair<FMT>(c, 0);
+              ka[0][2 + h] = half_pair<FMT>(c, 1);
+              ka[1][h] = half_pair<FMT>(c, 2);
+              ka[1][2 + h] = half_pair<FMT>(c, 3);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = W - 1; w >= 0; --w)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) mma(d, ka[k], q[w][b][k][n][0], q[w][b][k][n][1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[x][n][i] = fmaf(d[i], ks[i >> 1][b], p[x][n][i]);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[x][n][i] *= qf[n][i & 1];
+      }
+      uint32_t out_mask = 0;  // bit: this score is of a token that the row does not see
+      if (edge) {
+#pragma unroll
+        for (int x = 0; x < TL; ++x)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int k = 16 * x + 8 * (i >> 1) + (int)g, j = j0 + k;
+              if (!(seen >> k & 1) || j < lo[n][i & 1] || j >= hi[n][i & 1]) {
+                p[x][n][i] = -INFINITY;
+                out_mask |= 1u << ((x * NR + n) * 4 + i);
+              }
+            }
+      }
+
+      // the maxima: m moves when a score passes it
+      for (;;) {
+        float most = -1.0f;
+#pragma unroll
+        for (int x = 0; x < TL; ++x)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, p[x][n][i] - m[n][i & 1]);
+        if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < TL; ++x) top = fmaxf(top, fmaxf(p[x][n][j], p[x][n][2 + j]));
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            if (top <= m[n][j]) continue;
+            const float next = ceilf(top) + kRoom, up = next - m[n][j];
+            l[n][j] *= ex2(-up);
+            m[n][j] = next;
+            // weights are relative to m F: F takes the move, as far as it can
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+              const float f = (float)((int)(__float_as_uint(F[b][n][j]) >> 23) - 127), want = f + up, have = fminf(want, 126.0f);
+              F[b][n][j] = __uint_as_float((uint32_t)((int)have + 127) << 23);
+              if (have < want) {
+                const float down = ex2(have - want);
+                acc[b][0][n][j] *= down; acc[b][0][n][2 + j] *= down;
+                acc[b][1][n][j] *= down; acc[b][1][n][2 + j] *= down;
+              }
+            }
+          }
+      }
+#pragma unroll
+      for (int x = 0; x < TL; ++x)
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[x][n][i] = ex2(p[x][n][i] - m[n][i & 1]);
+            l[n][i & 1] += p[x][n][i];
+          }
+
+      // values, block by block
+      float vs[TL][2][C::kScale];
+#pragma unroll
+      for (int x = 0; x < TL; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < C::kScale; c += 4) {
+            const uint32_t w = lds4(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + c);
+            scales2(w, vs[x][h][c], vs[x][h][c + 1]);
+            scales2(w >> 16, vs[x][h][c + 2], vs[x][h][c + 3]);
+          }
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        uint32_t w[W][TL][NR][2];
+        for (;;) {
+          uint32_t most = 0;
+#pragma unroll
+          for (int x = 0; x < TL; ++x)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float u = p[x][n][2 * h] * vs[x][h][b] * F[b][n][0], v = p[x][n][2 * h + 1] * vs[x][h][b] * F[b][n][1];
+                if (edge) {  // a token that is not seen weighs nothing, whatever its scale
+                  if (out_mask >> ((x * NR + n) * 4 + 2 * h) & 1) u = 0.0f;
+                  if (out_mask >> ((x * NR + n) * 4 + 2 * h + 1) & 1) v = 0.0f;
+                }
+                w[0][x][n][h] = pack_half(u, v);
+                most = max_half2(most, w[0][x][n][h]);
+                if (WIDE) {
+                  const float2 f = unpack_half(w[0][x][n][h]);
+                  w[W - 1][x][n][h] = pack_half(u - f.x, v - f.y);
+                }
+              }
+          const float2 f = unpack_half(most);
+          if (!__any_sync(0xFFFFFFFFu, fmaxf(f.x, f.y) > kTop)) break;
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float top = 0.0f;
+#pragma unroll
+              for (int x = 0; x < TL; ++x)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  if (!(out_mask >> ((x * NR + n) * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][n][2 * h + j] * vs[x][h][b] * F[b][n][j]);
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+              if (!(top > kTop)) continue;
+              // (F is a normal number: p is at most 1, VX at most 2^127)
+              const int down = (int)(__float_as_uint(top) >> 23) - 127 - kAim;
+              const float by = __uint_as_float((uint32_t)(127 - down) << 23);
+              F[b][n][j] *= by;
+              acc[b][0][n][j] *= by; acc[b][0][n][2 + j] *= by;
+              acc[b][1][n][j] *= by; acc[b][1][n][2 + j] *= by;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < TL; ++x) {
+          uint32_t va[2][4];
+          const uint32_t at = stage + C::kCodes + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128;
+          constexpr uint32_t line = 127;
+          const uint32_t blk = (b * C::kGroup) & line;
+          if (C::kBits == 8) {
+            uint32_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = lds4(at + (v_at[i] ^ blk));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // elements 0, 1 and 2, 3 of the lane's four
+              const uint32_t y0 = __byte_perm(c[0], c[1], h ? 0x7362 : 0x5140), y1 = __byte_perm(c[2], c[3], h ? 0x7362 : 0x5140);
+              va[h][0] = half_pair<FMT>(y0, 0);
+              va[h][1] = half_pair<FMT>(y0, 1);
+              va[h][2] = half_pair<FMT>(y1, 0);
+              va[h][3] = half_pair<FMT>(y1, 1);
+            }
+          } else {
+            const uint32_t c0 = lds2(at + (v_at[0] ^ blk)) | lds2(at + (v_at[2] ^ blk)) << 16;
+            const uint32_t c1 = lds2(at + (v_at[1] ^ blk)) | lds2(at + (v_at[3] ^ blk)) << 16;
+            // bytes: elements 0, 2 (and 1, 3) of tokens 2 t, 2 t + 1, then of those 8 further on
+            const uint32_t y0 = (c0 & 0x0F0F0F0Fu) | (c1 & 0x0F0F0F0Fu) << 4, y1 = (c0 >> 4 & 0x0F0F0F0Fu) | (c1 & 0xF0F0F0F0u);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              va[h][0] = half_pair<FMT>(y0, h);
+              va[h][1] = half_pair<FMT>(y1, h);
+              va[h][2] = half_pair<FMT>(y0, 2 + h);
+              va[h][3] = half_pair<FMT>(y1, 2 + h);
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            uint32_t wb[W][2];
+#pragma unroll
+            for (int k = 0; k < W; ++k)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) wb[k][h] = transpose8(w[k][x][n][h]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (WIDE) {  // the sum over tokens in FP32 additions, which round to nearest
+                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                mma(d, va[h], wb[W - 1][0], wb[W - 1][1]);
+                mma(d, va[h], wb[0][0], wb[0][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[b][h][n][i] += d[i];
+              } else {
+                mma(acc[b][h][n], va[h], wb[0][0], wb[0][1]);
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();  // the stage may be filled again
+    }
+
+    // ---- the block's warps joined ----------------------------------------------------------------------------
+    float lse2[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
+        lse2[n][j] = l[n][j] == 0.0f ? -INFINITY : m[n][j] + lg2(l[n][j]);
+        if (g == 0) join_lse[warp * 16 + n * 8 + 2 * t + j] = lse2[n][j];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float all[kWarps], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, all[w] = join_lse[w * 16 + n * 8 + 2 * t + j]);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) sum += all[w] == -INFINITY ? 0.0f : ex2(all[w] - top);
+        // this warp's share of the whole, over its own sum
+        const float mine = l[n][j] == 0.0f ? 0.0f : ex2(lse2[n][j] - top) / (l[n][j] * sum) * C::kUnit;
+        lse2[n][j] = sum == 0.0f ? -INFINITY : top + lg2(sum);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          const float by = 1.0f / F[b][n][j];  // a power of two
+          acc[b][0][n][j] *= mine; acc[b][0][n][2 + j] *= mine;
+          acc[b][1][n][j] *= mine; acc[b][1][n][2 + j] *= mine;
+          acc[b][0][n][j] *= by; acc[b][0][n][2 + j] *= by;
+          acc[b][1][n][j] *= by; acc[b][1][n][2 + j] *= by;
+        }
+      }
+    const bool whole = s.start >= first && s.end <= last;
+    const uint32_t slot = blockIdx.x * 2 + (s.start >= first ? 1 : 0);
+    constexpr int JB = C::kJoinDim / 32;  // blocks at a time
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int b0 = 0; b0 < B; b0 += JB) {
+        auto at = [&](uint32_t half, int b, int j) { return reinterpret_cast<float4*>(join + (half * 8 + 2 * t + j) * C::kJoinDim + (b - b0) * 32 + 4 * g); };
+        auto put = [&](uint32_t half) {
+#pragma unroll
+          for (int b = b0; b < b0 + JB; ++b)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *at(half, b, j) = make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
+        };
+        auto add = [&](uint32_t half) {
+#pragma unroll
+          for (int b = b0; b < b0 + JB; ++b)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float4 v = *at(half, b, j);
+              acc[b][0][n][j] += v.x; acc[b][0][n][2 + j] += v.y;
+              acc[b][1][n][j] += v.z; acc[b][1][n][2 + j] += v.w;
+            }
+        };
+        if (warp >= 2) put(warp - 2);
+        __syncthreads();
+        if (warp < 2) add(warp);
+        if (warp == 1) put(1);
+        __syncthreads();
+        if (warp == 0) {
+          add(1);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t in_tile = n * 8 + 2 * t + j, r = group0 + in_tile;
+            if (r >= a.rows) continue;
+            const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
+            const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
+#pragma unroll
+            for (int b = b0; b < b0 + JB; ++b) {
+              const float4 v = make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
+              if (!whole) *reinterpret_cast<float4*>(a.parts + ((size_t)slot * (8 * NR) + in_tile) * DIM + b * 32 + 4 * g) = v;
+              else if (WIDE) *reinterpret_cast<float4*>((float*)a.out + row * DIM + b * 32 + 4 * g) = v;
+              else *reinterpret_cast<uint2*>((uint16_t*)a.out + row * DIM + b * 32 + 4 * g) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            }
+            if (b0 == 0 && g == 0) {
+              if (!whole) a.part_lse[slot * (8 * NR) + in_tile] = lse2[n][j];
+              else if (a.lse) a.lse[row] = lse2[n][j] * kLn2;
+            }
+          }
+        }
+        if (NR * B > JB) __syncthreads();  // before the buffer is used again
+      }
+    if (s.end >= last) break;
+    a.next(s);
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+template <int FMT, int DIM, int NR, bool WIDE>
+cudaError_t launch_instance(const Args& a, uint32_t ctas, cudaStream_t stream) {
+  using C = Cfg<FMT, DIM, WIDE>;
+  auto kernel = kv_attention_kernel<FMT, DIM, NR, WIDE>;
+  // (a function attribute per device: set on every call, it costs less than a microsecond)
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kShared);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(ctas), dim3(kWarps * 32), C::kShared, stream, a);
+}
+template <int FMT, int DIM>
+cudaError_t launch_dim(const Args& a, bool wide, uint32_t ctas, cudaStream_t stream) {
+  if (wide) return launch_instance<FMT, DIM, 1, true>(a, ctas, stream);
+  if (a.row_tile == 8) return launch_instance<FMT, DIM, 1, false>(a, ctas, stream);
+  return launch_instance<FMT, DIM, DIM <= 128 ? 2 : 1, false>(a, ctas, stream);
+}
+template <int FMT>
+cudaError_t launch_format(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream) {
+  switch (dim) {
+    case 64: return launch_dim<FMT, 64>(a, wide, ctas, stream);
+    case 96: return launch_dim<FMT, 96>(a, wide, ctas, stream);
+    case 128: return launch_dim<FMT, 128>(a, wide, ctas, stream);
+    case 192: return launch_dim<FMT, 192>(a, wide, ctas, stream);
+    default: return launch_dim<FMT, 256>(a, wide, ctas, stream);
+  }
+}
+
+}  // namespace attn
+}  // namespace mx

@@ -1,0 +1,132 @@
+// What the kernels of mx_kv_attention share: their arguments, and how the tiles of all sequences are dealt out.
+#pragma once
+
+#include "mx_device.cuh"
+
+namespace mx {
+namespace attn {
+
+constexpr int kWarps = 4;         // of a block
+constexpr uint32_t kCtas = 296;   // blocks at most: two on each of 148 SMs
+// A block's fewest tiles: one per warp.
+constexpr uint32_t kLeast = kWarps;
+
+// The tiles first .. of one sequence b for one key-value head and one tile of query rows: units start .. end - 1 of the
+// whole list, which runs over sequences, then heads and tiles of rows, then tiles of tokens.
+struct Segment {
+  uint32_t b, hr;            // hr: head * row tiles + row tile
+  uint32_t start, end;
+  uint32_t first_tile;       // tile number (of all the sequence's tokens) of unit `start`
+  uint32_t begin, length;    // tokens that some query sees: begin .. length - 1
+  template <class A> __device__ uint32_t head(const A& a) const { return fastdiv(hr, a.by_row_tiles); }
+  template <class A> __device__ uint32_t row_tile(const A& a) const { return hr - head(a) * a.row_tiles; }
+};
+
+// What a warp keeps of all lengths: lane i has the units of sequences i * chunk .. (i + 1) * chunk - 1.
+struct Share {
+  uint32_t total, per;       // units in all, and of a block
+  uint32_t before;           // units before this lane's sequences
+  uint32_t mine;
+};
+
+struct Args {
+  const uint8_t *k_elems, *k_scales, *v_elems, *v_scales;
+  const void* q;
+  const int32_t *table, *lengths;
+  void* out;
+  float *lse, *parts, *part_lse;  // parts: [2 * blocks][row tile][dim]
+  int64_t q_stride;
+  uint32_t pages, page_size, heads, batch, new_tokens, q_heads, max_pages, window;
+  uint32_t group, rows;           // query heads of a key-value head; query rows of one: new_tokens * group
+  uint32_t row_tile, row_tiles;   // query rows of a unit, units of them
+  uint32_t tokens, chunk;         // tokens of a tile; sequences of a lane
+  FastDiv by_page, by_group, by_row_tiles;
+  float scale_log2;
+
+  __device__ __forceinline__ uint32_t length(uint32_t b) const {
+    const int n = lengths[b];
+    return n < 0 ? 0 : min((uint32_t)n, max_pages * page_size);
+  }
+  // First token that the earliest query sees.
+  __device__ __forceinline__ uint32_t begin(uint32_t length) const {
+    const int64_t e = (int64_t)length - (new_tokens - 1) - window;
+    return window == 0 || e < 0 ? 0 : (uint32_t)e;
+  }
+  __device__ __forceinline__ uint32_t tiles(uint32_t length) const {
+    return length == 0 ? 0 : (length + tokens - 1) / tokens - begin(length) / tokens;
+  }
+  __device__ __forceinline__ void fill(Segment& s) const {
+    s.length = length(s.b);
+    s.begin = begin(s.length);
+    s.first_tile = s.begin / tokens;
+    s.end = s.start + tiles(s.length);
+  }
+  // The next segment that has units (there is one).
+  __device__ __forceinline__ void next(Segment& s) const {
+    const uint32_t n = s.end - s.start;
+    s.start = s.end;
+    if (s.hr + 1 < heads * row_tiles) {
+      ++s.hr;
+      s.end = s.start + n;
+      return;
+    }
+    s.hr = 0;
+    do {
+      ++s.b;
+      fill(s);
+    } while (s.end == s.start);
+  }
+  __device__ __forceinline__ Share share(uint32_t lane) const {
+    Share r;
+    r.mine = 0;
+    for (uint32_t b = lane * chunk; b < min((lane + 1) * chunk, batch); ++b) r.mine += tiles(length(b));
+    r.mine *= heads * row_tiles;
+    uint32_t sum = r.mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      if (lane >= (uint32_t)d) sum += v;
+    }
+    r.before = sum - r.mine;
+    r.total = __shfl_sync(0xFFFFFFFFu, sum, 31);
+    r.per = max((r.total + gridDim.x - 1) / gridDim.x, kLeast);
+    return r;
+  }
+  // The segment of a unit below total.
+  __device__ __forceinline__ Segment find(const Share& share, uint32_t unit, uint32_t lane) const {
+    const uint32_t who = __ffs(__ballot_sync(0xFFFFFFFFu, unit >= share.before && unit - share.before < share.mine)) - 1;
+    Segment s;
+    uint32_t at = __shfl_sync(0xFFFFFFFFu, share.before, who), n;
+    for (uint32_t b0 = who * chunk;; b0 += 32) {  // (its sequences 32 at a time)
+      const uint32_t b = b0 + lane;
+      const uint32_t mine = b < min((who + 1) * chunk, batch) ? tiles(length(b)) * heads * row_tiles : 0;
+      uint32_t sum = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+        if (lane >= (uint32_t)d) sum += v;
+      }
+      const uint32_t hit = __ballot_sync(0xFFFFFFFFu, unit < at + sum);
+      if (hit) {
+        const uint32_t w = __ffs(hit) - 1;
+        s.b = b0 + w;
+        at += __shfl_sync(0xFFFFFFFFu, sum - mine, w);
+        n = __shfl_sync(0xFFFFFFFFu, mine, w) / (heads * row_tiles);
+        break;
+      }
+      at += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    }
+    s.hr = (unit - at) / n;
+    s.start = at + s.hr * n;
+    fill(s);
+    return s;
+  }
+};
+
+cudaError_t launch_e4m3(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream);
+cudaError_t launch_e5m2(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream);
+cudaError_t launch_e2m1(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream);
+cudaError_t launch_int8(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream);
+
+}  // namespace attn
+}  // namespace mx

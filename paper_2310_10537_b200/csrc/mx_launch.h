@@ -247,7 +247,7 @@ struct KvAttentionArgs {
   int sm_count;
   cudaStream_t stream;
 };
-size_t kv_attention_workspace(const KvArgs& kv, int64_t batch, int64_t new_tokens, int64_t q_heads);
+size_t kv_attention_workspace(const KvArgs& kv);
 cudaError_t launch_kv_attention(const KvAttentionArgs& a);
 
 }  // namespace mx

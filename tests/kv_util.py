@@ -54,12 +54,13 @@ def random_cache(pages, page_size, heads, dim, fmt, g, spread=4, middle=None):
 
 
 def attention64(q, cache, table, lengths, scale, window):
-    """out, lse in FP64, and what the error bounds are made of: sum p |v|, the largest sum |q||k| scale and |score|."""
+    """out, lse in FP64, and what the error bounds are made of: sum p |v|, the largest sum |q||k| scale (with
+    2^-9 of max |q| sum |k| scale), and per block the largest p X times the sum of the elements |P|."""
     pages, heads, ps, _ = cache.k_elems.shape
     B, T, Hq, D = q.shape
     G = Hq // heads
     out = torch.zeros((B, T, Hq, D), dtype=torch.float64, device=q.device)
-    absv = torch.zeros_like(out)
+    absv, least = torch.zeros_like(out), torch.zeros_like(out)
     lse = torch.full((B, T, Hq), -math.inf, dtype=torch.float64, device=q.device)
     size = torch.zeros_like(lse)
     for b in range(B):
@@ -80,24 +81,35 @@ def attention64(q, cache, table, lengths, scale, window):
             s = torch.einsum("hgd,nhd->hgn", x, k) * scale
             w = torch.softmax(s, 2)
             out[b, i] = torch.einsum("hgn,nhd->hgd", w, v).reshape(Hq, D)
+            x_v = torch.exp2(cache.v_scales[p, :, o].double() - 127)[..., :D // 32]      # [n, heads, blocks]
+            peak = (w.unsqueeze(3) * x_v.permute(1, 0, 2).unsqueeze(1)).amax(2)           # largest weight of a block [h, g, blocks]
+            codes = (v / x_v.repeat_interleave(32, -1)).abs().sum(0)                      # sum of the elements [h, d]
+            small = peak.repeat_interleave(32, -1) * codes.unsqueeze(1)
             absv[b, i] = torch.einsum("hgn,nhd->hgd", w, v.abs()).reshape(Hq, D)
+            least[b, i] = small.reshape(Hq, D)
             lse[b, i] = torch.logsumexp(s, 2).reshape(Hq)
-            size[b, i] = (torch.einsum("hgd,nhd->hgn", x.abs(), k.abs()) * abs(scale)).amax(2).reshape(Hq)
-    return out, lse, absv, size
+            size[b, i] = (torch.einsum("hgd,nhd->hgn", x.abs() + 2.0 ** -9 * x.abs().amax(2, keepdim=True), k.abs()) * abs(scale)).amax(2).reshape(Hq)
+    return out, lse, absv, size, least
 
 
-def bounds(dtype, want, absv, size, dim, tokens):
+def bounds(dtype, want, absv, size, least, dim, tokens):
     """How far out and lse may be from the definition.
 
     Scores: `dim` products, exact in FP32, and their sum, scale and subtraction of the maximum: each step off by at
     most 2^-23 of sum |q||k| scale (the tensor core's additions may truncate), in all (dim + 16) 2^-23 size for the
     score in units of e.  A weight is off by that and by 2^-21 (the exponential), for its use in the products by half a step of FP16
     (BF16 results) or of two FP16 terms, 2^-22 (FP32).  The weights' sum and the sums over tokens add at most 2^-23 of sum p |v| for each 16 tokens and 64 more
-    for the joins.  The result is rounded once."""
+    for the joins.  The result is rounded once.
+
+    FP16 has steps of 2^-24 below 2^-14.  Queries enter with their largest element in [2^7, 2^8): smaller ones are off by at most
+    2^-25 / 2^7 = 2^-32 of it, which in 2^-23 times `size` is 2^-9 max |q| sum |k|.  Weights w = p X F, X the value's block scale,
+    enter with the largest of a row and block in [2^8, 2^15]: off by at most 2^-25 / 2^8 = 2^-33 of the largest p X, times the
+    element P that it multiplies.  Summed over tokens that is 2^-33 max(p X) sum |P|, 2^-33 of `least`.
+    (Both matter where a large weight meets a tiny element of its block and a tiny weight a large one.)"""
     u = 2.0 ** -23
     score = (dim + 16) * u * size.unsqueeze(3)
     half = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
     rel = 2 * score + 2.0 ** -20 + half + 2 * (tokens / 16 + 64) * u
-    out = absv * rel + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
+    out = absv * rel + 2.0 ** -33 * least + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
     lse = score.squeeze(3) + 2.0 ** -20 + (tokens / 16 + 64) * u
     return out + 1e-38, lse

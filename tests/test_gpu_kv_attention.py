@@ -34,8 +34,8 @@ def _check(q, cache, table, lengths, scale=None, window=0, got=None, **kw):
     scale = q.shape[-1] ** -0.5 if scale is None else scale
     out, lse = mx.mx_kv_attention(q, cache, table, lengths, scale, window, return_lse=True, **kw) if got is None else got
     assert out.dtype == q.dtype and out.shape == q.shape and lse.shape == q.shape[:-1]
-    want, wlse, absv, size = attention64(q, cache, table, lengths, scale, window)
-    tol, ltol = bounds(q.dtype, want, absv, size, q.shape[-1], int(lengths.max()))
+    want, wlse, absv, size, least = attention64(q, cache, table, lengths, scale, window)
+    tol, ltol = bounds(q.dtype, want, absv, size, least, q.shape[-1], int(lengths.max()))
     empty = wlse == -math.inf
     assert torch.equal(lse == -math.inf, empty)
     assert not out[empty].any()
