@@ -32,9 +32,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
   // part 0 is the second slot of this block, the others are the first ones of the blocks behind it
   auto slot = [&](uint32_t p) { return (size_t)((blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile; };
   float top = -INFINITY, total = 0.0f;
+#pragma unroll 1
   for (uint32_t p = lane; p < parts; p += 32) top = fmaxf(top, a.part_lse[slot(p)]);
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+#pragma unroll 1
   for (uint32_t p = lane; p < parts; p += 32) {
     const float v = a.part_lse[slot(p)];
     total += v == -INFINITY ? 0.0f : exp2f(v - top);
@@ -92,7 +94,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.row_tile = row_tile(k.rows, a.kv.dim, wide);
   k.row_tiles = (k.rows + k.row_tile - 1) / k.row_tile;
   const int64_t row_bytes = a.kv.dim * (a.kv.fmt == MX_E2M1 ? 4 : 8) / 8;
-  k.tokens = row_bytes <= 128 ? 32 : 16;  // (Cfg::kTokens)
+  k.tile_log2 = (uint32_t)tile_log2((int)row_bytes);
   k.chunk = (k.batch + 31) / 32;
   k.by_page = make_fastdiv(k.page_size); k.by_group = make_fastdiv(k.group); k.by_row_tiles = make_fastdiv(k.row_tiles);
   k.scale_log2 = a.scale * 1.4426950408889634f;

@@ -6,9 +6,9 @@
 // Both inner sums are tensor-core products of FP16 operands with FP32 accumulators: codes of every format are exact in
 // FP16 (INT8 as the integer), queries are scaled by a power of two into its range.  A key's block scale multiplies the
 // FP32 sum of its block.  A value's scale depends on the token, the axis that its product sums over, so it joins the
-// softmax weight: w[j, r, b] = 2^{s - m[r]} VX[j, b] F[r, b], where m and F are powers of two kept per row (and block) that
-// hold w below 2^15: F follows the largest contribution seen so far, as m follows the largest score.  Both move
-// only when a tile breaks the bound (a vote of the warp), by factors that are exact.
+// softmax weight: w[j, r, b] = 2^{s - m[r]} VX[j, b] F[r, b], with the reference m[r] of a row's scores and a power of two F[r, b]
+// that holds the row's largest w of the block so far below 2^15.  Both move only when a tile breaks their bound (a vote of the
+// warp), and what has been summed moves with them.  No row depends on what else its tile of rows holds.
 // Rounded to FP16: w, half a step 2^-11 of a weight (BF16 results, whose own rounding is 2^-8), or two FP16 terms, 2^-22 (FP32
 // results; the queries too).  Scores, maxima, sums and accumulators are FP32.
 //
@@ -28,6 +28,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "mx_device.cuh"
 #include "mx_kv_attention_args.h"
 #include "mx_rows.cuh"
@@ -37,9 +39,9 @@ namespace attn {
 
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.4028234663852886e38f;  // the reference before any score
-constexpr float kRoom = 6.0f;                       // a moved m leaves the new maximum this far below it
+constexpr float kRoom = 2.0f;                       // a moved m leaves the new maximum up to a factor 2^3 below it
 constexpr float kTop = 32768.0f;                    // weights stay at or below this
-constexpr int kAim = 8;                             // log2 of the largest weight after F has moved
+constexpr int kAim = 12;                            // log2 of the largest weight after F has moved
 constexpr float kMost = 8.507059173023462e37f;      // 2^126, F's largest value
 
 // Shape of a kernel instance.
@@ -51,8 +53,9 @@ struct Cfg {
   static constexpr int kGroup = 4 * kBits;                 // bytes of a block's codes
   // rows in shared memory: whole powers of two, so that the 16-byte units can be permuted within lines of 128 bytes
   static constexpr int kPitch = kRow <= 32 ? 32 : kRow <= 64 ? 64 : kRow <= 128 ? 128 : 256;
-  static constexpr int kTiles = kPitch <= 128 ? 2 : 1;     // MMA tiles of 16 tokens
-  static constexpr int kTokens = 16 * kTiles;
+  static constexpr int kTokens = 1 << tile_log2(kRow);
+  static constexpr int kTiles = kTokens / 16;              // MMA tiles of 16 tokens
+  static constexpr int kMine = kTokens <= 32 ? 1 : kTokens / 32;  // tokens whose place in the cache a lane looks up
   static constexpr int kScale = (kBlocks + 3) / 4 * 4;     // bytes of a row's scales
   static constexpr int kUnits = kRow / 16;                 // 16-byte units of a row
   static constexpr int kCopies = kTokens * kUnits / 32;    // of these a lane copies
@@ -140,6 +143,9 @@ __device__ __forceinline__ uint32_t row_at(uint32_t r) {
   return (r >> 2) * 128 + (((r & 3) << 5) ^ (((r >> 2) & 1) << 4));
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
@@ -197,44 +203,64 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
   const uint32_t last = min(first + share.per, share.total);  // this block's tiles are first .. last - 1
 
   // ---- the copies' side: which tokens the next tile to copy holds -------------------------------------------
-  Segment ls = a.find(share, first, lane);
-  uint32_t lu = first + warp;   // the tile to copy next
-  uint32_t page = 0, off = 0;   // of this lane's token in it
-  bool there = false;
+  Segment s = a.find(share, first, lane), ls = s;
+  uint32_t unit = first + warp, lu = unit;  // the tiles to work on and to copy next
+  uint32_t page[C::kMine], off[C::kMine];   // of this lane's tokens in the tile to copy: tokens lane, 32 + lane
+  bool there[C::kMine];
   auto look_up = [&] {
     if (lu >= last) return;
+#pragma unroll 1
     while (lu >= ls.end) a.next(ls);
-    const uint32_t j = (ls.first_tile + (lu - ls.start)) * C::kTokens + (lane % C::kTokens);
-    there = j < ls.length && j >= ls.begin;
-    if (there) {
+#pragma unroll
+    for (int i = 0; i < C::kMine; ++i) {
+      const uint32_t j = (ls.first_tile + (lu - ls.start)) * C::kTokens + 32 * i + (lane % C::kTokens);
+      there[i] = j < ls.length && j >= ls.begin;
       const uint32_t p = fastdiv(j, a.by_page);
-      off = j - p * a.page_size;
-      page = (uint32_t)__ldg(a.table + (size_t)ls.b * a.max_pages + p);
+      off[i] = j - p * a.page_size;
+      page[i] = 0;
+      if (there[i]) page[i] = (uint32_t)a.table[(size_t)ls.b * a.max_pages + p];
     }
   };
   uint32_t fill = 0;  // the stage to fill next
   auto copy_tile = [&] {
     if (lu < last) {
-      const bool ok = there && page < a.pages;  // (a negative entry is a large one)
-      const uint32_t row = ok ? (page * a.heads + ls.head(a)) * a.page_size + off : 0;
-      const uint32_t seen = __ballot_sync(0xFFFFFFFFu, ok);
       const uint32_t stage = base + fill * C::kStage, scales = stage + 2 * C::kCodes;
+      uint32_t row[C::kMine], seen[C::kMine];
+      bool all = true;
 #pragma unroll
-      for (int i = 0; i < C::kCopies; ++i) {
-        const uint32_t n = lane + 32 * i, r = n / C::kUnits, u = n % C::kUnits;
-        const size_t at = (size_t)__shfl_sync(0xFFFFFFFFu, row, r) * C::kRow + u * 16;
-        const bool has = seen >> r & 1;
-        const uint32_t to = stage + (row_at<C>(r) ^ ((u & 7) << 4)) + (u >> 3) * 128;
-        copy16(to, a.k_elems + at, has);
-        copy16(to + C::kCodes, a.v_elems + at, has);
+      for (int i = 0; i < C::kMine; ++i) {
+        const bool ok = there[i] && page[i] < a.pages;  // (a negative entry is a large one)
+        row[i] = ok ? (page[i] * a.heads + ls.head(a)) * a.page_size + off[i] : 0;
+        seen[i] = __ballot_sync(0xFFFFFFFFu, ok);
+        all = all && seen[i] == 0xFFFFFFFFu;
+        if (C::kTokens >= 32) {
+          copy_small<C::kScale>(scales + (32 * i + lane) * C::kScale, a.k_scales + (size_t)row[i] * C::kScale, ok);
+          copy_small<C::kScale>(scales + (C::kTokens + 32 * i + lane) * C::kScale, a.v_scales + (size_t)row[i] * C::kScale, ok);
+        } else {  // keys' by the lower half of the warp, values' by the upper
+          copy_small<C::kScale>(scales + lane * C::kScale, (lane < 16 ? a.k_scales : a.v_scales) + (size_t)row[i] * C::kScale, ok);
+        }
+        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + 2 * C::kTokens * C::kScale + 4 * i), "r"(seen[i]) : "memory");
       }
-      if (TL == 2) {
-        copy_small<C::kScale>(scales + lane * C::kScale, a.k_scales + (size_t)row * C::kScale, ok);
-        copy_small<C::kScale>(scales + (32 + lane) * C::kScale, a.v_scales + (size_t)row * C::kScale, ok);
-      } else {  // keys' by the lower half of the warp, values' by the upper
-        copy_small<C::kScale>(scales + lane * C::kScale, (lane < 16 ? a.k_scales : a.v_scales) + (size_t)row * C::kScale, ok);
-      }
-      if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + 2 * C::kTokens * C::kScale), "r"(seen) : "memory");
+      auto codes = [&](auto whole) {
+#pragma unroll
+        for (int i = 0; i < C::kCopies; ++i) {
+          const uint32_t n = lane + 32 * i, r = n / C::kUnits, u = n % C::kUnits;
+          // (which of a lane's two tokens: known at compile time where the units of 32 tokens are whole rounds of the warp)
+          const int mine = C::kMine == 1 ? 0 : 32 * i / (32 * C::kUnits);
+          const size_t at = (size_t)__shfl_sync(0xFFFFFFFFu, row[mine], r % 32) * C::kRow + u * 16;
+          const uint32_t to = stage + (row_at<C>(r) ^ ((u & 7) << 4)) + (u >> 3) * 128;
+          if constexpr (decltype(whole)::value) {
+            copy16(to, a.k_elems + at);
+            copy16(to + C::kCodes, a.v_elems + at);
+          } else {
+            const bool has = seen[mine] >> (r % 32) & 1;
+            copy16(to, a.k_elems + at, has);
+            copy16(to + C::kCodes, a.v_elems + at, has);
+          }
+        }
+      };
+      if (all) codes(std::true_type());
+      else codes(std::false_type());
       lu += kWarps;
       fill = fill + 1 == C::kStages ? 0 : fill + 1;
       look_up();
@@ -242,8 +268,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   look_up();
-#pragma unroll
-  for (int i = 0; i < C::kStages - 1; ++i) copy_tile();
+  uint32_t ahead = C::kStages;  // copies before the next tile: the first one finds all stages free
 
   // lane offsets of the codes: keys of tokens g, g + 8; values of tokens 2 t, 2 t + 1 (and 8 further on)
   const uint32_t k_at[2] = {row_at<C>(g) + t * (C::kGroup / 4), row_at<C>(g + 8) + t * (C::kGroup / 4)};
@@ -251,8 +276,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
   for (int i = 0; i < 4; ++i) v_at[i] = row_at<C>(2 * t + (i & 1) + (i & 2) * 4) + g * (C::kGroup / 8);
 
-  uint32_t use = 0, unit = first + warp;
-  Segment s = a.find(share, first, lane);
+  uint32_t use = 0;
   for (;;) {
     // ---- one sequence and head: the queries ------------------------------------------------------------------
     const uint32_t seg_end = min(s.end, last);
@@ -268,8 +292,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
       if (r < a.rows) {
         const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
         const size_t at = ((size_t)s.b * a.new_tokens + i) * a.q_stride + (size_t)head * DIM + t * 8;
+        Raw8<WIDE ? MX_F32 : MX_BF16> raw[B];
 #pragma unroll
-        for (int b = 0; b < B; ++b) widen(load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32), x[b]);
+        for (int b = 0; b < B; ++b) raw[b] = load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32);
+#pragma unroll
+        for (int b = 0; b < B; ++b) widen(raw[b], x[b]);
       } else {
 #pragma unroll
         for (int b = 0; b < B; ++b)
@@ -301,7 +328,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
               q[W - 1][b][k][n][j] = pack_half(u - h.x, v - h.y);
             }
           }
-      const float f = a.scale_log2 * C::kUnit / half2 / half1;
+      // (1 / half is a power of two as well)
+      const float f = a.scale_log2 * C::kUnit * __uint_as_float((uint32_t)(127 + (e - e / 2)) << 23) * __uint_as_float((uint32_t)(127 + e / 2) << 23);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         qf[n][j] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + j) * 4);
@@ -334,17 +362,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
           for (int i = 0; i < 4; ++i) acc[b][h][n][i] = 0.0f;
 
     // ---- its tiles ----------------------------------------------------------------------------------------
+#pragma unroll 1
     for (; unit < seg_end; unit += kWarps) {
-      copy_tile();
+#pragma unroll 1
+      for (; ahead > 0; --ahead) copy_tile();
+      ahead = 1;
       asm volatile("cp.async.wait_group %0;" ::"n"(C::kStages - 1) : "memory");
       __syncwarp();
       const uint32_t stage = base + use * C::kStage, scales = stage + 2 * C::kCodes;
       use = use + 1 == C::kStages ? 0 : use + 1;
-      const uint32_t seen = lds4(scales + 2 * C::kTokens * C::kScale);
+      uint32_t seen[C::kMine];
       const int j0 = (int)(s.first_tile + (unit - s.start)) * C::kTokens;
-      const bool edge = seen != 0xFFFFFFFFu || j0 < all_lo || j0 + C::kTokens > all_hi;
+      bool edge = j0 < all_lo || j0 + C::kTokens > all_hi;
+#pragma unroll
+      for (int i = 0; i < C::kMine; ++i) {
+        seen[i] = lds4(scales + 2 * C::kTokens * C::kScale + 4 * i);
+        edge = edge || seen[i] != 0xFFFFFFFFu;
+      }
 
-      // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1
+      // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1, without the rows' factors
       float p[TL][NR][4];
 #pragma unroll
       for (int x = 0; x < TL; ++x) {
@@ -355,7 +391,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
           for (int c = 0; c < C::kScale; c += 4) {
             const uint32_t w = lds4(scales + (16 * x + 8 * h + g) * C::kScale + c);
             scales2(w, ks[h][c], ks[h][c + 1]);
-            scales2(w >> 16, ks[h][c + 2], ks[h][c + 3]);
+            if (c + 2 < B) scales2(w >> 16, ks[h][c + 2], ks[h][c + 3]);
           }
 #pragma unroll
         for (int n = 0; n < NR; ++n)
@@ -392,12 +428,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
             for (int i = 0; i < 4; ++i) p[x][n][i] = fmaf(d[i], ks[i >> 1][b], p[x][n][i]);
           }
         }
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[x][n][i] *= qf[n][i & 1];
       }
-      uint32_t out_mask = 0;  // bit: this score is of a token that the row does not see
+      uint32_t hidden = 0;  // bit: this score is of a token that the row does not see
       if (edge) {
 #pragma unroll
         for (int x = 0; x < TL; ++x)
@@ -406,14 +438,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * x + 8 * (i >> 1) + (int)g, j = j0 + k;
-              if (!(seen >> k & 1) || j < lo[n][i & 1] || j >= hi[n][i & 1]) {
-                p[x][n][i] = -INFINITY;
-                out_mask |= 1u << ((x * NR + n) * 4 + i);
-              }
+              if (!(seen[x / 2 % C::kMine] >> (k % 32) & 1) || j < lo[n][i & 1] || j >= hi[n][i & 1]) hidden |= 1u << ((x * NR + n) * 4 + i);
             }
       }
 
-      // the maxima: m moves when a score passes it
+      // weights without the values' scales: m moves when a score passes it
+      float y[TL][NR][4];
       for (;;) {
         float most = -1.0f;
 #pragma unroll
@@ -421,7 +451,22 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
           for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, p[x][n][i] - m[n][i & 1]);
+            for (int i = 0; i < 4; ++i) y[x][n][i] = fmaf(p[x][n][i], qf[n][i & 1], -m[n][i & 1]);
+        if (edge) {
+#pragma unroll
+          for (int x = 0; x < TL; ++x)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (hidden >> ((x * NR + n) * 4 + i) & 1) y[x][n][i] = -INFINITY;
+        }
+#pragma unroll
+        for (int x = 0; x < TL; ++x)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, y[x][n][i]);
         if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
 #pragma unroll
         for (int n = 0; n < NR; ++n)
@@ -429,24 +474,23 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
           for (int j = 0; j < 2; ++j) {
             float top = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < TL; ++x) top = fmaxf(top, fmaxf(p[x][n][j], p[x][n][2 + j]));
+            for (int x = 0; x < TL; ++x)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                if (!(hidden >> ((x * NR + n) * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][n][2 * h + j] * qf[n][j]);
 #pragma unroll
             for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            if (top <= m[n][j]) continue;
-            const float next = ceilf(top) + kRoom, up = next - m[n][j];
-            l[n][j] *= ex2(-up);
+            const bool moves = top > m[n][j];
+            const float next = moves ? ceilf(top) + kRoom : m[n][j], by = moves ? ex2(m[n][j] - next) : 1.0f;
             m[n][j] = next;
-            // weights are relative to m F: F takes the move, as far as it can
+            l[n][j] *= by;
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-              const float f = (float)((int)(__float_as_uint(F[b][n][j]) >> 23) - 127), want = f + up, have = fminf(want, 126.0f);
-              F[b][n][j] = __uint_as_float((uint32_t)((int)have + 127) << 23);
-              if (have < want) {
-                const float down = ex2(have - want);
-                acc[b][0][n][j] *= down; acc[b][0][n][2 + j] *= down;
-                acc[b][1][n][j] *= down; acc[b][1][n][2 + j] *= down;
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                acc[b][h][n][j] *= by;
+                acc[b][h][n][2 + j] *= by;
               }
-            }
           }
       }
 #pragma unroll
@@ -455,74 +499,95 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
         for (int n = 0; n < NR; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[x][n][i] = ex2(p[x][n][i] - m[n][i & 1]);
+            p[x][n][i] = ex2(y[x][n][i]);
             l[n][i & 1] += p[x][n][i];
           }
 
-      // values, block by block
-      float vs[TL][2][C::kScale];
+      // weights with the values' scales: F moves when one passes kTop
+      uint32_t w[W][B][TL][NR][2];
+      for (;;) {
+        uint32_t most = 0;
 #pragma unroll
-      for (int x = 0; x < TL; ++x)
+        for (int x = 0; x < TL; ++x) {
+          float vs[2][C::kScale];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int c = 0; c < C::kScale; c += 4) {
-            const uint32_t w = lds4(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + c);
-            scales2(w, vs[x][h][c], vs[x][h][c + 1]);
-            scales2(w >> 16, vs[x][h][c + 2], vs[x][h][c + 3]);
-          }
+            for (int c = 0; c < C::kScale; c += 4) {
+              const uint32_t v = lds4(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + c);
+              scales2(v, vs[h][c], vs[h][c + 1]);
+              if (c + 2 < B) scales2(v >> 16, vs[h][c + 2], vs[h][c + 3]);
+            }
 #pragma unroll
-      for (int b = 0; b < B; ++b) {
-        uint32_t w[W][TL][NR][2];
-        for (;;) {
-          uint32_t most = 0;
+          for (int b = 0; b < B; ++b)
 #pragma unroll
-          for (int x = 0; x < TL; ++x)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float u = p[x][n][2 * h] * vs[x][h][b] * F[b][n][0], v = p[x][n][2 * h + 1] * vs[x][h][b] * F[b][n][1];
-                if (edge) {  // a token that is not seen weighs nothing, whatever its scale
-                  if (out_mask >> ((x * NR + n) * 4 + 2 * h) & 1) u = 0.0f;
-                  if (out_mask >> ((x * NR + n) * 4 + 2 * h + 1) & 1) v = 0.0f;
-                }
-                w[0][x][n][h] = pack_half(u, v);
-                most = max_half2(most, w[0][x][n][h]);
+              for (int n = 0; n < NR; ++n) {
+                // p is at most 1 and VX at most 2^127, F follows their product
+                const float u = p[x][n][2 * h] * vs[h][b] * F[b][n][0], v = p[x][n][2 * h + 1] * vs[h][b] * F[b][n][1];
+                const uint32_t c = pack_half(u, v);
+                w[0][b][x][n][h] = c;
+                most = max_half2(most, c);
                 if (WIDE) {
-                  const float2 f = unpack_half(w[0][x][n][h]);
-                  w[W - 1][x][n][h] = pack_half(u - f.x, v - f.y);
+                  const float2 r = unpack_half(c);
+                  w[W - 1][b][x][n][h] = pack_half(u - r.x, v - r.y);
                 }
               }
-          const float2 f = unpack_half(most);
-          if (!__any_sync(0xFFFFFFFFu, fmaxf(f.x, f.y) > kTop)) break;
+        }
+        const float2 top2 = unpack_half(most);
+        if (!__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
+        // F moves to where the largest is in [2^kAim, 2^(kAim + 1)), never up: a smaller F only costs small weights their digits
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            float top[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < TL; ++x)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float v, other;
+                scales2(lds2(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + b / 2 * 2) >> 8 * (b % 2), v, other);
+                top[0] = fmaxf(top[0], p[x][n][2 * h] * v);
+                top[1] = fmaxf(top[1], p[x][n][2 * h + 1] * v);
+              }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) top[j] = fmaxf(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], d));
+              const int e = (int)(__float_as_uint(top[j]) >> 23) - 127, have = (int)(__float_as_uint(F[b][n][j]) >> 23) - 127;
+              const int next = min(have, kAim - e);
+              const float by = next < have ? ex2((float)(next - have)) : 1.0f;
+              F[b][n][j] = __uint_as_float((uint32_t)(127 + next) << 23);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                acc[b][h][n][j] *= by;
+                acc[b][h][n][2 + j] *= by;
+              }
+            }
+          }
+      }
+      if (edge) {  // a token that is not seen weighs nothing, whatever its scale
+#pragma unroll
+        for (int x = 0; x < TL; ++x)
 #pragma unroll
           for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float top = 0.0f;
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t two = hidden >> ((x * NR + n) * 4 + 2 * h) & 3, keep = (two & 1 ? 0u : 0xFFFFu) | (two & 2 ? 0u : 0xFFFF0000u);
 #pragma unroll
-              for (int x = 0; x < TL; ++x)
+              for (int k = 0; k < W; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                  if (!(out_mask >> ((x * NR + n) * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][n][2 * h + j] * vs[x][h][b] * F[b][n][j]);
-#pragma unroll
-              for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-              if (!(top > kTop)) continue;
-              // (F is a normal number: p is at most 1, VX at most 2^127)
-              const int down = (int)(__float_as_uint(top) >> 23) - 127 - kAim;
-              const float by = __uint_as_float((uint32_t)(127 - down) << 23);
-              F[b][n][j] *= by;
-              acc[b][0][n][j] *= by; acc[b][0][n][2 + j] *= by;
-              acc[b][1][n][j] *= by; acc[b][1][n][2 + j] *= by;
+                for (int b = 0; b < B; ++b) w[k][b][x][n][h] &= keep;
             }
-        }
+      }
+#pragma unroll
+      for (int b = 0; b < B; ++b)
 #pragma unroll
         for (int x = 0; x < TL; ++x) {
           uint32_t va[2][4];
-          const uint32_t at = stage + C::kCodes + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128;
-          constexpr uint32_t line = 127;
-          const uint32_t blk = (b * C::kGroup) & line;
+          const uint32_t at = stage + C::kCodes + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128, blk = (b * C::kGroup) & 127;
           if (C::kBits == 8) {
             uint32_t c[4];
 #pragma unroll
@@ -554,7 +619,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
             for (int k = 0; k < W; ++k)
 #pragma unroll
-              for (int h = 0; h < 2; ++h) wb[k][h] = transpose8(w[k][x][n][h]);
+              for (int h = 0; h < 2; ++h) wb[k][h] = transpose8(w[k][b][x][n][h]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               if (WIDE) {  // the sum over tokens in FP32 additions, which round to nearest
@@ -569,7 +634,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
             }
           }
         }
-      }
       __syncwarp();  // the stage may be filled again
     }
 

@@ -11,6 +11,10 @@ constexpr uint32_t kCtas = 296;   // blocks at most: two on each of 148 SMs
 // A block's fewest tiles: one per warp.
 constexpr uint32_t kLeast = kWarps;
 
+// Tokens of a tile: 64 where their codes are short, so that what a tile costs whatever its size counts less; 16 for rows above 128
+// bytes, for the shared memory.
+__host__ __device__ constexpr int tile_log2(int row_bytes) { return row_bytes <= 64 ? 6 : row_bytes <= 128 ? 5 : 4; }
+
 // The tiles first .. of one sequence b for one key-value head and one tile of query rows: units start .. end - 1 of the
 // whole list, which runs over sequences, then heads and tiles of rows, then tiles of tokens.
 struct Segment {
@@ -39,7 +43,7 @@ struct Args {
   uint32_t pages, page_size, heads, batch, new_tokens, q_heads, max_pages, window;
   uint32_t group, rows;           // query heads of a key-value head; query rows of one: new_tokens * group
   uint32_t row_tile, row_tiles;   // query rows of a unit, units of them
-  uint32_t tokens, chunk;         // tokens of a tile; sequences of a lane
+  uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
   FastDiv by_page, by_group, by_row_tiles;
   float scale_log2;
 
@@ -53,12 +57,12 @@ struct Args {
     return window == 0 || e < 0 ? 0 : (uint32_t)e;
   }
   __device__ __forceinline__ uint32_t tiles(uint32_t length) const {
-    return length == 0 ? 0 : (length + tokens - 1) / tokens - begin(length) / tokens;
+    return length == 0 ? 0 : ((length - 1) >> tile_log2) + 1 - (begin(length) >> tile_log2);
   }
   __device__ __forceinline__ void fill(Segment& s) const {
     s.length = length(s.b);
     s.begin = begin(s.length);
-    s.first_tile = s.begin / tokens;
+    s.first_tile = s.begin >> tile_log2;
     s.end = s.start + tiles(s.length);
   }
   // The next segment that has units (there is one).
@@ -71,22 +75,34 @@ struct Args {
       return;
     }
     s.hr = 0;
+#pragma unroll 1
     do {
       ++s.b;
       fill(s);
     } while (s.end == s.start);
   }
-  __device__ __forceinline__ Share share(uint32_t lane) const {
-    Share r;
-    r.mine = 0;
-    for (uint32_t b = lane * chunk; b < min((lane + 1) * chunk, batch); ++b) r.mine += tiles(length(b));
-    r.mine *= heads * row_tiles;
-    uint32_t sum = r.mine;
+  __device__ __forceinline__ static uint32_t scan(uint32_t v, uint32_t lane) {  // inclusive sums over the lanes
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-      if (lane >= (uint32_t)d) sum += v;
+      const uint32_t u = __shfl_up_sync(0xFFFFFFFFu, v, d);
+      if (lane >= (uint32_t)d) v += u;
     }
+    return v;
+  }
+  __device__ __forceinline__ Share share(uint32_t lane) const {
+    Share r;
+    uint32_t n = 0;
+    const uint32_t e = min((lane + 1) * chunk, batch);
+#pragma unroll 1
+    for (uint32_t b = lane * chunk; b < e; b += 4) {  // (four lengths in flight)
+      uint32_t v[4];
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) v[i] = b + i < e ? length(b + i) : 0;
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) n += tiles(v[i]);
+    }
+    r.mine = n * heads * row_tiles;
+    const uint32_t sum = scan(r.mine, lane);
     r.before = sum - r.mine;
     r.total = __shfl_sync(0xFFFFFFFFu, sum, 31);
     r.per = max((r.total + gridDim.x - 1) / gridDim.x, kLeast);
@@ -95,30 +111,30 @@ struct Args {
   // The segment of a unit below total.
   __device__ __forceinline__ Segment find(const Share& share, uint32_t unit, uint32_t lane) const {
     const uint32_t who = __ffs(__ballot_sync(0xFFFFFFFFu, unit >= share.before && unit - share.before < share.mine)) - 1;
+    uint32_t at = __shfl_sync(0xFFFFFFFFu, share.before, who);
     Segment s;
-    uint32_t at = __shfl_sync(0xFFFFFFFFu, share.before, who), n;
-    for (uint32_t b0 = who * chunk;; b0 += 32) {  // (its sequences 32 at a time)
-      const uint32_t b = b0 + lane;
-      const uint32_t mine = b < min((who + 1) * chunk, batch) ? tiles(length(b)) * heads * row_tiles : 0;
-      uint32_t sum = mine;
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
-        if (lane >= (uint32_t)d) sum += v;
+    s.b = who;
+    if (chunk > 1) {
+#pragma unroll 1
+      for (uint32_t b0 = who * chunk;; b0 += 32) {  // its sequences, 32 at a time
+        const uint32_t b = b0 + lane;
+        const uint32_t mine = b < min((who + 1) * chunk, batch) ? tiles(length(b)) * heads * row_tiles : 0, sum = scan(mine, lane);
+        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, unit - at < sum);
+        if (hit) {
+          const uint32_t w = __ffs(hit) - 1;
+          s.b = b0 + w;
+          at += __shfl_sync(0xFFFFFFFFu, sum - mine, w);
+          break;
+        }
+        at += __shfl_sync(0xFFFFFFFFu, sum, 31);
       }
-      const uint32_t hit = __ballot_sync(0xFFFFFFFFu, unit < at + sum);
-      if (hit) {
-        const uint32_t w = __ffs(hit) - 1;
-        s.b = b0 + w;
-        at += __shfl_sync(0xFFFFFFFFu, sum - mine, w);
-        n = __shfl_sync(0xFFFFFFFFu, mine, w) / (heads * row_tiles);
-        break;
-      }
-      at += __shfl_sync(0xFFFFFFFFu, sum, 31);
     }
+    s.start = 0;
+    fill(s);
+    const uint32_t n = s.end;
     s.hr = (unit - at) / n;
     s.start = at + s.hr * n;
-    fill(s);
+    s.end = s.start + n;
     return s;
   }
 };

@@ -55,7 +55,7 @@ def random_cache(pages, page_size, heads, dim, fmt, g, spread=4, middle=None):
 
 def attention64(q, cache, table, lengths, scale, window):
     """out, lse in FP64, and what the error bounds are made of: sum p |v|, the largest sum |q||k| scale (with
-    2^-9 of max |q| sum |k| scale), and per block the largest p X times the sum of the elements |P|."""
+    2^-9 of max |q| sum |k| scale), and per block what FP16's smallest steps are relative to (see bounds)."""
     pages, heads, ps, _ = cache.k_elems.shape
     B, T, Hq, D = q.shape
     G = Hq // heads
@@ -82,7 +82,7 @@ def attention64(q, cache, table, lengths, scale, window):
             w = torch.softmax(s, 2)
             out[b, i] = torch.einsum("hgn,nhd->hgd", w, v).reshape(Hq, D)
             x_v = torch.exp2(cache.v_scales[p, :, o].double() - 127)[..., :D // 32]      # [n, heads, blocks]
-            peak = (w.unsqueeze(3) * x_v.permute(1, 0, 2).unsqueeze(1)).amax(2)           # largest weight of a block [h, g, blocks]
+            peak = (w.unsqueeze(3) * x_v.permute(1, 0, 2).unsqueeze(1)).amax(2)           # largest weight times scale [h, g, blocks]
             codes = (v / x_v.repeat_interleave(32, -1)).abs().sum(0)                      # sum of the elements [h, d]
             small = peak.repeat_interleave(32, -1) * codes.unsqueeze(1)
             absv[b, i] = torch.einsum("hgn,nhd->hgd", w, v.abs()).reshape(Hq, D)
@@ -102,14 +102,15 @@ def bounds(dtype, want, absv, size, least, dim, tokens):
     for the joins.  The result is rounded once.
 
     FP16 has steps of 2^-24 below 2^-14.  Queries enter with their largest element in [2^7, 2^8): smaller ones are off by at most
-    2^-25 / 2^7 = 2^-32 of it, which in 2^-23 times `size` is 2^-9 max |q| sum |k|.  Weights w = p X F, X the value's block scale,
-    enter with the largest of a row and block in [2^8, 2^15]: off by at most 2^-25 / 2^8 = 2^-33 of the largest p X, times the
-    element P that it multiplies.  Summed over tokens that is 2^-33 max(p X) sum |P|, 2^-33 of `least`.
+    2^-25 / 2^7 = 2^-32 of it, which in 2^-23 times `size` is 2^-9 max |q| sum |k|.  Weights w = p X F, X the value's block scale and
+    p = e^(s - m) enter with a row's largest of a block in [2^12, 2^15]: F >= 2^12 / max p X, and each is off by at most
+    2^-25 / F <= 2^-37 max p X, times the element P that it multiplies, divided by the sum of p.  Over tokens that is 2^-37 of `least`,
+    the largest softmax weight times X, times the sum of |P|.
     (Both matter where a large weight meets a tiny element of its block and a tiny weight a large one.)"""
     u = 2.0 ** -23
     score = (dim + 16) * u * size.unsqueeze(3)
     half = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
     rel = 2 * score + 2.0 ** -20 + half + 2 * (tokens / 16 + 64) * u
-    out = absv * rel + 2.0 ** -33 * least + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
+    out = absv * rel + 2.0 ** -37 * least + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
     lse = score.squeeze(3) + 2.0 ** -20 + (tokens / 16 + 64) * u
     return out + 1e-38, lse
