@@ -11,72 +11,122 @@ namespace {
 constexpr int kJoinWarps = 8;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Query row blockIdx.y (of its tile of rows) of the sequence and head that begins in block blockIdx.x of the attention kernel and
-// goes on behind it, if there is one.  Warps take the parts in turn, a lane four elements: out = sum of the parts'
-// means by their weights 2^lse, in the order of the parts within a warp and then of the warps.
-template <int DTYPE>
+// A few query rows (ROWS of their tile of rows, the ones blockIdx.y * ROWS ..) of the sequence and head that begins in block blockIdx.x
+// of the attention kernel and goes on behind it, if there is one.  The warps of a row take its parts in turn, a lane four elements:
+// out = sum of the parts' means by their weights 2^lse over the sum of the weights, in the order of the parts within a warp and
+// then of the warps.
+template <int DTYPE, int ROWS>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, uint32_t dim) {
-  __shared__ float sums[kJoinWarps][256];
+  constexpr uint32_t kPer = kJoinWarps / ROWS;  // warps of a row
+  __shared__ float4 sums[kJoinWarps][64];
+  __shared__ float2 weights[kJoinWarps];        // the largest lse of a warp's parts, the sum of their weights
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // (the lengths are there: the attention kernel let this one start when it had waited for them)
-  const Share share = a.share(lane);
-  const uint32_t first = blockIdx.x * share.per, last = first + share.per;
-  Segment s = {};
-  if (last < share.total) s = a.find(share, last, lane);
-  const uint32_t in_tile = blockIdx.y, r = s.row_tile(a) * a.row_tile + in_tile;
+  // Sequences without a token to see, which have no tile.  (The lengths are there: the attention kernel let this one start when
+  // it had waited for them.)
+  const uint32_t rows = a.new_tokens * a.q_heads;
+  for (uint32_t b = blockIdx.y * gridDim.x + blockIdx.x; b < a.batch; b += gridDim.x * gridDim.y) {
+    if (a.tiles(a.length(b)) != 0) continue;
+    for (uint32_t i = threadIdx.x; i < rows * (dim / 8); i += kJoinWarps * 32) {
+      const float zero[8] = {};
+      store8<DTYPE>(a.out, (size_t)b * rows * dim + (size_t)i * 8, zero);
+    }
+    if (a.lse)
+      for (uint32_t i = threadIdx.x; i < rows; i += kJoinWarps * 32) a.lse[(size_t)b * rows + i] = -INFINITY;
+  }
   // every block waits, also one without work: the stream's next kernel goes by this grid's end
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (last >= share.total || s.start < first || s.start >= last || r >= a.rows) return;
-  const uint32_t parts = (s.end - 1) / share.per - blockIdx.x + 1;
-  // part 0 is the second slot of this block, the others are the first ones of the blocks behind it
-  auto slot = [&](uint32_t p) { return (size_t)((blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile; };
+  const Unfinished s = a.unfinished[blockIdx.x];
+  if (s.parts == 0) return;
+  const uint32_t head0 = fastdiv(s.hr, a.by_row_tiles), row_tile = s.hr - head0 * a.row_tiles;
+  const uint32_t in_tile = blockIdx.y * ROWS + warp / kPer, r = row_tile * a.row_tile + in_tile;
   float top = -INFINITY, total = 0.0f;
+  float4 sum[2] = {};
+  if (r < a.rows) {
+    constexpr int kBatch = 8;  // parts in flight
 #pragma unroll 1
-  for (uint32_t p = lane; p < parts; p += 32) top = fmaxf(top, a.part_lse[slot(p)]);
+    for (uint32_t p0 = warp % kPer; p0 < s.parts; p0 += kPer * kBatch) {
+      float lse[kBatch];
+      float4 x[kBatch][2];
+      float most = top;
 #pragma unroll
-  for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-#pragma unroll 1
-  for (uint32_t p = lane; p < parts; p += 32) {
-    const float v = a.part_lse[slot(p)];
-    total += v == -INFINITY ? 0.0f : exp2f(v - top);
-  }
+      for (int k = 0; k < kBatch; ++k) {
+        const uint32_t p = p0 + k * kPer;
+        lse[k] = -INFINITY;
+        x[k][0] = x[k][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (p < s.parts) {
+          // part 0 is the second slot of this block, the others are the first ones of the blocks behind it
+          const size_t at = (size_t)((blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile;
+          lse[k] = a.part_lse[at];
+          if (lane * 4 < dim) x[k][0] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4);
+          if (lane * 4 + 128 < dim) x[k][1] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4 + 128);
+        }
+      }
 #pragma unroll
-  for (int d = 1; d < 32; d *= 2) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
-  for (uint32_t e = lane * 4; e < dim; e += 128) {
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (uint32_t p = warp; p < parts; p += kJoinWarps) {
-      const size_t at = slot(p);
-      const float v = a.part_lse[at], w = v == -INFINITY ? 0.0f : exp2f(v - top);
-      const float4 x = *reinterpret_cast<const float4*>(a.parts + at * dim + e);
-      if (v != -INFINITY) {
-        sum.x = fmaf(w, x.x, sum.x); sum.y = fmaf(w, x.y, sum.y);
-        sum.z = fmaf(w, x.z, sum.z); sum.w = fmaf(w, x.w, sum.w);
+      for (int k = 0; k < kBatch; ++k) most = fmaxf(most, lse[k]);
+      const float keep = top == -INFINITY ? 0.0f : exp2f(top - most);
+      top = most;
+      total *= keep;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sum[h].x *= keep; sum[h].y *= keep; sum[h].z *= keep; sum[h].w *= keep;
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (lse[k] == -INFINITY) continue;  // nothing seen in this part
+        const float w = exp2f(lse[k] - top);
+        total += w;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          sum[h].x = fmaf(w, x[k][h].x, sum[h].x); sum[h].y = fmaf(w, x[k][h].y, sum[h].y);
+          sum[h].z = fmaf(w, x[k][h].z, sum[h].z); sum[h].w = fmaf(w, x[k][h].w, sum[h].w);
+        }
       }
     }
-    *reinterpret_cast<float4*>(&sums[warp][e]) = sum;
   }
+  sums[warp][lane] = sum[0];
+  sums[warp][32 + lane] = sum[1];
+  if (lane == 0) weights[warp] = make_float2(top, total);
   __syncthreads();
-  const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
-  const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
-  for (uint32_t e = threadIdx.x; e < dim; e += kJoinWarps * 32) {
-    float v = 0.0f;
+  // a row's warps put out a part of it each
+  const uint32_t w0 = warp / kPer * kPer;
+  float most = -INFINITY, all = 0.0f, by[kPer];
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) v += sums[w][e];
-    store1<DTYPE>(a.out, row * dim + e, total == 0.0f ? 0.0f : v / total);
+  for (uint32_t w = 0; w < kPer; ++w) most = fmaxf(most, weights[w0 + w].x);
+#pragma unroll
+  for (uint32_t w = 0; w < kPer; ++w) {
+    const float2 v = weights[w0 + w];
+    by[w] = v.y == 0.0f ? 0.0f : exp2f(v.x - most);
+    all += v.y * by[w];
   }
-  if (a.lse && threadIdx.x == 0) a.lse[row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * kLn2;
+  if (r >= a.rows) return;
+  const uint32_t i = fastdiv(r, a.by_group), head = head0 * a.group + (r - i * a.group);
+  const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
+  for (uint32_t e = warp % kPer * 32 + lane; e < dim / 4; e += kPer * 32) {
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (uint32_t w = 0; w < kPer; ++w) {
+      const float4 u = sums[w0 + w][e];
+      if (by[w] == 0.0f) continue;
+      v.x = fmaf(by[w], u.x, v.x); v.y = fmaf(by[w], u.y, v.y);
+      v.z = fmaf(by[w], u.z, v.z); v.w = fmaf(by[w], u.w, v.w);
+    }
+    const float whole = all == 0.0f ? 0.0f : 1.0f / all;
+    v.x *= whole; v.y *= whole; v.z *= whole; v.w *= whole;
+    if (DTYPE == MX_BF16) *reinterpret_cast<uint2*>((uint16_t*)a.out + row * dim + e * 4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    else *reinterpret_cast<float4*>((float*)a.out + row * dim + e * 4) = v;
+  }
+  if (a.lse && warp % kPer == 0 && lane == 0) a.lse[row] = all == 0.0f ? -INFINITY : (most + log2f(all)) * kLn2;
 }
 
 // Query rows of a unit: 8, or 16 where there are more (FP32 and rows above 128 elements: 8, for the registers).
 uint32_t row_tile(int64_t rows, int64_t dim, bool wide) { return rows > 8 && dim <= 128 && !wide ? 16 : 8; }
-size_t part_bytes(uint32_t rows, int64_t dim) { return ((size_t)2 * kCtas * rows * (size_t)(dim + 1) * 4 + 255) / 256 * 256; }
+size_t workspace_bytes(uint32_t rows, int64_t dim) { return kCtas * (sizeof(Unfinished) + (size_t)2 * rows * (size_t)(dim + 1) * 4); }
 
 }  // namespace
 }  // namespace attn
 
-size_t kv_attention_workspace(const KvArgs& kv) { return attn::part_bytes(16, kv.dim); }
+size_t kv_attention_workspace(const KvArgs& kv) { return attn::workspace_bytes(16, kv.dim); }
 
 cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   using namespace attn;
@@ -93,14 +143,15 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.rows = k.new_tokens * k.group;
   k.row_tile = row_tile(k.rows, a.kv.dim, wide);
   k.row_tiles = (k.rows + k.row_tile - 1) / k.row_tile;
-  const int64_t row_bytes = a.kv.dim * (a.kv.fmt == MX_E2M1 ? 4 : 8) / 8;
-  k.tile_log2 = (uint32_t)tile_log2((int)row_bytes);
+  k.tile_log2 = (uint32_t)tile_log2((int)a.kv.dim, a.kv.fmt == MX_E2M1 ? 4 : 8);
   k.chunk = (k.batch + 31) / 32;
   k.by_page = make_fastdiv(k.page_size); k.by_group = make_fastdiv(k.group); k.by_row_tiles = make_fastdiv(k.row_tiles);
   k.scale_log2 = a.scale * 1.4426950408889634f;
-  k.parts = (float*)a.workspace;
+  k.unfinished = (Unfinished*)a.workspace;
+  k.parts = (float*)(k.unfinished + kCtas);
   k.part_lse = k.parts + (size_t)2 * kCtas * k.row_tile * (size_t)a.kv.dim;
-  const uint32_t ctas = (uint32_t)a.sm_count * 2 < kCtas ? (uint32_t)a.sm_count * 2 : kCtas;
+  const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, (int)k.row_tile / 8, wide)), ctas = most < kCtas ? most : kCtas;
+  k.by_grid = make_fastdiv(ctas);
   cudaError_t e;
   switch (a.kv.fmt) {
     case MX_E4M3: e = launch_e4m3(k, (int)a.kv.dim, wide, ctas, a.stream); break;
@@ -109,9 +160,13 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
     default: e = launch_int8(k, (int)a.kv.dim, wide, ctas, a.stream); break;
   }
   if (e != cudaSuccess) return e;
-  const dim3 grid(ctas, k.row_tile), block(kJoinWarps * 32);
-  return wide ? launch_pdl(kv_join_kernel<MX_F32>, grid, block, 0, a.stream, k, (uint32_t)a.kv.dim)
-              : launch_pdl(kv_join_kernel<MX_BF16>, grid, block, 0, a.stream, k, (uint32_t)a.kv.dim);
+  // Few sequences and heads have many parts each: a block for every row.  Many have few: blocks of four rows.
+  auto join = [&](auto kernel, uint32_t rows) {
+    return launch_pdl(kernel, dim3(ctas, k.row_tile / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
+  };
+  const bool many = (int64_t)k.batch * k.heads * k.row_tiles * 8 < ctas;
+  if (wide) return many ? join(kv_join_kernel<MX_F32, 1>, 1) : join(kv_join_kernel<MX_F32, 4>, 4);
+  return many ? join(kv_join_kernel<MX_BF16, 1>, 1) : join(kv_join_kernel<MX_BF16, 4>, 4);
 }
 
 }  // namespace mx

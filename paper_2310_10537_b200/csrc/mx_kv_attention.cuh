@@ -21,7 +21,7 @@
 // end of a sequence.
 //
 // Split.  The tiles of all sequences, heads and groups of rows, one after the other, are dealt out in equal runs to
-// two blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
+// two or three blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
 // otherwise it leaves a part (its weighted mean and the log of its weight) and a second kernel joins the parts, in the
 // order of the tiles: results do not depend on timing.
 #pragma once
@@ -45,15 +45,18 @@ constexpr int kAim = 12;                            // log2 of the largest weigh
 constexpr float kMost = 8.507059173023462e37f;      // 2^126, F's largest value
 
 // Shape of a kernel instance.
-template <int FMT, int DIM, bool WIDE>
+constexpr int kSharedOfSm = 228 * 1024;
+constexpr int kJoinPitch = 36;  // words of a block of 32 elements in the buffer that joins the warps: rows 2 t in different banks
+template <int FMT, int DIM, int NR, bool WIDE>
 struct Cfg {
+  static constexpr int kResident = blocks_per_sm(DIM, NR, WIDE);
   static constexpr int kBits = FmtTraits<FMT>::bits;
   static constexpr int kBlocks = DIM / 32;
   static constexpr int kRow = DIM * kBits / 8;             // bytes of a row's codes
   static constexpr int kGroup = 4 * kBits;                 // bytes of a block's codes
   // rows in shared memory: whole powers of two, so that the 16-byte units can be permuted within lines of 128 bytes
   static constexpr int kPitch = kRow <= 32 ? 32 : kRow <= 64 ? 64 : kRow <= 128 ? 128 : 256;
-  static constexpr int kTokens = 1 << tile_log2(kRow);
+  static constexpr int kTokens = 1 << tile_log2(DIM, kBits);
   static constexpr int kTiles = kTokens / 16;              // MMA tiles of 16 tokens
   static constexpr int kMine = kTokens <= 32 ? 1 : kTokens / 32;  // tokens whose place in the cache a lane looks up
   static constexpr int kScale = (kBlocks + 3) / 4 * 4;     // bytes of a row's scales
@@ -61,9 +64,8 @@ struct Cfg {
   static constexpr int kCopies = kTokens * kUnits / 32;    // of these a lane copies
   static constexpr int kCodes = kTokens * kPitch;
   static constexpr int kStage = 2 * kCodes + 2 * kTokens * kScale + 128;  // codes, scales, the mask of seen tokens
-  static constexpr int kJoinDim = DIM < 128 ? DIM : DIM == 192 ? 96 : 128;  // elements of a row joined at a time
-  static constexpr int kJoin = 2 * 8 * kJoinDim * 4 + kWarps * 16 * 4;
-  static constexpr int kFit = (115712 - kJoin) / (kWarps * kStage);       // two blocks per SM
+  static constexpr int kJoin = kWarps * 8 * kJoinPitch * 4 + 2 * kWarps * 16 * 4;
+  static constexpr int kFit = (kSharedOfSm / kResident - 1024 - kJoin) / (kWarps * kStage);
   static constexpr int kStages = kFit < 4 ? kFit : 4;
   static constexpr int kShared = kWarps * kStages * kStage + kJoin;
   static_assert(kStages >= 2 && kTokens * kUnits % 32 == 0, "tiles in flight");
@@ -74,6 +76,11 @@ struct Cfg {
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float lg2(float x) {
@@ -108,6 +115,18 @@ __device__ __forceinline__ void scales2(uint32_t two, float& a, float& b) {
   asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
   a = __uint_as_float(d << 16);
   b = __uint_as_float(d & 0xFFFF0000u);
+}
+
+// The scales of a token (as many as its row has blocks).
+template <class C>
+__device__ __forceinline__ void load_scales(uint32_t at, float (&s)[C::kScale]) {
+#pragma unroll
+  for (int c = 0; c < C::kScale; c += 4) {
+    uint32_t w;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at + c));
+    scales2(w, s[c], s[c + 1]);
+    if (c + 2 < C::kBlocks) scales2(w >> 16, s[c + 2], s[c + 3]);
+  }
 }
 
 // Codes as FP16 pairs.  `w` holds four 8-bit codes (4-bit: all eight of the lane's): pair 0 are codes 0, 1.
@@ -171,36 +190,27 @@ __device__ __forceinline__ uint32_t lds2(uint32_t a) {
 
 // The instance for rows of DIM elements in format FMT, NR times 8 query rows at a time.
 template <int FMT, int DIM, int NR, bool WIDE>
-__global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args a) {
-  using C = Cfg<FMT, DIM, WIDE>;
+__global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_attention_kernel(const Args a) {
+  using C = Cfg<FMT, DIM, NR, WIDE>;
   constexpr int B = C::kBlocks, TL = C::kTiles, W = WIDE ? 2 : 1;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (C::kStages * C::kStage);
-  float* join = reinterpret_cast<float*>(smem + kWarps * C::kStages * C::kStage);  // [2][8][kJoinDim]
-  float* join_lse = join + 2 * 8 * C::kJoinDim;                                    // [kWarps][16]
+  float* join = reinterpret_cast<float*>(smem + kWarps * C::kStages * C::kStage);  // [kWarps][8][kJoinPitch]
+  float2* join_ml = reinterpret_cast<float2*>(join + kWarps * 8 * kJoinPitch);     // [kWarps][16]
 
   // The lengths come from the kernels before this one.  The join may be scheduled only after this point, so that it, too,
   // finds them written.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // sequences without a tile
-  for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    if (a.tiles(a.length(b)) != 0) continue;
-    const uint32_t rows = a.new_tokens * a.q_heads;
-    for (uint32_t i = threadIdx.x; i < rows * (DIM / 8); i += kWarps * 32) {
-      const float zero[8] = {};
-      store8<WIDE ? MX_F32 : MX_BF16>(a.out, ((size_t)b * rows) * DIM + (size_t)i * 8, zero);
-    }
-    if (a.lse)
-      for (uint32_t i = threadIdx.x; i < rows; i += kWarps * 32) a.lse[(size_t)b * rows + i] = -INFINITY;
-  }
-
   const Share share = a.share(lane);
   const uint32_t first = blockIdx.x * share.per;
-  if (first >= share.total) return;
   const uint32_t last = min(first + share.per, share.total);  // this block's tiles are first .. last - 1
+  if (first >= share.total) {
+    if (threadIdx.x == 0) a.unfinished[blockIdx.x] = {0, 0, 0, 0};
+    return;
+  }
 
   // ---- the copies' side: which tokens the next tile to copy holds -------------------------------------------
   Segment s = a.find(share, first, lane), ls = s;
@@ -268,7 +278,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   look_up();
-  uint32_t ahead = C::kStages;  // copies before the next tile: the first one finds all stages free
+  uint32_t ahead = C::kStages - 1;  // copies to start before the first tile
 
   // lane offsets of the codes: keys of tokens g, g + 8; values of tokens 2 t, 2 t + 1 (and 8 further on)
   const uint32_t k_at[2] = {row_at<C>(g) + t * (C::kGroup / 4), row_at<C>(g + 8) + t * (C::kGroup / 4)};
@@ -284,25 +294,25 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
     uint32_t q[W][B][2][NR][2];
     float qf[NR][2];
     int lo[NR][2], hi[NR][2];  // tokens that the lane's rows 2 t, 2 t + 1 see
+    Raw8<WIDE ? MX_F32 : MX_BF16> raw[NR][B];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const uint32_t r = group0 + n * 8 + g;
-      float x[B][8];
-      float amax = 0.0f;
-      if (r < a.rows) {
-        const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
-        const size_t at = ((size_t)s.b * a.new_tokens + i) * a.q_stride + (size_t)head * DIM + t * 8;
-        Raw8<WIDE ? MX_F32 : MX_BF16> raw[B];
+      const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
+      const size_t at = ((size_t)s.b * a.new_tokens + i) * a.q_stride + (size_t)head * DIM + t * 8;
 #pragma unroll
-        for (int b = 0; b < B; ++b) raw[b] = load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32);
-#pragma unroll
-        for (int b = 0; b < B; ++b) widen(raw[b], x[b]);
-      } else {
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[b][j] = 0.0f;
+      for (int b = 0; b < B; ++b) {
+        raw[n][b] = {};
+        if (r < a.rows) raw[n][b] = load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32);
       }
+    }
+#pragma unroll 1
+    for (; ahead > 0; --ahead) copy_tile();  // (the first copies are under way while the queries are prepared)
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float x[B][8], amax = 0.0f;
+#pragma unroll
+      for (int b = 0; b < B; ++b) widen(raw[n][b], x[b]);
 #pragma unroll
       for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -361,15 +371,17 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[b][h][n][i] = 0.0f;
 
+    bool fresh = true;  // m and F have not been set by a tile of this sequence
+
     // ---- its tiles ----------------------------------------------------------------------------------------
 #pragma unroll 1
     for (; unit < seg_end; unit += kWarps) {
-#pragma unroll 1
-      for (; ahead > 0; --ahead) copy_tile();
-      ahead = 1;
+      copy_tile();
       asm volatile("cp.async.wait_group %0;" ::"n"(C::kStages - 1) : "memory");
       __syncwarp();
       const uint32_t stage = base + use * C::kStage, scales = stage + 2 * C::kCodes;
+      const uint32_t k_of[2] = {stage + k_at[0], stage + k_at[1]};  // (stages begin at whole lines)
+      const uint32_t v_of[4] = {stage + v_at[0], stage + v_at[1], stage + v_at[2], stage + v_at[3]};
       use = use + 1 == C::kStages ? 0 : use + 1;
       uint32_t seen[C::kMine];
       const int j0 = (int)(s.first_tile + (unit - s.start)) * C::kTokens;
@@ -386,13 +398,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
       for (int x = 0; x < TL; ++x) {
         float ks[2][C::kScale];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int c = 0; c < C::kScale; c += 4) {
-            const uint32_t w = lds4(scales + (16 * x + 8 * h + g) * C::kScale + c);
-            scales2(w, ks[h][c], ks[h][c + 1]);
-            if (c + 2 < B) scales2(w >> 16, ks[h][c + 2], ks[h][c + 3]);
-          }
+        for (int h = 0; h < 2; ++h) load_scales<C>(scales + (16 * x + 8 * h + g) * C::kScale, ks[h]);
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -402,7 +408,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
           uint32_t ka[2][4];  // two steps of 16 elements
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t at = stage + x * 16 * C::kPitch + (k_at[h] ^ ((b * C::kGroup) & 127)) + (b * C::kGroup) / 128 * 128;
+            const uint32_t at = (k_of[h] ^ ((b * C::kGroup) & 127)) + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128;
             if (C::kBits == 8) {
               const uint2 c = lds8(at);
               ka[0][h] = half_pair<FMT>(c.x, 0);
@@ -444,7 +450,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 
       // weights without the values' scales: m moves when a score passes it
       float y[TL][NR][4];
-      for (;;) {
+      for (bool moves = fresh;; moves = false) {
+        if (!moves) {
         float most = -1.0f;
 #pragma unroll
         for (int x = 0; x < TL; ++x)
@@ -468,6 +475,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, y[x][n][i]);
         if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
+        }
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -505,19 +513,14 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 
       // weights with the values' scales: F moves when one passes kTop
       uint32_t w[W][B][TL][NR][2];
-      for (;;) {
+      for (bool moves = fresh;; moves = false) {
+        if (!moves) {
         uint32_t most = 0;
 #pragma unroll
         for (int x = 0; x < TL; ++x) {
           float vs[2][C::kScale];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < C::kScale; c += 4) {
-              const uint32_t v = lds4(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + c);
-              scales2(v, vs[h][c], vs[h][c + 1]);
-              if (c + 2 < B) scales2(v >> 16, vs[h][c + 2], vs[h][c + 3]);
-            }
+          for (int h = 0; h < 2; ++h) load_scales<C>(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale, vs[h]);
 #pragma unroll
           for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -537,28 +540,39 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
         }
         const float2 top2 = unpack_half(most);
         if (!__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
+        }
         // F moves to where the largest is in [2^kAim, 2^(kAim + 1)), never up: a smaller F only costs small weights their digits
+        float top[B][NR][2];
+#pragma unroll
+        for (int x = 0; x < TL; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float v[C::kScale];
+            load_scales<C>(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale, v);
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+              for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) top[b][n][j] = fmaxf(x + h == 0 ? 0.0f : top[b][n][j], p[x][n][2 * h + j] * v[b]);
+          }
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2)
+#pragma unroll
+          for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) top[b][n][j] = fmaxf(top[b][n][j], __shfl_xor_sync(0xFFFFFFFFu, top[b][n][j], d));
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            float top[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int x = 0; x < TL; ++x)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float v, other;
-                scales2(lds2(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale + b / 2 * 2) >> 8 * (b % 2), v, other);
-                top[0] = fmaxf(top[0], p[x][n][2 * h] * v);
-                top[1] = fmaxf(top[1], p[x][n][2 * h + 1] * v);
-              }
+          for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-#pragma unroll
-              for (int d = 4; d < 32; d *= 2) top[j] = fmaxf(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], d));
-              const int e = (int)(__float_as_uint(top[j]) >> 23) - 127, have = (int)(__float_as_uint(F[b][n][j]) >> 23) - 127;
+              const int e = (int)(__float_as_uint(top[b][n][j]) >> 23) - 127, have = (int)(__float_as_uint(F[b][n][j]) >> 23) - 127;
               const int next = min(have, kAim - e);
-              const float by = next < have ? ex2((float)(next - have)) : 1.0f;
+              const float by = ex2((float)(next - have));  // 1 where F stays
               F[b][n][j] = __uint_as_float((uint32_t)(127 + next) << 23);
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
@@ -566,8 +580,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
                 acc[b][h][n][2 + j] *= by;
               }
             }
-          }
       }
+      fresh = false;
       if (edge) {  // a token that is not seen weighs nothing, whatever its scale
 #pragma unroll
         for (int x = 0; x < TL; ++x)
@@ -587,11 +601,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 #pragma unroll
         for (int x = 0; x < TL; ++x) {
           uint32_t va[2][4];
-          const uint32_t at = stage + C::kCodes + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128, blk = (b * C::kGroup) & 127;
+          const uint32_t blk = (b * C::kGroup) & 127, at = C::kCodes + x * 16 * C::kPitch + (b * C::kGroup) / 128 * 128;
           if (C::kBits == 8) {
             uint32_t c[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] = lds4(at + (v_at[i] ^ blk));
+            for (int i = 0; i < 4; ++i) c[i] = lds4((v_of[i] ^ blk) + at);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // elements 0, 1 and 2, 3 of the lane's four
               const uint32_t y0 = __byte_perm(c[0], c[1], h ? 0x7362 : 0x5140), y1 = __byte_perm(c[2], c[3], h ? 0x7362 : 0x5140);
@@ -601,8 +615,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
               va[h][3] = half_pair<FMT>(y1, 1);
             }
           } else {
-            const uint32_t c0 = lds2(at + (v_at[0] ^ blk)) | lds2(at + (v_at[2] ^ blk)) << 16;
-            const uint32_t c1 = lds2(at + (v_at[1] ^ blk)) | lds2(at + (v_at[3] ^ blk)) << 16;
+            const uint32_t c0 = lds2((v_of[0] ^ blk) + at) | lds2((v_of[2] ^ blk) + at) << 16;
+            const uint32_t c1 = lds2((v_of[1] ^ blk) + at) | lds2((v_of[3] ^ blk) + at) << 16;
             // bytes: elements 0, 2 (and 1, 3) of tokens 2 t, 2 t + 1, then of those 8 further on
             const uint32_t y0 = (c0 & 0x0F0F0F0Fu) | (c1 & 0x0F0F0F0Fu) << 4, y1 = (c0 >> 4 & 0x0F0F0F0Fu) | (c1 & 0xF0F0F0F0u);
 #pragma unroll
@@ -637,92 +651,87 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
       __syncwarp();  // the stage may be filled again
     }
 
-    // ---- the block's warps joined ----------------------------------------------------------------------------
-    float lse2[NR][2];
+    // ---- the block's warps joined: sum of acc 2^(m - M) / F over sum of l 2^(m - M) -------------------------------
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
-        lse2[n][j] = l[n][j] == 0.0f ? -INFINITY : m[n][j] + lg2(l[n][j]);
-        if (g == 0) join_lse[warp * 16 + n * 8 + 2 * t + j] = lse2[n][j];
+        if (g == 0) join_ml[warp * 16 + n * 8 + 2 * t + j] = make_float2(m[n][j], l[n][j]);
       }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float all[kWarps], top = -INFINITY, sum = 0.0f;
+        float top = kLowest, sum = 0.0f;
+        float2 ml[kWarps];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, all[w] = join_lse[w * 16 + n * 8 + 2 * t + j]);
+        for (int w = 0; w < kWarps; ++w) {
+          ml[w] = join_ml[w * 16 + n * 8 + 2 * t + j];
+          top = fmaxf(top, ml[w].x);
+        }
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum += all[w] == -INFINITY ? 0.0f : ex2(all[w] - top);
-        // this warp's share of the whole, over its own sum
-        const float mine = l[n][j] == 0.0f ? 0.0f : ex2(lse2[n][j] - top) / (l[n][j] * sum) * C::kUnit;
-        lse2[n][j] = sum == 0.0f ? -INFINITY : top + lg2(sum);
+        for (int w = 0; w < kWarps; ++w) sum = fmaf(ml[w].y, ex2(ml[w].x - top), sum);
+        const float mine = sum == 0.0f ? 0.0f : ex2(m[n][j] - top) * C::kUnit * rcp(sum);
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-          const float by = 1.0f / F[b][n][j];  // a power of two
-          acc[b][0][n][j] *= mine; acc[b][0][n][2 + j] *= mine;
-          acc[b][1][n][j] *= mine; acc[b][1][n][2 + j] *= mine;
-          acc[b][0][n][j] *= by; acc[b][0][n][2 + j] *= by;
-          acc[b][1][n][j] *= by; acc[b][1][n][2 + j] *= by;
+          const float by = __uint_as_float((254u << 23) - __float_as_uint(F[b][n][j]));  // 1 / F, a power of two
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            acc[b][h][n][j] = acc[b][h][n][j] * mine * by;
+            acc[b][h][n][2 + j] = acc[b][h][n][2 + j] * mine * by;
+          }
         }
       }
     const bool whole = s.start >= first && s.end <= last;
-    const uint32_t slot = blockIdx.x * 2 + (s.start >= first ? 1 : 0);
-    constexpr int JB = C::kJoinDim / 32;  // blocks at a time
+    // a thread puts out two elements of one row of each block, row tid / 16 of the eight
+    const uint32_t out_row = threadIdx.x / 16, out_at = threadIdx.x % 16 * 2;
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int n = 0; n < NR; ++n) {
+      const uint32_t in_tile = n * 8 + out_row, r = group0 + in_tile;
+      const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
+      const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
+      const size_t part = (size_t)(blockIdx.x * 2 + (s.start >= first ? 1 : 0)) * (8 * NR) + in_tile;
+      if (out_at == 0 && r < a.rows && (!whole || a.lse)) {
+        float top = kLowest, sum = 0.0f;
 #pragma unroll
-      for (int b0 = 0; b0 < B; b0 += JB) {
-        auto at = [&](uint32_t half, int b, int j) { return reinterpret_cast<float4*>(join + (half * 8 + 2 * t + j) * C::kJoinDim + (b - b0) * 32 + 4 * g); };
-        auto put = [&](uint32_t half) {
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, join_ml[w * 16 + in_tile].x);
 #pragma unroll
-          for (int b = b0; b < b0 + JB; ++b)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) *at(half, b, j) = make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
-        };
-        auto add = [&](uint32_t half) {
-#pragma unroll
-          for (int b = b0; b < b0 + JB; ++b)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float4 v = *at(half, b, j);
-              acc[b][0][n][j] += v.x; acc[b][0][n][2 + j] += v.y;
-              acc[b][1][n][j] += v.z; acc[b][1][n][2 + j] += v.w;
-            }
-        };
-        if (warp >= 2) put(warp - 2);
-        __syncthreads();
-        if (warp < 2) add(warp);
-        if (warp == 1) put(1);
-        __syncthreads();
-        if (warp == 0) {
-          add(1);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t in_tile = n * 8 + 2 * t + j, r = group0 + in_tile;
-            if (r >= a.rows) continue;
-            const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
-            const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
-#pragma unroll
-            for (int b = b0; b < b0 + JB; ++b) {
-              const float4 v = make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
-              if (!whole) *reinterpret_cast<float4*>(a.parts + ((size_t)slot * (8 * NR) + in_tile) * DIM + b * 32 + 4 * g) = v;
-              else if (WIDE) *reinterpret_cast<float4*>((float*)a.out + row * DIM + b * 32 + 4 * g) = v;
-              else *reinterpret_cast<uint2*>((uint16_t*)a.out + row * DIM + b * 32 + 4 * g) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-            }
-            if (b0 == 0 && g == 0) {
-              if (!whole) a.part_lse[slot * (8 * NR) + in_tile] = lse2[n][j];
-              else if (a.lse) a.lse[row] = lse2[n][j] * kLn2;
-            }
-          }
-        }
-        if (NR * B > JB) __syncthreads();  // before the buffer is used again
+        for (int w = 0; w < kWarps; ++w) sum = fmaf(join_ml[w * 16 + in_tile].y, ex2(join_ml[w * 16 + in_tile].x - top), sum);
+        const float lse2 = sum == 0.0f ? -INFINITY : top + lg2(sum);
+        if (whole) a.lse[row] = lse2 * kLn2;
+        else a.part_lse[part] = lse2;
       }
-    if (s.end >= last) break;
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          *reinterpret_cast<float4*>(join + (warp * 8 + 2 * t + j) * kJoinPitch + 4 * g) =
+              make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
+        __syncthreads();
+        float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 u = *reinterpret_cast<const float2*>(join + (w * 8 + out_row) * kJoinPitch + out_at);
+          v.x += u.x;
+          v.y += u.y;
+        }
+        if (r < a.rows) {
+          if (!whole) *reinterpret_cast<float2*>(a.parts + part * DIM + b * 32 + out_at) = v;
+          else if (WIDE) *reinterpret_cast<float2*>((float*)a.out + row * DIM + b * 32 + out_at) = v;
+          else *reinterpret_cast<uint32_t*>((uint16_t*)a.out + row * DIM + b * 32 + out_at) = pack_bf16(v.x, v.y);
+        }
+        __syncthreads();  // before the buffer is used again
+      }
+    }
+    if (s.end >= last) {
+      // the sequence that begins here and goes on is joined from this block's part and those of the blocks behind it
+      if (threadIdx.x == 0)
+        a.unfinished[blockIdx.x] = {s.b, s.hr, s.start >= first && s.end > last ? (s.end - 1) / share.per - blockIdx.x + 1 : 0, 0};
+      break;
+    }
     a.next(s);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -730,7 +739,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) kv_attention_kernel(const Args
 
 template <int FMT, int DIM, int NR, bool WIDE>
 cudaError_t launch_instance(const Args& a, uint32_t ctas, cudaStream_t stream) {
-  using C = Cfg<FMT, DIM, WIDE>;
+  using C = Cfg<FMT, DIM, NR, WIDE>;
   auto kernel = kv_attention_kernel<FMT, DIM, NR, WIDE>;
   // (a function attribute per device: set on every call, it costs less than a microsecond)
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kShared);

@@ -7,13 +7,15 @@ namespace mx {
 namespace attn {
 
 constexpr int kWarps = 4;         // of a block
-constexpr uint32_t kCtas = 296;   // blocks at most: two on each of 148 SMs
+constexpr uint32_t kCtas = 444;   // blocks at most: three on each of 148 SMs
+// Blocks per SM of an instance, by its registers.
+__host__ __device__ constexpr int blocks_per_sm(int dim, int rows8, bool wide) { return dim <= 128 && rows8 == 1 && !wide ? 3 : 2; }
 // A block's fewest tiles: one per warp.
 constexpr uint32_t kLeast = kWarps;
 
-// Tokens of a tile: 64 where their codes are short, so that what a tile costs whatever its size counts less; 16 for rows above 128
-// bytes, for the shared memory.
-__host__ __device__ constexpr int tile_log2(int row_bytes) { return row_bytes <= 64 ? 6 : row_bytes <= 128 ? 5 : 4; }
+// Tokens of a tile: 64 of 64 elements, so that what a tile costs whatever its size counts less (their weights for every block still fit the
+// registers); 16 for rows above 128 bytes, for the shared memory.
+__host__ __device__ constexpr int tile_log2(int dim, int bits) { return dim <= 64 ? 6 : dim * bits <= 1024 ? 5 : 4; }
 
 // The tiles first .. of one sequence b for one key-value head and one tile of query rows: units start .. end - 1 of the
 // whole list, which runs over sequences, then heads and tiles of rows, then tiles of tokens.
@@ -31,6 +33,12 @@ struct Share {
   uint32_t total, per;       // units in all, and of a block
   uint32_t before;           // units before this lane's sequences
   uint32_t mine;
+  uint32_t length;           // of this lane's only sequence, where lanes have one
+};
+
+// A sequence and head whose tiles go on behind the block that they begin in: parts of them (0: there is none).
+struct Unfinished {
+  uint32_t b, hr, parts, unused;
 };
 
 struct Args {
@@ -39,12 +47,13 @@ struct Args {
   const int32_t *table, *lengths;
   void* out;
   float *lse, *parts, *part_lse;  // parts: [2 * blocks][row tile][dim]
+  Unfinished* unfinished;         // [blocks]
   int64_t q_stride;
   uint32_t pages, page_size, heads, batch, new_tokens, q_heads, max_pages, window;
   uint32_t group, rows;           // query heads of a key-value head; query rows of one: new_tokens * group
   uint32_t row_tile, row_tiles;   // query rows of a unit, units of them
   uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
-  FastDiv by_page, by_group, by_row_tiles;
+  FastDiv by_page, by_group, by_row_tiles, by_grid;
   float scale_log2;
 
   __device__ __forceinline__ uint32_t length(uint32_t b) const {
@@ -59,8 +68,8 @@ struct Args {
   __device__ __forceinline__ uint32_t tiles(uint32_t length) const {
     return length == 0 ? 0 : ((length - 1) >> tile_log2) + 1 - (begin(length) >> tile_log2);
   }
-  __device__ __forceinline__ void fill(Segment& s) const {
-    s.length = length(s.b);
+  __device__ __forceinline__ void fill(Segment& s, uint32_t length) const {
+    s.length = length;
     s.begin = begin(s.length);
     s.first_tile = s.begin >> tile_log2;
     s.end = s.start + tiles(s.length);
@@ -78,7 +87,7 @@ struct Args {
 #pragma unroll 1
     do {
       ++s.b;
-      fill(s);
+      fill(s, length(s.b));
     } while (s.end == s.start);
   }
   __device__ __forceinline__ static uint32_t scan(uint32_t v, uint32_t lane) {  // inclusive sums over the lanes
@@ -92,20 +101,26 @@ struct Args {
   __device__ __forceinline__ Share share(uint32_t lane) const {
     Share r;
     uint32_t n = 0;
-    const uint32_t e = min((lane + 1) * chunk, batch);
+    r.length = 0;
+    if (chunk == 1) {
+      if (lane < batch) r.length = length(lane);
+      n = tiles(r.length);
+    } else {
+      const uint32_t e = min((lane + 1) * chunk, batch);
 #pragma unroll 1
-    for (uint32_t b = lane * chunk; b < e; b += 4) {  // (four lengths in flight)
-      uint32_t v[4];
+      for (uint32_t b = lane * chunk; b < e; b += 4) {  // (four lengths in flight)
+        uint32_t v[4];
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) v[i] = b + i < e ? length(b + i) : 0;
+        for (uint32_t i = 0; i < 4; ++i) v[i] = b + i < e ? length(b + i) : 0;
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) n += tiles(v[i]);
+        for (uint32_t i = 0; i < 4; ++i) n += tiles(v[i]);
+      }
     }
     r.mine = n * heads * row_tiles;
     const uint32_t sum = scan(r.mine, lane);
     r.before = sum - r.mine;
     r.total = __shfl_sync(0xFFFFFFFFu, sum, 31);
-    r.per = max((r.total + gridDim.x - 1) / gridDim.x, kLeast);
+    r.per = max(fastdiv(r.total + gridDim.x - 1, by_grid), kLeast);
     return r;
   }
   // The segment of a unit below total.
@@ -114,6 +129,7 @@ struct Args {
     uint32_t at = __shfl_sync(0xFFFFFFFFu, share.before, who);
     Segment s;
     s.b = who;
+    uint32_t tokens = __shfl_sync(0xFFFFFFFFu, share.length, who);
     if (chunk > 1) {
 #pragma unroll 1
       for (uint32_t b0 = who * chunk;; b0 += 32) {  // its sequences, 32 at a time
@@ -129,8 +145,9 @@ struct Args {
         at += __shfl_sync(0xFFFFFFFFu, sum, 31);
       }
     }
+    if (chunk > 1) tokens = length(s.b);
     s.start = 0;
-    fill(s);
+    fill(s, tokens);
     const uint32_t n = s.end;
     s.hr = (unit - at) / n;
     s.start = at + s.hr * n;
