@@ -12,7 +12,7 @@ constexpr int kJoinWarps = 8;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // A few query rows (ROWS of their tile of rows, the ones blockIdx.y * ROWS ..) of the sequence and head that begins in block blockIdx.x
-// of the attention kernel and goes on behind it, if there is one.  The warps of a row take its parts in turn, a lane four elements:
+// of the attention kernel and goes on behind it, if there is one; with by_segment of the blockIdx.x-th of all.  The warps of a row take its parts in turn, a lane four elements:
 // out = sum of the parts' means by their weights 2^lse over the sum of the weights, in the order of the parts within a warp and
 // then of the warps.
 template <int DTYPE, int ROWS>
@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
   }
   // every block waits, also one without work: the stream's next kernel goes by this grid's end
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (a.by_segment && a.tiles(a.length(blockIdx.x / (a.heads * a.row_tiles))) == 0) return;  // (nobody has written its entry)
   const Unfinished s = a.unfinished[blockIdx.x];
   if (s.parts == 0) return;
   const uint32_t head0 = fastdiv(s.hr, a.by_row_tiles), row_tile = s.hr - head0 * a.row_tiles;
@@ -56,7 +57,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
         x[k][0] = x[k][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p < s.parts) {
           // part 0 is the second slot of this block, the others are the first ones of the blocks behind it
-          const size_t at = (size_t)((blockIdx.x + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile;
+          const size_t at = (size_t)((s.block + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile;
           lse[k] = a.part_lse[at];
           if (lane * 4 < dim) x[k][0] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4);
           if (lane * 4 + 128 < dim) x[k][1] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4 + 128);
@@ -150,7 +151,15 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.unfinished = (Unfinished*)a.workspace;
   k.parts = (float*)(k.unfinished + kCtas);
   k.part_lse = k.parts + (size_t)2 * kCtas * k.row_tile * (size_t)a.kv.dim;
-  const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, (int)k.row_tile / 8, wide)), ctas = most < kCtas ? most : kCtas;
+  const uint32_t segments = k.batch * k.heads * k.row_tiles;  // (below 2^31, as the units are)
+  const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, (int)k.row_tile / 8, wide));
+  // no more blocks than the longest sequences that the table can hold would employ
+  const int64_t units = (int64_t)segments * (((a.max_pages * a.kv.page_size) >> k.tile_log2) + 1);
+  uint32_t ctas = most < kCtas ? most : kCtas;
+  if (units < (int64_t)ctas * kLeast) ctas = (uint32_t)((units + kLeast - 1) / kLeast);
+  // Few sequences and heads may have many parts each: a block of the join for every row of each.  Many have few: blocks of four rows
+  // for each block of this kernel.
+  k.by_segment = segments * 8 <= kCtas;
   k.by_grid = make_fastdiv(ctas);
   cudaError_t e;
   switch (a.kv.fmt) {
@@ -160,13 +169,11 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
     default: e = launch_int8(k, (int)a.kv.dim, wide, ctas, a.stream); break;
   }
   if (e != cudaSuccess) return e;
-  // Few sequences and heads have many parts each: a block for every row.  Many have few: blocks of four rows.
-  auto join = [&](auto kernel, uint32_t rows) {
-    return launch_pdl(kernel, dim3(ctas, k.row_tile / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
+  auto join = [&](auto kernel, uint32_t blocks, uint32_t rows) {
+    return launch_pdl(kernel, dim3(blocks, k.row_tile / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
   };
-  const bool many = (int64_t)k.batch * k.heads * k.row_tiles * 8 < ctas;
-  if (wide) return many ? join(kv_join_kernel<MX_F32, 1>, 1) : join(kv_join_kernel<MX_F32, 4>, 4);
-  return many ? join(kv_join_kernel<MX_BF16, 1>, 1) : join(kv_join_kernel<MX_BF16, 4>, 4);
+  if (wide) return k.by_segment ? join(kv_join_kernel<MX_F32, 1>, segments, 1) : join(kv_join_kernel<MX_F32, 4>, ctas, 4);
+  return k.by_segment ? join(kv_join_kernel<MX_BF16, 1>, segments, 1) : join(kv_join_kernel<MX_BF16, 4>, ctas, 4);
 }
 
 }  // namespace mx

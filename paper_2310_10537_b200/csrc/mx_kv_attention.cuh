@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
   const uint32_t first = blockIdx.x * share.per;
   const uint32_t last = min(first + share.per, share.total);  // this block's tiles are first .. last - 1
   if (first >= share.total) {
-    if (threadIdx.x == 0) a.unfinished[blockIdx.x] = {0, 0, 0, 0};
+    if (threadIdx.x == 0 && !a.by_segment) a.unfinished[blockIdx.x] = {0, 0, 0, 0};
     return;
   }
 
@@ -726,12 +726,12 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
         __syncthreads();  // before the buffer is used again
       }
     }
-    if (s.end >= last) {
-      // the sequence that begins here and goes on is joined from this block's part and those of the blocks behind it
-      if (threadIdx.x == 0)
-        a.unfinished[blockIdx.x] = {s.b, s.hr, s.start >= first && s.end > last ? (s.end - 1) / share.per - blockIdx.x + 1 : 0, 0};
-      break;
+    // the sequence that begins here and goes on is joined from this block's part and those of the blocks behind it
+    if (threadIdx.x == 0 && (a.by_segment ? s.start >= first : s.end >= last)) {
+      const uint32_t parts = s.start >= first && s.end > last ? (s.end - 1) / share.per - blockIdx.x + 1 : 0;
+      a.unfinished[a.by_segment ? s.b * a.heads * a.row_tiles + s.hr : blockIdx.x] = {s.b, s.hr, parts, blockIdx.x};
     }
+    if (s.end >= last) break;
     a.next(s);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");

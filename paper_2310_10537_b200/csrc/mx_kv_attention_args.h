@@ -36,9 +36,10 @@ struct Share {
   uint32_t length;           // of this lane's only sequence, where lanes have one
 };
 
-// A sequence and head whose tiles go on behind the block that they begin in: parts of them (0: there is none).
+// A sequence and head whose tiles go on behind the block that they begin in: that block, and how many parts there are (0: none,
+// it is finished).
 struct Unfinished {
-  uint32_t b, hr, parts, unused;
+  uint32_t b, hr, parts, block;
 };
 
 struct Args {
@@ -47,7 +48,7 @@ struct Args {
   const int32_t *table, *lengths;
   void* out;
   float *lse, *parts, *part_lse;  // parts: [2 * blocks][row tile][dim]
-  Unfinished* unfinished;         // [blocks]
+  Unfinished* unfinished;         // of each block, or (by_segment) of each sequence, head and tile of rows that has tiles
   int64_t q_stride;
   uint32_t pages, page_size, heads, batch, new_tokens, q_heads, max_pages, window;
   uint32_t group, rows;           // query heads of a key-value head; query rows of one: new_tokens * group
@@ -55,6 +56,7 @@ struct Args {
   uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
   FastDiv by_page, by_group, by_row_tiles, by_grid;
   float scale_log2;
+  bool by_segment;
 
   __device__ __forceinline__ uint32_t length(uint32_t b) const {
     const int n = lengths[b];
