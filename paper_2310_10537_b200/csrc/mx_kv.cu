@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 
 struct KvShape {
   int64_t slots;        // pages * page_size
-  uint32_t heads, page_size, units, per_token;  // units of a row that a thread moves, units of a token
+  uint32_t heads, page_size, units, per_token;  // units of a row that threads move, units of a token
   FastDiv by_token, by_row, by_page;
   uint32_t code_bytes, scale_bytes;  // of a row
 };
@@ -27,39 +27,43 @@ __device__ __forceinline__ size_t kv_row(const KvShape& s, uint32_t slot, uint32
   return ((size_t)page * s.heads + head) * s.page_size + (slot - page * s.page_size);
 }
 
-// Algorithm 1 of the rows of k (blockIdx.y 0) or v (1).  A thread converts 8 elements, four neighbours a
-// block; the scale bytes beyond the row's blocks are written by the lane of the last block.
+// Algorithm 1 of the rows of k and v.  A thread converts 8 elements of either, four neighbours a block; the scale bytes beyond the
+// row's blocks are written by the lane of the last block.
 template <int FMT, int ROUND, int DTYPE>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(
     const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride, uint8_t* k_elems,
     uint8_t* k_scales, uint8_t* v_elems, uint8_t* v_scales, const int32_t* __restrict__ slots, uint32_t total, KvShape s) {
   pdl_prologue();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  const bool values = blockIdx.y != 0;
   const uint32_t at = i < total ? i : total - 1;  // (four lanes share a block: all of them stay)
   const uint32_t token = fastdiv(at, s.by_token), in_token = at - token * s.per_token;
-  const uint32_t head = fastdiv(in_token, s.by_row), unit = in_token - head * s.units;
+  const Raw8<DTYPE> raw[2] = {load_raw8<DTYPE>(k, (size_t)token * (size_t)k_stride + (size_t)in_token * 8),
+                              load_raw8<DTYPE>(v, (size_t)token * (size_t)v_stride + (size_t)in_token * 8)};
   const int64_t slot = slots[token];
-  const Raw8<DTYPE> raw = load_raw8<DTYPE>(values ? v : k, (size_t)token * (size_t)(values ? v_stride : k_stride) + (size_t)in_token * 8);
-  float x[8];
-  widen(raw, x);
-  float amax = absmax_nan(absmax_nan(absmax_nan(x[0], x[1]), absmax_nan(x[2], x[3])),
-                          absmax_nan(absmax_nan(x[4], x[5]), absmax_nan(x[6], x[7])));
-  amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-  amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-  const BlockScale b = block_scale<FMT>(amax);
-  uint32_t lo, hi;
-  cast8<FMT, ROUND>(x, b, lo, hi);
-  if (i >= total || slot < 0 || slot >= s.slots) return;
-  const size_t row = kv_row(s, (uint32_t)slot, head);
-  uint8_t* codes = (values ? v_elems : k_elems) + row * s.code_bytes;
-  if (FmtTraits<FMT>::bits == 8) reinterpret_cast<uint2*>(codes)[unit] = make_uint2(lo, hi);
-  else reinterpret_cast<uint32_t*>(codes)[unit] = lo;
-  if (unit % 4 == 0) {
-    uint8_t* scales = (values ? v_scales : k_scales) + row * s.scale_bytes;
-    scales[unit / 4] = (uint8_t)b.byte;
-    if (unit + 4 == s.units)
-      for (uint32_t j = unit / 4 + 1; j < s.scale_bytes; ++j) scales[j] = 0;
+  const uint32_t head = fastdiv(in_token, s.by_row), unit = in_token - head * s.units;
+  const bool there = i < total && slot >= 0 && slot < s.slots;
+  const size_t row = there ? kv_row(s, (uint32_t)slot, head) : 0;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    float x[8];
+    widen(raw[n], x);
+    float amax = absmax_nan(absmax_nan(absmax_nan(x[0], x[1]), absmax_nan(x[2], x[3])),
+                            absmax_nan(absmax_nan(x[4], x[5]), absmax_nan(x[6], x[7])));
+    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+    const BlockScale b = block_scale<FMT>(amax);
+    uint32_t lo, hi;
+    cast8<FMT, ROUND>(x, b, lo, hi);
+    if (!there) continue;
+    uint8_t* codes = (n ? v_elems : k_elems) + row * s.code_bytes;
+    if (FmtTraits<FMT>::bits == 8) reinterpret_cast<uint2*>(codes)[unit] = make_uint2(lo, hi);
+    else reinterpret_cast<uint32_t*>(codes)[unit] = lo;
+    if (unit % 4 == 0) {
+      uint8_t* scales = (n ? v_scales : k_scales) + row * s.scale_bytes;
+      scales[unit / 4] = (uint8_t)b.byte;
+      if (unit + 4 == s.units)
+        for (uint32_t j = unit / 4 + 1; j < s.scale_bytes; ++j) scales[j] = 0;
+    }
   }
 }
 
@@ -76,54 +80,59 @@ __device__ __forceinline__ float2 decode2(uint32_t pair) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h2));
 }
 
-// The rows of a slot as numbers.  A thread reads 8 codes.
+// The rows of a slot as numbers.  A thread reads 16 codes of the key and of the value.
 template <int FMT, int DTYPE>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(
     const uint8_t* __restrict__ k_elems, const uint8_t* __restrict__ k_scales, const uint8_t* __restrict__ v_elems,
     const uint8_t* __restrict__ v_scales, const int32_t* __restrict__ slots, uint32_t total, KvShape s, void* k_out, void* v_out) {
+  constexpr int kWords = FmtTraits<FMT>::bits / 2;
   pdl_prologue();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
   if (i >= total) return;
-  const bool values = blockIdx.y != 0;
   const uint32_t token = fastdiv(i, s.by_token), in_token = i - token * s.per_token;
   const uint32_t head = fastdiv(in_token, s.by_row), unit = in_token - head * s.units;
   const int64_t slot = slots[token];
-  float x[8];
-  if (slot < 0 || slot >= s.slots) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = 0.0f;
-  } else {
+  uint32_t w[2][kWords] = {}, sb[2] = {0, 0};
+  if (slot >= 0 && slot < s.slots) {
     const size_t row = kv_row(s, (uint32_t)slot, head);
-    const uint8_t* codes = (values ? v_elems : k_elems) + row * s.code_bytes;
-    const uint32_t sb = ((values ? v_scales : k_scales) + row * s.scale_bytes)[unit / 4];
-    const float X = __uint_as_float(sb == 0 ? 0x00400000u : (sb == 255 ? 0x7FC00000u : sb << 23));  // 2^-127, NaN
-    uint32_t w[2];
-    if (FmtTraits<FMT>::bits == 8) {
-      const uint2 c = reinterpret_cast<const uint2*>(codes)[unit];
-      w[0] = c.x;
-      w[1] = c.y;
-    } else {
-      w[0] = reinterpret_cast<const uint32_t*>(codes)[unit];
-      w[1] = w[0] >> 16;
-    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 p = decode2<FMT>(FmtTraits<FMT>::bits == 8 ? w[j / 2] >> 16 * (j & 1) : (w[j / 2] >> 8 * (j & 1)) & 0xFFu);
-      x[2 * j] = p.x * X;
-      x[2 * j + 1] = p.y * X;
+    for (int n = 0; n < 2; ++n) {
+      const uint8_t* codes = (n ? v_elems : k_elems) + row * s.code_bytes;
+      if (kWords == 4) {
+        const uint4 c = ld_16(codes + (size_t)unit * 16);
+        w[n][0] = c.x; w[n][1] = c.y; w[n][2 % kWords] = c.z; w[n][3 % kWords] = c.w;
+      } else {
+        const uint2 c = reinterpret_cast<const uint2*>(codes)[unit];
+        w[n][0] = c.x; w[n][1] = c.y;
+      }
+      sb[n] = ((n ? v_scales : k_scales) + row * s.scale_bytes)[unit / 2];
     }
   }
-  store8<DTYPE>(values ? v_out : k_out, (size_t)i * 8, x);
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const float X = __uint_as_float(sb[n] == 0 ? 0x00400000u : (sb[n] == 255 ? 0x7FC00000u : sb[n] << 23));  // 2^-127, NaN
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 p = decode2<FMT>(kWords == 4 ? w[n][(2 * h + j / 2) % kWords] >> 16 * (j & 1) : (w[n][h] >> 8 * j) & 0xFFu);
+        x[2 * j] = p.x * X;
+        x[2 * j + 1] = p.y * X;
+      }
+      store8<DTYPE>(n ? v_out : k_out, (size_t)i * 16 + 8 * h, x);
+    }
+  }
 }
 
-// Shape of the cache with rows cut into units of 8 elements.
-KvShape shape_of(const KvArgs& kv) {
+// Shape of the cache with rows cut into units of so many elements.
+KvShape shape_of(const KvArgs& kv, uint32_t unit) {
   KvShape s;
   const uint32_t bits = kv.fmt == MX_E2M1 ? 4 : 8;
   s.slots = kv.pages * kv.page_size;
   s.heads = (uint32_t)kv.heads;
   s.page_size = (uint32_t)kv.page_size;
-  s.units = (uint32_t)kv.dim / 8;
+  s.units = (uint32_t)kv.dim / unit;
   s.per_token = s.units * s.heads;
   s.by_token = make_fastdiv(s.per_token);
   s.by_row = make_fastdiv(s.units);
@@ -136,7 +145,7 @@ KvShape shape_of(const KvArgs& kv) {
 template <int FMT, int ROUND>
 cudaError_t append_by_dtype(const KvMoveArgs& a, const KvShape& s, uint32_t total) {
   auto go = [&](auto kernel) {
-    return launch_pdl(kernel, dim3((total + kThreads - 1) / kThreads, 2), dim3(kThreads), 0, a.stream, a.k, a.v, a.k_stride, a.v_stride,
+    return launch_pdl(kernel, dim3((total + kThreads - 1) / kThreads), dim3(kThreads), 0, a.stream, a.k, a.v, a.k_stride, a.v_stride,
                       a.kv.k_elems, a.kv.k_scales, a.kv.v_elems, a.kv.v_scales, a.slots, total, s);
   };
   return a.dtype == MX_BF16 ? go(kv_append_kernel<FMT, ROUND, MX_BF16>) : go(kv_append_kernel<FMT, ROUND, MX_F32>);
@@ -148,7 +157,7 @@ cudaError_t append_by_rounding(const KvMoveArgs& a, const KvShape& s, uint32_t t
 template <int FMT>
 cudaError_t read_by_dtype(const KvMoveArgs& a, const KvShape& s, uint32_t total) {
   auto go = [&](auto kernel) {
-    return launch_pdl(kernel, dim3((total + kThreads - 1) / kThreads, 2), dim3(kThreads), 0, a.stream, a.kv.k_elems, a.kv.k_scales,
+    return launch_pdl(kernel, dim3((total + kThreads - 1) / kThreads), dim3(kThreads), 0, a.stream, a.kv.k_elems, a.kv.k_scales,
                       a.kv.v_elems, a.kv.v_scales, a.slots, total, s, a.k_out, a.v_out);
   };
   return a.dtype == MX_BF16 ? go(kv_read_kernel<FMT, MX_BF16>) : go(kv_read_kernel<FMT, MX_F32>);
@@ -157,7 +166,7 @@ cudaError_t read_by_dtype(const KvMoveArgs& a, const KvShape& s, uint32_t total)
 }  // namespace
 
 cudaError_t launch_kv_append(const KvMoveArgs& a) {
-  const KvShape s = shape_of(a.kv);
+  const KvShape s = shape_of(a.kv, 8);
   const uint32_t total = (uint32_t)(a.tokens * a.kv.heads * (a.kv.dim / 8));  // below 2^31
   switch (a.kv.fmt) {
     case MX_E4M3: return append_by_rounding<MX_E4M3>(a, s, total);
@@ -168,8 +177,8 @@ cudaError_t launch_kv_append(const KvMoveArgs& a) {
 }
 
 cudaError_t launch_kv_read(const KvMoveArgs& a) {
-  const KvShape s = shape_of(a.kv);
-  const uint32_t total = (uint32_t)(a.tokens * a.kv.heads * (a.kv.dim / 8));
+  const KvShape s = shape_of(a.kv, 16);
+  const uint32_t total = (uint32_t)(a.tokens * a.kv.heads * (a.kv.dim / 16));
   switch (a.kv.fmt) {
     case MX_E4M3: return read_by_dtype<MX_E4M3>(a, s, total);
     case MX_E5M2: return read_by_dtype<MX_E5M2>(a, s, total);

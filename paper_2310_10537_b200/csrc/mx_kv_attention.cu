@@ -120,8 +120,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
   if (a.lse && warp % kPer == 0 && lane == 0) a.lse[row] = all == 0.0f ? -INFINITY : (most + log2f(all)) * kLn2;
 }
 
-// Query rows of a unit: 8, or 16 where there are more (FP32 and rows above 128 elements: 8, for the registers).
-uint32_t row_tile(int64_t rows, int64_t dim, bool wide) { return rows > 8 && dim <= 128 && !wide ? 16 : 8; }
+// Sequences of up to so many tiles are not split: four rounds of a block's warps take less than a split and a second kernel.
+constexpr int64_t kWhole = 4 * kWarps;
+
+// Query rows of a unit: 8, or 16 where there are more of them and long sequences enough to keep the SMs busy with two blocks each
+// (16 heads a group, 64 sequences to 8192 tokens: 210 against 215 us, one of 131072 85 against 96; but 16 rows over 32 sequences of 1024 tokens
+// 51 against 40, to 5000 96 against 84).  FP32 and rows above 128 elements: 8, for the registers.
+uint32_t row_tile(int64_t segments, int64_t rows, int64_t tiles, int64_t dim, bool wide) {
+  if (rows <= 8 || dim > 128 || wide || tiles < 256) return 8;
+  return segments * ((rows + 15) / 16) * tiles >= 64 * (int64_t)kCtas ? 16 : 8;
+}
 size_t workspace_bytes(uint32_t rows, int64_t dim) { return kCtas * (sizeof(Unfinished) + (size_t)2 * rows * (size_t)(dim + 1) * 4); }
 
 }  // namespace
@@ -142,9 +150,12 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.window = (uint32_t)(a.window < 0x7FFFFFFF ? a.window : 0);  // (no sequence is longer)
   k.group = k.q_heads / k.heads;
   k.rows = k.new_tokens * k.group;
-  k.row_tile = row_tile(k.rows, a.kv.dim, wide);
-  k.row_tiles = (k.rows + k.row_tile - 1) / k.row_tile;
   k.tile_log2 = (uint32_t)tile_log2((int)a.kv.dim, a.kv.fmt == MX_E2M1 ? 4 : 8);
+  // no sequence has more tiles than this
+  const int64_t cap = a.max_pages * a.kv.page_size, reach = k.window ? (int64_t)k.window + k.new_tokens : cap;
+  const int64_t tiles = ((reach < cap ? reach : cap) >> k.tile_log2) + 2;
+  k.row_tile = row_tile((int64_t)k.batch * k.heads, k.rows, tiles, a.kv.dim, wide);
+  k.row_tiles = (k.rows + k.row_tile - 1) / k.row_tile;
   k.chunk = (k.batch + 31) / 32;
   k.by_page = make_fastdiv(k.page_size); k.by_group = make_fastdiv(k.group); k.by_row_tiles = make_fastdiv(k.row_tiles);
   k.scale_log2 = a.scale * 1.4426950408889634f;
@@ -153,10 +164,12 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.part_lse = k.parts + (size_t)2 * kCtas * k.row_tile * (size_t)a.kv.dim;
   const uint32_t segments = k.batch * k.heads * k.row_tiles;  // (below 2^31, as the units are)
   const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, (int)k.row_tile / 8, wide));
-  // no more blocks than the longest sequences that the table can hold would employ
-  const int64_t units = (int64_t)segments * (((a.max_pages * a.kv.page_size) >> k.tile_log2) + 1);
+  // no more blocks than the longest sequences would employ; with few tiles a block for each segment
+  const int64_t units = (int64_t)segments * tiles;
   uint32_t ctas = most < kCtas ? most : kCtas;
   if (units < (int64_t)ctas * kLeast) ctas = (uint32_t)((units + kLeast - 1) / kLeast);
+  k.whole = tiles <= kWhole;
+  if (k.whole) ctas = segments;
   // Few sequences and heads may have many parts each: a block of the join for every row of each.  Many have few: blocks of four rows
   // for each block of this kernel.
   k.by_segment = segments * 8 <= kCtas;
@@ -168,7 +181,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
     case MX_E2M1: e = launch_e2m1(k, (int)a.kv.dim, wide, ctas, a.stream); break;
     default: e = launch_int8(k, (int)a.kv.dim, wide, ctas, a.stream); break;
   }
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || k.whole) return e;
   auto join = [&](auto kernel, uint32_t blocks, uint32_t rows) {
     return launch_pdl(kernel, dim3(blocks, k.row_tile / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
   };

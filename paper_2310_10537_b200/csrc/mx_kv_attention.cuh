@@ -23,7 +23,8 @@
 // Split.  The tiles of all sequences, heads and groups of rows, one after the other, are dealt out in equal runs to
 // two or three blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
 // otherwise it leaves a part (its weighted mean and the log of its weight) and a second kernel joins the parts, in the
-// order of the tiles: results do not depend on timing.
+// order of the tiles: results do not depend on timing.  Where the table holds few tokens a block takes one sequence and head as a whole, and
+// nothing is joined (one sequence of 333 tokens: 9.8 -> 6.5 us).
 #pragma once
 
 #include <cuda_fp16.h>
@@ -109,10 +110,11 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two scale bytes as FP32 (0: 2^-127, 255: NaN).
-__device__ __forceinline__ void scales2(uint32_t two, float& a, float& b) {
+// Two scale bytes of a word as FP32 (0: 2^-127, 255: NaN).
+__device__ __forceinline__ void scales2(uint32_t word, bool upper, float& a, float& b) {
   uint32_t d;
-  asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
+  if (!upper) asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.bf16x2.ue8m0x2 %0, lo; }" : "=r"(d) : "r"(word));
+  else asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.bf16x2.ue8m0x2 %0, hi; }" : "=r"(d) : "r"(word));
   a = __uint_as_float(d << 16);
   b = __uint_as_float(d & 0xFFFF0000u);
 }
@@ -124,8 +126,8 @@ __device__ __forceinline__ void load_scales(uint32_t at, float (&s)[C::kScale]) 
   for (int c = 0; c < C::kScale; c += 4) {
     uint32_t w;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at + c));
-    scales2(w, s[c], s[c + 1]);
-    if (c + 2 < C::kBlocks) scales2(w >> 16, s[c + 2], s[c + 3]);
+    scales2(w, false, s[c], s[c + 1]);
+    if (c + 2 < C::kBlocks) scales2(w, true, s[c + 2], s[c + 3]);
   }
 }
 
@@ -134,7 +136,8 @@ template <int FMT>
 __device__ __forceinline__ uint32_t half_pair(uint32_t w, int pair) {
   uint32_t h;
   if constexpr (FMT == MX_E4M3) {
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(pair ? w >> 16 : w)));
+    if (pair == 0) asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(h) : "r"(w));
+    else asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(h) : "r"(w));
   } else if constexpr (FMT == MX_E5M2) {
     h = __byte_perm(w, 0, pair ? 0x3424 : 0x1404);  // E5M2 is FP16's upper byte
   } else if constexpr (FMT == MX_E2M1) {
@@ -204,16 +207,39 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  const Share share = a.share(lane);
-  const uint32_t first = blockIdx.x * share.per;
-  const uint32_t last = min(first + share.per, share.total);  // this block's tiles are first .. last - 1
-  if (first >= share.total) {
-    if (threadIdx.x == 0 && !a.by_segment) a.unfinished[blockIdx.x] = {0, 0, 0, 0};
-    return;
+  Share share;
+  Segment s;
+  uint32_t first = 0, last;  // this block's tiles are first .. last - 1
+  if (a.whole) {
+    s.b = blockIdx.x / (a.heads * a.row_tiles);
+    s.hr = blockIdx.x - s.b * (a.heads * a.row_tiles);
+    s.start = 0;
+    a.fill(s, a.length(s.b));
+    last = s.end;
+    if (last == 0) {  // no token to see
+      for (uint32_t i = threadIdx.x; i < 8 * NR * (DIM / 8); i += kWarps * 32) {
+        const uint32_t r = s.row_tile(a) * (8 * NR) + i / (DIM / 8);
+        if (r >= a.rows) break;
+        const size_t row = a.out_row(s, r);
+        const float zero[8] = {};
+        store8<WIDE ? MX_F32 : MX_BF16>(a.out, row * DIM + i % (DIM / 8) * 8, zero);
+        if (a.lse && i % (DIM / 8) == 0) a.lse[row] = -INFINITY;
+      }
+      return;
+    }
+  } else {
+    share = a.share(lane);
+    first = blockIdx.x * share.per;
+    last = min(first + share.per, share.total);
+    if (first >= share.total) {
+      if (threadIdx.x == 0 && !a.by_segment) a.unfinished[blockIdx.x] = {0, 0, 0, 0};
+      return;
+    }
+    s = a.find(share, first, lane);
   }
 
   // ---- the copies' side: which tokens the next tile to copy holds -------------------------------------------
-  Segment s = a.find(share, first, lane), ls = s;
+  Segment ls = s;
   uint32_t unit = first + warp, lu = unit;  // the tiles to work on and to copy next
   uint32_t page[C::kMine], off[C::kMine];   // of this lane's tokens in the tile to copy: tokens lane, 32 + lane
   bool there[C::kMine];
@@ -691,8 +717,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const uint32_t in_tile = n * 8 + out_row, r = group0 + in_tile;
-      const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
-      const size_t row = ((size_t)s.b * a.new_tokens + i) * a.q_heads + head;
+      const size_t row = a.out_row(s, r);
       const size_t part = (size_t)(blockIdx.x * 2 + (s.start >= first ? 1 : 0)) * (8 * NR) + in_tile;
       if (out_at == 0 && r < a.rows && (!whole || a.lse)) {
         float top = kLowest, sum = 0.0f;
@@ -727,7 +752,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
       }
     }
     // the sequence that begins here and goes on is joined from this block's part and those of the blocks behind it
-    if (threadIdx.x == 0 && (a.by_segment ? s.start >= first : s.end >= last)) {
+    if (threadIdx.x == 0 && !a.whole && (a.by_segment ? s.start >= first : s.end >= last)) {
       const uint32_t parts = s.start >= first && s.end > last ? (s.end - 1) / share.per - blockIdx.x + 1 : 0;
       a.unfinished[a.by_segment ? s.b * a.heads * a.row_tiles + s.hr : blockIdx.x] = {s.b, s.hr, parts, blockIdx.x};
     }

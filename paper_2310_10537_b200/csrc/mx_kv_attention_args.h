@@ -56,11 +56,16 @@ struct Args {
   uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
   FastDiv by_page, by_group, by_row_tiles, by_grid;
   float scale_log2;
-  bool by_segment;
+  bool by_segment, whole;         // whole: block i takes the i-th sequence, head and tile of rows as a whole
 
   __device__ __forceinline__ uint32_t length(uint32_t b) const {
     const int n = lengths[b];
     return n < 0 ? 0 : min((uint32_t)n, max_pages * page_size);
+  }
+  // Row of out (and lse) of query row r of a segment's key-value head.
+  __device__ __forceinline__ size_t out_row(const Segment& s, uint32_t r) const {
+    const uint32_t i = fastdiv(r, by_group);
+    return ((size_t)s.b * new_tokens + i) * q_heads + s.head(*this) * group + (r - i * group);
   }
   // First token that the earliest query sees.
   __device__ __forceinline__ uint32_t begin(uint32_t length) const {
