@@ -651,14 +651,19 @@ int mx_kv_read(const mx_kv_t* kv, const int32_t* slots, int64_t tokens, void* k_
  *   query i of new_tokens is token lengths[b] - new_tokens + i and sees the tokens up to itself, with
  *   window > 0 only the last `window` of them.  Query head a reads key-value head a / (q_heads / heads).
  *     s_j = scale * <q, K_j>;   out = sum_j e^{s_j} V_j / sum_j e^{s_j};   lse = ln sum_j e^{s_j}
- *   out      [batch x new_tokens x q_heads x dim] of opts->dtype, contiguous, 16-byte aligned
+ *   out      [batch x new_tokens x q_heads x dim] of opts->dtype, contiguous, 16-byte aligned, not overlapping q
  *   lse      NULL, or FP32 [batch x new_tokens x q_heads]
- * A query that sees no token gets out = 0 and lse = -Inf.  K and V are the values mx_dequantize gives; scores,
- * maxima and sums are FP32.  What lies in slots that no query sees (NaN scales, stale codes) has no influence.
+ * A query that sees no token gets out = 0 and lse = -Inf (one whose scores are all -Inf likewise).  K and V are the
+ * values mx_dequantize gives; scores, maxima and sums are FP32.  For the products over the tokens a weight times its value's
+ * block scale is rounded to FP16 (BF16 results) or to two FP16 terms (FP32 results), 2^-37 at least of the
+ * largest such product of the row and block.  An Inf or NaN in a query makes its result NaN.  What lies in slots that no query sees
+ * (NaN scales, stale codes) has no influence.
  *   workspace  mx_kv_attention_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and
  *              after; two calls that may overlap need one each
- * dim 64, 96, 128, 192 or 256; q_heads a multiple of heads; scale finite; batch * new_tokens * q_heads below
- * 2^31, max_pages * page_size below 2^31.
+ * dim 64, 96, 128, 192 or 256; q_heads a multiple of heads; scale finite; batch * new_tokens * q_heads and
+ * max_pages * page_size below 2^31, and so is batch * heads * ceil(new_tokens * q_heads / heads / 8) *
+ * (max_pages * page_size / 16 + 1).  It is made for few new tokens: 8 queries of a key-value head (tokens and
+ * heads of its group alike) share one pass over the cache.
  * Errors: MX_ERR_NULL, MX_ERR_SHAPE, MX_ERR_FMT, MX_ERR_ALIGN, MX_ERR_UNSUPPORTED (another dim, 6-bit
  * formats, pad_k128, extents beyond the limits), MX_ERR_WORKSPACE, MX_ERR_CUDA.
  */

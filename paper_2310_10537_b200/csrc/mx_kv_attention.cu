@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
   const Unfinished s = a.unfinished[blockIdx.x];
   if (s.parts == 0) return;
   const uint32_t head0 = fastdiv(s.hr, a.by_row_tiles), row_tile = s.hr - head0 * a.row_tiles;
-  const uint32_t in_tile = blockIdx.y * ROWS + warp / kPer, r = row_tile * a.row_tile + in_tile;
+  const uint32_t in_tile = blockIdx.y * ROWS + warp / kPer, r = row_tile * kRows + in_tile;
   float top = -INFINITY, total = 0.0f;
   float4 sum[2] = {};
   if (r < a.rows) {
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
         x[k][0] = x[k][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p < s.parts) {
           // part 0 is the second slot of this block, the others are the first ones of the blocks behind it
-          const size_t at = (size_t)((s.block + p) * 2 + (p == 0 ? 1 : 0)) * a.row_tile + in_tile;
+          const size_t at = (size_t)((s.block + p) * 2 + (p == 0 ? 1 : 0)) * kRows + in_tile;
           lse[k] = a.part_lse[at];
           if (lane * 4 < dim) x[k][0] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4);
           if (lane * 4 + 128 < dim) x[k][1] = *reinterpret_cast<const float4*>(a.parts + at * dim + lane * 4 + 128);
@@ -120,22 +120,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
   if (a.lse && warp % kPer == 0 && lane == 0) a.lse[row] = all == 0.0f ? -INFINITY : (most + log2f(all)) * kLn2;
 }
 
-// Sequences of up to so many tiles are not split: four rounds of a block's warps take less than a split and a second kernel.
-constexpr int64_t kWhole = 4 * kWarps;
+// Sequences of up to so many tiles are not split, more where there are blocks enough without: eight rounds of a block's warps take less than
+// a split and a second kernel (8 heads of 128, 16 sequences to 450 tokens 8.8 against 12.3 us, to 900 13.3 against 14.9, to 1800 21 against 17; 64
+// sequences to 900 24 against 32, to 1800 41 against 44, to 4000 78 against 67; 128 sequences to 1800 63 against 72, to 4000 121 against 124).
+constexpr int64_t kWhole = 8 * kWarps;
 
-// Query rows of a unit: 8, or 16 where there are more of them and long sequences enough to keep the SMs busy with two blocks each
-// (16 heads a group, 64 sequences to 8192 tokens: 210 against 215 us, one of 131072 85 against 96; but 16 rows over 32 sequences of 1024 tokens
-// 51 against 40, to 5000 96 against 84).  FP32 and rows above 128 elements: 8, for the registers.
-uint32_t row_tile(int64_t segments, int64_t rows, int64_t tiles, int64_t dim, bool wide) {
-  if (rows <= 8 || dim > 128 || wide || tiles < 256) return 8;
-  return segments * ((rows + 15) / 16) * tiles >= 64 * (int64_t)kCtas ? 16 : 8;
-}
-size_t workspace_bytes(uint32_t rows, int64_t dim) { return kCtas * (sizeof(Unfinished) + (size_t)2 * rows * (size_t)(dim + 1) * 4); }
+size_t workspace_bytes(int64_t dim) { return kCtas * (sizeof(Unfinished) + (size_t)2 * kRows * (size_t)(dim + 1) * 4); }
 
 }  // namespace
 }  // namespace attn
 
-size_t kv_attention_workspace(const KvArgs& kv) { return attn::workspace_bytes(16, kv.dim); }
+size_t kv_attention_workspace(const KvArgs& kv) { return attn::workspace_bytes(kv.dim); }
 
 cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   using namespace attn;
@@ -146,29 +141,28 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.q_stride = a.q_stride;
   k.pages = (uint32_t)a.kv.pages; k.page_size = (uint32_t)a.kv.page_size; k.heads = (uint32_t)a.kv.heads;
   k.batch = (uint32_t)a.batch; k.new_tokens = (uint32_t)a.new_tokens; k.q_heads = (uint32_t)a.q_heads;
-  k.max_pages = (uint32_t)a.max_pages;
+  k.max_pages = a.kv.pages > 0 ? (uint32_t)a.max_pages : 0;  // (no page: nobody sees a token)
   k.window = (uint32_t)(a.window < 0x7FFFFFFF ? a.window : 0);  // (no sequence is longer)
   k.group = k.q_heads / k.heads;
   k.rows = k.new_tokens * k.group;
   k.tile_log2 = (uint32_t)tile_log2((int)a.kv.dim, a.kv.fmt == MX_E2M1 ? 4 : 8);
   // no sequence has more tiles than this
-  const int64_t cap = a.max_pages * a.kv.page_size, reach = k.window ? (int64_t)k.window + k.new_tokens : cap;
+  const int64_t cap = (int64_t)k.max_pages * a.kv.page_size, reach = k.window ? (int64_t)k.window + k.new_tokens : cap;
   const int64_t tiles = ((reach < cap ? reach : cap) >> k.tile_log2) + 2;
-  k.row_tile = row_tile((int64_t)k.batch * k.heads, k.rows, tiles, a.kv.dim, wide);
-  k.row_tiles = (k.rows + k.row_tile - 1) / k.row_tile;
+  k.row_tiles = (k.rows + kRows - 1) / kRows;
   k.chunk = (k.batch + 31) / 32;
   k.by_page = make_fastdiv(k.page_size); k.by_group = make_fastdiv(k.group); k.by_row_tiles = make_fastdiv(k.row_tiles);
   k.scale_log2 = a.scale * 1.4426950408889634f;
   k.unfinished = (Unfinished*)a.workspace;
   k.parts = (float*)(k.unfinished + kCtas);
-  k.part_lse = k.parts + (size_t)2 * kCtas * k.row_tile * (size_t)a.kv.dim;
+  k.part_lse = k.parts + (size_t)2 * kCtas * kRows * (size_t)a.kv.dim;
   const uint32_t segments = k.batch * k.heads * k.row_tiles;  // (below 2^31, as the units are)
-  const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, (int)k.row_tile / 8, wide));
+  const uint32_t most = (uint32_t)(a.sm_count * blocks_per_sm((int)a.kv.dim, wide));
   // no more blocks than the longest sequences would employ; with few tiles a block for each segment
   const int64_t units = (int64_t)segments * tiles;
   uint32_t ctas = most < kCtas ? most : kCtas;
+  k.whole = tiles <= kWhole * (1 + segments / ctas);
   if (units < (int64_t)ctas * kLeast) ctas = (uint32_t)((units + kLeast - 1) / kLeast);
-  k.whole = tiles <= kWhole;
   if (k.whole) ctas = segments;
   // Few sequences and heads may have many parts each: a block of the join for every row of each.  Many have few: blocks of four rows
   // for each block of this kernel.
@@ -183,7 +177,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   }
   if (e != cudaSuccess || k.whole) return e;
   auto join = [&](auto kernel, uint32_t blocks, uint32_t rows) {
-    return launch_pdl(kernel, dim3(blocks, k.row_tile / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
+    return launch_pdl(kernel, dim3(blocks, kRows / rows), dim3(kJoinWarps * 32), 0, a.stream, k, (uint32_t)a.kv.dim);
   };
   if (wide) return k.by_segment ? join(kv_join_kernel<MX_F32, 1>, segments, 1) : join(kv_join_kernel<MX_F32, 4>, ctas, 4);
   return k.by_segment ? join(kv_join_kernel<MX_BF16, 1>, segments, 1) : join(kv_join_kernel<MX_BF16, 4>, ctas, 4);

@@ -13,7 +13,7 @@
 // results; the queries too).  Scores, maxima, sums and accumulators are FP32.
 //
 // Layout.  A warp takes kTokens tokens at a time: S^T = K Q^T has the tokens on the M side of the MMA and the query rows
-// on its N side, 8 or 16 of them (a group of 4 query heads wastes half of 8, not three quarters of 16), then
+// on its N side, 8 of them (a group of 4 query heads wastes half of 8, not three quarters of 16), then
 // O^T = V^T W^T with the row's elements on the M side.  W^T comes out of S^T's accumulators by 8 x 8 transposes
 // in registers.  The order of the elements within a block and of the tokens within a tile is free in these sums, and chosen
 // such that a lane's codes are consecutive bytes: no shuffling of codes but the pairing of neighbouring tokens' values.
@@ -28,8 +28,6 @@
 #pragma once
 
 #include <cuda_fp16.h>
-
-#include <type_traits>
 
 #include "mx_device.cuh"
 #include "mx_kv_attention_args.h"
@@ -48,9 +46,9 @@ constexpr float kMost = 8.507059173023462e37f;      // 2^126, F's largest value
 // Shape of a kernel instance.
 constexpr int kSharedOfSm = 228 * 1024;
 constexpr int kJoinPitch = 36;  // words of a block of 32 elements in the buffer that joins the warps: rows 2 t in different banks
-template <int FMT, int DIM, int NR, bool WIDE>
+template <int FMT, int DIM, bool WIDE>
 struct Cfg {
-  static constexpr int kResident = blocks_per_sm(DIM, NR, WIDE);
+  static constexpr int kResident = blocks_per_sm(DIM, WIDE);
   static constexpr int kBits = FmtTraits<FMT>::bits;
   static constexpr int kBlocks = DIM / 32;
   static constexpr int kRow = DIM * kBits / 8;             // bytes of a row's codes
@@ -191,10 +189,10 @@ __device__ __forceinline__ uint32_t lds2(uint32_t a) {
   return v;
 }
 
-// The instance for rows of DIM elements in format FMT, NR times 8 query rows at a time.
-template <int FMT, int DIM, int NR, bool WIDE>
-__global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_attention_kernel(const Args a) {
-  using C = Cfg<FMT, DIM, NR, WIDE>;
+// The instance for rows of DIM elements in format FMT; WIDE: FP32 queries and results.
+template <int FMT, int DIM, bool WIDE>
+__global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_attention_kernel(const Args a) {
+  using C = Cfg<FMT, DIM, WIDE>;
   constexpr int B = C::kBlocks, TL = C::kTiles, W = WIDE ? 2 : 1;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
@@ -217,8 +215,8 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
     a.fill(s, a.length(s.b));
     last = s.end;
     if (last == 0) {  // no token to see
-      for (uint32_t i = threadIdx.x; i < 8 * NR * (DIM / 8); i += kWarps * 32) {
-        const uint32_t r = s.row_tile(a) * (8 * NR) + i / (DIM / 8);
+      for (uint32_t i = threadIdx.x; i < 8 * (DIM / 8); i += kWarps * 32) {
+        const uint32_t r = s.row_tile(a) * 8 + i / (DIM / 8);
         if (r >= a.rows) break;
         const size_t row = a.out_row(s, r);
         const float zero[8] = {};
@@ -277,26 +275,46 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
         }
         if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(scales + 2 * C::kTokens * C::kScale + 4 * i), "r"(seen[i]) : "memory");
       }
-      auto codes = [&](auto whole) {
+      // 16-byte units lane, 32 + lane, .. of the tile, and where they go: the lane's part of that, and (where a row is a power of two of
+      // them) a constant one, which meet in an exclusive or within a line
+      constexpr bool kEven = (C::kUnits & (C::kUnits - 1)) == 0;
+      const uint32_t u0 = lane % C::kUnits, to0 = stage + (row_at<C>(lane / C::kUnits) ^ ((u0 & 7) << 4)) + (u0 >> 3) * 128;
+      auto place = [&](int i) {
+        if (kEven) {
+          const uint32_t c = row_at<C>(32 * i / C::kUnits);
+          return (to0 ^ (c & 127)) + (c & ~127u);
+        }
+        const uint32_t r = (lane + 32 * i) / C::kUnits, u = (lane + 32 * i) % C::kUnits;
+        return stage + (row_at<C>(r) ^ ((u & 7) << 4)) + (u >> 3) * 128;
+      };
+      // (every lane takes part in the exchange and the vote: no condition stands before them)
+      const uint32_t row0 = __shfl_sync(0xFFFFFFFFu, row[0], 0);
+      bool run = all;  // tokens one after the other in memory, as within a page
+#pragma unroll
+      for (int i = 0; i < C::kMine; ++i) run = run & (row[i] == row0 + 32 * i + lane % C::kTokens);
+      run = __all_sync(0xFFFFFFFFu, run);
+      if (run) {
+        const size_t at = (size_t)row0 * C::kRow + lane * 16;
+        const uint8_t *k = a.k_elems + at, *v = a.v_elems + at;
+#pragma unroll
+        for (int i = 0; i < C::kCopies; ++i) {
+          const uint32_t to = place(i);
+          copy16(to, k + i * 512);
+          copy16(to + C::kCodes, v + i * 512);
+        }
+      } else {
 #pragma unroll
         for (int i = 0; i < C::kCopies; ++i) {
           const uint32_t n = lane + 32 * i, r = n / C::kUnits, u = n % C::kUnits;
           // (which of a lane's two tokens: known at compile time where the units of 32 tokens are whole rounds of the warp)
           const int mine = C::kMine == 1 ? 0 : 32 * i / (32 * C::kUnits);
           const size_t at = (size_t)__shfl_sync(0xFFFFFFFFu, row[mine], r % 32) * C::kRow + u * 16;
-          const uint32_t to = stage + (row_at<C>(r) ^ ((u & 7) << 4)) + (u >> 3) * 128;
-          if constexpr (decltype(whole)::value) {
-            copy16(to, a.k_elems + at);
-            copy16(to + C::kCodes, a.v_elems + at);
-          } else {
-            const bool has = seen[mine] >> (r % 32) & 1;
-            copy16(to, a.k_elems + at, has);
-            copy16(to + C::kCodes, a.v_elems + at, has);
-          }
+          const bool has = seen[mine] >> (r % 32) & 1;
+          const uint32_t to = place(i);
+          copy16(to, a.k_elems + at, has);
+          copy16(to + C::kCodes, a.v_elems + at, has);
         }
-      };
-      if (all) codes(std::true_type());
-      else codes(std::false_type());
+      }
       lu += kWarps;
       fill = fill + 1 == C::kStages ? 0 : fill + 1;
       look_up();
@@ -316,86 +334,75 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
   for (;;) {
     // ---- one sequence and head: the queries ------------------------------------------------------------------
     const uint32_t seg_end = min(s.end, last);
-    const uint32_t group0 = s.row_tile(a) * (8 * NR);  // first query row of this tile of rows
-    uint32_t q[W][B][2][NR][2];
-    float qf[NR][2];
-    int lo[NR][2], hi[NR][2];  // tokens that the lane's rows 2 t, 2 t + 1 see
-    Raw8<WIDE ? MX_F32 : MX_BF16> raw[NR][B];
+    const uint32_t group0 = s.row_tile(a) * 8;  // first query row of this tile of rows
+    uint32_t q[W][B][2][2];
+    float qf[2];
+    int lo[2], hi[2];  // tokens that the lane's rows 2 t, 2 t + 1 see
+    Raw8<WIDE ? MX_F32 : MX_BF16> raw[B];
+    const uint32_t q_row = group0 + g, q_token = fastdiv(q_row, a.by_group), q_head = s.head(a) * a.group + (q_row - q_token * a.group);
+    const size_t q_at = ((size_t)s.b * a.new_tokens + q_token) * a.q_stride + (size_t)q_head * DIM + t * 8;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const uint32_t r = group0 + n * 8 + g;
-      const uint32_t i = fastdiv(r, a.by_group), head = s.head(a) * a.group + (r - i * a.group);
-      const size_t at = ((size_t)s.b * a.new_tokens + i) * a.q_stride + (size_t)head * DIM + t * 8;
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        raw[n][b] = {};
-        if (r < a.rows) raw[n][b] = load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, at + b * 32);
-      }
+    for (int b = 0; b < B; ++b) {
+      raw[b] = {};
+      if (q_row < a.rows) raw[b] = load_raw8<WIDE ? MX_F32 : MX_BF16>(a.q, q_at + b * 32);
     }
 #pragma unroll 1
     for (; ahead > 0; --ahead) copy_tile();  // (the first copies are under way while the queries are prepared)
+    float x[B][8], amax = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      float x[B][8], amax = 0.0f;
+    for (int b = 0; b < B; ++b) widen(raw[b], x[b]);
 #pragma unroll
-      for (int b = 0; b < B; ++b) widen(raw[n][b], x[b]);
+    for (int b = 0; b < B; ++b)
 #pragma unroll
-      for (int b = 0; b < B; ++b)
+      for (int j = 0; j < 8; ++j) amax = absmax_nan(amax, x[b][j]);
+    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+    // q' = q * 2^-e with the largest element in [2^7, 2^8): FP16 then holds what is 2^-22 of it to full precision.
+    // Inf or NaN make the row NaN.
+    const uint32_t ab = __float_as_uint(amax) & 0x7FFFFFFFu;
+    const int e = ab == 0 ? 0 : (int)(ab >> 23) - 134;  // -134 .. 120
+    const float half1 = ab >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - e / 2) << 23);
+    const float half2 = __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) amax = absmax_nan(amax, x[b][j]);
-      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-      // q' = q * 2^-e with the largest element in [2^7, 2^8): FP16 then holds what is 2^-22 of it to full precision.
-      // Inf or NaN make the row NaN.
-      const uint32_t ab = __float_as_uint(amax) & 0x7FFFFFFFu;
-      const int e = ab == 0 ? 0 : (int)(ab >> 23) - 134;  // -134 .. 120
-      const float half1 = ab >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - e / 2) << 23);
-      const float half2 = __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+    for (int b = 0; b < B; ++b)
 #pragma unroll
-      for (int b = 0; b < B; ++b)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float u = x[b][4 * k + 2 * j] * half1 * half2, v = x[b][4 * k + 2 * j + 1] * half1 * half2;
-            q[0][b][k][n][j] = pack_half(u, v);
-            if (WIDE) {
-              const float2 h = unpack_half(q[0][b][k][n][j]);
-              q[W - 1][b][k][n][j] = pack_half(u - h.x, v - h.y);
-            }
+        for (int j = 0; j < 2; ++j) {
+          const float u = x[b][4 * k + 2 * j] * half1 * half2, v = x[b][4 * k + 2 * j + 1] * half1 * half2;
+          q[0][b][k][j] = pack_half(u, v);
+          if (WIDE) {
+            const float2 h = unpack_half(q[0][b][k][j]);
+            q[W - 1][b][k][j] = pack_half(u - h.x, v - h.y);
           }
-      // (1 / half is a power of two as well)
-      const float f = a.scale_log2 * C::kUnit * __uint_as_float((uint32_t)(127 + (e - e / 2)) << 23) * __uint_as_float((uint32_t)(127 + e / 2) << 23);
+        }
+    // (1 / half is a power of two as well)
+    const float f = a.scale_log2 * C::kUnit * __uint_as_float((uint32_t)(127 + (e - e / 2)) << 23) * __uint_as_float((uint32_t)(127 + e / 2) << 23);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        qf[n][j] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + j) * 4);
-        const uint32_t row = group0 + n * 8 + 2 * t + j;
-        const int i = row < a.rows ? (int)fastdiv(row, a.by_group) : (int)a.new_tokens - 1;
-        hi[n][j] = (int)s.length - ((int)a.new_tokens - 1 - i);
-        lo[n][j] = a.window ? max(hi[n][j] - (int)a.window, 0) : 0;
-      }
+    for (int j = 0; j < 2; ++j) {
+      qf[j] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + j) * 4);
+      const uint32_t row = group0 + 2 * t + j;
+      const int i = row < a.rows ? (int)fastdiv(row, a.by_group) : (int)a.new_tokens - 1;
+      hi[j] = (int)s.length - ((int)a.new_tokens - 1 - i);
+      lo[j] = a.window ? max(hi[j] - (int)a.window, 0) : 0;
     }
     // tiles between these are seen by all rows
     const int all_lo = a.window ? max((int)s.length - (int)a.window, 0) : 0, all_hi = (int)s.length - ((int)a.new_tokens - 1);
 
-    float m[NR][2], l[NR][2], F[B][NR][2], acc[B][2][NR][4];
+    float m[2], l[2], F[B][2], acc[B][2][4];
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int j = 0; j < 2; ++j) {
+      m[j] = kLowest;
+      l[j] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        m[n][j] = kLowest;
-        l[n][j] = 0.0f;
-#pragma unroll
-        for (int b = 0; b < B; ++b) F[b][n][j] = kMost;
-      }
+      for (int b = 0; b < B; ++b) F[b][j] = kMost;
+    }
 #pragma unroll
     for (int b = 0; b < B; ++b)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[b][h][n][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) acc[b][h][i] = 0.0f;
 
     bool fresh = true;  // m and F have not been set by a tile of this sequence
 
@@ -419,16 +426,14 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
       }
 
       // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1, without the rows' factors
-      float p[TL][NR][4];
+      float p[TL][4];
 #pragma unroll
       for (int x = 0; x < TL; ++x) {
         float ks[2][C::kScale];
 #pragma unroll
         for (int h = 0; h < 2; ++h) load_scales<C>(scales + (16 * x + 8 * h + g) * C::kScale, ks[h]);
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[x][n][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) p[x][i] = 0.0f;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
           uint32_t ka[2][4];  // two steps of 16 elements
@@ -449,16 +454,13 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
               ka[1][2 + h] = half_pair<FMT>(c, 3);
             }
           }
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          for (int w = W - 1; w >= 0; --w)
 #pragma unroll
-            for (int w = W - 1; w >= 0; --w)
+            for (int k = 0; k < 2; ++k) mma(d, ka[k], q[w][b][k][0], q[w][b][k][1]);
 #pragma unroll
-              for (int k = 0; k < 2; ++k) mma(d, ka[k], q[w][b][k][n][0], q[w][b][k][n][1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[x][n][i] = fmaf(d[i], ks[i >> 1][b], p[x][n][i]);
-          }
+          for (int i = 0; i < 4; ++i) p[x][i] = fmaf(d[i], ks[i >> 1][b], p[x][i]);
         }
       }
       uint32_t hidden = 0;  // bit: this score is of a token that the row does not see
@@ -466,109 +468,95 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
 #pragma unroll
         for (int x = 0; x < TL; ++x)
 #pragma unroll
-          for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int k = 16 * x + 8 * (i >> 1) + (int)g, j = j0 + k;
-              if (!(seen[x / 2 % C::kMine] >> (k % 32) & 1) || j < lo[n][i & 1] || j >= hi[n][i & 1]) hidden |= 1u << ((x * NR + n) * 4 + i);
-            }
+          for (int i = 0; i < 4; ++i) {
+            const int k = 16 * x + 8 * (i >> 1) + (int)g, j = j0 + k;
+            if (!(seen[x / 2 % C::kMine] >> (k % 32) & 1) || j < lo[i & 1] || j >= hi[i & 1]) hidden |= 1u << (x * 4 + i);
+          }
       }
 
       // weights without the values' scales: m moves when a score passes it
-      float y[TL][NR][4];
+      float y[TL][4];
       for (bool moves = fresh;; moves = false) {
         if (!moves) {
-        float most = -1.0f;
-#pragma unroll
-        for (int x = 0; x < TL; ++x)
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[x][n][i] = fmaf(p[x][n][i], qf[n][i & 1], -m[n][i & 1]);
-        if (edge) {
+          float most = -1.0f;
 #pragma unroll
           for (int x = 0; x < TL; ++x)
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (hidden >> ((x * NR + n) * 4 + i) & 1) y[x][n][i] = -INFINITY;
-        }
-#pragma unroll
-        for (int x = 0; x < TL; ++x)
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, y[x][n][i]);
-        if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
-        }
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float top = -INFINITY;
+            for (int i = 0; i < 4; ++i) y[x][i] = fmaf(p[x][i], qf[i & 1], -m[i & 1]);
+          if (edge) {
 #pragma unroll
             for (int x = 0; x < TL; ++x)
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
-                if (!(hidden >> ((x * NR + n) * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][n][2 * h + j] * qf[n][j]);
-#pragma unroll
-            for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            const bool moves = top > m[n][j];
-            const float next = moves ? ceilf(top) + kRoom : m[n][j], by = moves ? ex2(m[n][j] - next) : 1.0f;
-            m[n][j] = next;
-            l[n][j] *= by;
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                acc[b][h][n][j] *= by;
-                acc[b][h][n][2 + j] *= by;
-              }
+              for (int i = 0; i < 4; ++i)
+                if (hidden >> (x * 4 + i) & 1) y[x][i] = -INFINITY;
           }
+#pragma unroll
+          for (int x = 0; x < TL; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, y[x][i]);
+          if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < TL; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][2 * h + j] * qf[j]);
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+          const bool moves = top > m[j];
+          const float next = moves ? ceilf(top) + kRoom : m[j], by = moves ? ex2(m[j] - next) : 1.0f;
+          m[j] = next;
+          l[j] *= by;
+#pragma unroll
+          for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              acc[b][h][j] *= by;
+              acc[b][h][2 + j] *= by;
+            }
+        }
       }
 #pragma unroll
       for (int x = 0; x < TL; ++x)
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[x][n][i] = ex2(y[x][n][i]);
-            l[n][i & 1] += p[x][n][i];
-          }
+        for (int i = 0; i < 4; ++i) {
+          p[x][i] = ex2(y[x][i]);
+          l[i & 1] += p[x][i];
+        }
 
       // weights with the values' scales: F moves when one passes kTop
-      uint32_t w[W][B][TL][NR][2];
+      uint32_t w[W][B][TL][2];
       for (bool moves = fresh;; moves = false) {
         if (!moves) {
-        uint32_t most = 0;
+          uint32_t most = 0;
 #pragma unroll
-        for (int x = 0; x < TL; ++x) {
-          float vs[2][C::kScale];
+          for (int x = 0; x < TL; ++x) {
+            float vs[2][C::kScale];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) load_scales<C>(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale, vs[h]);
+            for (int h = 0; h < 2; ++h) load_scales<C>(scales + (C::kTokens + 16 * x + 8 * h + g) * C::kScale, vs[h]);
 #pragma unroll
-          for (int b = 0; b < B; ++b)
+            for (int b = 0; b < B; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int n = 0; n < NR; ++n) {
+              for (int h = 0; h < 2; ++h) {
                 // p is at most 1 and VX at most 2^127, F follows their product
-                const float u = p[x][n][2 * h] * vs[h][b] * F[b][n][0], v = p[x][n][2 * h + 1] * vs[h][b] * F[b][n][1];
+                const float u = p[x][2 * h] * vs[h][b] * F[b][0], v = p[x][2 * h + 1] * vs[h][b] * F[b][1];
                 const uint32_t c = pack_half(u, v);
-                w[0][b][x][n][h] = c;
+                w[0][b][x][h] = c;
                 most = max_half2(most, c);
                 if (WIDE) {
                   const float2 r = unpack_half(c);
-                  w[W - 1][b][x][n][h] = pack_half(u - r.x, v - r.y);
+                  w[W - 1][b][x][h] = pack_half(u - r.x, v - r.y);
                 }
               }
-        }
-        const float2 top2 = unpack_half(most);
-        if (!__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
+          }
+          const float2 top2 = unpack_half(most);
+          if (!__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
         }
         // F moves to where the largest is in [2^kAim, 2^(kAim + 1)), never up: a smaller F only costs small weights their digits
-        float top[B][NR][2];
+        float top[B][2];
 #pragma unroll
         for (int x = 0; x < TL; ++x)
 #pragma unroll
@@ -578,49 +566,41 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
 #pragma unroll
             for (int b = 0; b < B; ++b)
 #pragma unroll
-              for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) top[b][n][j] = fmaxf(x + h == 0 ? 0.0f : top[b][n][j], p[x][n][2 * h + j] * v[b]);
+              for (int j = 0; j < 2; ++j) top[b][j] = fmaxf(x + h == 0 ? 0.0f : top[b][j], p[x][2 * h + j] * v[b]);
           }
 #pragma unroll
         for (int d = 4; d < 32; d *= 2)
 #pragma unroll
           for (int b = 0; b < B; ++b)
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) top[b][n][j] = fmaxf(top[b][n][j], __shfl_xor_sync(0xFFFFFFFFu, top[b][n][j], d));
+            for (int j = 0; j < 2; ++j) top[b][j] = fmaxf(top[b][j], __shfl_xor_sync(0xFFFFFFFFu, top[b][j], d));
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
-          for (int n = 0; n < NR; ++n)
+          for (int j = 0; j < 2; ++j) {
+            const int e = (int)(__float_as_uint(top[b][j]) >> 23) - 127, have = (int)(__float_as_uint(F[b][j]) >> 23) - 127;
+            const int next = min(have, kAim - e);
+            const float by = ex2((float)(next - have));  // 1 where F stays
+            F[b][j] = __uint_as_float((uint32_t)(127 + next) << 23);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int e = (int)(__float_as_uint(top[b][n][j]) >> 23) - 127, have = (int)(__float_as_uint(F[b][n][j]) >> 23) - 127;
-              const int next = min(have, kAim - e);
-              const float by = ex2((float)(next - have));  // 1 where F stays
-              F[b][n][j] = __uint_as_float((uint32_t)(127 + next) << 23);
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                acc[b][h][n][j] *= by;
-                acc[b][h][n][2 + j] *= by;
-              }
+            for (int h = 0; h < 2; ++h) {
+              acc[b][h][j] *= by;
+              acc[b][h][2 + j] *= by;
             }
+          }
       }
       fresh = false;
       if (edge) {  // a token that is not seen weighs nothing, whatever its scale
 #pragma unroll
         for (int x = 0; x < TL; ++x)
 #pragma unroll
-          for (int n = 0; n < NR; ++n)
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t two = hidden >> (x * 4 + 2 * h) & 3, keep = (two & 1 ? 0u : 0xFFFFu) | (two & 2 ? 0u : 0xFFFF0000u);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t two = hidden >> ((x * NR + n) * 4 + 2 * h) & 3, keep = (two & 1 ? 0u : 0xFFFFu) | (two & 2 ? 0u : 0xFFFF0000u);
+            for (int k = 0; k < W; ++k)
 #pragma unroll
-              for (int k = 0; k < W; ++k)
-#pragma unroll
-                for (int b = 0; b < B; ++b) w[k][b][x][n][h] &= keep;
-            }
+              for (int b = 0; b < B; ++b) w[k][b][x][h] &= keep;
+          }
       }
 #pragma unroll
       for (int b = 0; b < B; ++b)
@@ -653,24 +633,21 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
               va[h][3] = half_pair<FMT>(y1, 2 + h);
             }
           }
+          uint32_t wb[W][2];
 #pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            uint32_t wb[W][2];
+          for (int k = 0; k < W; ++k)
 #pragma unroll
-            for (int k = 0; k < W; ++k)
+            for (int h = 0; h < 2; ++h) wb[k][h] = transpose8(w[k][b][x][h]);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) wb[k][h] = transpose8(w[k][b][x][n][h]);
+          for (int h = 0; h < 2; ++h) {
+            if (WIDE) {  // the sum over tokens in FP32 additions, which round to nearest
+              float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              mma(d, va[h], wb[W - 1][0], wb[W - 1][1]);
+              mma(d, va[h], wb[0][0], wb[0][1]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (WIDE) {  // the sum over tokens in FP32 additions, which round to nearest
-                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                mma(d, va[h], wb[W - 1][0], wb[W - 1][1]);
-                mma(d, va[h], wb[0][0], wb[0][1]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[b][h][n][i] += d[i];
-              } else {
-                mma(acc[b][h][n], va[h], wb[0][0], wb[0][1]);
-              }
+              for (int i = 0; i < 4; ++i) acc[b][h][i] += d[i];
+            } else {
+              mma(acc[b][h], va[h], wb[0][0], wb[0][1]);
             }
           }
         }
@@ -679,77 +656,70 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
 
     // ---- the block's warps joined: sum of acc 2^(m - M) / F over sum of l 2^(m - M) -------------------------------
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int j = 0; j < 2; ++j) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) l[n][j] += __shfl_xor_sync(0xFFFFFFFFu, l[n][j], d);
-        if (g == 0) join_ml[warp * 16 + n * 8 + 2 * t + j] = make_float2(m[n][j], l[n][j]);
-      }
+      for (int d = 4; d < 32; d *= 2) l[j] += __shfl_xor_sync(0xFFFFFFFFu, l[j], d);
+      if (g == 0) join_ml[warp * 16 + 2 * t + j] = make_float2(m[j], l[j]);
+    }
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < NR; ++n)
+    for (int j = 0; j < 2; ++j) {
+      float top = kLowest, sum = 0.0f;
+      float2 ml[kWarps];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float top = kLowest, sum = 0.0f;
-        float2 ml[kWarps];
+      for (int w = 0; w < kWarps; ++w) {
+        ml[w] = join_ml[w * 16 + 2 * t + j];
+        top = fmaxf(top, ml[w].x);
+      }
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          ml[w] = join_ml[w * 16 + n * 8 + 2 * t + j];
-          top = fmaxf(top, ml[w].x);
-        }
+      for (int w = 0; w < kWarps; ++w) sum = fmaf(ml[w].y, ex2(ml[w].x - top), sum);
+      const float mine = sum == 0.0f ? 0.0f : ex2(m[j] - top) * C::kUnit * rcp(sum);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum = fmaf(ml[w].y, ex2(ml[w].x - top), sum);
-        const float mine = sum == 0.0f ? 0.0f : ex2(m[n][j] - top) * C::kUnit * rcp(sum);
+      for (int b = 0; b < B; ++b) {
+        const float by = __uint_as_float((254u << 23) - __float_as_uint(F[b][j]));  // 1 / F, a power of two
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-          const float by = __uint_as_float((254u << 23) - __float_as_uint(F[b][n][j]));  // 1 / F, a power of two
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            acc[b][h][n][j] = acc[b][h][n][j] * mine * by;
-            acc[b][h][n][2 + j] = acc[b][h][n][2 + j] * mine * by;
-          }
+        for (int h = 0; h < 2; ++h) {
+          acc[b][h][j] = acc[b][h][j] * mine * by;
+          acc[b][h][2 + j] = acc[b][h][2 + j] * mine * by;
         }
       }
+    }
     const bool whole = s.start >= first && s.end <= last;
     // a thread puts out two elements of one row of each block, row tid / 16 of the eight
     const uint32_t out_row = threadIdx.x / 16, out_at = threadIdx.x % 16 * 2;
+    const uint32_t r = group0 + out_row;
+    const size_t row = a.out_row(s, r);
+    const size_t part = (size_t)(blockIdx.x * 2 + (s.start >= first ? 1 : 0)) * 8 + out_row;
+    if (out_at == 0 && r < a.rows && (!whole || a.lse)) {
+      float top = kLowest, sum = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const uint32_t in_tile = n * 8 + out_row, r = group0 + in_tile;
-      const size_t row = a.out_row(s, r);
-      const size_t part = (size_t)(blockIdx.x * 2 + (s.start >= first ? 1 : 0)) * (8 * NR) + in_tile;
-      if (out_at == 0 && r < a.rows && (!whole || a.lse)) {
-        float top = kLowest, sum = 0.0f;
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, join_ml[w * 16 + out_row].x);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, join_ml[w * 16 + in_tile].x);
+      for (int w = 0; w < kWarps; ++w) sum = fmaf(join_ml[w * 16 + out_row].y, ex2(join_ml[w * 16 + out_row].x - top), sum);
+      const float lse2 = sum == 0.0f ? -INFINITY : top + lg2(sum);
+      if (whole) a.lse[row] = lse2 * kLn2;
+      else a.part_lse[part] = lse2;
+    }
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum = fmaf(join_ml[w * 16 + in_tile].y, ex2(join_ml[w * 16 + in_tile].x - top), sum);
-        const float lse2 = sum == 0.0f ? -INFINITY : top + lg2(sum);
-        if (whole) a.lse[row] = lse2 * kLn2;
-        else a.part_lse[part] = lse2;
+    for (int b = 0; b < B; ++b) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<float4*>(join + (warp * 8 + 2 * t + j) * kJoinPitch + 4 * g) =
+            make_float4(acc[b][0][j], acc[b][0][2 + j], acc[b][1][j], acc[b][1][2 + j]);
+      __syncthreads();
+      float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 u = *reinterpret_cast<const float2*>(join + (w * 8 + out_row) * kJoinPitch + out_at);
+        v.x += u.x;
+        v.y += u.y;
       }
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          *reinterpret_cast<float4*>(join + (warp * 8 + 2 * t + j) * kJoinPitch + 4 * g) =
-              make_float4(acc[b][0][n][j], acc[b][0][n][2 + j], acc[b][1][n][j], acc[b][1][n][2 + j]);
-        __syncthreads();
-        float2 v = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float2 u = *reinterpret_cast<const float2*>(join + (w * 8 + out_row) * kJoinPitch + out_at);
-          v.x += u.x;
-          v.y += u.y;
-        }
-        if (r < a.rows) {
-          if (!whole) *reinterpret_cast<float2*>(a.parts + part * DIM + b * 32 + out_at) = v;
-          else if (WIDE) *reinterpret_cast<float2*>((float*)a.out + row * DIM + b * 32 + out_at) = v;
-          else *reinterpret_cast<uint32_t*>((uint16_t*)a.out + row * DIM + b * 32 + out_at) = pack_bf16(v.x, v.y);
-        }
-        __syncthreads();  // before the buffer is used again
+      if (r < a.rows) {
+        if (!whole) *reinterpret_cast<float2*>(a.parts + part * DIM + b * 32 + out_at) = v;
+        else if (WIDE) *reinterpret_cast<float2*>((float*)a.out + row * DIM + b * 32 + out_at) = v;
+        else *reinterpret_cast<uint32_t*>((uint16_t*)a.out + row * DIM + b * 32 + out_at) = pack_bf16(v.x, v.y);
       }
+      __syncthreads();  // before the buffer is used again
     }
     // the sequence that begins here and goes on is joined from this block's part and those of the blocks behind it
     if (threadIdx.x == 0 && !a.whole && (a.by_segment ? s.start >= first : s.end >= last)) {
@@ -762,29 +732,23 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, NR, WIDE)) kv_
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <int FMT, int DIM, int NR, bool WIDE>
+template <int FMT, int DIM, bool WIDE>
 cudaError_t launch_instance(const Args& a, uint32_t ctas, cudaStream_t stream) {
-  using C = Cfg<FMT, DIM, NR, WIDE>;
-  auto kernel = kv_attention_kernel<FMT, DIM, NR, WIDE>;
+  using C = Cfg<FMT, DIM, WIDE>;
+  auto kernel = kv_attention_kernel<FMT, DIM, WIDE>;
   // (a function attribute per device: set on every call, it costs less than a microsecond)
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kShared);
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(ctas), dim3(kWarps * 32), C::kShared, stream, a);
 }
-template <int FMT, int DIM>
-cudaError_t launch_dim(const Args& a, bool wide, uint32_t ctas, cudaStream_t stream) {
-  if (wide) return launch_instance<FMT, DIM, 1, true>(a, ctas, stream);
-  if (a.row_tile == 8) return launch_instance<FMT, DIM, 1, false>(a, ctas, stream);
-  return launch_instance<FMT, DIM, DIM <= 128 ? 2 : 1, false>(a, ctas, stream);
-}
 template <int FMT>
 cudaError_t launch_format(const Args& a, int dim, bool wide, uint32_t ctas, cudaStream_t stream) {
   switch (dim) {
-    case 64: return launch_dim<FMT, 64>(a, wide, ctas, stream);
-    case 96: return launch_dim<FMT, 96>(a, wide, ctas, stream);
-    case 128: return launch_dim<FMT, 128>(a, wide, ctas, stream);
-    case 192: return launch_dim<FMT, 192>(a, wide, ctas, stream);
-    default: return launch_dim<FMT, 256>(a, wide, ctas, stream);
+    case 64: return wide ? launch_instance<FMT, 64, true>(a, ctas, stream) : launch_instance<FMT, 64, false>(a, ctas, stream);
+    case 96: return wide ? launch_instance<FMT, 96, true>(a, ctas, stream) : launch_instance<FMT, 96, false>(a, ctas, stream);
+    case 128: return wide ? launch_instance<FMT, 128, true>(a, ctas, stream) : launch_instance<FMT, 128, false>(a, ctas, stream);
+    case 192: return wide ? launch_instance<FMT, 192, true>(a, ctas, stream) : launch_instance<FMT, 192, false>(a, ctas, stream);
+    default: return wide ? launch_instance<FMT, 256, true>(a, ctas, stream) : launch_instance<FMT, 256, false>(a, ctas, stream);
   }
 }
 

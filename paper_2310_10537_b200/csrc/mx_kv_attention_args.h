@@ -7,9 +7,10 @@ namespace mx {
 namespace attn {
 
 constexpr int kWarps = 4;         // of a block
+constexpr uint32_t kRows = 8;     // query rows of a unit, the N side of an MMA
 constexpr uint32_t kCtas = 444;   // blocks at most: three on each of 148 SMs
 // Blocks per SM of an instance, by its registers.
-__host__ __device__ constexpr int blocks_per_sm(int dim, int rows8, bool wide) { return dim <= 128 && rows8 == 1 && !wide ? 3 : 2; }
+__host__ __device__ constexpr int blocks_per_sm(int dim, bool wide) { return dim <= 128 && !wide ? 3 : 2; }
 // A block's fewest tiles: one per warp.
 constexpr uint32_t kLeast = kWarps;
 
@@ -47,12 +48,12 @@ struct Args {
   const void* q;
   const int32_t *table, *lengths;
   void* out;
-  float *lse, *parts, *part_lse;  // parts: [2 * blocks][row tile][dim]
+  float *lse, *parts, *part_lse;  // parts: [2 * blocks][kRows][dim]
   Unfinished* unfinished;         // of each block, or (by_segment) of each sequence, head and tile of rows that has tiles
   int64_t q_stride;
   uint32_t pages, page_size, heads, batch, new_tokens, q_heads, max_pages, window;
   uint32_t group, rows;           // query heads of a key-value head; query rows of one: new_tokens * group
-  uint32_t row_tile, row_tiles;   // query rows of a unit, units of them
+  uint32_t row_tiles;             // units of kRows query rows
   uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
   FastDiv by_page, by_group, by_row_tiles, by_grid;
   float scale_log2;

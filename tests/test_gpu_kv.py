@@ -133,3 +133,22 @@ def test_python_refusals():
     for bad in (dict(dtype=torch.float16), dict(slots=slots.long()), dict(slots=slots.view(1, 3)), dict(out=(x, x[:2]))):
         with pytest.raises((ValueError, TypeError, mx.MxError)):
             mx.mx_kv_read(**(dict(cache=cache, slots=slots) | bad))
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 5 GB of keys and as many of values: its last pages written, read and attended over like those of a small one."""
+    heads, dim, ps, pages, tokens = 8, 128, 64, 80000, 150
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn(tokens, heads, dim, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(1, 2 * heads, dim, generator=g, device="cuda").bfloat16()
+    length = torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    small, large = mx.mx_kv_cache(3, ps, heads, dim, mx.MX_E4M3), mx.mx_kv_cache(pages, ps, heads, dim, mx.MX_E4M3)
+    assert large.k_elems.numel() > 1 << 32
+    got = []
+    for cache, table in ((small, [0, 1, 2]), (large, [pages - 1, pages // 2, pages - 3])):
+        table = torch.tensor([table], dtype=torch.int32, device="cuda")
+        slots = (table[0, :, None] * ps + torch.arange(ps, dtype=torch.int32, device="cuda")).view(-1)[:tokens].contiguous()
+        mx.mx_kv_append(cache, k, v, slots)
+        got.append((*mx.mx_kv_read(cache, slots), mx.mx_kv_attention(q, cache, table, length)))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert not large.k_elems[:pages // 2].any() and not large.v_scales[pages // 2 + 1:pages - 3].any()

@@ -55,6 +55,69 @@ def test_formats_and_rows(dim, fmt, dtype):
         _check(*_problem(lengths, heads, group, dim, ps, fmt, dtype, seed))
 
 
+def _wide(problem, tokens):
+    """The same with a table that could hold `tokens` tokens of each sequence: long enough for them to be split."""
+    q, cache, table, lengths = problem
+    more = -(-tokens // cache.k_elems.shape[2]) - table.shape[1]
+    return q, cache, torch.nn.functional.pad(table, (0, max(more, 0)), value=-1).contiguous(), lengths
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_split_sequences(dim, fmt, dtype):
+    """Few sequences, of which several blocks work on one; many, of which one block works on several."""
+    _check(*_wide(_problem([1, 0, 63, 64, 65, 700, 1500, 0], 2, 4, dim, 32, fmt, dtype, 11, new=3), 10000), window=0)
+    _check(*_wide(_problem([1500, 3, 900], 1, 11, dim, 24, fmt, dtype, 12), 10000), window=611)
+    _check(*_wide(_problem([(37 * i) % 300 for i in range(70)], 2, 2, dim, 16, fmt, dtype, 13), 10000))
+
+
+def test_long_sequences_of_one_head():
+    """More parts than a warp has lanes, for both results."""
+    for dtype, dim in ((torch.bfloat16, 128), (torch.float32, 64)):
+        _check(*_problem([70000], 1, 3, dim, 128, mx.MX_E4M3, dtype, 14))
+        _check(*_wide(_problem([20000, 5], 1, 8, dim, 48, mx.MX_E2M1, dtype, 15, new=2), 90000), window=15000)
+
+
+def test_tokens_that_lie_one_after_the_other():
+    """Whole tiles in a row in memory, across pages too, and tiles with a gap or a hidden page among them."""
+    for dim, fmt in ((64, mx.MX_E4M3), (128, mx.MX_E4M3), (256, mx.MX_INT8), (128, mx.MX_E2M1), (96, mx.MX_E5M2)):
+        for heads in (1, 2):
+            q, cache, table, lengths = _problem([400, 256, 130], heads, 4, dim, 16, fmt, torch.bfloat16, 16 + heads)
+            n = int((table >= 0).sum())
+            table[table >= 0] = torch.arange(n, dtype=torch.int32, device="cuda")
+            _check(q, cache, table, lengths)
+            table[0, 5] = -1
+            table[1, 3], table[1, 4] = int(table[1, 4]), int(table[1, 3])
+            _check(q, cache, table, lengths)
+
+
+def test_two_calls_with_a_workspace_of_their_own():
+    probs = [_wide(_problem([2000, 50], 2, 4, 64, 16, mx.MX_E4M3, torch.bfloat16, 30 + i), 30000) for i in range(2)]
+    want = [mx.mx_kv_attention(*p) for p in probs]
+    need = 1 << 25
+    spaces = [torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda") for _ in probs]
+    graphs = []
+    for p, ws in zip(probs, spaces):
+        mx.mx_kv_attention(*p, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = mx.mx_kv_attention(*p, workspace=ws)
+        graphs.append((g, out))
+    streams = [torch.cuda.Stream() for _ in probs]
+    for _ in range(4):
+        for (g, out), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                out.fill_(7)
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, w) for (_, out), w in zip(graphs, want))
+    # one workspace, one call after the other on a stream
+    a = [mx.mx_kv_attention(*probs[i % 2], workspace=spaces[0]) for i in range(4)]
+    assert all(torch.equal(o, want[i % 2]) for i, o in enumerate(a))
+
+
 @pytest.mark.parametrize("group", [1, 2, 3, 7, 8, 9, 15, 16, 17, 32, 33, 71])
 def test_groups(group):
     for dtype in (torch.bfloat16, torch.float32):
@@ -87,6 +150,11 @@ def test_lengths_beyond_the_table_and_below_zero():
     lengths[1] = -5
     _check(q, cache, table, lengths)
     _check(q, cache, table[:, :0].contiguous(), lengths)
+    # a cache without pages, tables short and long
+    empty = mx.mx_kv_cache(0, 16, 2, 64, mx.MX_E4M3)
+    for t in (table, torch.zeros((3, 4000), dtype=torch.int32, device="cuda")):
+        out, lse = mx.mx_kv_attention(q, empty, t, lengths, return_lse=True)
+        assert not out.any() and bool((lse == -math.inf).all())
 
 
 def test_pages_outside_the_cache_are_not_seen():
