@@ -17,6 +17,8 @@
 // O^T = V^T W^T with the row's elements on the M side.  W^T comes out of S^T's accumulators by 8 x 8 transposes
 // in registers.  The order of the elements within a block and of the tokens within a tile is free in these sums, and chosen
 // such that a lane's codes are consecutive bytes: no shuffling of codes but the pairing of neighbouring tokens' values.
+// (The tensor core's block-scaled instructions do not fit: a value's scale changes along the axis that is summed over, and the rows are 8.  The
+// plain FP8 form, mma of the codes as they are by queries in three E5M2 terms, runs at a fraction of the FP16 one's rate here: 110 -> 162 us.)
 // The warps of a block have their own tiles and their own asynchronous copies, kStages tiles deep, and meet only at the
 // end of a sequence.
 //
@@ -24,7 +26,14 @@
 // two or three blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
 // otherwise it leaves a part (its weighted mean and the log of its weight) and a second kernel joins the parts, in the
 // order of the tiles: results do not depend on timing.  Where the table holds few tokens a block takes one sequence and head as a whole, and
-// nothing is joined (one sequence of 333 tokens: 9.8 -> 6.5 us).
+// nothing is joined (one sequence of 333 tokens: 10.0 -> 7.6 us).
+//
+// What bounds it.  Large batches the cache's bytes: 64 sequences of up to 8192 tokens, 8 heads of 128 with 4 queries each, E4M3, 109 us (5.7 of
+// the 6.55 TB/s that a copy reaches; further sequences add theirs at 6.2), one of 131072 tokens 53 us.  What is left there: 2 us until the first tile, the
+// flush of a block's last sequence, 4 us of the join, and blocks that finish 10 % apart.  Below 30 us these fixed parts
+// count for more than the bytes.  Rows of 4 bits and groups of more than 8 queries: instructions (about 700 a tile of 32 tokens, of
+// which the conversion of the codes 160 and the weights 170, issued at 60 % of the rate): 4-bit rows reach 3.0 TB/s, 16 queries a
+// head 3.0.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -36,7 +45,7 @@
 namespace mx {
 namespace attn {
 
-constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234663852886e38f;  // the reference before any score
 constexpr float kRoom = 2.0f;                       // a moved m leaves the new maximum up to a factor 2^3 below it
 constexpr float kTop = 32768.0f;                    // weights stay at or below this
@@ -474,15 +483,16 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           }
       }
 
-      // weights without the values' scales: m moves when a score passes it
+      // Weights without the values' scales: m moves when a score passes it, once at most.  The score is rounded before m is taken from it, as it is
+      // where the largest is found: a fused difference could be above zero for a score that rounds to m, and m would not move.
       float y[TL][4];
-      for (bool moves = fresh;; moves = false) {
-        if (!moves) {
+      for (bool moved = false, move = fresh;; move = false) {
+        if (!move) {
           float most = -1.0f;
 #pragma unroll
           for (int x = 0; x < TL; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[x][i] = fmaf(p[x][i], qf[i & 1], -m[i & 1]);
+            for (int i = 0; i < 4; ++i) y[x][i] = __fsub_rn(__fmul_rn(p[x][i], qf[i & 1]), m[i & 1]);
           if (edge) {
 #pragma unroll
             for (int x = 0; x < TL; ++x)
@@ -494,8 +504,9 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           for (int x = 0; x < TL; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = fmaxf(most, y[x][i]);
-          if (!__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
+          if (moved || !__any_sync(0xFFFFFFFFu, most > 0.0f)) break;
         }
+        moved = true;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           float top = -INFINITY;
@@ -503,7 +514,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           for (int x = 0; x < TL; ++x)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][2 * h + j] * qf[j]);
+              if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, __fmul_rn(p[x][2 * h + j], qf[j]));
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
           const bool moves = top > m[j];
@@ -527,10 +538,10 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           l[i & 1] += p[x][i];
         }
 
-      // weights with the values' scales: F moves when one passes kTop
+      // weights with the values' scales: F moves when one passes kTop, once at most
       uint32_t w[W][B][TL][2];
-      for (bool moves = fresh;; moves = false) {
-        if (!moves) {
+      for (bool moved = false, move = fresh;; move = false) {
+        if (!move) {
           uint32_t most = 0;
 #pragma unroll
           for (int x = 0; x < TL; ++x) {
@@ -553,8 +564,9 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
               }
           }
           const float2 top2 = unpack_half(most);
-          if (!__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
+          if (moved || !__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
         }
+        moved = true;
         // F moves to where the largest is in [2^kAim, 2^(kAim + 1)), never up: a smaller F only costs small weights their digits
         float top[B][2];
 #pragma unroll

@@ -82,7 +82,7 @@ struct Args {
     s.first_tile = s.begin >> tile_log2;
     s.end = s.start + tiles(s.length);
   }
-  // The next segment that has units (there is one).
+  // The next segment that has units.  (There is one, unless somebody writes the lengths meanwhile: then one without tokens, without end.)
   __device__ __forceinline__ void next(Segment& s) const {
     const uint32_t n = s.end - s.start;
     s.start = s.end;
@@ -94,6 +94,11 @@ struct Args {
     s.hr = 0;
 #pragma unroll 1
     do {
+      if (s.b + 1 >= batch) {
+        s.end = 0xFFFFFFFFu;
+        s.length = 0;
+        return;
+      }
       ++s.b;
       fill(s, length(s.b));
     } while (s.end == s.start);
@@ -136,11 +141,11 @@ struct Args {
     const uint32_t who = __ffs(__ballot_sync(0xFFFFFFFFu, unit >= share.before && unit - share.before < share.mine)) - 1;
     uint32_t at = __shfl_sync(0xFFFFFFFFu, share.before, who);
     Segment s;
-    s.b = who;
+    s.b = min(who, batch - 1);
     uint32_t tokens = __shfl_sync(0xFFFFFFFFu, share.length, who);
     if (chunk > 1) {
 #pragma unroll 1
-      for (uint32_t b0 = who * chunk;; b0 += 32) {  // its sequences, 32 at a time
+      for (uint32_t b0 = who * chunk; b0 < batch; b0 += 32) {  // its sequences, 32 at a time
         const uint32_t b = b0 + lane;
         const uint32_t mine = b < min((who + 1) * chunk, batch) ? tiles(length(b)) * heads * row_tiles : 0, sum = scan(mine, lane);
         const uint32_t hit = __ballot_sync(0xFFFFFFFFu, unit - at < sum);
@@ -156,8 +161,8 @@ struct Args {
     if (chunk > 1) tokens = length(s.b);
     s.start = 0;
     fill(s, tokens);
-    const uint32_t n = s.end;
-    s.hr = (unit - at) / n;
+    const uint32_t n = max(s.end, 1u);
+    s.hr = min((unit - at) / n, heads * row_tiles - 1);
     s.start = at + s.hr * n;
     s.end = s.start + n;
     return s;

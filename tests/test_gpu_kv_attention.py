@@ -1,6 +1,7 @@
 """Attention of the newest tokens over the paged cache against its definition in 64 bits (bounds: kv_util.bounds)."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -239,6 +240,57 @@ def test_values_of_seen_tokens_differ_by_many_powers_of_two(dtype):
         cache.k_elems[p, 0, o, 0] = 0x00 if weight > 0 else 0x40
         cache.v_scales[p, 0, o, :2] = far
         _check(q, cache, table, lengths, scale=abs(weight) * math.log(2))
+
+
+def _scale_just_above(n, value):
+    """A scale whose product with log2 e in FP32, times `value`, is above the integer n by less than half a step of FP32 (so that it
+    rounds to n)."""
+    log2e = np.float32(1.4426950408889634)
+    s = np.float32(n / value / float(log2e))
+    for _ in range(50):
+        s = np.nextafter(s, np.float32(0))
+    for _ in range(100):
+        f = s * log2e
+        if float(f) * value > n and np.float32(f * np.float32(value)) == n:
+            return float(s)
+        s = np.nextafter(s, np.float32(np.inf))
+    return None
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_scores_that_round_to_the_reference(dtype):
+    """The reference of the running maximum is an integer (in powers of two).  Scores that exceed it by less than half a step
+    pass it or do not, but the kernel may not be of two minds about it."""
+    found = 0
+    for n in (8, 7, 9, 10):
+        # the first tiles' scores lie in (n - 3, n - 2], which puts the reference at n
+        for value, code, first in ((1.5, 0x3C, 0x38), (1.75, 0x3E, 0x3A), (1.25, 0x3A, 0x34), (1.375, 0x3B, 0x38)):
+            scale = _scale_just_above(n, value)
+            v0 = {0x38: 1.0, 0x3A: 1.25, 0x34: 0.75}[first]
+            if scale is None or not n - 3 < n / value * v0 <= n - 2:
+                continue
+            found += 1
+            q, cache, table, lengths = _problem([700], 1, 1, 64, 16, mx.MX_E4M3, dtype, 33)
+            q.zero_()
+            q[..., 0] = 1.0
+            cache.k_elems.zero_()
+            cache.k_scales.fill_(127)
+            for j in range(700):
+                cache.k_elems[int(table[0, j // 16]), 0, j % 16, 0] = first if j < 256 else code
+            _check(q, cache, table, lengths, scale=scale)
+            _check(*_wide((q, cache, table, lengths), 9000), scale=scale)
+    assert found
+
+
+def test_very_large_scores():
+    """Scores of 2^30 and more, whose steps are larger than one."""
+    for qs in (1e8, 1e12, 1e20):
+        q, cache, table, lengths = _problem([300, 20], 2, 4, 64, 16, mx.MX_E4M3, torch.float32, 34)
+        out, lse = mx.mx_kv_attention(q * qs, cache, table, lengths, return_lse=True)
+        want, wlse, _, size, _ = attention64(q * qs, cache, table, lengths, 0.125, 0)
+        assert bool(torch.isfinite(out).all()) and bool(((lse.double() - wlse).abs() <= (64 + 16) * 2.0 ** -23 * size + 2.0 ** -20).all())
+        # the scores lie so far apart that the largest takes all: its value, with a weight of 1 within the divisions' 2^-20
+        assert float((out.double() - want).abs().max()) <= 2.0 ** -20 * float(want.abs().max())
 
 
 def test_one_large_score():
