@@ -517,17 +517,21 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
               if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, __fmul_rn(p[x][2 * h + j], qf[j]));
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-          const bool moves = top > m[j];
-          const float next = moves ? ceilf(top) + kRoom : m[j], by = moves ? ex2(m[j] - next) : 1.0f;
+          const float next = top > m[j] ? ceilf(top) + kRoom : m[j], up = top > m[j] ? next - m[j] : 0.0f;
           m[j] = next;
-          l[j] *= by;
+          l[j] *= ex2(-up);
+          // F takes the move, as far as it can, so that what is summed keeps its size: a large value that a larger score has made
+          // small does not hold F down
 #pragma unroll
-          for (int b = 0; b < B; ++b)
+          for (int b = 0; b < B; ++b) {
+            const float want = (float)((int)(__float_as_uint(F[b][j]) >> 23) - 127) + up, have = fminf(want, 126.0f), by = ex2(have - want);
+            F[b][j] = __uint_as_float((uint32_t)((int)have + 127) << 23);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               acc[b][h][j] *= by;
               acc[b][h][2 + j] *= by;
             }
+          }
         }
       }
 #pragma unroll
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           if (moved || !__any_sync(0xFFFFFFFFu, fmaxf(top2.x, top2.y) > kTop)) break;
         }
         moved = true;
-        // F moves to where the largest is in [2^kAim, 2^(kAim + 1)), never up: a smaller F only costs small weights their digits
+        // F moves down to where the largest is in [2^kAim, 2^(kAim + 1)); up only with m
         float top[B][2];
 #pragma unroll
         for (int x = 0; x < TL; ++x)

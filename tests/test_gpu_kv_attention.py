@@ -242,6 +242,24 @@ def test_values_of_seen_tokens_differ_by_many_powers_of_two(dtype):
         _check(q, cache, table, lengths, scale=abs(weight) * math.log(2))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("first", [True, False])
+def test_a_large_value_that_a_larger_score_makes_small(first, dtype):
+    """Tokens of 2^60 times the others' values whose weights are 2^-90 of theirs, in the tiles before or behind them."""
+    q, cache, table, lengths = _problem([900], 1, 1, 128, 16, mx.MX_E4M3, dtype, 35)
+    q.zero_()
+    q[..., 0] = 1.0
+    cache.k_elems.zero_()
+    cache.k_scales.fill_(127)
+    for j in range(900):
+        large = (j < 450) == first
+        cache.k_elems[int(table[0, j // 16]), 0, j % 16, 0] = 0x00 if large else 0x38  # 0 or 1.0
+        cache.v_scales[int(table[0, j // 16]), 0, j % 16] = 160 if large else 100
+    for scale in (90 * math.log(2), 20 * math.log(2), 60 * math.log(2)):
+        _check(q, cache, table, lengths, scale=scale)
+        _check(*_wide((q, cache, table, lengths), 9000), scale=scale)
+
+
 def _scale_just_above(n, value):
     """A scale whose product with log2 e in FP32, times `value`, is above the integer n by less than half a step of FP32 (so that it
     rounds to n)."""
