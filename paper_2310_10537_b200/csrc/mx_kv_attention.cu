@@ -123,6 +123,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const Args a, 
 // Sequences of up to so many tiles are not split, more where there are blocks enough without: eight rounds of a block's warps take less than
 // a split and a second kernel (8 heads of 128, 16 sequences to 450 tokens 8.8 against 12.3 us, to 900 13.3 against 14.9, to 1800 21 against 17; 64
 // sequences to 900 24 against 32, to 1800 41 against 44, to 4000 78 against 67; 128 sequences to 1800 63 against 72, to 4000 121 against 124).
+// At most four times that: one long sequence among many short ones would keep its block long after all others.
 constexpr int64_t kWhole = 8 * kWarps;
 
 size_t workspace_bytes(int64_t dim) { return kCtas * (sizeof(Unfinished) + (size_t)2 * kRows * (size_t)(dim + 1) * 4); }
@@ -161,7 +162,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   // no more blocks than the longest sequences would employ; with few tiles a block for each segment
   const int64_t units = (int64_t)segments * tiles;
   uint32_t ctas = most < kCtas ? most : kCtas;
-  k.whole = tiles <= kWhole * (1 + segments / ctas);
+  k.whole = tiles <= kWhole * (segments / ctas < 3 ? 1 + segments / ctas : 4);
   if (units < (int64_t)ctas * kLeast) ctas = (uint32_t)((units + kLeast - 1) / kLeast);
   if (k.whole) ctas = segments;
   // Few sequences and heads may have many parts each: a block of the join for every row of each.  Many have few: blocks of four rows

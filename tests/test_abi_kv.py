@@ -83,6 +83,6 @@ def test_attention():
         ({1: _at(batch=-1)}, mx.MX_ERR_SHAPE), ({1: _at(new_tokens=0)}, mx.MX_ERR_SHAPE), ({1: _at(q_heads=3)}, mx.MX_ERR_SHAPE), ({1: _at(q_heads=0)}, mx.MX_ERR_SHAPE),
         ({1: _at(max_pages=-1)}, mx.MX_ERR_SHAPE), ({1: _at(window=-1)}, mx.MX_ERR_SHAPE), ({1: _at(scale=NAN)}, mx.MX_ERR_SHAPE), ({1: _at(scale=INF)}, mx.MX_ERR_SHAPE),
         ({1: _at(q_stride=255)}, mx.MX_ERR_SHAPE), ({1: _at(q_stride=1 << 50)}, mx.MX_ERR_SHAPE), ({1: _at(batch=1 << 40)}, mx.MX_ERR_SHAPE), ({1: _at(batch=1 << 30)}, mx.MX_ERR_UNSUPPORTED),
-        ({1: _at(max_pages=1 << 28)}, mx.MX_ERR_UNSUPPORTED), ({1: _at(batch=0, q_heads=1 << 40, q_stride=1 << 46)}, mx.MX_ERR_UNSUPPORTED),
+        ({1: _at(max_pages=1 << 28)}, mx.MX_ERR_UNSUPPORTED), ({1: _at(batch=1 << 14, max_pages=1 << 20)}, mx.MX_ERR_UNSUPPORTED), ({1: _at(batch=0, q_heads=1 << 40, q_stride=1 << 46)}, mx.MX_ERR_UNSUPPORTED),
         ({2: P + 8}, mx.MX_ERR_ALIGN), ({1: _at(q_stride=258)}, mx.MX_ERR_ALIGN), ({3: P + 2}, mx.MX_ERR_ALIGN), ({4: P + 1}, mx.MX_ERR_ALIGN), ({5: P + 4}, mx.MX_ERR_ALIGN),
         ({6: P + 2}, mx.MX_ERR_ALIGN), ({8: P + 16}, mx.MX_ERR_ALIGN), ({9: need - 1}, mx.MX_ERR_WORKSPACE), ({1: _at(batch=0), 2: None}, mx.MX_OK)])
