@@ -29,7 +29,7 @@ __device__ __forceinline__ size_t kv_row(const KvShape& s, uint32_t slot, uint32
   return ((size_t)page * s.heads + head) * s.page_size + (slot - page * s.page_size);
 }
 
-// Algorithm 1 of the rows of k and v.  A thread converts 8 elements of either, four neighbours a block; the scale bytes beyond the
+// Algorithm 1 of the rows of k and v.  A thread converts 16 elements of either, two neighbours a block; the scale bytes beyond the
 // row's blocks are written by the lane of the last block.
 template <int FMT, int ROUND, int DTYPE>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(
@@ -37,34 +37,42 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(
     uint8_t* k_scales, uint8_t* v_elems, uint8_t* v_scales, const int32_t* __restrict__ slots, uint32_t total, KvShape s) {
   pdl_prologue();
   const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-  const uint32_t at = i < total ? i : total - 1;  // (four lanes share a block: all of them stay)
+  const uint32_t at = i < total ? i : total - 1;  // (two lanes share a block: both of them stay)
   const uint32_t token = fastdiv(at, s.by_token), in_token = at - token * s.per_token;
-  const Raw8<DTYPE> raw[2] = {load_raw8<DTYPE>(k, (size_t)token * (size_t)k_stride + (size_t)in_token * 8),
-                              load_raw8<DTYPE>(v, (size_t)token * (size_t)v_stride + (size_t)in_token * 8)};
+  Raw8<DTYPE> raw[2][2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      raw[n][h] = load_raw8<DTYPE>(n ? v : k, (size_t)token * (size_t)(n ? v_stride : k_stride) + (size_t)in_token * 16 + 8 * h);
   const int64_t slot = slots[token];
   const uint32_t head = fastdiv(in_token, s.by_row), unit = in_token - head * s.units;
   const bool there = i < total && slot >= 0 && slot < s.slots;
   const size_t row = there ? kv_row(s, (uint32_t)slot, head) : 0;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    float x[8];
-    widen(raw[n], x);
-    float amax = absmax_nan(absmax_nan(absmax_nan(x[0], x[1]), absmax_nan(x[2], x[3])),
-                            absmax_nan(absmax_nan(x[4], x[5]), absmax_nan(x[6], x[7])));
-    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-    const BlockScale b = block_scale<FMT>(amax);
-    uint32_t lo, hi;
-    cast8<FMT, ROUND>(x, b, lo, hi);
+    float x[2][8], amax[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      widen(raw[n][h], x[h]);
+      amax[h] = absmax_nan(absmax_nan(absmax_nan(x[h][0], x[h][1]), absmax_nan(x[h][2], x[h][3])),
+                           absmax_nan(absmax_nan(x[h][4], x[h][5]), absmax_nan(x[h][6], x[h][7])));
+    }
+    amax[0] = absmax_nan(amax[0], amax[1]);
+    amax[0] = absmax_nan(amax[0], __shfl_xor_sync(0xFFFFFFFFu, amax[0], 1));
+    const BlockScale b = block_scale<FMT>(amax[0]);
+    uint32_t lo[2], hi[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) cast8<FMT, ROUND>(x[h], b, lo[h], hi[h]);
     if (!there) continue;
     uint8_t* codes = (n ? v_elems : k_elems) + row * s.code_bytes;
-    if (FmtTraits<FMT>::bits == 8) reinterpret_cast<uint2*>(codes)[unit] = make_uint2(lo, hi);
-    else reinterpret_cast<uint32_t*>(codes)[unit] = lo;
-    if (unit % 4 == 0) {
+    if (FmtTraits<FMT>::bits == 8) reinterpret_cast<uint4*>(codes)[unit] = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+    else reinterpret_cast<uint2*>(codes)[unit] = make_uint2(lo[0], lo[1]);
+    if (unit % 2 == 0) {
       uint8_t* scales = (n ? v_scales : k_scales) + row * s.scale_bytes;
-      scales[unit / 4] = (uint8_t)b.byte;
-      if (unit + 4 == s.units)
-        for (uint32_t j = unit / 4 + 1; j < s.scale_bytes; ++j) scales[j] = 0;
+      scales[unit / 2] = (uint8_t)b.byte;
+      if (unit + 2 == s.units)
+        for (uint32_t j = unit / 2 + 1; j < s.scale_bytes; ++j) scales[j] = 0;
     }
   }
 }
@@ -168,8 +176,8 @@ cudaError_t read_by_dtype(const KvMoveArgs& a, const KvShape& s, uint32_t total)
 }  // namespace
 
 cudaError_t launch_kv_append(const KvMoveArgs& a) {
-  const KvShape s = shape_of(a.kv, 8);
-  const uint32_t total = (uint32_t)(a.tokens * a.kv.heads * (a.kv.dim / 8));  // below 2^31
+  const KvShape s = shape_of(a.kv, 16);
+  const uint32_t total = (uint32_t)(a.tokens * a.kv.heads * (a.kv.dim / 16));  // below 2^31
   switch (a.kv.fmt) {
     case MX_E4M3: return append_by_rounding<MX_E4M3>(a, s, total);
     case MX_E5M2: return append_by_rounding<MX_E5M2>(a, s, total);
