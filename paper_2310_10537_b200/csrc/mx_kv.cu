@@ -121,16 +121,25 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const float X = __uint_as_float(sb[n] == 0 ? 0x00400000u : (sb[n] == 255 ? 0x7FC00000u : sb[n] << 23));  // 2^-127, NaN
+    float x[2][8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x[8];
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 p = decode2<FMT>(kWords == 4 ? w[n][(2 * h + j / 2) % kWords] >> 16 * (j & 1) : (w[n][h] >> 8 * j) & 0xFFu);
-        x[2 * j] = p.x * X;
-        x[2 * j + 1] = p.y * X;
+        x[h][2 * j] = p.x * X;
+        x[h][2 * j + 1] = p.y * X;
       }
-      store8<DTYPE>(n ? v_out : k_out, (size_t)i * 16 + 8 * h, x);
+    void* out = n ? v_out : k_out;
+    uint16_t* at = (uint16_t*)out + (size_t)i * 16;
+    if (DTYPE == MX_BF16 && ((uintptr_t)at & 31u) == 0) {  // a whole sector: two stores would each write half of every one
+      uint32_t o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = pack_bf16(x[j / 4][2 * (j % 4)], x[j / 4][2 * (j % 4) + 1]);
+      st_32(at, o);
+    } else {
+      store8<DTYPE>(out, (size_t)i * 16, x[0]);
+      store8<DTYPE>(out, (size_t)i * 16 + 8, x[1]);
     }
   }
 }

@@ -74,6 +74,10 @@ def test_read_gives_the_values(fmt, dtype):
         if tokens > 2:
             slots[0] = slots[2]  # the same slot twice is fine here
         k, v = mx.mx_kv_read(cache, slots, dtype)
+        # results that begin in the middle of a 32-byte sector
+        odd = [torch.empty(k.numel() + 16 // k.element_size(), dtype=dtype, device="cuda")[16 // k.element_size():].view(k.shape) for _ in range(2)]
+        assert mx.mx_kv_read(cache, slots, dtype, out=tuple(odd)) is not None
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(odd, (k, v)))
         assert k.shape == v.shape == (tokens, heads, dim) and k.dtype == v.dtype == dtype
         ok = (slots >= 0) & (slots < pages * ps)
         page, off = slots[ok].long() // ps, slots[ok].long() % ps
