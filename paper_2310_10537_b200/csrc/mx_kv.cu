@@ -2,9 +2,10 @@
 // back as numbers (see mx_kv_t in mx.h).
 //
 // Both are streams: append reads 2 or 4 bytes and writes bits / 8 + 1 / 32 per element, read does the
-// reverse.  A thread moves a key's and a value's units at once, so that what finding a slot's row costs (a division and a few
-// multiplications) is paid once for both: 8192 tokens of 8 heads of 128, BF16 to E4M3, 11.7 -> 9.7 us (5.2 of the 6.55 TB/s that a copy
-// reaches), 16384 tokens back to BF16 24 -> 21 (4.9).  Two units of each a thread were no faster.
+// reverse.  A thread moves 16 elements of a key and of a value, so that what finding a slot's row costs (a division and a few
+// multiplications) is paid once for both, and every store is whole sectors: 8192 tokens of 8 heads of 128, BF16 to E4M3, 11.7 us with 8
+// elements of either, 9.7 with 8 of both, 7.3 so (inputs that change from call to call: 9.4, 5.4 of the 6.55 TB/s that a copy reaches);
+// 16384 tokens back to BF16 24, 21 with half sectors, 13.4 (17.8, 5.7 TB/s).  A whole block a thread: 22.
 #include <cuda_fp16.h>
 
 #include "mx_device.cuh"
