@@ -59,6 +59,7 @@ template <int FMT, int DIM, bool WIDE>
 struct Cfg {
   static constexpr int kResident = blocks_per_sm(DIM, WIDE);
   static constexpr int kBits = FmtTraits<FMT>::bits;
+  static constexpr bool kOdd = FMT == MX_E4M3 || FMT == MX_E5M2;  // formats with codes of NaN or Inf
   static constexpr int kBlocks = DIM / 32;
   static constexpr int kRow = DIM * kBits / 8;             // bytes of a row's codes
   static constexpr int kGroup = 4 * kBits;                 // bytes of a block's codes
@@ -72,7 +73,8 @@ struct Cfg {
   static constexpr int kCopies = kTokens * kUnits / 32;    // of these a lane copies
   static constexpr int kCodes = kTokens * kPitch;
   static constexpr int kStage = 2 * kCodes + 2 * kTokens * kScale + 128;  // codes, scales, the mask of seen tokens
-  static constexpr int kJoin = kWarps * 8 * kJoinPitch * 4 + 2 * kWarps * 16 * 4;
+  static constexpr int kNotes = kOdd ? 8 * DIM / 16 * 4 : 0;  // odd elements of values, two bits a row and element
+  static constexpr int kJoin = kWarps * 8 * kJoinPitch * 4 + 2 * kWarps * 16 * 4 + kNotes;
   static constexpr int kFit = (kSharedOfSm / kResident - 1024 - kJoin) / (kWarps * kStage);
   static constexpr int kStages = kFit < 4 ? kFit : 4;
   static constexpr int kShared = kWarps * kStages * kStage + kJoin;
@@ -163,6 +165,12 @@ __device__ __forceinline__ uint32_t half_pair(uint32_t w, int pair) {
   return h;
 }
 
+// The upper bit of every byte of four FP8 codes that is NaN or Inf: E4M3 0x7F, E5M2 0x7C .. 0x7F, of either sign.
+template <int FMT>
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w) {
+  return ((w & 0x7F7F7F7Fu) + (FMT == MX_E4M3 ? 0x01010101u : 0x04040404u)) & 0x80808080u;
+}
+
 // Byte offset of a row (0 .. kTokens - 1) in a tile's codes, its 16-byte units permuted such that the four or eight rows that a
 // warp reads at a time lie in different banks; byte x of the row is at offset ^ x (+ 128 for the second line of a row of 256).
 template <class C>
@@ -192,14 +200,52 @@ __device__ __forceinline__ uint32_t lds4(uint32_t a) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
 __device__ __forceinline__ uint32_t lds2(uint32_t a) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
   return v;
 }
 
-// The instance for rows of DIM elements in format FMT; WIDE: FP32 queries and results.
+// NaN and Inf codes among a tile's values that some rows see and others do not, those of its tokens 0 .. head - 1 and tail .. end - 1, become 0
+// in the tile, and are noted for each row and element that sees them: two bits in odd[row * DIM / 16 + element / 16], 1 for Inf, 2 for -Inf,
+// 3 for NaN (or both infinities).  Codes of tokens that are not there are 0.  (Where the two ranges meet, what is done twice does no harm.)
 template <int FMT, int DIM, bool WIDE>
+__device__ __forceinline__ void take_out_odd(const Args& a, uint32_t codes, uint32_t* odd, int head, int tail, int end, int j0, uint32_t group0, int length,
+                                             uint32_t lane) {
+  using C = Cfg<FMT, DIM, WIDE>;
+#pragma unroll 1
+  for (int n = (int)lane; n < (head + end - tail) * C::kUnits; n += 32) {
+    const int m = n / C::kUnits;
+    const uint32_t k = (uint32_t)(m < head ? m : tail + m - head), u = (uint32_t)n % C::kUnits;
+    const uint32_t at = codes + (row_at<C>(k) ^ ((u & 7) << 4)) + (u >> 3) * 128;
+    const uint4 v = lds16(at);
+    if ((odd_codes<FMT>(v.x) | odd_codes<FMT>(v.y) | odd_codes<FMT>(v.z) | odd_codes<FMT>(v.w)) == 0) continue;
+#pragma unroll 1
+    for (uint32_t w = 0; w < 4; ++w) {
+      const uint32_t c = lds4(at + 4 * w);
+#pragma unroll 1
+      for (uint32_t mask = odd_codes<FMT>(c); mask; mask &= mask - 1) {
+        const uint32_t e = (__ffs(mask) - 1) / 8, code = c >> 8 * e & 0xFFu;
+        const uint32_t bits = FMT == MX_E5M2 && (code & 0x7Fu) == 0x7Cu ? (code & 0x80u ? 2 : 1) : 3;
+#pragma unroll 1
+        for (uint32_t r = 0; r < 8 && group0 + r < a.rows; ++r) {
+          const int hi = length - (int)(a.new_tokens - 1 - fastdiv(group0 + r, a.by_group)), j = j0 + (int)k;
+          if (j < hi && (a.window == 0 || j >= hi - (int)a.window)) atomicOr(odd + r * (DIM / 16) + u, bits << 2 * (4 * w + e));
+        }
+      }
+      asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 4 * w), "r"(c & ~((odd_codes<FMT>(c) >> 7) * 0xFFu)) : "memory");
+    }
+  }
+}
+
+// The instance for rows of DIM elements in format FMT; WIDE: FP32 queries and results; NOTES: several new tokens, which see different tokens, of a
+// format with NaN and Inf codes (an instance of its own: what it does beside the rest costs 1 to 3 % also where a condition keeps it from running).
+template <int FMT, int DIM, bool WIDE, bool NOTES>
 __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_attention_kernel(const Args a) {
   using C = Cfg<FMT, DIM, WIDE>;
   constexpr int B = C::kBlocks, TL = C::kTiles, W = WIDE ? 2 : 1;
@@ -208,6 +254,11 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (C::kStages * C::kStage);
   float* join = reinterpret_cast<float*>(smem + kWarps * C::kStages * C::kStage);  // [kWarps][8][kJoinPitch]
   float2* join_ml = reinterpret_cast<float2*>(join + kWarps * 8 * kJoinPitch);     // [kWarps][16]
+  uint32_t* odd = reinterpret_cast<uint32_t*>(join_ml + kWarps * 16);              // [8][DIM / 16] (see take_out_odd)
+  if (NOTES) {
+    for (uint32_t i = threadIdx.x; i < DIM / 2; i += kWarps * 32) odd[i] = 0;
+    __syncthreads();
+  }
 
   // The lengths come from the kernels before this one.  The join may be scheduled only after this point, so that it, too,
   // finds them written.
@@ -474,6 +525,13 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
       }
       uint32_t hidden = 0;  // bit: this score is of a token that the row does not see
       if (edge) {
+        // A weight of zero does not keep a NaN or Inf code of a value out of the product.  Those of tokens that some rows see and others do
+        // not, the oldest and the newest ones, are taken out and noted.  (What is hidden from all is not copied.)
+        if (NOTES) {
+          const int end = min((int)s.length - j0, C::kTokens);
+          take_out_odd<FMT, DIM, WIDE>(a, stage + C::kCodes, odd, min(max(all_lo - j0, 0), end), min(max(all_hi - j0, 0), end), end, j0, group0, (int)s.length, lane);
+          __syncwarp();
+        }
 #pragma unroll
         for (int x = 0; x < TL; ++x)
 #pragma unroll
@@ -730,6 +788,14 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
         v.x += u.x;
         v.y += u.y;
       }
+      if (NOTES) {
+        const uint32_t bits = odd[out_row * (DIM / 16) + b * 2 + out_at / 16] >> out_at % 16 * 2;
+        const float inf = INFINITY;
+        if (bits & 1) v.x += inf;
+        if (bits & 2) v.x -= inf;
+        if (bits & 4) v.y += inf;
+        if (bits & 8) v.y -= inf;
+      }
       if (r < a.rows) {
         if (!whole) *reinterpret_cast<float2*>(a.parts + part * DIM + b * 32 + out_at) = v;
         else if (WIDE) *reinterpret_cast<float2*>((float*)a.out + row * DIM + b * 32 + out_at) = v;
@@ -743,6 +809,10 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
       a.unfinished[a.by_segment ? s.b * a.heads * a.row_tiles + s.hr : blockIdx.x] = {s.b, s.hr, parts, blockIdx.x};
     }
     if (s.end >= last) break;
+    if (NOTES) {  // (all have read them: the barrier above)
+      for (uint32_t i = threadIdx.x; i < DIM / 2; i += kWarps * 32) odd[i] = 0;
+      __syncthreads();
+    }
     a.next(s);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -751,7 +821,10 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
 template <int FMT, int DIM, bool WIDE>
 cudaError_t launch_instance(const Args& a, uint32_t ctas, cudaStream_t stream) {
   using C = Cfg<FMT, DIM, WIDE>;
-  auto kernel = kv_attention_kernel<FMT, DIM, WIDE>;
+  auto kernel = kv_attention_kernel<FMT, DIM, WIDE, false>;
+  if constexpr (C::kOdd) {
+    if (a.new_tokens > 1) kernel = kv_attention_kernel<FMT, DIM, WIDE, true>;
+  }
   // (a function attribute per device: set on every call, it costs less than a microsecond)
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kShared);
   if (e != cudaSuccess) return e;
