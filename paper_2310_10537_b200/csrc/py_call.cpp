@@ -438,9 +438,8 @@ int64_t token_stride(const at::Tensor& t, const char* name, int dev, c10::Scalar
     fail(PyExc_ValueError, std::string(name) + " has to be " + c10::toString(dtype) + " [.., " + std::to_string(heads) + ", " +
                                std::to_string(dim) + "], not " + describe(t.scalar_type(), t.sizes()));
   const bool rows = (dim < 2 || t.stride(n - 1) == 1) && (heads < 2 || t.stride(n - 2) == dim);
-  const bool lead = n < 4 || t.size(0) < 2 || t.size(1) == 0 || t.stride(0) == t.size(1) * t.stride(1);
+  const bool lead = n < 4 || t.size(0) < 2 || t.size(1) < 2 || t.stride(0) == t.size(1) * t.stride(1);  // (of one token stride(1) says nothing)
   if (!rows || !lead) fail(PyExc_ValueError, std::string(name) + " has to have contiguous heads and evenly spaced tokens");
-  // of a single token the stride says nothing
   if (n == 4 && t.size(1) < 2) return t.size(0) < 2 ? heads * dim : t.stride(0);
   return t.size(n - 3) < 2 ? heads * dim : t.stride(n - 3);
 }
