@@ -1,5 +1,7 @@
 // mx_kv_attention: its workspace, the choice of an instance, and the kernel that joins the parts of sequences that more than one
 // block worked on (the attention itself: mx_kv_attention.cuh).
+#include <math.h>
+
 #include "mx_kv_attention_args.h"
 #include "mx_launch.h"
 #include "mx_rows.cuh"
@@ -153,7 +155,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a) {
   k.row_tiles = (k.rows + kRows - 1) / kRows;
   k.chunk = (k.batch + 31) / 32;
   k.by_page = make_fastdiv(k.page_size); k.by_group = make_fastdiv(k.group); k.by_row_tiles = make_fastdiv(k.row_tiles);
-  k.scale_log2 = a.scale * 1.4426950408889634f;
+  k.scale_mant = frexpf(a.scale, &k.scale_exp) * 1.4426950408889634f;  // (the product itself may be out of range)
   k.unfinished = (Unfinished*)a.workspace;
   k.parts = (float*)(k.unfinished + kCtas);
   k.part_lse = k.parts + (size_t)2 * kCtas * kRows * (size_t)a.kv.dim;

@@ -1,25 +1,29 @@
 // Attention of the newest tokens over a paged cache of MX rows (see mx_kv_attention in mx.h).
 //
 // Mathematics.  For the query rows r of one sequence that share a key-value head, with s in units of log2 e,
-//   s[j, r] = qf[r] * sum_b KX[j, b] * (sum_{d in block b} KP[j, d] * q'[r, d])        q = q' * a power of two
+//   s[j, r] = sum_b KX[j, b] * c[r, b] * (sum_{d in block b} KP[j, d] * q'[r, d])        scale * q = c[r, b] * q'
 //   out[r, d] = sum_j 2^{s[j, r]} VX[j, b(d)] VP[j, d] / sum_j 2^{s[j, r]}
 // Both inner sums are tensor-core products of FP16 operands with FP32 accumulators: codes of every format are exact in
-// FP16 (INT8 as the integer), queries are scaled by a power of two into its range.  A key's block scale multiplies the
-// FP32 sum of its block.  A value's scale depends on the token, the axis that its product sums over, so it joins the
+// FP16 (INT8 as the integer), queries are scaled into its range by a power of two for each row and block, so that a block whose queries are
+// small and whose keys are large counts like any other.  Its factor c (from shared memory, two rows in one multiplication) comes before the key's
+// block scale: the products stay in FP32's range where the score does.  (One power for a row, applied after the sum, lost such blocks
+// and overflowed; the factors cost 64 sequences to 8192 1 %.)  A value's scale depends on the token, the axis that its product sums over, so it joins the
 // softmax weight: w[j, r, b] = 2^{s - m[r]} VX[j, b] F[r, b], with the reference m[r] of a row's scores and a power of two F[r, b]
 // that holds the row's largest w of the block so far in FP16's range.  A row's m, and a row and block's F, move only when a tile breaks their own
 // bound (looked at after a vote of the warp), and what has been summed moves with them: no row depends on what else its tile of rows holds.
 // (F's room goes up to FP16's largest number: with a bound of 2^15 rows of 256 elements took 227 us for 217, 4-bit ones 86 for 82.)
 // Rounded to FP16: w, half a step 2^-11 of a weight (BF16 results, whose own rounding is 2^-8), or two FP16 terms, 2^-22 (FP32
-// results; the queries too).  Scores, maxima, sums and accumulators are FP32.
+// results; the queries too).  BF16 queries are exact down to 2^-31 of their block's largest element, and off by 2^-39 of that below; FP32 ones
+// by 2^-22 of themselves or 2^-50 of that.  Scores, maxima, sums and accumulators are FP32.
 //
 // Layout.  A warp takes kTokens tokens at a time: S^T = K Q^T has the tokens on the M side of the MMA and the query rows
 // on its N side, 8 of them (a group of 4 query heads wastes half of 8, not three quarters of 16), then
 // O^T = V^T W^T with the row's elements on the M side.  W^T comes out of S^T's accumulators by 8 x 8 transposes
 // in registers.  The order of the elements within a block and of the tokens within a tile is free in these sums, and chosen
 // such that a lane's codes are consecutive bytes: no shuffling of codes but the pairing of neighbouring tokens' values.
-// (The tensor core's block-scaled instructions do not fit: a value's scale changes along the axis that is summed over, and the rows are 8.  The
-// plain FP8 form, mma of the codes as they are by queries in three E5M2 terms, runs at a fraction of the FP16 one's rate here: 110 -> 162 us.)
+// (The tensor core's block-scaled instructions do not fit the values, whose scales change along the axis that is summed over.  They would fit the
+// scores, with queries in several terms of 8 bits; that is not tried.  The plain FP8 form, mma.sync of the codes as they are by queries in three E5M2
+// terms, runs at a fraction of the FP16 one's rate here: 110 -> 162 us.)
 // The warps of a block have their own tiles and their own asynchronous copies, kStages tiles deep, and meet only at the
 // end of a sequence.
 //
@@ -54,6 +58,9 @@ constexpr float kPast = 65520.0f;                   // .. to which it rounds wha
 constexpr int kAim = 12;                            // log2 of the largest weight after F has moved
 constexpr float kMost = 8.507059173023462e37f;      // 2^126, F's largest value
 
+constexpr uint32_t kOneByLower = 0x3A000000u;       // 2^-11
+constexpr float kLower = 2048.0f;                   // of a query's second FP16 term, which would else be among FP16's smallest numbers
+
 // Shape of a kernel instance.
 constexpr int kSharedOfSm = 228 * 1024;
 constexpr int kJoinPitch = 36;  // words of a block of 32 elements in the buffer that joins the warps: rows 2 t in different banks
@@ -85,6 +92,13 @@ struct Cfg {
   static constexpr float kUnit = FMT == MX_INT8 ? 0.015625f : 1.0f;
 };
 
+// 2^n for -149 <= n <= 127, 0 below.
+__device__ __forceinline__ float pow2(int n) {
+  return __uint_as_float(n >= -126 ? (uint32_t)(127 + n) << 23 : n >= -149 ? 1u << (149 + n) : 0u);
+}
+// The power of two that a block with the largest magnitude `bits` (not 0) is divided by, which puts that in [2^14, 2^15): -127 .. 113 (Inf and NaN: 114).
+// (Below 2^-113 it stays smaller: FP32's smallest numbers are whole multiples of FP16's then.)
+__device__ __forceinline__ int block_exp(uint32_t bits) { return max((int)(bits >> 23), 14) - 141; }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -99,6 +113,10 @@ __device__ __forceinline__ float lg2(float x) {
   float y;
   asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+__device__ __forceinline__ void mul2(float& x, float& y, const uint2& by) {  // in one instruction
+  asm("{ .reg .b64 a, b; mov.b64 a, {%0, %1}; mov.b64 b, {%2, %3}; mul.rn.f32x2 a, a, b; mov.b64 {%0, %1}, a; }"
+      : "+f"(x), "+f"(y) : "r"(by.x), "r"(by.y));
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   uint32_t d;
@@ -267,6 +285,12 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
+  // Powers of two of this warp's queries by block and row, in its part of the buffer that joins the warps (in use only between two
+  // sequences): [B][8], of which a lane reads rows 2 t, 2 t + 1.
+  float* q_by = join + warp * 8 * kJoinPitch;
+  const int scale_exp = a.scale_exp + (FMT == MX_INT8 ? -6 : 0);  // (the integer n of an INT8 code stands for n / 64)
+  const uint32_t q_by_at = (uint32_t)__cvta_generic_to_shared(q_by) + t * 8;
+
   Share share;
   Segment s;
   uint32_t first = 0, last;  // this block's tiles are first .. last - 1
@@ -398,7 +422,6 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
     const uint32_t seg_end = min(s.end, last);
     const uint32_t group0 = s.row_tile(a) * 8;  // first query row of this tile of rows
     uint32_t q[W][B][2][2];
-    float qf[2];
     int lo[2], hi[2];  // tokens that the lane's rows 2 t, 2 t + 1 see
     Raw8<WIDE ? MX_F32 : MX_BF16> raw[B];
     const uint32_t q_row = group0 + g, q_token = fastdiv(q_row, a.by_group), q_head = s.head(a) * a.group + (q_row - q_token * a.group);
@@ -410,39 +433,53 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
     }
 #pragma unroll 1
     for (; ahead > 0; --ahead) copy_tile();  // (the first copies are under way while the queries are prepared)
-    float x[B][8], amax = 0.0f;
+    float x[B][8];
+    uint32_t ab[B];     // largest magnitude of a block, its bits
+    int most = -1024;   // largest power of two in a factor of the row
 #pragma unroll
-    for (int b = 0; b < B; ++b) widen(raw[b], x[b]);
-#pragma unroll
-    for (int b = 0; b < B; ++b)
+    for (int b = 0; b < B; ++b) {
+      widen(raw[b], x[b]);
+      float amax = 0.0f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) amax = absmax_nan(amax, x[b][j]);
-    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-    amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-    // q' = q * 2^-e with the largest element in [2^7, 2^8): FP16 then holds what is 2^-22 of it to full precision.
-    // Inf or NaN make the row NaN.
-    const uint32_t ab = __float_as_uint(amax) & 0x7FFFFFFFu;
-    const int e = ab == 0 ? 0 : (int)(ab >> 23) - 134;  // -134 .. 120
-    const float half1 = ab >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - e / 2) << 23);
-    const float half2 = __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+      amax = absmax_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+      ab[b] = __float_as_uint(amax) & 0x7FFFFFFFu;
+      if (ab[b]) most = max(most, block_exp(ab[b]) + scale_exp);
+    }
+    // Products by a factor of 2^60 or less, and not much less, leave the range of FP32 only where the score does.
+    const int rest = most > 60 ? min(most - 60, 127) : most < -60 && most > -1024 ? max(most + 60, -126) : 0;
+    // q' = q * 2^-e with a block's largest element in [2^14, 2^15): FP16 then holds what is 2^-28 of it to full precision.  Inf or NaN make
+    // the row NaN.
 #pragma unroll
-    for (int b = 0; b < B; ++b)
+    for (int b = 0; b < B; ++b) {
+      const int e = ab[b] ? block_exp(ab[b]) : 0;
+      const float into = ab[b] >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float u = x[b][4 * k + 2 * j] * half1 * half2, v = x[b][4 * k + 2 * j + 1] * half1 * half2;
+          const float u = x[b][4 * k + 2 * j] * into, v = x[b][4 * k + 2 * j + 1] * into;
           q[0][b][k][j] = pack_half(u, v);
           if (WIDE) {
             const float2 h = unpack_half(q[0][b][k][j]);
-            q[W - 1][b][k][j] = pack_half(u - h.x, v - h.y);
+            q[W - 1][b][k][j] = pack_half((u - h.x) * kLower, (v - h.y) * kLower);
           }
         }
-    // (1 / half is a power of two as well)
-    const float f = a.scale_log2 * C::kUnit * __uint_as_float((uint32_t)(127 + (e - e / 2)) << 23) * __uint_as_float((uint32_t)(127 + e / 2) << 23);
+    }
+#pragma unroll
+    for (int b0 = 0; b0 < B; b0 += 4) {  // the factors of four blocks, one of them a lane
+      uint32_t bits = ab[b0];
+#pragma unroll
+      for (int b = b0 + 1; b < b0 + 4 && b < B; ++b) bits = t == b - b0 ? ab[b] : bits;
+      const float by = a.scale_mant * pow2(min((bits ? block_exp(bits) : 0) + scale_exp - rest, 127));
+      if (b0 + t < B) q_by[(b0 + t) * 8 + g] = by;
+    }
+    if (t == 0) q_by[B * 8 + g] = pow2(rest);
+    const bool extreme = __any_sync(0xFFFFFFFFu, rest != 0);
+    __syncwarp();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      qf[j] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + j) * 4);
       const uint32_t row = group0 + 2 * t + j;
       const int i = row < a.rows ? (int)fastdiv(row, a.by_group) : (int)a.new_tokens - 1;
       hi[j] = (int)s.length - ((int)a.new_tokens - 1 - i);
@@ -487,7 +524,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
         edge = edge || seen[i] != 0xFFFFFFFFu;
       }
 
-      // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1, without the rows' factors
+      // scores of tokens 16 x + g, 16 x + g + 8 for rows 2 t, 2 t + 1
       float p[TL][4];
 #pragma unroll
       for (int x = 0; x < TL; ++x) {
@@ -518,11 +555,28 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           }
           float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int w = W - 1; w >= 0; --w)
+          for (int w = W - 1; w >= 0; --w) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) mma(d, ka[k], q[w][b][k][0], q[w][b][k][1]);
+            if (w > 0) {
+              const uint2 lower = make_uint2(kOneByLower, kOneByLower);
+              mul2(d[0], d[1], lower);
+              mul2(d[2], d[3], lower);
+            }
+          }
+          const uint2 by = lds8(q_by_at + b * 32);
+          mul2(d[0], d[1], by);
+          mul2(d[2], d[3], by);
 #pragma unroll
           for (int i = 0; i < 4; ++i) p[x][i] = fmaf(d[i], ks[i >> 1][b], p[x][i]);
+        }
+      }
+      if (extreme) {
+        const uint2 by = lds8(q_by_at + B * 32);
+#pragma unroll
+        for (int x = 0; x < TL; ++x) {
+          mul2(p[x][0], p[x][1], by);
+          mul2(p[x][2], p[x][3], by);
         }
       }
       uint32_t hidden = 0;  // bit: this score is of a token that the row does not see
@@ -543,8 +597,8 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           }
       }
 
-      // Weights without the values' scales: m moves when a score passes it, once at most.  The score is rounded before m is taken from it, as it is
-      // where the largest is found: a fused difference could be above zero for a score that rounds to m, and m would not move.
+      // Weights without the values' scales: m moves when a score passes it, once at most.  (The scores are rounded numbers here, the same ones as
+      // where the largest is found: nothing can be above m in one place and not in the other.)
       float y[TL][4];
       for (bool moved = false, move = fresh;; move = false) {
         if (!move) {
@@ -552,7 +606,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
 #pragma unroll
           for (int x = 0; x < TL; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[x][i] = __fsub_rn(__fmul_rn(p[x][i], qf[i & 1]), m[i & 1]);
+            for (int i = 0; i < 4; ++i) y[x][i] = p[x][i] - m[i & 1];
           if (edge) {
 #pragma unroll
             for (int x = 0; x < TL; ++x)
@@ -574,7 +628,7 @@ __global__ void __launch_bounds__(kWarps * 32, blocks_per_sm(DIM, WIDE)) kv_atte
           for (int x = 0; x < TL; ++x)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, __fmul_rn(p[x][2 * h + j], qf[j]));
+              if (!(hidden >> (x * 4 + 2 * h + j) & 1)) top = fmaxf(top, p[x][2 * h + j]);
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
           const float next = top > m[j] ? ceilf(top) + kRoom : m[j], up = top > m[j] ? next - m[j] : 0.0f;

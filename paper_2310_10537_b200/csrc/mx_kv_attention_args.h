@@ -56,7 +56,8 @@ struct Args {
   uint32_t row_tiles;             // units of kRows query rows
   uint32_t tile_log2, chunk;      // log2 of a tile's tokens; sequences of a lane
   FastDiv by_page, by_group, by_row_tiles, by_grid;
-  float scale_log2;
+  float scale_mant;               // scale * log2 e = scale_mant * 2^scale_exp
+  int scale_exp;
   bool by_segment, whole;         // whole: block i takes the i-th sequence, head and tile of rows as a whole
 
   __device__ __forceinline__ uint32_t length(uint32_t b) const {
