@@ -604,10 +604,10 @@ class KvCache(NamedTuple):
 
 
 def mx_kv_cache(pages: int, page_size: int, heads: int, dim: int, fmt: int, device="cuda") -> KvCache:
-    """An empty cache (all bytes zero) for ``pages`` pages of ``page_size`` tokens."""
-    desc = mx_kv_t(None, None, None, None, pages, page_size, heads, dim, fmt)
-    rows = pages * heads * page_size
-    if rows and not _lib.mx_kv_elems_bytes(ctypes.byref(desc)):
+    """An empty cache (all bytes zero) for ``pages`` pages of ``page_size`` tokens: ``dim`` a multiple of 32, ``fmt`` of 8 or 4 bits.
+    (:func:`mx_kv_attention` takes ``dim`` 64, 96, 128, 192 and 256.)"""
+    desc = mx_kv_t(None, None, None, None, pages or 1, page_size, heads, dim, fmt)  # (none at all: what a page would have to be)
+    if not _lib.mx_kv_elems_bytes(ctypes.byref(desc)):
         raise ValueError(f"no cache of {pages} pages x {heads} heads x {page_size} tokens x {dim} in format {fmt}")
     code, scale = dim * mx_fmt_bits(fmt) // 8, (dim + 127) // 128 * 4
     zeros = lambda n: torch.zeros((pages, heads, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
