@@ -633,7 +633,7 @@ def mx_kv_attention(q: torch.Tensor, cache: KvCache, table: torch.Tensor, length
     """Attention of the newest tokens ``q`` [batch, heads, dim], or [batch, new tokens, heads, dim], over the cached
     tokens of their sequences: sequence b has ``lengths[b]`` tokens (the new ones included) in the pages ``table[b]``
     (int32 [batch, pages of a sequence]).  ``scale`` defaults to dim ** -0.5; ``window`` > 0: a query sees its last
-    ``window`` tokens only.  Returns out, shaped as q, or (out, lse)."""
+    ``window`` tokens only.  Returns out, shaped as q, or (out, lse); an ``out`` given must not share memory with q."""
     return _py_call.kv_attention(q, cache, table, lengths, scale, window, return_lse, out, workspace)
 
 

@@ -510,6 +510,10 @@ PyObject* kv_attention(Args a) {
     on_device(*out, "out", dev);
     if (out->scalar_type() != dt || out->sizes() != q.sizes())
       fail(PyExc_ValueError, "out has to be " + describe(dt, q.sizes()) + ", not " + describe(out->scalar_type(), out->sizes()));
+    const int64_t tokens = t.batch * t.new_tokens, width = t.q_heads * kv.dim, esz = (int64_t)q.element_size();
+    const char *qb = (const char*)q.data_ptr(), *ob = (const char*)out->data_ptr();
+    if (tokens > 0 && width > 0 && qb < ob + tokens * width * esz && ob < qb + ((tokens - 1) * t.q_stride + width) * esz)
+      fail(PyExc_ValueError, "out shares memory with q, which other blocks still read");
   } else {
     made = n == 4 ? make(q, dt, {t.batch, t.new_tokens, t.q_heads, kv.dim}) : make(q, dt, {t.batch, t.q_heads, kv.dim});
   }
