@@ -601,7 +601,7 @@ int mx_gemm_grouped_k_ex(const void* A, const uint8_t* sA, const void* B, const 
  * An MX block lies along a head's row, the axis that the products with the queries reduce over and the
  * only one a single token fills.  Token `offset` of page p is slot p * page_size + offset.
  *   dim a nonzero multiple of 32; page_size >= 1 (any, also one that is no power of two); fmt an 8- or 4-bit
- *   format (6-bit rows are no whole 16-byte units: MX_ERR_UNSUPPORTED); all four tensors 16-byte
+ *   format (6-bit codes are not taken here: MX_ERR_UNSUPPORTED); all four tensors 16-byte
  *   aligned; pages * page_size below 2^31 and pages * page_size * heads below 2^32 - 1.
  * mx_kv_elems_bytes / mx_kv_scales_bytes: bytes of one codes and one scales tensor (the pointers may be
  * NULL there); 0 on bad arguments.

@@ -31,14 +31,14 @@
 // two or three blocks per SM, whatever the lengths.  A block that holds the whole of a sequence's tiles for a head writes the result,
 // otherwise it leaves a part (its weighted mean and the log of its weight) and a second kernel joins the parts, in the
 // order of the tiles: results do not depend on timing.  Where the table holds few tokens a block takes one sequence and head as a whole, and
-// nothing is joined (one sequence of 333 tokens: 10.0 -> 7.6 us).
+// nothing is joined (one sequence of 333 tokens: 10.6 -> 7.2 us).
 //
-// What bounds it.  Large batches the cache's bytes: 64 sequences of up to 8192 tokens, 8 heads of 128 with 4 queries each, E4M3, 109 us (5.7 of
-// the 6.55 TB/s that a copy reaches; further sequences add theirs at 6.2), one of 131072 tokens 53 us.  What is left there: 2 us until the first tile, the
-// flush of a block's last sequence, 4 us of the join, and blocks that finish 10 % apart.  Below 30 us these fixed parts
-// count for more than the bytes.  Rows of 4 bits and groups of more than 8 queries: instructions (about 700 a tile of 32 tokens, of
-// which the conversion of the codes 160 and the weights 170, issued at 60 % of the rate): 4-bit rows reach 3.0 TB/s, 16 queries a
-// head 3.0.
+// What bounds it.  Large batches the cache's bytes: 64 sequences of up to 8192 tokens, 8 heads of 128 with 4 queries each, E4M3, 111 us (5.6 of
+// the 6.55 TB/s that a copy reaches; 121 us where every call has inputs of its own; further sequences add theirs at 6.4), one of 131072 tokens 54 to 56.
+// What is left there: 2 us until the first tile, the flush of a block's last sequence, 4 us of the join, and blocks that finish 10 % apart.  Below 30 us
+// these fixed parts count for more than the bytes.  Rows of 4 bits and groups of more than 8 queries: instructions (about 700 a tile of 32
+// tokens, of which the conversion of the codes 160 and the weights 170, issued at 60 % of the rate): 4-bit rows reach 2.9 TB/s, 16 queries
+// a head 2.9.
 #pragma once
 
 #include <cuda_fp16.h>
