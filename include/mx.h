@@ -658,7 +658,7 @@ int mx_kv_read(const mx_kv_t* kv, const int32_t* slots, int64_t tokens, void* k_
  * queries: exact down to 2^-31 of the largest element of their block of 32, off by 2^-39 of it below) or to two FP16 terms (FP32: off by 2^-22 of
  * itself, or by 2^-50 of it); in the products over the tokens a weight times its value's block scale, to FP16 (BF16 results) or to two FP16
  * terms (FP32 results): off by 2^-11 or 2^-22 of itself, and where it is small by 2^-37 of the largest such product of the row and
- * block.  A query's result does not depend on the other queries.  An Inf or NaN in a query makes its result NaN.  A NaN or Inf element of a value
+ * block.  What the other queries hold does not change a query's result.  An Inf or NaN in a query makes its result NaN.  A NaN or Inf element of a value
  * makes that element NaN, or Inf or NaN, in the queries that see its token, and in no other; what lies in slots that no query sees
  * (NaN scales, stale codes) has no influence.
  *   workspace  mx_kv_attention_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and
